@@ -274,6 +274,113 @@ int qstate_scan_host(const qstate_cfg* cfg, qstate_buf* ping, qstate_buf* pong,
 int qstate_scan_fp32(const qstate_cfg* cfg, float* S, const qstate_inputs* x, int32_t t_begin,
                      int32_t t_end, float* o, void* stream);
 
+/* ---- paged cache of attention layers ------------------------------------------------------
+ * The attention layers beside the recurrent ones in a hybrid model (the paper's subject are the
+ * latter; it does not treat the former).  Their keys and values are kept in pages of `page`
+ * tokens that requests take from one pool.  A serving step is
+ *   qstate_kv_plan    block table, slots of the step's new tokens, free list   (once a step)
+ *   qstate_kv_append  the new tokens' keys and values into their slots          (each layer)
+ *   qstate_kv_attend  one new token of each request against its pages           (each layer)
+ * With n cached tokens of a request (the new one among them, so append before attend),
+ * z_t = scale q.k_t and t in [max(0, n - window), n) (window = 0: [0, n)):
+ *   lse = log sum_t e^{z_t},   o = sum_t e^{z_t - lse} v_t.
+ * A request with n = 0 gets o = 0 and lse = -inf.  Products are taken in 16 bits with FP32 sums;
+ * the softmax and its statistics are FP32. */
+#define QSTATE_KV_HEADS 0   /* keys and values per head; Hq a multiple of Hkv, query head h reads
+                               head h / (Hq / Hkv); dk = dv in {64, 128, 256}                  */
+#define QSTATE_KV_LATENT 1  /* one vector of dk entries a token, shared by all heads (Hkv = 1): the
+                               whole of it is the key, its first dv entries are the value (the
+                               absorbed form of latent attention); dv in {128, 256, 512},
+                               dk - dv in {0, 32, 64}                                          */
+#define QSTATE_KV_BF16 0    /* type of q, k, v and o                                            */
+#define QSTATE_KV_F16 1
+#define QSTATE_KV_16 0      /* the cache holds that type                                       */
+#define QSTATE_KV_E4M3 1    /* the cache holds 8-bit floats (4 exponent bits, 3 mantissa bits) times
+                               2^(e - 127), e a byte for each token and head: the smallest power with
+                               |x| <= 448 * 2^(e - 127), so that only the rounding of the codes (to
+                               nearest, ties to even) loses anything.  e = 255: the vector was not
+                               finite and reads as NaN.  HEADS and BF16 only                    */
+
+typedef struct qstate_kv_cfg {
+    int32_t kind;            /* QSTATE_KV_HEADS or QSTATE_KV_LATENT                            */
+    int32_t Hq, Hkv, dk, dv; /* 1 <= Hq <= 1024                                                */
+    int32_t page;            /* tokens of a page: a power of two, 1 to 1024                    */
+    int32_t n_pages;         /* pages of the pool; n_pages * page < 2^31                        */
+    int32_t max_pages;       /* columns of the block table; max_pages * page < 2^31             */
+    int32_t dtype;           /* QSTATE_KV_BF16 or QSTATE_KV_F16                                 */
+    int32_t store;           /* QSTATE_KV_16 or QSTATE_KV_E4M3                                  */
+    int32_t window;          /* last tokens that are seen; 0: all                              */
+    float scale;             /* of the scores; finite                                          */
+} qstate_kv_cfg;
+
+/* One layer's cache (device): k (n_pages, Hkv, page, dk), v (n_pages, Hkv, page, dv), 16-byte
+ * aligned; v is NULL for LATENT.  k_exp and v_exp, (n_pages, Hkv, page) bytes, for E4M3 only.
+ * What lies behind a request's last token is never used, whatever its bits. */
+typedef struct qstate_kv_cache {
+    void* k;
+    void* v;
+    uint8_t* k_exp;
+    uint8_t* v_exp;
+} qstate_kv_cache;
+
+/* Who holds which page (device).  table (R, max_pages): the pages of each request, in order.
+ * lens (R): its cached tokens.  free_list (n_pages): the pages nobody holds, a stack of
+ * free_count[0] entries.  lens_out and free_out receive the new lengths and count; they may be
+ * lens and free_count themselves. */
+typedef struct qstate_kv_pages {
+    int32_t* table;
+    const int32_t* lens;
+    int32_t* lens_out;
+    int32_t* free_list;
+    const int32_t* free_count;
+    int32_t* free_out;
+} qstate_kv_pages;
+
+/* The step's tokens, request after request (device, written by qstate_kv_plan).  cu (R + 1):
+ * exclusive prefix sum of max(n_new, 0), held at 2^31 - 1.  For each of T rows: slot (page id * page
+ * + place in the page), pos (place in the request) and req (the request), all -1 in rows behind
+ * cu[R]; a refused request's rows have slot -1.  pos and req may be NULL.  ok (R bytes): 1 where
+ * the request got its pages or has ended, 0 where it was refused. */
+typedef struct qstate_kv_slots {
+    int32_t* cu;
+    int32_t* slot;
+    int32_t* pos;
+    int32_t* req;
+    uint8_t* ok;
+    int32_t T;
+} qstate_kv_slots;
+
+/* Bytes of one layer's k (or, with v != 0, its v; 0 for LATENT) array, and of the work space: 256-byte
+ * aligned device memory, zeroed once after it is made, left zeroed where that matters by every call.
+ * One work space serves any number of layers and calls in stream order, not two streams at once. */
+size_t qstate_kv_cache_bytes(const qstate_kv_cfg* cfg, int32_t v);
+size_t qstate_kv_work_bytes(const qstate_kv_cfg* cfg);
+int qstate_kv_validate(const qstate_kv_cfg* cfg);
+
+/* Pages and slots of a step of R requests (0 <= R <= 8192), n_new[r] tokens to come each; n_new[r] < 0: the
+ * request has ended, its pages go back (its length becomes 0, its row of the table stays).  The
+ * pages that come back are laid on the free list in request order; the others take theirs from the
+ * top, in request order.  A request is refused (ok 0, length and table unchanged) if its rows end
+ * behind T, if it would need more than max_pages, or if it needs pages and they, with those of the
+ * requests before it, are more than there are.  Page ids outside the pool and lengths outside the
+ * table set the device status.  Only page, n_pages and max_pages of cfg matter. */
+int qstate_kv_plan(const qstate_kv_cfg* cfg, const qstate_kv_pages* pages, const int32_t* n_new, int32_t R,
+                   const qstate_kv_slots* slots, void* work, void* stream);
+
+/* T rows of keys and values (device, T x Hkv x d; strides in elements between rows and between heads,
+ * a head's entries side by side) into slots slot[0..T).  A negative slot is skipped; one outside the pool
+ * is skipped and sets the device status.  Slots are distinct.  v is NULL for LATENT. */
+int qstate_kv_append(const qstate_kv_cfg* cfg, const qstate_kv_cache* cache, const void* k, int64_t k_row,
+                     int64_t k_head, const void* v, int64_t v_row, int64_t v_head, const int32_t* slot, int32_t T,
+                     void* stream);
+
+/* One token of each of R requests: q (R x Hq x dk, strides as above), o (R, Hq, dv; 16-byte aligned), lse
+ * (R, Hq, float32; may be NULL), table (R, max_pages), lens (R).  Lengths outside the table and page ids outside the
+ * pool set the device status; their tokens count as not there. */
+int qstate_kv_attend(const qstate_kv_cfg* cfg, const qstate_kv_cache* cache, const void* q, int64_t q_row,
+                     int64_t q_head, const int32_t* table, const int32_t* lens, int32_t R, void* o, float* lse,
+                     void* work, void* stream);
+
 /* Synchronise `stream`, read and clear the device status word.  QSTATE_OK; QSTATE_ETIMEOUT if a
  * bounded wait of the chunked form gave up (the call's results are not valid; the kernel still
  * waited for its products before freeing tensor memory, so later calls are unaffected);

@@ -23,6 +23,11 @@ UNIT_ROW, UNIT_HEAD = 0, 1
 (WEIGHT_OURS, WEIGHT_RANGE, WEIGHT_GAMMA_RAW, WEIGHT_NRANGE, WEIGHT_PERSIST, WEIGHT_WBFACTOR,
  WEIGHT_NOERASE, WEIGHT_SHUFFLE, WEIGHT_UNIFORM) = range(9)
 
+# paged cache of attention layers (see include/qstate.h)
+KV_HEADS, KV_LATENT = 0, 1
+KV_BF16, KV_F16 = 0, 1
+KV_16, KV_E4M3 = 0, 1
+
 
 class QstateError(RuntimeError):
     def __init__(self, code: int, msg: str):
@@ -56,12 +61,33 @@ class _Inputs(ct.Structure):
                 ("T", ct.c_int32), ("a", ct.c_void_p), ("w", ct.c_void_p)]
 
 
+class _KvCfg(ct.Structure):
+    _fields_ = [("kind", ct.c_int32), ("Hq", ct.c_int32), ("Hkv", ct.c_int32), ("dk", ct.c_int32), ("dv", ct.c_int32),
+                ("page", ct.c_int32), ("n_pages", ct.c_int32), ("max_pages", ct.c_int32), ("dtype", ct.c_int32),
+                ("store", ct.c_int32), ("window", ct.c_int32), ("scale", ct.c_float)]
+
+
+class _KvCache(ct.Structure):
+    _fields_ = [("k", ct.c_void_p), ("v", ct.c_void_p), ("k_exp", ct.c_void_p), ("v_exp", ct.c_void_p)]
+
+
+class _KvPages(ct.Structure):
+    _fields_ = [("table", ct.c_void_p), ("lens", ct.c_void_p), ("lens_out", ct.c_void_p), ("free_list", ct.c_void_p),
+                ("free_count", ct.c_void_p), ("free_out", ct.c_void_p)]
+
+
+class _KvSlots(ct.Structure):
+    _fields_ = [("cu", ct.c_void_p), ("slot", ct.c_void_p), ("pos", ct.c_void_p), ("req", ct.c_void_p),
+                ("ok", ct.c_void_p), ("T", ct.c_int32)]
+
+
 EXPORTS = ["qstate_validate", "qstate_region_bytes", "qstate_units", "qstate_scale_groups",
            "qstate_bits_per_element", "qstate_init", "qstate_alloc_bits", "qstate_pack",
            "qstate_unpack", "qstate_quant_decay", "qstate_quant_decay_noalloc", "qstate_step",
            "qstate_scan", "qstate_scan_host",
            "qstate_scan_fp32", "qstate_check", "qstate_set_wait_limit", "qstate_set_scan_partitions",
-           "qstate_scan_partition_count", "qstate_last_error"]
+           "qstate_scan_partition_count", "qstate_last_error", "qstate_kv_validate", "qstate_kv_cache_bytes",
+           "qstate_kv_work_bytes", "qstate_kv_plan", "qstate_kv_append", "qstate_kv_attend"]
 
 _lib = None
 
@@ -111,9 +137,19 @@ def load(path: str | None = None, build_if_missing: bool = False):
     L.qstate_set_scan_partitions.argtypes = [ct.c_int32]
     L.qstate_scan_partition_count.argtypes = [ct.c_void_p, ct.c_void_p, ct.c_void_p]
     L.qstate_last_error.restype = ct.c_char_p
+    KC, I32, I64 = ct.POINTER(_KvCfg), ct.c_int32, ct.c_int64
+    L.qstate_kv_validate.argtypes = [KC]
+    L.qstate_kv_cache_bytes.argtypes = [KC, I32]
+    L.qstate_kv_cache_bytes.restype = ct.c_size_t
+    L.qstate_kv_work_bytes.argtypes = [KC]
+    L.qstate_kv_work_bytes.restype = ct.c_size_t
+    L.qstate_kv_plan.argtypes = [P, P, P, I32, P, P, P]
+    L.qstate_kv_append.argtypes = [P, P, P, I64, I64, P, I64, I64, P, I32, P]
+    L.qstate_kv_attend.argtypes = [P, P, P, I64, I64, P, P, I32, P, P, P, P]
     for name in EXPORTS:
         if name not in ("qstate_region_bytes", "qstate_units", "qstate_scale_groups",
-                        "qstate_bits_per_element", "qstate_last_error"):
+                        "qstate_bits_per_element", "qstate_last_error", "qstate_kv_cache_bytes",
+                        "qstate_kv_work_bytes"):
             getattr(L, name).restype = ct.c_int
     _lib = L
     return L
@@ -393,3 +429,225 @@ def qstate_scan_partition_count(cfg: Config, x: Inputs, stats: Stats) -> int:
     """Batch partitions a scan with these arguments would use now (0 if they are invalid)."""
     c, xi, st = cfg.c(), x.c(), stats.c()
     return int(_lib_or_raise().qstate_scan_partition_count(ct.byref(c), ct.byref(xi), ct.byref(st)))
+
+
+# ---- paged cache of attention layers -------------------------------------------------------------
+# Descriptions and tensors of these calls stay the same from step to step, so their structures are made
+# once, with the frozen object that holds them.
+def _keep(obj, struct=None, **more):
+    """Keeps a structure, its address and whatever else belongs to a frozen object."""
+    if struct is not None:
+        more.update(_c=struct, _at=ct.addressof(struct))
+    for name, value in more.items():
+        object.__setattr__(obj, name, value)
+
+
+@dataclass(frozen=True)
+class KvConfig:
+    """One attention layer's paged cache (mirrors ``qstate_kv_cfg``).  A description for
+    qstate_kv_plan alone needs page, n_pages and max_pages only."""
+    page: int
+    n_pages: int
+    max_pages: int
+    kind: int = KV_HEADS
+    Hq: int = 1
+    Hkv: int = 1
+    dk: int = 64
+    dv: int = 64
+    dtype: int = KV_BF16
+    store: int = KV_16
+    window: int = 0
+    scale: float = 1.0
+
+    def __post_init__(self):
+        _keep(self, _KvCfg(self.kind, self.Hq, self.Hkv, self.dk, self.dv, self.page, self.n_pages, self.max_pages,
+                           self.dtype, self.store, self.window, self.scale))
+
+    @property
+    def torch_dtype(self):
+        import torch
+        return torch.float16 if self.dtype == KV_F16 else torch.bfloat16
+
+
+def kv_validate(cfg: KvConfig) -> None:
+    _check(_lib_or_raise().qstate_kv_validate(ct.byref(cfg._c)))
+
+
+def _typed(t, name, *dtypes):
+    """Address of a contiguous CUDA tensor of one of the types (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    return _ptr(t)
+
+
+def _sized(t, name, n):
+    if t is not None and t.numel() != n:
+        raise ValueError(f"{name} must have {n} entries, got {t.numel()}")
+
+
+@dataclass(frozen=True)
+class KvCache:
+    """One layer's cache (device tensors, caller-owned): k (n_pages, Hkv, page, dk), v (n_pages, Hkv, page, dv)
+    or None for latents, and for e4m3 the exponent bytes (n_pages, Hkv, page)."""
+    k: object
+    v: object = None
+    k_exp: object = None
+    v_exp: object = None
+
+    def __post_init__(self):
+        import torch
+        types = (torch.bfloat16, torch.float16, torch.float8_e4m3fn)
+        _keep(self, _KvCache(_typed(self.k, "k", *types), _typed(self.v, "v", *types),
+                             _typed(self.k_exp, "k_exp", torch.uint8), _typed(self.v_exp, "v_exp", torch.uint8)), _fits=None)
+
+    def _check(self, cfg):
+        """The cache belongs to the description; looked at once for each description."""
+        if self._fits is cfg:
+            return
+        import torch
+        kv_validate(cfg)
+        rows = cfg.n_pages * cfg.Hkv * cfg.page
+        dtype = torch.float8_e4m3fn if cfg.store == KV_E4M3 else cfg.torch_dtype
+        for t, name, d in ((self.k, "k", cfg.dk), (self.v, "v", cfg.dv)):
+            _sized(t, name, rows * d)
+            if t is not None and t.dtype != dtype:
+                raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+        _sized(self.k_exp, "k_exp", rows)
+        _sized(self.v_exp, "v_exp", rows)
+        _keep(self, _fits=cfg)
+
+
+def new_kv_cache(cfg: KvConfig, device="cuda") -> KvCache:
+    import torch
+    kv_validate(cfg)
+    e4m3 = cfg.store == KV_E4M3
+    shape = (cfg.n_pages, cfg.Hkv, cfg.page)
+    arr = lambda d: torch.zeros(shape + (d,), dtype=torch.float8_e4m3fn if e4m3 else cfg.torch_dtype, device=device)  # noqa: E731
+    exp = lambda: torch.full(shape, 127, dtype=torch.uint8, device=device) if e4m3 else None  # noqa: E731
+    return KvCache(arr(cfg.dk), None if cfg.kind == KV_LATENT else arr(cfg.dv), exp(), exp())
+
+
+@dataclass(frozen=True)
+class KvPages:
+    """Who holds which page: table (R, max_pages), lens (R), free_list (n_pages), free_count (1), int32."""
+    table: object
+    lens: object
+    free_list: object
+    free_count: object
+
+    def __post_init__(self):
+        import torch
+        names = ("table", "lens", "free_list", "free_count")
+        _keep(self, _args=[_typed(getattr(self, n), n, torch.int32) for n in names], R=self.lens.numel())
+
+
+def new_kv_pages(cfg: KvConfig, R: int, device="cuda") -> KvPages:
+    """Tables of R requests without tokens; every page is free, the lowest on top."""
+    import torch
+    return KvPages(torch.full((R, cfg.max_pages), -1, dtype=torch.int32, device=device),
+                   torch.zeros(R, dtype=torch.int32, device=device),
+                   torch.arange(cfg.n_pages - 1, -1, -1, dtype=torch.int32, device=device),
+                   torch.full((1,), cfg.n_pages, dtype=torch.int32, device=device))
+
+
+@dataclass(frozen=True)
+class KvSlots:
+    """A step's tokens, as qstate_kv_plan lays them out: cu (R + 1), slot, pos, req (T; pos and req may
+    be None), int32, and ok (R), uint8."""
+    cu: object
+    slot: object
+    pos: object
+    req: object
+    ok: object
+
+    def __post_init__(self):
+        import torch
+        ptrs = [_typed(getattr(self, n), n, torch.int32) for n in ("cu", "slot", "pos", "req")]
+        T = self.slot.numel()
+        _sized(self.pos, "pos", T)
+        _sized(self.req, "req", T)
+        _keep(self, _KvSlots(*ptrs, _typed(self.ok, "ok", torch.uint8), T), T=T)
+
+
+def new_kv_slots(R: int, T: int, device="cuda") -> KvSlots:
+    import torch
+    i32 = lambda n: torch.empty(n, dtype=torch.int32, device=device)  # noqa: E731
+    return KvSlots(i32(R + 1), i32(T), i32(T), i32(T), torch.empty(R, dtype=torch.uint8, device=device))
+
+
+def new_kv_work(cfg: KvConfig, device="cuda"):
+    """Work space of a layer's calls (zeroed); serves any number of calls in stream order."""
+    import torch
+    kv_validate(cfg)
+    return torch.zeros(int(_lib_or_raise().qstate_kv_work_bytes(ct.byref(cfg._c))), dtype=torch.uint8, device=device)
+
+
+def _work(cfg, work):
+    """The work space's address; its size is looked at once for each description."""
+    if getattr(work, "_kv_fits", None) is not cfg:
+        need = int(_lib_or_raise().qstate_kv_work_bytes(ct.byref(cfg._c)))
+        if work.numel() * work.element_size() < need:
+            raise ValueError(f"the work space needs {need} bytes")
+        _ptr(work)
+        work._kv_fits = cfg
+    return work.data_ptr()
+
+
+def qstate_kv_plan(cfg: KvConfig, pages: KvPages, n_new, slots: KvSlots, work, lens_out=None, free_out=None,
+                   stream=None) -> None:
+    """Pages and slots of a step (see include/qstate.h).  The new lengths and free count go to lens_out and
+    free_out, in place without them."""
+    import torch
+    R = pages.R
+    if n_new.dtype is not torch.int32 or n_new.numel() != R or pages.table.numel() != R * cfg.max_pages:
+        raise ValueError(f"n_new must be int32 of {R} entries, and the table {R} x {cfg.max_pages}")
+    if pages.free_list.numel() != cfg.n_pages or slots.cu.numel() != R + 1 or slots.ok.numel() != R:
+        raise ValueError(f"free_list must have {cfg.n_pages} entries, cu {R + 1} and ok {R}")
+    table, lens, free_list, free = pages._args
+    if lens_out is not None:
+        _sized(lens_out, "lens_out", R)
+    c = _KvPages(table, lens, lens if lens_out is None else _typed(lens_out, "lens_out", torch.int32), free_list, free,
+                 free if free_out is None else _typed(free_out, "free_out", torch.int32))
+    _check(_lib_or_raise().qstate_kv_plan(cfg._at, ct.addressof(c), _ptr(n_new), R, slots._at, _work(cfg, work),
+                                          _stream(stream)))
+
+
+def _rows(t, name, cfg, heads, d):
+    """Address, row stride and head stride of a (rows, heads, d) tensor whose entries lie side by side."""
+    if t.dtype is not cfg.torch_dtype or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor of {cfg.torch_dtype}")
+    shape, (row, head, one) = t.shape, t.stride()
+    if shape[1] != heads or shape[2] != d or one != 1:
+        raise ValueError(f"{name} must be (rows, {heads}, {d}) with entries side by side, got {tuple(shape)}")
+    return t.data_ptr(), row, head
+
+
+def qstate_kv_append(cfg: KvConfig, cache: KvCache, k, v, slot, stream=None) -> None:
+    """Rows k, v (T, Hkv, d), any strides but the last, into slots slot[0..T); v is None for latents."""
+    import torch
+    cache._check(cfg)
+    T = slot.numel()
+    kp, kr, kh = _rows(k, "k", cfg, cfg.Hkv, cfg.dk)
+    vp, vr, vh = (None, 0, 0) if v is None else _rows(v, "v", cfg, cfg.Hkv, cfg.dv)
+    if k.shape[0] != T or (v is not None and v.shape[0] != T):
+        raise ValueError(f"k and v must have {T} rows")
+    _check(_lib_or_raise().qstate_kv_append(cfg._at, cache._at, kp, kr, kh, vp, vr, vh, _typed(slot, "slot", torch.int32),
+                                            T, _stream(stream)))
+
+
+def qstate_kv_attend(cfg: KvConfig, cache: KvCache, q, table, lens, o, lse, work, stream=None) -> None:
+    """One token of each request: q (R, Hq, dk), any strides but the last, against its pages; o (R, Hq, dv),
+    lse (R, Hq) float32 or None."""
+    import torch
+    cache._check(cfg)
+    R = lens.numel()
+    qp, qr, qh = _rows(q, "q", cfg, cfg.Hq, cfg.dk)
+    if q.shape[0] != R or table.numel() != R * cfg.max_pages:
+        raise ValueError(f"q must have {R} rows, and the table {R} x {cfg.max_pages}")
+    _sized(o, "o", R * cfg.Hq * cfg.dv)
+    _sized(lse, "lse", R * cfg.Hq)
+    _check(_lib_or_raise().qstate_kv_attend(cfg._at, cache._at, qp, qr, qh, _typed(table, "table", torch.int32),
+                                            _typed(lens, "lens", torch.int32), R, _typed(o, "o", cfg.torch_dtype),
+                                            _typed(lse, "lse", torch.float32), _work(cfg, work), _stream(stream)))

@@ -69,8 +69,10 @@ using namespace qs;
 static __device__ int qs_status_word;
 
 namespace {
-
 thread_local char g_err[512] = "";
+}  // namespace
+
+namespace qs {
 
 int fail(int code, const char* fmt, ...) {
     va_list ap;
@@ -83,6 +85,10 @@ int fail(int code, const char* fmt, ...) {
 int cuda_fail(cudaError_t e, const char* what) {
     return fail(QSTATE_ECUDA, "%s: %s (%s)", what, cudaGetErrorName(e), cudaGetErrorString(e));
 }
+
+}  // namespace qs
+
+namespace {
 
 constexpr int kMaxDevices = 64;
 std::mutex g_mu;
@@ -117,9 +123,11 @@ int* status_word(cudaError_t* err, int* dev_out = nullptr) {
     return g_status_addr[dev];
 }
 
+}  // namespace
+
 // The status word of the current device for a call that launches work; refused (EDEVICE) once
 // the device has been marked unusable.
-int acquire_status(int** out) {
+int qs::acquire_status(int** out) {
     cudaError_t e = cudaSuccess;
     int dev = -1;
     int* p = status_word(&e, &dev);
@@ -130,6 +138,8 @@ int acquire_status(int** out) {
     *out = p;
     return QSTATE_OK;
 }
+
+namespace {
 
 long long units_of(const qstate_cfg* c) {
     return c->unit_kind == QSTATE_UNIT_ROW ? static_cast<long long>(c->H) * c->dk : c->H;
@@ -931,11 +941,12 @@ int qstate_check(void* stream) {
         if (v & QS_DEV_TEARDOWN) g_unusable[dev].store(true);
         const int code = (v & QS_DEV_TEARDOWN) ? QSTATE_EDEVICE
                          : (v & QS_DEV_TIMEOUT) ? QSTATE_ETIMEOUT : QSTATE_EDEVICE;
-        return fail(code, "device status 0x%x:%s%s%s%s%s", v,
+        return fail(code, "device status 0x%x:%s%s%s%s%s%s", v,
                     (v & QS_DEV_LAYOUT) ? " inconsistent widths/offsets" : "",
                     (v & QS_DEV_RATE) ? " decay rate not positive/finite" : "",
                     (v & QS_DEV_TIMEOUT) ? " tensor-core product timed out" : "",
                     (v & QS_DEV_CHUNK) ? " decay over a 16-token block beyond the chunked form's range" : "",
+                    (v & QS_DEV_PAGES) ? " page, slot or length outside the cache" : "",
                     (v & QS_DEV_TEARDOWN) ? " the wait before freeing tensor memory gave up too: device marked unusable" : "");
     }
     if (g_unusable[dev].load())
