@@ -128,8 +128,8 @@ cudaError_t quant_decay_scratch(float** out);
 // Head of the work space: int32 counters, all zero between calls.
 constexpr int kKvTicket = 0;          // qstate_kv_plan in place: CTAs that have read the old lengths
 constexpr int kKvJoin = 64;           // qstate_kv_attend: parts that are done, by first worker
-constexpr int kKvWorkers = 960;       // most CTAs of an attention launch
-constexpr int kKvHeadBytes = 4096;
+constexpr int kKvWorkers = 608;       // most CTAs of an attention launch (4 on each of 152 SMs)
+constexpr int kKvHeadBytes = 8192;    // 64 + 3 * kKvWorkers counters
 constexpr int kKvMaxRequests = 8192;
 
 struct KvPlanParams {
@@ -167,15 +167,23 @@ struct KvAttendParams {
     int R, Hq, Hkv, dk, dv, page_shift, n_pages, max_pages, window;
     float scale;
     int* join;       // counters of the work space
-    float* part;     // partial results
+    float* part;     // partial results: sums, then references and weights
+    float* part_ml;
+    int q_aligned;   // q can be read in 16 bytes
     int* status;
 };
 
 cudaError_t launch_kv_plan(const KvPlanParams& p, cudaStream_t stream);
 cudaError_t launch_kv_append(const qstate_kv_cfg& c, const KvAppendParams& p, cudaStream_t stream);
 cudaError_t launch_kv_attend(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
-// bytes of partial results that an attention launch may use
-size_t kv_part_bytes(const qstate_kv_cfg& c);
+cudaError_t launch_kv_heads_64(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
+cudaError_t launch_kv_heads_128(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
+cudaError_t launch_kv_heads_256(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
+// partial results that an attention launch may use: bytes of sums, bytes of references and weights
+struct KvPartBytes {
+    size_t sums, ml;
+};
+KvPartBytes kv_part_bytes(const qstate_kv_cfg& c);
 
 // the calling thread's error text and the device status word (qs_api.cu)
 int fail(int code, const char* fmt, ...);

@@ -91,9 +91,15 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attend_plain_kernel(const KvAt
 
 }  // namespace
 
-size_t kv_part_bytes(const qstate_kv_cfg&) { return 0; }
+KvPartBytes kv_part_bytes(const qstate_kv_cfg& c) {
+    if (c.kind == QSTATE_KV_LATENT) return {0, 0};
+    return {static_cast<size_t>(kKvWorkers) * 2 * 16 * c.dv * sizeof(float), static_cast<size_t>(kKvWorkers) * 2 * 16 * 16};
+}
 
 cudaError_t launch_kv_attend(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream) {
+    if (c.kind == QSTATE_KV_HEADS)
+        return c.dk == 64 ? launch_kv_heads_64(c, p, stream)
+                          : c.dk == 128 ? launch_kv_heads_128(c, p, stream) : launch_kv_heads_256(c, p, stream);
     kv_attend_plain_kernel<<<p.R * p.Hq, kWarps * 32, 0, stream>>>(p, c.dtype == QSTATE_KV_F16,
                                                                   c.store == QSTATE_KV_E4M3);
     return cudaGetLastError();

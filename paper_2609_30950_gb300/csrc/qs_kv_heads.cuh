@@ -1,0 +1,570 @@
+// qs_kv_heads.cuh -- one new token of each request against keys and values per head.
+//
+// z_t = scale q.k_t, o = sum_t e^{z_t} v_t / sum_t e^{z_t}, in base 2 and against a running reference m:
+// p_t = 2^{z_t - m}.  Every key and value is used once by the G query heads that share it, 2 G
+// operations a byte in 16 bits, so the cache's bytes are the bound up to G of about 140.
+//
+// Tiles (qs_kv_tiles.cuh) of 64 tokens (128 in e4m3) of one request and key head, up to 16 query heads
+// as the 16 rows of the matrix products; more query heads are further groups, which find the tile
+// in L2.  A tile is four chunks, one a warp.  Each warp keeps its own ring of chunks (cp.async, zeros in
+// place of what is not to be seen, rows swizzled so that neither the copies nor the fragment loads
+// meet in a bank) and its own m, sums and o, so that warps meet only where a row of work ends: there
+// they lay their o into the ring's slot just used and join it.
+//  - m follows a row's maximum only when that has grown by more than 2^8: a vote, no reduction, on the
+//    way.  p is at most 2^8 then, which changes nothing about its relative precision.
+//  - p goes into the second product as hi + lo of two 16-bit values: one alone would add as much
+//    error as the rounding of o itself.  With up to 8 heads lo takes the rows that are left over,
+//    at no cost.
+//  - e4m3: codes are exact in f16, so both products run in f16.  q is scaled by a power of two for
+//    each head first (its entries under 2^-14 of the largest lose bits of 2^-25 of it, as sums in 32
+//    bits do); the keys' powers multiply the scores, and the values' powers are added to them in
+//    base 2, with a reference of their own, so that p times the power stays in f16's range.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "qs_kv_tiles.cuh"
+
+namespace qs {
+namespace kv {
+
+constexpr int kHeadRows = 16;
+constexpr float kLazy = 8.0f;
+
+template <int D, bool kE4M3, int kStages>
+struct HeadsShape {
+    static constexpr int kWarps = 4, kThreads = kWarps * 32;
+    static constexpr int kChunk = kE4M3 ? 32 : 16, kTile = kWarps * kChunk;
+    static constexpr int kRow = kE4M3 ? D : 2 * D, kSeg = kRow / 16;
+    static constexpr int kTensor = kChunk * kRow, kSlot = 2 * kTensor;   // 64 D bytes: 16 x D floats
+    static constexpr int kRing = kWarps * kStages * kSlot;
+    static constexpr int kQ = kRing, kExps = kQ + kHeadRows * 2 * D;
+    static constexpr int kMl = kExps + (kE4M3 ? kWarps * kStages * 64 : 0);
+    static constexpr int kWeights = kMl + kWarps * kHeadRows * 16;       // join: weights of parts
+    static constexpr int kMaxParts = (kKvWorkers + kJoinFan - 1) / kJoinFan;
+    static constexpr int kRowSums = kWeights + kHeadRows * kMaxParts * 4;
+    static constexpr int kQScale = kRowSums + kHeadRows * 16;
+    static constexpr int kMasks = kQScale + kHeadRows * 4;
+    static constexpr int kScratch = kMasks + kWarps * kStages * 4 + 16 - (kWarps * kStages * 4) % 16;
+    static constexpr int kBytes = kScratch + 16 * 8;
+
+    // byte of 16-byte piece `seg` of a row in a tile: eight rows at one piece, and two rows at four pieces,
+    // lie in different banks
+    static __device__ __forceinline__ int at(int row, int seg) {
+        if (kSeg == 4) return row * kRow + ((seg ^ ((row >> 1) & 3)) << 4);
+        return row * kRow + ((seg ^ (((row & 1) << 2) | ((row >> 1) & 3))) << 4);
+    }
+    static __device__ __forceinline__ int q_at(int row, int seg) {
+        return row * 2 * D + ((seg ^ (((row & 1) << 2) | ((row >> 1) & 3))) << 4);
+    }
+    // float of (row, column) where a warp lays its o down
+    static __device__ __forceinline__ int o_at(int row, int col) {
+        return row * D + (col ^ (kE4M3 ? (row & 1) << 4 : (row & 3) << 3));
+    }
+};
+
+// Joins n parts of a row, CTA first + i stride holding part i; fin(row, 4 columns, sum, M of the values, M, L).
+template <class S, int D, class Fin>
+__device__ void join_parts(const KvAttendParams& p, char* smem, int heads, int first, int stride, int n, bool first_holds_1,
+                           Fin fin) {
+    float* const weights = reinterpret_cast<float*>(smem + S::kWeights);
+    float4* const sums = reinterpret_cast<float4*>(smem + S::kRowSums);
+    const float4* const ml = reinterpret_cast<const float4*>(p.part_ml);
+    const int row = threadIdx.x >> 3, i0 = threadIdx.x & 7;   // 8 threads a head
+    auto slot_of = [&](int i) { return part_slot(first + i * stride, i == 0 && first_holds_1); };
+    float Mo = -INFINITY, M = -INFINITY, L = 0.0f;
+    for (int i = i0; i < n; i += 8) {
+        const float4 x = __ldcg(ml + slot_of(i) * kHeadRows + row);
+        Mo = fmaxf(Mo, x.x);
+        M = fmaxf(M, x.y);
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+        Mo = fmaxf(Mo, __shfl_xor_sync(kFull, Mo, o));
+        M = fmaxf(M, __shfl_xor_sync(kFull, M, o));
+    }
+    for (int i = i0; i < n; i += 8) {
+        const float4 x = __ldcg(ml + slot_of(i) * kHeadRows + row);
+        L += x.z * part_weight(x.y, M);
+        weights[row * S::kMaxParts + i] = part_weight(x.x, Mo);
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) L += __shfl_xor_sync(kFull, L, o);
+    if (i0 == 0) sums[row] = make_float4(Mo, M, L, 0.0f);
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < heads * (D / 4); idx += S::kThreads) {
+        const int r = idx / (D / 4);
+        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) {
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(p.part) +
+                                    static_cast<size_t>(slot_of(i)) * (kHeadRows * D / 4) + idx);
+            const float w = weights[r * S::kMaxParts + i];
+            acc.x += w * x.x;
+            acc.y += w * x.y;
+            acc.z += w * x.z;
+            acc.w += w * x.w;
+        }
+        fin(r, (idx - r * (D / 4)) * 4, acc, sums[r]);
+    }
+    __syncthreads();
+}
+
+template <int D, bool kF16, bool kE4M3, bool kHalf, int kStages, int kCtas>
+__global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendParams p, const int per_group, const int groups_per_kv) {
+    using S = HeadsShape<D, kE4M3, kStages>;
+    constexpr bool kProd16 = kF16 || kE4M3;         // products in f16
+    constexpr bool kQInRegs = D <= 128;
+    constexpr int kSteps = D / 16, kOut = D / 8;
+    constexpr float kLog2e = 1.4426950408889634f;
+    extern __shared__ __align__(128) char smem[];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane >> 2, t4 = lane & 3;
+    const int groups = p.Hkv * groups_per_kv, G = p.Hq / p.Hkv;
+
+    // requests without tokens
+    for (int r = blockIdx.x; r < p.R; r += gridDim.x)
+        if (clamped_len(p, r, false) == 0) {
+            uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + static_cast<size_t>(r) * p.Hq * D);
+            for (int i = tid; i < p.Hq * (D / 8); i += S::kThreads) o[i] = make_uint4(0, 0, 0, 0);
+            if (p.lse)
+                for (int i = tid; i < p.Hq; i += S::kThreads) p.lse[static_cast<size_t>(r) * p.Hq + i] = -INFINITY;
+        }
+
+    const Share share = make_share<S::kThreads, S::kTile, S::kChunk>(p, groups, reinterpret_cast<long long*>(smem + S::kScratch));
+    if (share.u0 >= share.u1) return;
+
+    char* const ring = smem + warp * (kStages * S::kSlot);
+    const uint32_t ring32 = smem_u32(ring);
+    char* const exps = smem + S::kExps + warp * (kStages * 64);
+    uint32_t* const masks = reinterpret_cast<uint32_t*>(smem + S::kMasks) + warp * kStages;
+    const int page_mask = (1 << p.page_shift) - 1;
+    const bool one_page = (1 << p.page_shift) >= S::kChunk;   // a chunk lies in one page
+
+    // ---- copies ----
+    Walk<S::kTile, S::kChunk> fw;
+    fw.start(p, share);
+    int id = -1;
+    auto look_up = [&]() {   // page of this lane's token in the chunk to come
+        const int t = fw.span.base + (fw.tile * S::kWarps + warp) * S::kChunk + (one_page ? 0 : lane);
+        id = -1;
+        if (t < fw.span.end && (one_page || lane < S::kChunk))
+            id = __ldg(p.table + static_cast<size_t>(fw.r) * p.max_pages + (t >> p.page_shift));
+    };
+    auto fetch = [&](int stage) {
+        const int t0 = fw.span.base + (fw.tile * S::kWarps + warp) * S::kChunk, t = t0 + lane;
+        const int hk = fw.group / groups_per_kv;
+        const bool seen = lane < S::kChunk && t >= fw.span.begin && t < fw.span.end;
+        const bool there = id >= 0 && id < p.n_pages;
+        if (seen && !there) raise_status(p.status, QS_DEV_PAGES);
+        const uint32_t mask = __ballot_sync(kFull, seen && there);
+        if (lane == 0) masks[stage] = mask;
+        if (mask == 0) return;
+        const uint32_t dst = ring32 + stage * S::kSlot;
+        const long long head_row = (static_cast<long long>(there ? id : 0) * p.Hkv + hk) << p.page_shift;
+        if (one_page) {
+            const long long row0 = head_row + (t0 & page_mask);
+            const char* const k = static_cast<const char*>(p.k) + row0 * S::kRow;
+            const char* const v = static_cast<const char*>(p.v) + row0 * S::kRow;
+#pragma unroll
+            for (int i = 0; i < S::kChunk * S::kSeg / 32; ++i) {
+                const int e = i * 32 + lane, row = e / S::kSeg, seg = e % S::kSeg, to = S::at(row, seg);
+                const bool on = (mask >> row) & 1;
+                cp_async16(dst + to, on ? k + e * 16 : static_cast<const char*>(p.k), on);
+                cp_async16(dst + S::kTensor + to, on ? v + e * 16 : static_cast<const char*>(p.v), on);
+            }
+            if (kE4M3 && lane < 16) {
+                // exponents of four tokens a lane, keys' then values'; groups of four lie within a page of 4 and more
+                const int g = lane & 7;
+                if ((mask >> (4 * g)) & 15)
+                    cp_async4(smem_u32(exps + stage * 64 + lane * 4), (lane < 8 ? p.k_exp : p.v_exp) + row0 + 4 * g);
+            }
+        } else {
+            const long long mine = head_row + (t & page_mask);   // row of the pool that this lane's token is
+#pragma unroll 2
+            for (int i = 0; i < S::kChunk * S::kSeg / 32; ++i) {
+                const int e = i * 32 + lane, row = e / S::kSeg, seg = e % S::kSeg, to = S::at(row, seg);
+                const bool on = (mask >> row) & 1;
+                const long long at = __shfl_sync(kFull, mine, row) * S::kRow + seg * 16;
+                cp_async16(dst + to, static_cast<const char*>(p.k) + (on ? at : 0), on);
+                cp_async16(dst + S::kTensor + to, static_cast<const char*>(p.v) + (on ? at : 0), on);
+            }
+            if (kE4M3 && seen && there) {
+                exps[stage * 64 + lane] = p.k_exp[mine];
+                exps[stage * 64 + 32 + lane] = p.v_exp[mine];
+            }
+        }
+    };
+    look_up();
+    long long fetched = share.u0;
+    auto fetch_next = [&](int stage) {
+        if (fetched < share.u1) {
+            fetch(stage);
+            if (++fetched < share.u1) {
+                fw.next(p, groups);
+                look_up();
+            }
+        }
+        cp_commit();
+    };
+#pragma unroll
+    for (int s = 0; s < kStages; ++s) fetch_next(s);
+
+    // ---- products ----
+    Walk<S::kTile, S::kChunk> cw;
+    cw.start(p, share);
+    uint32_t qf[kQInRegs ? kSteps : 1][4];
+    float o[kOut][4], m[2], mo[2], l[2], zs[2];
+    int stage = 0, heads = 0, h0 = 0, began = -1;
+    const uint32_t q32 = smem_u32(smem + S::kQ);
+
+    auto q_frag = [&](uint32_t (&a)[4], int ks) {
+        if (!kE4M3) {
+            ldsm4(a, q32 + S::q_at((lane & 7) + ((lane >> 3) & 1) * 8, ks * 2 + (lane >> 4)));
+        } else {
+            // columns t4 16 + 4 (ks % 4) ... + 3 of 64-column block ks / 4: the order in which a lane finds its codes
+            const int col = (ks >> 2) * 64 + t4 * 16 + (ks & 3) * 4;
+            const uint2 x = *reinterpret_cast<const uint2*>(smem + S::kQ + S::q_at(quad, col >> 3) + (col & 7) * 2);
+            const uint2 y = *reinterpret_cast<const uint2*>(smem + S::kQ + S::q_at(quad + 8, col >> 3) + (col & 7) * 2);
+            a[0] = x.x, a[1] = y.x, a[2] = x.y, a[3] = y.y;
+        }
+    };
+
+    for (long long u = share.u0; u < share.u1; ++u) {
+        if (began < 0) {   // a row of work begins: its queries
+            began = cw.tile;
+            const int hk = cw.group / groups_per_kv, part = cw.group - hk * groups_per_kv;
+            h0 = hk * G + part * per_group;
+            heads = min(per_group, G - part * per_group);
+            const int row = tid >> 3, piece = tid & 7;
+            const uint16_t* const src = static_cast<const uint16_t*>(p.q) + cw.r * p.q_row + (h0 + row) * p.q_head;
+            uint4 x[D / 64];
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) {
+                const int e = (i * 8 + piece) * 8;
+                x[i] = make_uint4(0, 0, 0, 0);
+                if (row < heads) {
+                    if (p.q_aligned) {
+                        x[i] = *reinterpret_cast<const uint4*>(src + e);
+                    } else {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) w[j] = src[e + 2 * j] | static_cast<uint32_t>(src[e + 2 * j + 1]) << 16;
+                        x[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+            }
+            if (kE4M3) {
+                unsigned big = 0;   // |q| as integers order as the numbers do
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) {
+                    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) big = max(big, max(w[j] << 16 & 0x7fffffffu, w[j] & 0x7fff0000u));
+                }
+#pragma unroll
+                for (int s = 1; s < 8; s <<= 1) big = max(big, __shfl_xor_sync(kFull, big, s));
+                const int e = big == 0 ? 0 : min(max(static_cast<int>(big >> 23) - 127, -126), 126);
+                const float inv = __uint_as_float(static_cast<unsigned>(127 - e) << 23);
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) {
+                    uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 y = unpack2<false>(w[j]);
+                        w[j] = pack2<true>(y.x * inv, y.y * inv);
+                    }
+                    x[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+                top = __uint_as_float(static_cast<unsigned>(127 + e) << 23);
+                if (piece == 0) reinterpret_cast<float*>(smem + S::kQScale)[row] = top;
+            }
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) *reinterpret_cast<uint4*>(smem + S::kQ + S::q_at(row, i * 8 + piece)) = x[i];
+            __syncthreads();
+            if (kQInRegs) {
+#pragma unroll
+                for (int ks = 0; ks < kSteps; ++ks) q_frag(qf[ks], ks);
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                m[s] = mo[s] = -INFINITY;
+                l[s] = 0.0f;
+                zs[s] = p.scale * kLog2e;
+                if (kE4M3) zs[s] *= reinterpret_cast<const float*>(smem + S::kQScale)[quad + 8 * s];
+            }
+#pragma unroll
+            for (int i = 0; i < kOut; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
+        }
+
+        cp_wait<kStages - 1>();
+        __syncwarp();
+        const uint32_t mask = masks[stage];
+        const uint32_t kt = ring32 + stage * S::kSlot, vt = kt + S::kTensor;
+        const char* const kb = ring + stage * S::kSlot;
+#pragma unroll
+        for (int sb = 0; sb < S::kChunk / 16; ++sb) {
+            const uint32_t on = (mask >> (16 * sb)) & 0xffffu;
+            if (on == 0) continue;
+            float z[2][4] = {};
+            if (!kE4M3) {
+#pragma unroll
+                for (int ks = 0; ks < kSteps; ++ks) {
+                    uint32_t a[4], b[4];
+                    if (!kQInRegs) q_frag(a, ks);
+                    ldsm4(b, kt + S::at((lane & 7) + (lane >> 4) * 8, ks * 2 + ((lane >> 3) & 1)));
+                    mma<kProd16>(z[0], kQInRegs ? qf[ks] : a, b[0], b[1]);
+                    mma<kProd16>(z[1], kQInRegs ? qf[ks] : a, b[2], b[3]);
+                }
+            } else {
+#pragma unroll
+                for (int blk = 0; blk < D / 64; ++blk) {
+                    uint4 w[2];
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt)
+                        w[nt] = *reinterpret_cast<const uint4*>(kb + S::at(sb * 16 + nt * 8 + quad, blk * 4 + t4));
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        uint32_t a[4];
+                        if (!kQInRegs) q_frag(a, blk * 4 + s);
+#pragma unroll
+                        for (int nt = 0; nt < 2; ++nt) {
+                            const uint32_t c = s == 0 ? w[nt].x : s == 1 ? w[nt].y : s == 2 ? w[nt].z : w[nt].w;
+                            uint32_t b0, b1;
+                            asm("{.reg .b16 lo, hi; mov.b32 {lo, hi}, %2; cvt.rn.f16x2.e4m3x2 %0, lo; cvt.rn.f16x2.e4m3x2 %1, hi;}"
+                                : "=r"(b0), "=r"(b1) : "r"(c));
+                            mma<true>(z[nt], kQInRegs ? qf[blk * 4 + s] : a, b0, b1);
+                        }
+                    }
+                }
+            }
+            // scores in base 2; y also carries the values' powers
+            float y[2][4];
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) {
+                float ke[2] = {1.0f, 1.0f}, ve[2] = {0.0f, 0.0f};
+                if (kE4M3) {
+                    const int tok = sb * 16 + nt * 8 + 2 * t4;
+                    const uint16_t kx = *reinterpret_cast<const uint16_t*>(exps + stage * 64 + tok);
+                    const uint16_t vx = *reinterpret_cast<const uint16_t*>(exps + stage * 64 + 32 + tok);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const unsigned kj = (kx >> (8 * j)) & 255, vj = (vx >> (8 * j)) & 255;
+                        ke[j] = __uint_as_float(kj == 255 ? 0x7fffffffu : kj << 23);
+                        ve[j] = vj == 255 ? __uint_as_float(0x7fffffffu) : static_cast<float>(static_cast<int>(vj) - 127);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (kHalf && j >= 2) continue;
+                    float x = z[nt][j] * zs[j >> 1];
+                    if (kE4M3) x *= ke[j & 1];
+                    if (!((on >> (nt * 8 + 2 * t4 + (j & 1))) & 1)) x = -INFINITY;
+                    z[nt][j] = x;
+                    y[nt][j] = kE4M3 ? (x == -INFINITY ? x : x + ve[j & 1]) : x;
+                }
+            }
+            // the references follow only what has outgrown them
+            float top[2], topo[2];
+            bool grown = false;
+#pragma unroll
+            for (int s = 0; s < (kHalf ? 1 : 2); ++s) {
+                top[s] = fmaxf(fmaxf(z[0][2 * s], z[0][2 * s + 1]), fmaxf(z[1][2 * s], z[1][2 * s + 1]));
+                grown = grown || top[s] > m[s] + kLazy;
+                if (kE4M3) {
+                    topo[s] = fmaxf(fmaxf(y[0][2 * s], y[0][2 * s + 1]), fmaxf(y[1][2 * s], y[1][2 * s + 1]));
+                    grown = grown || topo[s] > mo[s] + kLazy;
+                }
+            }
+            if (__any_sync(kFull, grown)) {
+#pragma unroll
+                for (int s = 0; s < (kHalf ? 1 : 2); ++s) {
+                    const float now = fmaxf(m[s], max4(top[s])), nowo = kE4M3 ? fmaxf(mo[s], max4(topo[s])) : now;
+                    l[s] *= part_weight(m[s], now);
+                    const float c = part_weight(mo[s], nowo);
+                    m[s] = now;
+                    mo[s] = nowo;
+#pragma unroll
+                    for (int i = 0; i < kOut; ++i) {
+                        o[i][2 * s] *= c;
+                        o[i][2 * s + 1] *= c;
+                        if (kHalf) o[i][2] *= c, o[i][3] *= c;
+                    }
+                }
+            }
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int s = 0; s < (kHalf ? 1 : 2); ++s) {
+                const float mz = m[s] == -INFINITY ? 0.0f : m[s], my = mo[s] == -INFINITY ? 0.0f : mo[s];
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt) {
+                    const float p0 = exp2_fast(z[nt][2 * s] - mz), p1 = exp2_fast(z[nt][2 * s + 1] - mz);
+                    l[s] += p0 + p1;
+                    const float w0 = kE4M3 ? exp2_fast(y[nt][2 * s] - my) : p0;
+                    const float w1 = kE4M3 ? exp2_fast(y[nt][2 * s + 1] - my) : p1;
+                    const uint32_t h = pack2<kProd16>(w0, w1);
+                    hi[2 * nt + s] = h;
+                    if (!kE4M3) {
+                        const float2 r = unpack2<kProd16>(h);
+                        (kHalf ? hi : lo)[2 * nt + (kHalf ? 1 : s)] = pack2<kProd16>(w0 - r.x, w1 - r.y);
+                    } else if (kHalf) {
+                        hi[2 * nt + 1] = 0;
+                    }
+                }
+            }
+#pragma unroll
+            for (int np = 0; np < D / 16; ++np) {
+                if (!kE4M3) {
+                    uint32_t b[4];
+                    ldsm4t(b, vt + S::at((lane & 7) + ((lane >> 3) & 1) * 8, np * 2 + (lane >> 4)));
+                    mma<kProd16>(o[2 * np], hi, b[0], b[1]);
+                    mma<kProd16>(o[2 * np + 1], hi, b[2], b[3]);
+                    if (!kHalf) {
+                        mma<kProd16>(o[2 * np], lo, b[0], b[1]);
+                        mma<kProd16>(o[2 * np + 1], lo, b[2], b[3]);
+                    }
+                } else if ((np & 1) == 0) {
+                    // two pieces of 16 columns; a register holds columns 2c, 2c + 1 of two tokens
+                    uint32_t b[4];
+                    ldsm4t(b, vt + S::at(sb * 16 + (lane & 7) + ((lane >> 3) & 1) * 8, np + (lane >> 4)));
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        uint32_t even[2], odd[2];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const uint32_t w = __byte_perm(b[2 * s + j], 0, 0x3120);
+                            asm("{.reg .b16 lo, hi; mov.b32 {lo, hi}, %2; cvt.rn.f16x2.e4m3x2 %0, lo; cvt.rn.f16x2.e4m3x2 %1, hi;}"
+                                : "=r"(even[j]), "=r"(odd[j]) : "r"(w));
+                        }
+                        mma<true>(o[2 * (np + s)], hi, even[0], even[1]);
+                        mma<true>(o[2 * (np + s) + 1], hi, odd[0], odd[1]);
+                    }
+                }
+            }
+        }
+
+        const bool row_ends = cw.tile == cw.span.tiles - 1;
+        if (row_ends || u + 1 == share.u1) {
+            // ---- the warps' parts of this row ----
+            float* const mine = reinterpret_cast<float*>(ring + stage * S::kSlot);
+            float4* const ml = reinterpret_cast<float4*>(smem + S::kMl);
+            __syncwarp();
+#pragma unroll
+            for (int s = 0; s < (kHalf ? 1 : 2); ++s) {
+                const int row = quad + 8 * s;
+                const float sum = sum4(l[s]);
+                if (t4 == 0) ml[warp * kHeadRows + row] = make_float4(mo[s], m[s], sum, 0.0f);
+                if (!kE4M3) {
+#pragma unroll
+                    for (int i = 0; i < kOut; ++i) {
+                        float2 x = make_float2(o[i][2 * s], o[i][2 * s + 1]);
+                        if (kHalf) x.x += o[i][2], x.y += o[i][3];
+                        *reinterpret_cast<float2*>(mine + S::o_at(row, i * 8 + 2 * t4)) = x;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kOut; i += 2)   // columns 4 t4 ... + 3 of a 16-column piece
+                        *reinterpret_cast<float4*>(mine + S::o_at(row, i * 8 + 4 * t4)) =
+                            make_float4(o[i][2 * s], o[i + 1][2 * s], o[i][2 * s + 1], o[i + 1][2 * s + 1]);
+                }
+            }
+            __syncthreads();
+            const float* const all = reinterpret_cast<const float*>(smem + stage * S::kSlot);
+            const size_t out_row = static_cast<size_t>(cw.r) * p.Hq + h0;
+            auto finish = [&](int row, int col, float4 acc, float4 sums) {
+                // sums: references of values and weights, sum of weights
+                const float inv = sums.z == 0.0f ? 0.0f : 1.0f / sums.z;
+                const float c = kE4M3 && sums.x != sums.y ? inv * exp2_fast(sums.x - sums.y) : inv;
+                uint2 w;
+                w.x = pack2<kF16>(acc.x * c, acc.y * c);
+                w.y = pack2<kF16>(acc.z * c, acc.w * c);
+                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.o) + (out_row + row) * D + col) = w;
+                if (col == 0 && p.lse)
+                    p.lse[out_row + row] = sums.z == 0.0f ? -INFINITY : (sums.y + log2f(sums.z)) * 0.6931471805599453f;
+            };
+            const bool whole = began == 0 && row_ends;
+            const long long row_start = u - cw.tile;
+            const Joint j = whole ? Joint{0, 1} : joint_of(share.total, row_start, cw.span.tiles);
+            const int me = static_cast<int>(blockIdx.x) - j.first, slot = part_slot(blockIdx.x, me == 0);
+            for (int idx = tid; idx < heads * (D / 4); idx += S::kThreads) {
+                const int row = idx / (D / 4), col = (idx - row * (D / 4)) * 4;
+                float4 x[S::kWarps];
+                float Mo = -INFINITY, M = -INFINITY, L = 0.0f;
+#pragma unroll
+                for (int w = 0; w < S::kWarps; ++w) {
+                    x[w] = ml[w * kHeadRows + row];
+                    Mo = fmaxf(Mo, x[w].x);
+                    M = fmaxf(M, x[w].y);
+                }
+                float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                for (int w = 0; w < S::kWarps; ++w) {
+                    L += x[w].z * part_weight(x[w].y, M);
+                    const float c = part_weight(x[w].x, Mo);
+                    const float4 v = *reinterpret_cast<const float4*>(all + w * (kStages * S::kSlot / 4) + S::o_at(row, col));
+                    acc.x += c * v.x;
+                    acc.y += c * v.y;
+                    acc.z += c * v.z;
+                    acc.w += c * v.w;
+                }
+                const float4 sums = make_float4(Mo, M, L, 0.0f);
+                if (whole) {
+                    finish(row, col, acc, sums);
+                } else {
+                    reinterpret_cast<float4*>(p.part)[static_cast<size_t>(slot) * (kHeadRows * D / 4) + idx] = acc;
+                    if (col == 0) reinterpret_cast<float4*>(p.part_ml)[slot * kHeadRows + row] = sums;
+                }
+            }
+            if (!whole) {
+                int* const flag = reinterpret_cast<int*>(smem + S::kScratch);
+                int* const join = p.join;
+                if (j.n <= kJoinFan) {
+                    if (arrive_last(join + j.first, j.n, flag)) join_parts<S, D>(p, smem, heads, j.first, 1, j.n, true, finish);
+                } else {
+                    const int g = me / kJoinFan, lead = j.first + g * kJoinFan, many = min(kJoinFan, j.n - g * kJoinFan);
+                    if (arrive_last(join + (g == 0 ? kKvWorkers : 2 * kKvWorkers) + lead, many, flag)) {
+                        const int to = part_slot(lead, g == 0);
+                        join_parts<S, D>(p, smem, heads, lead, 1, many, g == 0, [&](int row, int col, float4 acc, float4 sums) {
+                            reinterpret_cast<float4*>(p.part)[static_cast<size_t>(to) * (kHeadRows * D / 4) + row * (D / 4) + col / 4] = acc;
+                            if (col == 0) reinterpret_cast<float4*>(p.part_ml)[to * kHeadRows + row] = sums;
+                        });
+                        const int leads = (j.n + kJoinFan - 1) / kJoinFan;
+                        if (arrive_last(join + j.first, leads, flag))
+                            join_parts<S, D>(p, smem, heads, j.first, kJoinFan, leads, true, finish);
+                    }
+                }
+            }
+            began = -1;
+            __syncthreads();   // parts and queries of the row are read
+        }
+        __syncwarp();
+        fetch_next(stage);
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+        if (u + 1 < share.u1) cw.next(p, groups);
+    }
+    cp_wait<0>();
+}
+
+template <int D, bool kF16, bool kE4M3, bool kHalf, int kStages, int kCtas>
+cudaError_t launch_heads(const KvAttendParams& p, int per_group, int groups_per_kv, cudaStream_t stream) {
+    using S = HeadsShape<D, kE4M3, kStages>;
+    auto* kernel = kv_heads_kernel<D, kF16, kE4M3, kHalf, kStages, kCtas>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
+    if (e != cudaSuccess) return e;
+    const int ctas = device_sm_count() * kCtas;
+    kernel<<<ctas < kKvWorkers ? ctas : kKvWorkers, S::kThreads, S::kBytes, stream>>>(p, per_group, groups_per_kv);
+    return cudaGetLastError();
+}
+
+// Heads of a group: G / ceil(G / 16), rounded up; up to 8 of them leave half of the products' rows free.
+template <int D, bool kF16, bool kE4M3, int kStages, int kCtas>
+cudaError_t launch_heads_of(const KvAttendParams& p, cudaStream_t stream) {
+    const int G = p.Hq / p.Hkv, n = (G + kHeadRows - 1) / kHeadRows, per = (G + n - 1) / n;
+    return per <= 8 ? launch_heads<D, kF16, kE4M3, true, kStages, kCtas>(p, per, n, stream)
+                    : launch_heads<D, kF16, kE4M3, false, kStages, kCtas>(p, per, n, stream);
+}
+
+}  // namespace kv
+}  // namespace qs
