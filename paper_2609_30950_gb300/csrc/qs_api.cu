@@ -102,6 +102,12 @@ std::atomic<bool> g_unusable[kMaxDevices] = {};
 // Limit of the chunked form's mbarrier waits for the following launches (qstate_set_wait_limit).
 std::atomic<int> g_wait_polls{kDefaultWaitPolls};
 
+}  // namespace
+
+int qs::wait_polls() { return g_wait_polls.load(); }
+
+namespace {
+
 // Address of the status word on the current device, looked up once per device and context
 // (again whenever the context's identity is unknown or has changed).
 int* status_word(cudaError_t* err, int* dev_out = nullptr) {

@@ -128,7 +128,8 @@ cudaError_t quant_decay_scratch(float** out);
 // Head of the work space: int32 counters, all zero between calls.
 constexpr int kKvTicket = 0;          // qstate_kv_plan in place: CTAs that have read the old lengths
 constexpr int kKvJoin = 64;           // qstate_kv_attend: parts that are done, by first worker
-constexpr int kKvWorkers = 608;       // most CTAs of an attention launch (4 on each of 152 SMs)
+constexpr int kKvSms = 152;           // SMs that an attention launch takes at most
+constexpr int kKvWorkers = 4 * kKvSms;  // and its CTAs
 constexpr int kKvHeadBytes = 8192;    // 64 + 3 * kKvWorkers counters
 constexpr int kKvMaxRequests = 8192;
 
@@ -169,19 +170,25 @@ struct KvAttendParams {
     int* join;       // counters of the work space
     float* part;     // partial results: sums, then references and weights
     float* part_ml;
+    int* split;      // latents: parts of the row that a worker begins (0: not split), and its request
     int q_aligned;   // q can be read in 16 bytes
+    int wait_polls;  // limit of the latent kernel's waits for copies and products
     int* status;
 };
 
 cudaError_t launch_kv_plan(const KvPlanParams& p, cudaStream_t stream);
 cudaError_t launch_kv_append(const qstate_kv_cfg& c, const KvAppendParams& p, cudaStream_t stream);
 cudaError_t launch_kv_attend(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
+cudaError_t launch_kv_latent_128(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
+cudaError_t launch_kv_latent_256(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
+cudaError_t launch_kv_latent_512(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
 cudaError_t launch_kv_heads_64(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
 cudaError_t launch_kv_heads_128(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
 cudaError_t launch_kv_heads_256(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
-// partial results that an attention launch may use: bytes of sums, bytes of references and weights
+// partial results that an attention launch may use: bytes of sums, of references and weights, of the list of
+// split rows
 struct KvPartBytes {
-    size_t sums, ml;
+    size_t sums, ml, split;
 };
 KvPartBytes kv_part_bytes(const qstate_kv_cfg& c);
 
@@ -189,6 +196,7 @@ KvPartBytes kv_part_bytes(const qstate_kv_cfg& c);
 int fail(int code, const char* fmt, ...);
 int cuda_fail(cudaError_t e, const char* what);
 int acquire_status(int** out);
+int wait_polls();
 // identity of the current CUDA context (false if unknown); see qs_api.cu
 bool current_context_id(unsigned long long* id);
 // streaming multiprocessors of the current device (cached per device)

@@ -78,7 +78,7 @@ size_t qstate_kv_cache_bytes(const qstate_kv_cfg* cfg, int32_t v) {
 size_t qstate_kv_work_bytes(const qstate_kv_cfg* cfg) {
     if (check_cfg(cfg)) return 0;
     const KvPartBytes b = kv_part_bytes(*cfg);
-    return kKvHeadBytes + b.sums + b.ml;
+    return kKvHeadBytes + b.sums + b.ml + b.split;
 }
 
 int qstate_kv_plan(const qstate_kv_cfg* cfg, const qstate_kv_pages* pages, const int32_t* n_new, int32_t R,
@@ -181,7 +181,10 @@ int qstate_kv_attend(const qstate_kv_cfg* cfg, const qstate_kv_cache* cache, con
     p.scale = cfg->scale;
     p.join = static_cast<int*>(work) + kKvJoin;
     p.part = reinterpret_cast<float*>(static_cast<char*>(work) + kKvHeadBytes);
-    p.part_ml = p.part + kv_part_bytes(*cfg).sums / sizeof(float);
+    const KvPartBytes bytes = kv_part_bytes(*cfg);
+    p.part_ml = p.part + bytes.sums / sizeof(float);
+    p.split = reinterpret_cast<int*>(p.part_ml + bytes.ml / sizeof(float));
+    p.wait_polls = wait_polls();
     p.q_aligned = aligned(q, 16) && q_row % 8 == 0 && q_head % 8 == 0;
     const cudaError_t e = launch_kv_attend(*cfg, p, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? QSTATE_OK : cuda_fail(e, "cache attention kernel");

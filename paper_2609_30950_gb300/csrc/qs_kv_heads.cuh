@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
                 for (int i = tid; i < p.Hq; i += S::kThreads) p.lse[static_cast<size_t>(r) * p.Hq + i] = -INFINITY;
         }
 
-    const Share share = make_share<S::kThreads, S::kTile, S::kChunk>(p, groups, reinterpret_cast<long long*>(smem + S::kScratch));
+    const Share share = make_share<S::kThreads, S::kTile, S::kChunk>(p, groups, blockIdx.x, gridDim.x, reinterpret_cast<long long*>(smem + S::kScratch));
     if (share.u0 >= share.u1) return;
 
     char* const ring = smem + warp * (kStages * S::kSlot);
@@ -486,7 +486,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
             };
             const bool whole = began == 0 && row_ends;
             const long long row_start = u - cw.tile;
-            const Joint j = whole ? Joint{0, 1} : joint_of(share.total, row_start, cw.span.tiles);
+            const Joint j = whole ? Joint{0, 1} : joint_of(share.total, row_start, cw.span.tiles, gridDim.x);
             const int me = static_cast<int>(blockIdx.x) - j.first, slot = part_slot(blockIdx.x, me == 0);
             for (int idx = tid; idx < heads * (D / 4); idx += S::kThreads) {
                 const int row = idx / (D / 4), col = (idx - row * (D / 4)) * 4;

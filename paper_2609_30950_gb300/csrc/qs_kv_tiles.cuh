@@ -56,7 +56,7 @@ __device__ __forceinline__ int share_owner(long long total, long long u, int cta
 
 // All threads of the CTA; `groups` rows a request.  scratch: kThreads / 32 + 4 long longs of shared memory.
 template <int kThreads, int kTile, int kGrain>
-__device__ Share make_share(const KvAttendParams& p, int groups, long long* scratch) {
+__device__ Share make_share(const KvAttendParams& p, int groups, int worker, int workers, long long* scratch) {
     constexpr int kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (p.R + kThreads - 1) / kThreads, r0 = min(p.R, tid * per), r1 = min(p.R, r0 + per);
@@ -79,8 +79,8 @@ __device__ Share make_share(const KvAttendParams& p, int groups, long long* scra
     before -= mine;
     Share s;
     s.total = all * groups;
-    s.u0 = share_start(s.total, blockIdx.x, gridDim.x);
-    s.u1 = share_start(s.total, blockIdx.x + 1, gridDim.x);
+    s.u0 = share_start(s.total, worker, workers);
+    s.u1 = share_start(s.total, worker + 1, workers);
     long long* const found = scratch + kWarps;
     const long long first = before * groups;
     if (s.u0 < s.u1 && s.u0 >= first && s.u0 < first + mine * groups) {
@@ -133,10 +133,10 @@ struct Joint {
     int first, n;
 };
 
-__device__ __forceinline__ Joint joint_of(long long total, long long row_start, int tiles) {
+__device__ __forceinline__ Joint joint_of(long long total, long long row_start, int tiles, int workers) {
     Joint j;
-    j.first = share_owner(total, row_start, gridDim.x);
-    j.n = share_owner(total, row_start + tiles - 1, gridDim.x) - j.first + 1;
+    j.first = share_owner(total, row_start, workers);
+    j.n = share_owner(total, row_start + tiles - 1, workers) - j.first + 1;
     return j;
 }
 
