@@ -11,9 +11,9 @@ KvPartBytes kv_part_bytes(const qstate_kv_cfg& c) {
         return {static_cast<size_t>(kKvWorkers) * 2 * 16 * c.dv * sizeof(float),
                 static_cast<size_t>(kKvWorkers) * 2 * 16 * 16, split};
     int N = 0;
-    const kv::LatentGeo g = kv::latent_geo(c.Hq, c.dk, c.dv, kKvSms, &N);
+    const kv::LatentGeo g = kv::latent_geo(c.Hq, c.dk, kKvSms, &N);
     const size_t rows = static_cast<size_t>(g.workers) * g.groups * 2 * N;
-    return {rows * c.dv * sizeof(float), rows * 8, split};
+    return {rows * c.dv * sizeof(float), rows * 16, split};
 }
 
 cudaError_t launch_kv_attend(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream) {

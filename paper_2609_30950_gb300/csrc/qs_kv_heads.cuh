@@ -121,17 +121,20 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane >> 2, t4 = lane & 3;
     const int groups = p.Hkv * groups_per_kv, G = p.Hq / p.Hkv;
 
-    // requests without tokens
-    for (int r = blockIdx.x; r < p.R; r += gridDim.x)
-        if (clamped_len(p, r, false) == 0) {
-            uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + static_cast<size_t>(r) * p.Hq * D);
-            for (int i = tid; i < p.Hq * (D / 8); i += S::kThreads) o[i] = make_uint4(0, 0, 0, 0);
-            if (p.lse)
-                for (int i = tid; i < p.Hq; i += S::kThreads) p.lse[static_cast<size_t>(r) * p.Hq + i] = -INFINITY;
-        }
-
     const Share share = make_share<S::kThreads, S::kTile, S::kChunk>(p, groups, blockIdx.x, gridDim.x, reinterpret_cast<long long*>(smem + S::kScratch));
-    if (share.u0 >= share.u1) return;
+    auto empty_rows = [&]() {   // requests without tokens
+        for (int r = blockIdx.x; r < p.R; r += gridDim.x)
+            if (clamped_len(p, r, false) == 0) {
+                uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + static_cast<size_t>(r) * p.Hq * D);
+                for (int i = tid; i < p.Hq * (D / 8); i += S::kThreads) o[i] = make_uint4(0, 0, 0, 0);
+                if (p.lse)
+                    for (int i = tid; i < p.Hq; i += S::kThreads) p.lse[static_cast<size_t>(r) * p.Hq + i] = -INFINITY;
+            }
+    };
+    if (share.u0 >= share.u1) {
+        empty_rows();
+        return;
+    }
 
     char* const ring = smem + warp * (kStages * S::kSlot);
     const uint32_t ring32 = smem_u32(ring);
@@ -544,6 +547,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
         stage = stage + 1 == kStages ? 0 : stage + 1;
         if (u + 1 < share.u1) cw.next(p, groups);
     }
+    empty_rows();
     cp_wait<0>();
 }
 

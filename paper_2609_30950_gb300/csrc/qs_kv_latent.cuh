@@ -11,13 +11,17 @@
 //     O^T [dv x heads]       += C^T [dv x 64] P        the same bytes with dv contiguous (M-major)
 // Tokens and dv are the products' rows, so up to 64 heads are their columns and few heads waste nothing;
 // more heads go to further CTAs that walk the same tiles at the same time and find them in L2.
-//   warps 0-3   softmax: 16 tokens each from S^T, p to shared memory in 16 bits; at a row's end o
-//   warp 4      issues the products; S of the next tile goes ahead of O of this one
-//   warps 5-8   copy tiles (and, where a row begins, its queries) with cp.async, zeros for what is not seen
+//   warps 0-7   softmax: 16 tokens and half of the heads each from S^T, p to shared memory in 16 bits; at
+//               a row's end o
+//   warp 8      issues the products
+//   warps 9-12  copy tiles (and, where a row begins, its queries) with cp.async, zeros for what is not seen
 // As in the kernel for heads, the softmax reference follows the maximum only when that has outgrown it by
-// 2^8; all tokens of a row share one reference, so the four warps vote.  p goes into the second product
-// as hi + lo of two 16-bit values, since one alone would add as much error as the rounding of o; lo lies
-// in the tile's last block where that holds no values and has been read by then.
+// 2^8; all tokens of a row share one reference, so the eight warps vote.  p has 16 bits in the second product
+// and o is divided by the sum of the rounded p, so that the weights in use add up to one; lse comes from
+// the sum before rounding.  That leaves o with about 1.4 times the error of its own rounding.  Carrying the
+// remainder of p in a second product would cost a second pass over the tile: at 64 heads of 512 + 64, S and O
+// read 147 KB of operands from shared memory for each tile, O with the remainder 49 KB more, and
+// shared memory, at 128 bytes a cycle, is what a tile of 74 KB waits for (105 us against 91 at 64 requests).
 #pragma once
 
 #include "qs_kv_tiles.cuh"
@@ -27,7 +31,8 @@ namespace qs {
 namespace kv {
 
 constexpr int kLatTile = 64;
-constexpr int kLatThreads = 9 * 32;
+constexpr int kLatSoftmax = 8, kLatIssuer = kLatSoftmax, kLatCopiers = 4;   // warps
+constexpr int kLatThreads = (kLatSoftmax + 1 + kLatCopiers) * 32;
 constexpr int kBlockBytes = kLatTile * 128;   // 64 tokens x 64 entries
 constexpr int kMaxStages = 4;
 constexpr float kLazyLatent = 8.0f;
@@ -41,11 +46,12 @@ struct LatentGeo {
 struct LatentMisc {
     uint64_t full[kMaxStages], free[kMaxStages], sready[2], pready, drain;
     uint64_t mask[kMaxStages];
-    float top[4][64], corr[64], ref[64], sum[64];
-    long long scratch[16];
+    float top[4][64], topr[4][64], corr[64], ref[64], inv[64];
     uint32_t tmem;
     int abort;
 };
+// two tiles of the widest latents stand beside 64 heads' queries and p
+static_assert(2 * 9 * kBlockBytes + 9 * 64 * 128 + 64 * 128 + sizeof(LatentMisc) <= 227 * 1024, "shared memory of an SM");
 
 // Products of 16-bit types, FP32 sums: M x N, A optionally M-major.
 __host__ __device__ constexpr uint32_t idesc_f16(bool f16, int M, int N, bool a_m_major) {
@@ -57,37 +63,45 @@ __host__ __device__ constexpr uint32_t idesc_f16(bool f16, int M, int N, bool a_
 __device__ __forceinline__ uint64_t desc_sw128(uint32_t addr, uint32_t lbo, uint32_t sbo) {
     return tc::smem_desc(addr, lbo, sbo) | (static_cast<uint64_t>(2u) << 61);
 }
-__device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+// Executed by a whole warp in step, issued by the lane whose `lead` is not 0: descriptors then stay in uniform
+// registers (issued from a branch that one lane takes, each product took 85 cycles).
+__device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate, uint32_t lead) {
     asm volatile(
-        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
+        "{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u), "r"(lead)
         : "memory");
+}
+__device__ __forceinline__ void commit_by(uint64_t* bar, uint32_t lead) {
+    asm volatile(
+        "{\n.reg .pred q;\nsetp.ne.b32 q, %1, 0;\n"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(smem_u32(bar)),
+        "r"(lead)
+        : "memory");
+}
+__device__ __forceinline__ uint32_t elect_lane() {
+    uint32_t lead;
+    asm volatile("{\n.reg .pred q;\nelect.sync _|q, 0xffffffff;\nselp.u32 %0, 1, 0, q;\n}\n" : "=r"(lead));
+    return lead;
 }
 // 16 lanes x 8 N columns: register 4 j + i of lane t is row t / 4 + 8 (i / 2), column 8 j + 2 (t % 4) + i % 2.
 template <int N>
 __device__ __forceinline__ void tmem_ld_rows(uint32_t at, float (&v)[4 * N]) {
-    static_assert(N == 2 || N == 4 || N == 8, "columns in eights");
+    static_assert(N == 1 || N == 2 || N == 4, "columns in eights");
     uint32_t r[4 * N];
-    if constexpr (N == 2)
+    if constexpr (N == 1)
+        asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%4];\ntcgen05.wait::ld.sync.aligned;\n"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+    else if constexpr (N == 2)
         asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\ntcgen05.wait::ld.sync.aligned;\n"
                      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                      : "r"(at) : "memory");
-    else if constexpr (N == 4)
+    else
         asm volatile(
             "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
             "tcgen05.wait::ld.sync.aligned;\n"
             : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
               "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-            : "r"(at) : "memory");
-    else
-        asm volatile(
-            "tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
-            "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\ntcgen05.wait::ld.sync.aligned;\n"
-            : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-              "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-              "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-              "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
             : "r"(at) : "memory");
 #pragma unroll
     for (int i = 0; i < 4 * N; ++i) v[i] = __uint_as_float(r[i]);
@@ -96,6 +110,9 @@ __device__ __forceinline__ void stmatrix4t(uint32_t at, uint32_t a, uint32_t b, 
     asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d)
                  : "memory");
 }
+__device__ __forceinline__ void stmatrix2t(uint32_t at, uint32_t a, uint32_t b) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x2.trans.shared.b16 [%0], {%1,%2};" ::"r"(at), "r"(a), "r"(b) : "memory");
+}
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(smem_u32(bar)) : "memory");
 }
@@ -103,10 +120,18 @@ __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
 __device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];\n" ::"r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 128;\n" ::: "memory"); }
+// Whether a phase of a barrier is complete, for the whole warp alike and without waiting.
+__device__ __forceinline__ bool warp_test(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    return __all_sync(kFull, ok != 0);
+}
+__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;\n" ::: "memory"); }
 __device__ __forceinline__ bool softmax_any(bool x) {
     int any;
-    asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %1, 0;\nbar.red.or.pred q, 1, 128, p;\nselp.s32 %0, 1, 0, q;\n}\n"
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %1, 0;\nbar.red.or.pred q, 1, 256, p;\nselp.s32 %0, 1, 0, q;\n}\n"
                  : "=r"(any) : "r"(static_cast<int>(x)) : "memory");
     return any != 0;
 }
@@ -129,45 +154,35 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
     using W = Walk<kLatTile, 1>;
     constexpr int kOCols = DV / 128 * kN, kCols = kOCols + 2 * kN;
     constexpr int kAlloc = kCols <= 32 ? 32 : kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-    constexpr int kPer = kN / 4;   // heads a lane holds
+    constexpr int kPer = kN / 8;   // heads a lane holds: 2 of each 8 of its warp's half
     constexpr float kLog2e = 1.4426950408889634f;
     extern __shared__ __align__(1024) char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     char* const tiles = smem;
     char* const queries = tiles + g.stages * g.blocks * kBlockBytes;
     char* const probs = queries + g.blocks * kN * 128;
-    const bool lo_in_tile = p.dk > DV;
-    LatentMisc& x = *reinterpret_cast<LatentMisc*>(probs + (lo_in_tile ? 1 : 2) * kN * 128);
+    LatentMisc& x = *reinterpret_cast<LatentMisc*>(probs + kN * 128);
     const int worker = blockIdx.x / g.groups, group = blockIdx.x - worker * g.groups;
     const int h0 = group * g.per_group, heads = min(g.per_group, p.Hq - h0);
     chain_release();   // the kernel that joins split rows may take its place
 
-    // requests without tokens
-    for (int r = worker; r < p.R; r += g.workers)
-        if (clamped_len(p, r, false) == 0) {
-            uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + (static_cast<size_t>(r) * p.Hq + h0) * DV);
-            for (int i = tid; i < heads * (DV / 8); i += kLatThreads) o[i] = make_uint4(0, 0, 0, 0);
-            if (p.lse)
-                for (int i = tid; i < heads; i += kLatThreads) p.lse[static_cast<size_t>(r) * p.Hq + h0 + i] = -INFINITY;
-        }
-
-    if (warp == 4) {
+    if (warp == kLatIssuer) {
         tc::tmem_alloc(&x.tmem, kAlloc);
         tc::tmem_relinquish();
     }
     if (tid == 0) {
         for (int s = 0; s < kMaxStages; ++s) {
-            tc::mbar_init(&x.full[s], 128 + 4);
+            tc::mbar_init(&x.full[s], kLatCopiers * 33);
             tc::mbar_init(&x.free[s], 1);
         }
         tc::mbar_init(&x.sready[0], 1);
         tc::mbar_init(&x.sready[1], 1);
-        tc::mbar_init(&x.pready, 4);
+        tc::mbar_init(&x.pready, kLatSoftmax);
         tc::mbar_init(&x.drain, 1);
         tc::mbar_fence_init();
         x.abort = 0;
     }
-    const Share share = make_share<kLatThreads, kLatTile, 1>(p, 1, worker, g.workers, x.scratch);
+    const Share share = make_share<kLatThreads, kLatTile, 1>(p, 1, worker, g.workers, reinterpret_cast<long long*>(x.top));
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
@@ -176,9 +191,9 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
     volatile int* const abort = &x.abort;
     if (group == 0 && tid == 0 && n <= 0) p.split[worker] = 0;
 
-    if (n > 0 && warp >= 5) {
+    if (n > 0 && warp > kLatIssuer) {
         // ---- copies ----
-        const int pw = warp - 5, page_mask = (1 << p.page_shift) - 1;
+        const int pw = warp - kLatIssuer - 1, page_mask = (1 << p.page_shift) - 1;
         W w;
         w.start(p, share);
         auto look_up = [&]() {
@@ -210,7 +225,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                 if (begins) {
                     const uint16_t* const q = static_cast<const uint16_t*>(p.q) + r * p.q_row + h0 * p.q_head;
                     for (int b = 0; b < g.blocks; ++b)
-                        for (int e = tid - 160; e < kN * 8; e += 128) {
+                        for (int e = pw * 32 + lane; e < kN * 8; e += kLatCopiers * 32) {
                             const int h = e >> 3, sg = e & 7, col = b * 64 + sg * 8;
                             const uint32_t to = smem_u32(queries + (b * kN + h) * 128 + ((sg ^ (h & 7)) << 4));
                             if (p.q_aligned) {
@@ -242,54 +257,82 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
         }
         cp_commit();
         cp_wait<0>();
-    } else if (n > 0 && warp == 4) {
+    } else if (n > 0 && warp == kLatIssuer) {
         // ---- products ----
-        if (lane == 0) {
-            constexpr uint32_t idS = idesc_f16(kF16, 64, kN, false), idO = idesc_f16(kF16, 128, kN, true);
-            const uint32_t q32 = smem_u32(queries), p32 = smem_u32(probs), t32 = smem_u32(tiles);
-            W w;
-            w.start(p, share);
-            auto scores = [&](int i) {
-                const int s = i % g.stages;
-                if (!role_wait(&x.full[s], (i / g.stages) & 1, abort, p)) return;
-                tc::fence_async_smem();   // the copies' writes, for the tensor core's reads
-                tc::fence_after_sync();
-                const uint32_t tile = t32 + s * g.blocks * kBlockBytes, d = tmem + kOCols + (i & 1) * kN;
-                for (int k = 0; k < p.dk / 16; ++k)
-                    mma_f16_ss(d, desc_sw128(tile + (k >> 2) * kBlockBytes + (k & 3) * 32, 16, 1024),
-                               desc_sw128(q32 + (k >> 2) * (kN * 128) + (k & 3) * 32, 16, 1024), idS, k > 0);
-                tc::mma_commit(&x.sready[i & 1]);
-            };
-            scores(0);
-            for (int i = 0; i < n; ++i) {
-                if (i + 1 < n) scores(i + 1);
-                const bool begins = i == 0 || w.tile == 0;
-                if (role_wait(&x.pready, i & 1, abort, p)) {
-                    tc::fence_after_sync();
-                    const int s = i % g.stages;
-                    const uint32_t tile = t32 + s * g.blocks * kBlockBytes;
-                    const uint32_t lo32 = lo_in_tile ? tile + DV / 64 * kBlockBytes : p32 + kN * 128;
+        constexpr uint32_t idS = idesc_f16(kF16, 64, kN, false), idO = idesc_f16(kF16, 128, kN, true);
+        const uint32_t lead = elect_lane(), tile_bytes = g.blocks * kBlockBytes;
+        const uint32_t q32 = smem_u32(queries), p32 = smem_u32(probs), t32 = smem_u32(tiles);
+        const uint64_t dq = desc_sw128(q32, 16, 1024), dp = desc_sw128(p32, 16, 1024);
+        const int full_blocks = p.dk >> 6;
+        W w;
+        w.start(p, share);
+        int ss = 0, so = 0;   // stages of the tiles whose S and whose O come next
+        auto scores = [&](int i) {
+            tc::fence_async_smem();   // the copies' writes, for the tensor core's reads
+            tc::fence_after_sync();
+            const uint64_t a = desc_sw128(t32 + ss * tile_bytes, 16, 1024);
+            const uint32_t d = tmem + kOCols + (i & 1) * kN;
+            for (int b = 0; b < full_blocks; ++b)
 #pragma unroll
-                    for (int c = 0; c < DV / 128; ++c)
+                for (int k = 0; k < 4; ++k)
+                    mma_f16_ss(d, a + b * (kBlockBytes / 16) + k * 2, dq + b * (kN * 8) + k * 2, idS, b > 0 || k > 0, lead);
+            if (full_blocks < g.blocks)   // half a block
 #pragma unroll
-                        for (int k = 0; k < kLatTile / 16; ++k) {
-                            const uint64_t a = desc_sw128(tile + 2 * c * kBlockBytes + k * 2048, kBlockBytes, 1024);
-                            mma_f16_ss(tmem + c * kN, a, desc_sw128(p32 + k * 32, 16, 1024), idO, !begins || k > 0);
-                            mma_f16_ss(tmem + c * kN, a, desc_sw128(lo32 + k * 32, 16, 1024), idO, true);
-                        }
-                    tc::mma_commit(&x.free[s]);
-                }
-                if (i + 1 < n) w.next(p, 1);
+                for (int k = 0; k < 2; ++k)
+                    mma_f16_ss(d, a + full_blocks * (kBlockBytes / 16) + k * 2, dq + full_blocks * (kN * 8) + k * 2, idS, true, lead);
+            commit_by(&x.sready[i & 1], lead);
+            ss = ss + 1 == g.stages ? 0 : ss + 1;
+        };
+        auto values = [&](bool begins) {
+            tc::fence_after_sync();
+            const uint64_t a = desc_sw128(t32 + so * tile_bytes, kBlockBytes, 1024);
+#pragma unroll
+            for (int c = 0; c < DV / 128; ++c)
+#pragma unroll
+                for (int k = 0; k < kLatTile / 16; ++k)
+                    mma_f16_ss(tmem + c * kN, a + c * (2 * kBlockBytes / 16) + k * (2048 / 16), dp + k * 2, idO, !begins || k > 0, lead);
+            commit_by(&x.free[so], lead);
+            so = so + 1 == g.stages ? 0 : so + 1;
+        };
+        // S runs one tile ahead of O where that tile is there, and never makes O wait for it: with two tiles in
+        // flight the copy of the next one waits for O
+        int is = 0, full_phase = 0, idle = 0;
+        bool live = true;
+        for (int io = 0; io < n && live;) {
+            bool did = false;
+            if (is < n && is <= io + 1 && warp_test(&x.full[ss], full_phase)) {
+                const int at = ss;
+                scores(is++);
+                if (at + 1 == g.stages) full_phase ^= 1;
+                did = true;
             }
+            if (io < is && warp_test(&x.pready, io & 1)) {
+                values(io == 0 || w.tile == 0);
+                if (++io < n) w.next(p, 1);
+                did = true;
+            }
+            if (!did) {
+                if (++idle > p.wait_polls || *abort) {
+                    if (!*abort) raise_status(p.status, QS_DEV_TIMEOUT);
+                    *abort = 1;
+                    live = false;
+                }
+            } else {
+                idle = 0;
+            }
+            live = __all_sync(kFull, live);
         }
     } else if (n > 0) {
         // ---- softmax ----
-        const int quad = lane >> 2, t4 = lane & 3;
-        const uint32_t tlane = tmem + (static_cast<uint32_t>(32 * warp) << 16);
+        const int quad = lane >> 2, t4 = lane & 3, sub = warp & 3, c0 = (warp >> 2) * (kN / 2);   // token quarter, first head
+        const uint32_t tlane = tmem + (static_cast<uint32_t>(32 * sub) << 16);
         const uint32_t p32 = smem_u32(probs);
         const float zs = p.scale * kLog2e;
-        float m[kPer], l[kPer];
+        // sums of p before and after its rounding
+        float m[kPer], l[kPer], lr[kPer];
         int prev = 0, s = 0, began = 0, split = 0;   // prev: stage of the tile before
+        // k: head c0 + 8 (k / 2) + 2 t4 + k % 2, at tokens quad and quad + 8 of the quarter
+        auto head = [&](int k) { return c0 + 8 * (k >> 1) + 2 * t4 + (k & 1); };
         W w;
         w.start(p, share);
         for (int i = 0; i < n; ++i) {
@@ -297,17 +340,17 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
             if (begins) {
                 began = w.tile;
 #pragma unroll
-                for (int k = 0; k < kPer; ++k) m[k] = -INFINITY, l[k] = 0.0f;
+                for (int k = 0; k < kPer; ++k) m[k] = -INFINITY, l[k] = lr[k] = 0.0f;
             }
             role_wait(&x.full[s], (i / g.stages) & 1, abort, p);
             role_wait(&x.sready[i & 1], (i >> 1) & 1, abort, p);
             tc::fence_after_sync();
             float z[2 * kPer];
-            tmem_ld_rows<kN / 8>(tlane + kOCols + (i & 1) * kN, z);
-            const uint32_t on = reinterpret_cast<volatile uint16_t*>(&x.mask[s])[warp];
+            tmem_ld_rows<kN / 16>(tlane + kOCols + (i & 1) * kN + c0, z);
+            const uint32_t on = reinterpret_cast<volatile uint16_t*>(&x.mask[s])[sub];
             bool grown = false;
 #pragma unroll
-            for (int k = 0; k < kPer; ++k) {   // k: head 8 (k / 2) + 2 t4 + k % 2, tokens quad and quad + 8
+            for (int k = 0; k < kPer; ++k) {
                 float& a = z[4 * (k >> 1) + (k & 1)];
                 float& b = z[4 * (k >> 1) + (k & 1) + 2];
                 a = (on >> quad) & 1 ? a * zs : -INFINITY;
@@ -321,24 +364,25 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                     float top = fmaxf(z[4 * (k >> 1) + (k & 1)], z[4 * (k >> 1) + (k & 1) + 2]);
 #pragma unroll
                     for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
-                    if (quad == 0) x.top[warp][8 * (k >> 1) + 2 * t4 + (k & 1)] = top;
+                    if (quad == 0) x.top[sub][head(k)] = top;
                 }
                 softmax_sync();
 #pragma unroll
                 for (int k = 0; k < kPer; ++k) {
-                    const int h = 8 * (k >> 1) + 2 * t4 + (k & 1);
+                    const int h = head(k);
                     const float now = fmaxf(fmaxf(fmaxf(x.top[0][h], x.top[1][h]), fmaxf(x.top[2][h], x.top[3][h])), m[k]);
                     const float c = part_weight(m[k], now);
                     l[k] *= c;
+                    lr[k] *= c;
                     m[k] = now;
-                    if (warp == 0 && quad == 0) x.corr[h] = c;
+                    if (sub == 0 && quad == 0) x.corr[h] = c;
                 }
                 softmax_sync();
                 if (!begins) {
                     role_wait(&x.free[prev], prev_parity, abort, p);   // the products so far are in
                     tc::fence_after_sync();
 #pragma unroll 1
-                    for (int c = 0; c < kOCols; c += 16) {
+                    for (int c = (warp >> 2) * 16; c < kOCols; c += 32) {
                         float v[16];
                         tc::tmem_ld16(tlane + c, v);
 #pragma unroll
@@ -348,7 +392,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                     tc::wait_st();
                 }
             }
-            uint32_t hi[kPer], lo[kPer];
+            uint32_t pk[kPer];
 #pragma unroll
             for (int k = 0; k < kPer; ++k) {
                 const float mz = m[k] == -INFINITY ? 0.0f : m[k];
@@ -359,19 +403,22 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                 l[k] += a + b;
             }
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                hi[j] = pack2<kF16>(z[2 * j], z[2 * j + 1]);
-                const float2 r = unpack2<kF16>(hi[j]);
-                lo[j] = pack2<kF16>(z[2 * j] - r.x, z[2 * j + 1] - r.y);
+            for (int j = 0; j < kPer; ++j) {   // j: heads of k = j & ~1 and the next, tokens quad + 8 (j % 2)
+                pk[j] = pack2<kF16>(z[2 * j], z[2 * j + 1]);
+                const float2 r = unpack2<kF16>(pk[j]);
+                lr[j & ~1] += r.x;
+                lr[j | 1] += r.y;
             }
-            const uint32_t lo32 = lo_in_tile ? smem_u32(tiles + (s * g.blocks + DV / 64) * kBlockBytes) : p32 + kN * 128;
             if (i > 0) role_wait(&x.free[prev], prev_parity, abort, p);   // p of the tile before has been read
+            if constexpr (kN == 16) {
+                const int h = c0 + (lane & 7), chunk = sub * 2 + ((lane >> 3) & 1);
+                stmatrix2t(p32 + h * 128 + ((chunk ^ (h & 7)) << 4), pk[0], pk[1]);
+            } else {
 #pragma unroll
-            for (int j = 0; j < kN / 8; j += 2) {
-                const int mat = lane >> 3, h = (j + (mat >> 1)) * 8 + (lane & 7), chunk = warp * 2 + (mat & 1);
-                const int to = h * 128 + ((chunk ^ (h & 7)) << 4);
-                stmatrix4t(p32 + to, hi[2 * j], hi[2 * j + 1], hi[2 * j + 2], hi[2 * j + 3]);
-                stmatrix4t(lo32 + to, lo[2 * j], lo[2 * j + 1], lo[2 * j + 2], lo[2 * j + 3]);
+                for (int j = 0; j < kN / 16; j += 2) {
+                    const int mat = lane >> 3, h = c0 + (j + (mat >> 1)) * 8 + (lane & 7), chunk = sub * 2 + (mat & 1);
+                    stmatrix4t(p32 + h * 128 + ((chunk ^ (h & 7)) << 4), pk[2 * j], pk[2 * j + 1], pk[2 * j + 2], pk[2 * j + 3]);
+                }
             }
             tc::fence_async_smem();
             tc::fence_before_sync();
@@ -382,13 +429,17 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                 // ---- the row's end ----
 #pragma unroll
                 for (int k = 0; k < kPer; ++k) {
-                    const int h = 8 * (k >> 1) + 2 * t4 + (k & 1);
-                    float sum = l[k];
+                    const int h = head(k);
+                    float sum = l[k], sumr = lr[k];
 #pragma unroll
-                    for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(kFull, sum, o);
+                    for (int o = 4; o < 32; o <<= 1) {
+                        sum += __shfl_xor_sync(kFull, sum, o);
+                        sumr += __shfl_xor_sync(kFull, sumr, o);
+                    }
                     if (quad == 0) {
-                        x.top[warp][h] = sum;
-                        if (warp == 0) x.ref[h] = m[k];
+                        x.top[sub][h] = sum;
+                        x.topr[sub][h] = sumr;
+                        if (sub == 0) x.ref[h] = m[k];
                     }
                 }
                 softmax_sync();
@@ -403,9 +454,10 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                 const size_t prow = (static_cast<size_t>(slot) * g.groups + group) * kN;
                 if (tid < kN) {
                     const float sum = x.top[0][tid] + x.top[1][tid] + x.top[2][tid] + x.top[3][tid], ref = x.ref[tid];
-                    x.sum[tid] = sum == 0.0f ? 0.0f : 1.0f / sum;
+                    const float sumr = x.topr[0][tid] + x.topr[1][tid] + x.topr[2][tid] + x.topr[3][tid];
+                    x.inv[tid] = sumr == 0.0f ? 0.0f : 1.0f / sumr;
                     if (!whole)
-                        reinterpret_cast<float2*>(p.part_ml)[prow + tid] = make_float2(ref, sum);
+                        reinterpret_cast<float4*>(p.part_ml)[prow + tid] = make_float4(ref, sum, sumr, 0.0f);
                     else if (p.lse && tid < heads)
                         p.lse[row + tid] = sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
                 }
@@ -417,15 +469,15 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                 role_wait(&x.free[s], (i / g.stages) & 1, abort, p);
                 tc::fence_after_sync();
 #pragma unroll 1
-                for (int c = 0; c < kOCols; c += 16) {
+                for (int c = (warp >> 2) * 16; c < kOCols; c += 32) {
                     float v[16];
                     tc::tmem_ld16(tlane + c, v);
-                    const int dim = (c / kN) * 128 + warp * 32 + lane, hb = c % kN;
+                    const int dim = (c / kN) * 128 + sub * 32 + lane, hb = c % kN;
                     if (whole) {
                         uint16_t* const o = static_cast<uint16_t*>(p.o) + (row + hb) * DV + dim;
 #pragma unroll
                         for (int k = 0; k < 16; ++k)
-                            if (hb + k < heads) o[k * DV] = static_cast<uint16_t>(pack2<kF16>(v[k] * x.sum[hb + k], 0.0f));
+                            if (hb + k < heads) o[k * DV] = static_cast<uint16_t>(pack2<kF16>(v[k] * x.inv[hb + k], 0.0f));
                     } else {
                         float* const o = p.part + (prow + hb) * DV + dim;
 #pragma unroll
@@ -440,12 +492,22 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
         }
         if (group == 0 && tid == 0) p.split[worker] = split;
     }
+    // requests without tokens
+    for (int r = worker; r < p.R; r += g.workers)
+        if (clamped_len(p, r, false) == 0) {
+            uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + (static_cast<size_t>(r) * p.Hq + h0) * DV);
+            for (int i = tid; i < heads * (DV / 8); i += kLatThreads) o[i] = make_uint4(0, 0, 0, 0);
+            if (p.lse)
+                for (int i = tid; i < heads; i += kLatThreads) p.lse[static_cast<size_t>(r) * p.Hq + h0 + i] = -INFINITY;
+        }
+
     tc::fence_before_sync();
     __syncthreads();
-    if (warp == 4) {
-        if (lane == 0 && *abort) {   // products may be under way: wait for them before tensor memory goes back
-            tc::mma_commit(&x.drain);
-            if (!tc::mbar_wait(&x.drain, 0, kDefaultWaitPolls)) raise_status(p.status, QS_DEV_TEARDOWN);
+    if (warp == kLatIssuer) {
+        if (*abort) {   // products may be under way: wait for them before tensor memory goes back
+            const uint32_t lead = elect_lane();
+            commit_by(&x.drain, lead);
+            if (lead && !tc::mbar_wait(&x.drain, 0, kDefaultWaitPolls)) raise_status(p.status, QS_DEV_TEARDOWN);
         }
         __syncwarp();
         tc::fence_after_sync();
@@ -453,60 +515,119 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
     }
 }
 
-// Joins the rows that several CTAs share: a warp for each of a split row's heads.  The CTA that begins a row
-// has left its request and the number of parts.
+// Joins the rows that several CTAs share.  The CTA that begins a row has left its request and the number of
+// parts.  An item is one head of a row of many parts, whose parts the block's warps share out, or eight
+// heads of a row of few, one a warp: either way some dozen loads are in flight for each warp.
+constexpr int kJoinWarps = 8, kFewParts = 8;
+
 template <int DV, bool kF16>
-__global__ void __launch_bounds__(128) kv_latent_join_kernel(const KvAttendParams p, const LatentGeo g, const int kN) {
+__global__ void __launch_bounds__(kJoinWarps * 32) kv_latent_join_kernel(const KvAttendParams p, const LatentGeo g, const int kN) {
+    __shared__ int s_parts[kKvWorkers], s_end[kKvWorkers];
+    __shared__ float4 s_acc[kJoinWarps][DV / 4];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     chain_wait();
-    const int per = (g.per_group + 3) / 4;
-    const int quad = blockIdx.x % per, rest = blockIdx.x / per, group = rest % g.groups, worker = rest / g.groups;
-    const int n = __ldcg(p.split + worker);
-    const int h = quad * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (n < 2 || h >= g.per_group || group * g.per_group + h >= p.Hq) return;
-    const int r = __ldcg(p.split + kKvWorkers + worker);
-    auto at = [&](int i) { return (static_cast<size_t>(part_slot(worker + i, i == 0)) * g.groups + group) * kN + h; };
-    const float2* const ml = reinterpret_cast<const float2*>(p.part_ml);
-    float M = -INFINITY, L = 0.0f;
-    for (int i = lane; i < n; i += 32) M = fmaxf(M, __ldcg(ml + at(i)).x);
+    for (int i = tid; i < g.workers; i += kJoinWarps * 32) s_parts[i] = __ldcg(p.split + i);
+    __syncthreads();
+    if (warp == 0) {
+        int before = 0;
+        for (int i0 = 0; i0 < g.workers; i0 += 32) {
+            const int n = i0 + lane < g.workers ? s_parts[i0 + lane] : 0;
+            int end = n < 2 ? 0 : g.groups * (n <= kFewParts ? (g.per_group + 7) / 8 : g.per_group);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(kFull, M, o));
-    float4 acc[DV / 128] = {};
-    for (int i0 = 0; i0 < n; i0 += 32) {
-        float2 mine = make_float2(-INFINITY, 0.0f);
-        if (i0 + lane < n) mine = __ldcg(ml + at(i0 + lane));
-        const float weight = part_weight(mine.x, M);
-        L += mine.y * weight;
-        const int many = min(32, n - i0);
-#pragma unroll 4
-        for (int i = 0; i < many; ++i) {
-            const float c = __shfl_sync(kFull, weight, i);
-            const float4* const src = reinterpret_cast<const float4*>(p.part + at(i0 + i) * DV) + lane;
-#pragma unroll
-            for (int k = 0; k < DV / 128; ++k) {
-                const float4 v = __ldcg(src + k * 32);
-                acc[k].x += c * v.x;
-                acc[k].y += c * v.y;
-                acc[k].z += c * v.z;
-                acc[k].w += c * v.w;
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(kFull, end, o);
+                if (lane >= o) end += y;
             }
+            if (i0 + lane < g.workers) s_end[i0 + lane] = before + end;
+            before += __shfl_sync(kFull, end, 31);
         }
     }
-    L = warp_sum(L);
-    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-    const size_t row = static_cast<size_t>(r) * p.Hq + group * g.per_group + h;
+    __syncthreads();
+    const int items = s_end[g.workers - 1];
+    const float4* const ml = reinterpret_cast<const float4*>(p.part_ml);   // reference, sums of p
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        int lo = 0;   // first worker whose items end behind this one
+        for (int k = g.workers; k > 0;) {
+            const int half = k >> 1;
+            if (s_end[lo + half] > item) {
+                k = half;
+            } else {
+                lo += half + 1;
+                k -= half + 1;
+            }
+        }
+        const int worker = lo, n = s_parts[worker], r = __ldcg(p.split + kKvWorkers + worker);
+        const bool few = n <= kFewParts;
+        const int per = few ? (g.per_group + 7) / 8 : g.per_group, rel = item - (worker > 0 ? s_end[worker - 1] : 0);
+        const int group = rel / per, h = few ? (rel - group * per) * 8 + warp : rel - group * per;
+        const bool mine = h < g.per_group && group * g.per_group + h < p.Hq;
+        const int i0 = few ? 0 : warp, step = few ? 1 : kJoinWarps;
+        auto at = [&](int i) { return (static_cast<size_t>(part_slot(worker + i, i == 0)) * g.groups + group) * kN + h; };
+        float M = -INFINITY, L = 0.0f, Lr = 0.0f;
+        float4 acc[DV / 128] = {};
+        if (mine) {
+            for (int i = lane; i < n; i += 32) M = fmaxf(M, __ldcg(ml + at(i)).x);
 #pragma unroll
-    for (int k = 0; k < DV / 128; ++k) {
-        uint2 w;
-        w.x = pack2<kF16>(acc[k].x * inv, acc[k].y * inv);
-        w.y = pack2<kF16>(acc[k].z * inv, acc[k].w * inv);
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.o) + row * DV + k * 128 + lane * 4) = w;
+            for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(kFull, M, o));
+            for (int i = lane; i < n; i += 32) {
+                const float4 y = __ldcg(ml + at(i));
+                L += y.y * part_weight(y.x, M);
+                Lr += y.z * part_weight(y.x, M);
+            }
+            L = warp_sum(L);
+            Lr = warp_sum(Lr);
+#pragma unroll 4
+            for (int i = i0; i < n; i += step) {
+                const float c = part_weight(__ldcg(ml + at(i)).x, M);
+                const float4* const src = reinterpret_cast<const float4*>(p.part + at(i) * DV) + lane;
+#pragma unroll
+                for (int k = 0; k < DV / 128; ++k) {
+                    const float4 v = __ldcg(src + k * 32);
+                    acc[k].x += c * v.x;
+                    acc[k].y += c * v.y;
+                    acc[k].z += c * v.z;
+                    acc[k].w += c * v.w;
+                }
+            }
+        }
+        const float inv = Lr == 0.0f ? 0.0f : 1.0f / Lr;
+        const size_t row = static_cast<size_t>(r) * p.Hq + group * g.per_group + h;
+        auto put = [&](int col, const float4& v) {
+            uint2 w;
+            w.x = pack2<kF16>(v.x * inv, v.y * inv);
+            w.y = pack2<kF16>(v.z * inv, v.w * inv);
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.o) + row * DV + col) = w;
+        };
+        if (few) {
+            if (mine)
+#pragma unroll
+                for (int k = 0; k < DV / 128; ++k) put(k * 128 + lane * 4, acc[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < DV / 128; ++k) s_acc[warp][k * 32 + lane] = acc[k];
+            __syncthreads();
+            if (mine && tid < DV / 4) {
+                float4 v = s_acc[0][tid];
+#pragma unroll
+                for (int w = 1; w < kJoinWarps; ++w) {
+                    const float4 y = s_acc[w][tid];
+                    v.x += y.x;
+                    v.y += y.y;
+                    v.z += y.z;
+                    v.w += y.w;
+                }
+                put(tid * 4, v);
+            }
+            __syncthreads();
+        }
+        if (mine && lane == 0 && (few || warp == 0) && p.lse)
+            p.lse[row] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
     }
-    if (lane == 0 && p.lse) p.lse[row] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
 }
 
 // Groups of at most 64 heads, products of 16, 32 or 64 columns; as many tiles in flight as fit beside the
 // queries, and two CTAs on an SM where each gets two.
-inline LatentGeo latent_geo(int Hq, int dk, int dv, int sms, int* cols) {
+inline LatentGeo latent_geo(int Hq, int dk, int sms, int* cols) {
     if (sms > kKvSms) sms = kKvSms;
     LatentGeo g;
     g.groups = (Hq + 63) / 64;
@@ -514,7 +635,7 @@ inline LatentGeo latent_geo(int Hq, int dk, int dv, int sms, int* cols) {
     const int N = g.per_group <= 16 ? 16 : g.per_group <= 32 ? 32 : 64;
     *cols = N;
     g.blocks = (dk + 63) / 64;
-    const int fixed = g.blocks * N * 128 + (dk > dv ? 1 : 2) * N * 128 + static_cast<int>(sizeof(LatentMisc)), tile = g.blocks * kBlockBytes;
+    const int fixed = g.blocks * N * 128 + N * 128 + static_cast<int>(sizeof(LatentMisc)), tile = g.blocks * kBlockBytes;
     constexpr int kMost = 227 * 1024, kHalf = 113 * 1024;
     const int limit = fixed + 2 * tile <= kHalf ? kHalf : kMost;
     g.stages = (limit - fixed) / tile;
@@ -533,14 +654,14 @@ cudaError_t launch_latent(const KvAttendParams& p, const LatentGeo& g, cudaStrea
     if (e != cudaSuccess) return e;
     kernel<<<g.workers * g.groups, kLatThreads, g.smem, stream>>>(p, g);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    const int grid = g.workers * g.groups * ((g.per_group + 3) / 4);
-    return launch_chained(kv_latent_join_kernel<DV, kF16>, grid, 128, 0, stream, true, p, g, kN);
+    const int grid = 2 * device_sm_count();
+    return launch_chained(kv_latent_join_kernel<DV, kF16>, grid, kJoinWarps * 32, 0, stream, true, p, g, kN);
 }
 
 template <int DV>
 cudaError_t launch_latent_of(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream) {
     int N = 0;
-    const LatentGeo g = latent_geo(p.Hq, p.dk, DV, device_sm_count(), &N);
+    const LatentGeo g = latent_geo(p.Hq, p.dk, device_sm_count(), &N);
     const bool f16 = c.dtype == QSTATE_KV_F16;
     if (N == 16) return f16 ? launch_latent<DV, 16, true>(p, g, stream) : launch_latent<DV, 16, false>(p, g, stream);
     if (N == 32) return f16 ? launch_latent<DV, 32, true>(p, g, stream) : launch_latent<DV, 32, false>(p, g, stream);
