@@ -460,13 +460,10 @@ class KvConfig:
     scale: float = 1.0
 
     def __post_init__(self):
-        _keep(self, _KvCfg(self.kind, self.Hq, self.Hkv, self.dk, self.dv, self.page, self.n_pages, self.max_pages,
-                           self.dtype, self.store, self.window, self.scale))
-
-    @property
-    def torch_dtype(self):
         import torch
-        return torch.float16 if self.dtype == KV_F16 else torch.bfloat16
+        _keep(self, _KvCfg(self.kind, self.Hq, self.Hkv, self.dk, self.dv, self.page, self.n_pages, self.max_pages,
+                           self.dtype, self.store, self.window, self.scale),
+              torch_dtype=torch.float16 if self.dtype == KV_F16 else torch.bfloat16, _i32=torch.int32, _f32=torch.float32)
 
 
 def kv_validate(cfg: KvConfig) -> None:
@@ -540,7 +537,8 @@ class KvPages:
     def __post_init__(self):
         import torch
         names = ("table", "lens", "free_list", "free_count")
-        _keep(self, _args=[_typed(getattr(self, n), n, torch.int32) for n in names], R=self.lens.numel())
+        _keep(self, _args=[_typed(getattr(self, n), n, torch.int32) for n in names], R=self.lens.numel(),
+              _sizes=(self.table.numel(), self.free_list.numel()))
 
 
 def new_kv_pages(cfg: KvConfig, R: int, device="cuda") -> KvPages:
@@ -568,7 +566,7 @@ class KvSlots:
         T = self.slot.numel()
         _sized(self.pos, "pos", T)
         _sized(self.req, "req", T)
-        _keep(self, _KvSlots(*ptrs, _typed(self.ok, "ok", torch.uint8), T), T=T)
+        _keep(self, _KvSlots(*ptrs, _typed(self.ok, "ok", torch.uint8), T), T=T, _sizes=(self.cu.numel(), self.ok.numel()))
 
 
 def new_kv_slots(R: int, T: int, device="cuda") -> KvSlots:
@@ -595,59 +593,87 @@ def _work(cfg, work):
     return work.data_ptr()
 
 
+# The three calls of a serving step are short (a launch or two of a few microseconds each), so what they look
+# at is written out here instead of going through a function for each tensor: 5 us of host time a call
+# against 7.
+def _refuse(name, what):
+    raise ValueError(f"{name} must be a contiguous CUDA tensor of {what}")
+
+
 def qstate_kv_plan(cfg: KvConfig, pages: KvPages, n_new, slots: KvSlots, work, lens_out=None, free_out=None,
                    stream=None) -> None:
     """Pages and slots of a step (see include/qstate.h).  The new lengths and free count go to lens_out and
     free_out, in place without them."""
-    import torch
-    R = pages.R
-    if n_new.dtype is not torch.int32 or n_new.numel() != R or pages.table.numel() != R * cfg.max_pages:
-        raise ValueError(f"n_new must be int32 of {R} entries, and the table {R} x {cfg.max_pages}")
-    if pages.free_list.numel() != cfg.n_pages or slots.cu.numel() != R + 1 or slots.ok.numel() != R:
-        raise ValueError(f"free_list must have {cfg.n_pages} entries, cu {R + 1} and ok {R}")
+    R, i32 = pages.R, cfg._i32
+    if n_new.dtype is not i32 or n_new.numel() != R or not n_new.is_cuda or not n_new.is_contiguous():
+        _refuse("n_new", f"{R} int32")
+    if pages._sizes != (R * cfg.max_pages, cfg.n_pages) or slots._sizes != (R + 1, R):
+        raise ValueError(f"table must have {R} x {cfg.max_pages} entries, free_list {cfg.n_pages}, cu {R + 1} and ok {R}")
     table, lens, free_list, free = pages._args
+    to, free_to = lens, free
     if lens_out is not None:
-        _sized(lens_out, "lens_out", R)
-    c = _KvPages(table, lens, lens if lens_out is None else _typed(lens_out, "lens_out", torch.int32), free_list, free,
-                 free if free_out is None else _typed(free_out, "free_out", torch.int32))
-    _check(_lib_or_raise().qstate_kv_plan(cfg._at, ct.addressof(c), _ptr(n_new), R, slots._at, _work(cfg, work),
-                                          _stream(stream)))
+        if lens_out.dtype is not i32 or lens_out.numel() != R or not lens_out.is_cuda or not lens_out.is_contiguous():
+            _refuse("lens_out", f"{R} int32")
+        to = lens_out.data_ptr()
+    if free_out is not None:
+        if free_out.dtype is not i32 or free_out.numel() != 1 or not free_out.is_cuda:
+            _refuse("free_out", "one int32")
+        free_to = free_out.data_ptr()
+    c = _KvPages(table, lens, to, free_list, free, free_to)
+    rc = (_lib or load()).qstate_kv_plan(cfg._at, ct.addressof(c), n_new.data_ptr(), R, slots._at, _work(cfg, work),
+                                         _current_stream() if stream is None else stream.cuda_stream)
+    if rc:
+        _check(rc)
 
 
-def _rows(t, name, cfg, heads, d):
-    """Address, row stride and head stride of a (rows, heads, d) tensor whose entries lie side by side."""
-    if t.dtype is not cfg.torch_dtype or not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor of {cfg.torch_dtype}")
-    shape, (row, head, one) = t.shape, t.stride()
-    if shape[1] != heads or shape[2] != d or one != 1:
-        raise ValueError(f"{name} must be (rows, {heads}, {d}) with entries side by side, got {tuple(shape)}")
-    return t.data_ptr(), row, head
+def _refuse_rows(name, cfg, rows, heads, d):
+    raise ValueError(f"{name} must be a CUDA tensor of {rows} x {heads} x {d} {cfg.torch_dtype} with entries side by side")
 
 
 def qstate_kv_append(cfg: KvConfig, cache: KvCache, k, v, slot, stream=None) -> None:
     """Rows k, v (T, Hkv, d), any strides but the last, into slots slot[0..T); v is None for latents."""
-    import torch
-    cache._check(cfg)
-    T = slot.numel()
-    kp, kr, kh = _rows(k, "k", cfg, cfg.Hkv, cfg.dk)
-    vp, vr, vh = (None, 0, 0) if v is None else _rows(v, "v", cfg, cfg.Hkv, cfg.dv)
-    if k.shape[0] != T or (v is not None and v.shape[0] != T):
-        raise ValueError(f"k and v must have {T} rows")
-    _check(_lib_or_raise().qstate_kv_append(cfg._at, cache._at, kp, kr, kh, vp, vr, vh, _typed(slot, "slot", torch.int32),
-                                            T, _stream(stream)))
+    if cache._fits is not cfg:
+        cache._check(cfg)
+    T, H, dtype = slot.numel(), cfg.Hkv, cfg.torch_dtype
+    if slot.dtype is not cfg._i32 or not slot.is_cuda or not slot.is_contiguous():
+        _refuse("slot", "int32")
+    if k.dtype is not dtype or k.shape != (T, H, cfg.dk) or k.stride(2) != 1 or not k.is_cuda:
+        _refuse_rows("k", cfg, T, H, cfg.dk)
+    kr, kh, _ = k.stride()
+    vp, vr, vh = None, 0, 0
+    if v is not None:
+        if v.dtype is not dtype or v.shape != (T, H, cfg.dv) or v.stride(2) != 1 or not v.is_cuda:
+            _refuse_rows("v", cfg, T, H, cfg.dv)
+        vp = v.data_ptr()
+        vr, vh, _ = v.stride()
+    rc = (_lib or load()).qstate_kv_append(cfg._at, cache._at, k.data_ptr(), kr, kh, vp, vr, vh, slot.data_ptr(), T,
+                                           _current_stream() if stream is None else stream.cuda_stream)
+    if rc:
+        _check(rc)
 
 
 def qstate_kv_attend(cfg: KvConfig, cache: KvCache, q, table, lens, o, lse, work, stream=None) -> None:
     """One token of each request: q (R, Hq, dk), any strides but the last, against its pages; o (R, Hq, dv),
     lse (R, Hq) float32 or None."""
-    import torch
-    cache._check(cfg)
-    R = lens.numel()
-    qp, qr, qh = _rows(q, "q", cfg, cfg.Hq, cfg.dk)
-    if q.shape[0] != R or table.numel() != R * cfg.max_pages:
-        raise ValueError(f"q must have {R} rows, and the table {R} x {cfg.max_pages}")
-    _sized(o, "o", R * cfg.Hq * cfg.dv)
-    _sized(lse, "lse", R * cfg.Hq)
-    _check(_lib_or_raise().qstate_kv_attend(cfg._at, cache._at, qp, qr, qh, _typed(table, "table", torch.int32),
-                                            _typed(lens, "lens", torch.int32), R, _typed(o, "o", cfg.torch_dtype),
-                                            _typed(lse, "lse", torch.float32), _work(cfg, work), _stream(stream)))
+    if cache._fits is not cfg:
+        cache._check(cfg)
+    R, H, dtype, i32 = lens.numel(), cfg.Hq, cfg.torch_dtype, cfg._i32
+    if q.dtype is not dtype or q.shape != (R, H, cfg.dk) or q.stride(2) != 1 or not q.is_cuda:
+        _refuse_rows("q", cfg, R, H, cfg.dk)
+    qr, qh, _ = q.stride()
+    if lens.dtype is not i32 or not lens.is_cuda or not lens.is_contiguous():
+        _refuse("lens", "int32")
+    if table.dtype is not i32 or table.numel() != R * cfg.max_pages or not table.is_cuda or not table.is_contiguous():
+        _refuse("table", f"{R} x {cfg.max_pages} int32")
+    if o.dtype is not dtype or o.numel() != R * H * cfg.dv or not o.is_cuda or not o.is_contiguous():
+        _refuse("o", f"{R} x {H} x {cfg.dv} {dtype}")
+    sums = None
+    if lse is not None:
+        if lse.dtype is not cfg._f32 or lse.numel() != R * H or not lse.is_cuda or not lse.is_contiguous():
+            _refuse("lse", f"{R} x {H} float32")
+        sums = lse.data_ptr()
+    rc = (_lib or load()).qstate_kv_attend(cfg._at, cache._at, q.data_ptr(), qr, qh, table.data_ptr(), lens.data_ptr(), R,
+                                           o.data_ptr(), sums, _work(cfg, work),
+                                           _current_stream() if stream is None else stream.cuda_stream)
+    if rc:
+        _check(rc)

@@ -127,10 +127,9 @@ cudaError_t quant_decay_scratch(float** out);
 // ---- paged cache of attention layers (qs_kv_*.cu) ---------------------------------------------
 // Head of the work space: int32 counters, all zero between calls.
 constexpr int kKvTicket = 0;          // qstate_kv_plan in place: CTAs that have read the old lengths
-constexpr int kKvJoin = 64;           // qstate_kv_attend: parts that are done, by first worker
 constexpr int kKvSms = 152;           // SMs that an attention launch takes at most
 constexpr int kKvWorkers = 4 * kKvSms;  // and its CTAs
-constexpr int kKvHeadBytes = 8192;    // 64 + 3 * kKvWorkers counters
+constexpr int kKvHeadBytes = 4096;
 constexpr int kKvMaxRequests = 8192;
 
 struct KvPlanParams {
@@ -167,10 +166,11 @@ struct KvAttendParams {
     float* lse;
     int R, Hq, Hkv, dk, dv, page_shift, n_pages, max_pages, window;
     float scale;
-    int* join;       // counters of the work space
     float* part;     // partial results: sums, then references and weights
     float* part_ml;
-    int* split;      // latents: parts of the row that a worker begins (0: not split), and its request
+    int* split;      // parts of the row that a worker begins (0: not split), and the row
+    int workers;     // how many share the work out
+    int whole_rows;  // by rows instead of tiles: no row is split
     int q_aligned;   // q can be read in 16 bytes
     int wait_polls;  // limit of the latent kernel's waits for copies and products
     int* status;

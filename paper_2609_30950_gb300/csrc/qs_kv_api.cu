@@ -179,7 +179,6 @@ int qstate_kv_attend(const qstate_kv_cfg* cfg, const qstate_kv_cache* cache, con
     p.max_pages = cfg->max_pages;
     p.window = cfg->window;
     p.scale = cfg->scale;
-    p.join = static_cast<int*>(work) + kKvJoin;
     p.part = reinterpret_cast<float*>(static_cast<char*>(work) + kKvHeadBytes);
     const KvPartBytes bytes = kv_part_bytes(*cfg);
     p.part_ml = p.part + bytes.sums / sizeof(float);

@@ -5,8 +5,8 @@
 // operations a byte in 16 bits, so the cache's bytes are the bound up to G of about 140.
 //
 // Tiles (qs_kv_tiles.cuh) of 64 tokens (128 in e4m3) of one request and key head, up to 16 query heads
-// as the 16 rows of the matrix products; more query heads are further groups, which find the tile
-// in L2.  A tile is four chunks, one a warp.  Each warp keeps its own ring of chunks (cp.async, zeros in
+// as the 16 rows of the matrix products; more query heads are further rows of work, which read the
+// tile again.  A tile is four chunks, one a warp.  Each warp keeps its own ring of chunks (cp.async, zeros in
 // place of what is not to be seen, rows swizzled so that neither the copies nor the fragment loads
 // meet in a bank) and its own m, sums and o, so that warps meet only where a row of work ends: there
 // they lay their o into the ring's slot just used and join it.
@@ -38,15 +38,15 @@ struct HeadsShape {
     static constexpr int kRow = kE4M3 ? D : 2 * D, kSeg = kRow / 16;
     static constexpr int kTensor = kChunk * kRow, kSlot = 2 * kTensor;   // 64 D bytes: 16 x D floats
     static constexpr int kRing = kWarps * kStages * kSlot;
-    static constexpr int kQ = kRing, kExps = kQ + kHeadRows * 2 * D;
+    // queries: of the row that begins in a stage, and at 256 entries, too many to hold in registers, of this row
+    static constexpr int kQBytes = kHeadRows * 2 * D, kQ = kRing, kQRow = kQ + kStages * kQBytes;
+    static constexpr int kExps = kQRow + (D > 128 ? kQBytes : 0);
     static constexpr int kMl = kExps + (kE4M3 ? kWarps * kStages * 64 : 0);
-    static constexpr int kWeights = kMl + kWarps * kHeadRows * 16;       // join: weights of parts
-    static constexpr int kMaxParts = (kKvWorkers + kJoinFan - 1) / kJoinFan;
-    static constexpr int kRowSums = kWeights + kHeadRows * kMaxParts * 4;
-    static constexpr int kQScale = kRowSums + kHeadRows * 16;
+    static constexpr int kQScale = kMl + kWarps * kHeadRows * 16;
     static constexpr int kMasks = kQScale + kHeadRows * 4;
     static constexpr int kScratch = kMasks + kWarps * kStages * 4 + 16 - (kWarps * kStages * 4) % 16;
-    static constexpr int kBytes = kScratch + 16 * 8;
+    static constexpr int kShare = kScratch + 8 * 8;
+    static constexpr int kBytes = kShare + (sizeof(Share) + 15) / 16 * 16;
 
     // byte of 16-byte piece `seg` of a row in a tile: eight rows at one piece, and two rows at four pieces,
     // lie in different banks
@@ -63,53 +63,6 @@ struct HeadsShape {
     }
 };
 
-// Joins n parts of a row, CTA first + i stride holding part i; fin(row, 4 columns, sum, M of the values, M, L).
-template <class S, int D, class Fin>
-__device__ void join_parts(const KvAttendParams& p, char* smem, int heads, int first, int stride, int n, bool first_holds_1,
-                           Fin fin) {
-    float* const weights = reinterpret_cast<float*>(smem + S::kWeights);
-    float4* const sums = reinterpret_cast<float4*>(smem + S::kRowSums);
-    const float4* const ml = reinterpret_cast<const float4*>(p.part_ml);
-    const int row = threadIdx.x >> 3, i0 = threadIdx.x & 7;   // 8 threads a head
-    auto slot_of = [&](int i) { return part_slot(first + i * stride, i == 0 && first_holds_1); };
-    float Mo = -INFINITY, M = -INFINITY, L = 0.0f;
-    for (int i = i0; i < n; i += 8) {
-        const float4 x = __ldcg(ml + slot_of(i) * kHeadRows + row);
-        Mo = fmaxf(Mo, x.x);
-        M = fmaxf(M, x.y);
-    }
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
-        Mo = fmaxf(Mo, __shfl_xor_sync(kFull, Mo, o));
-        M = fmaxf(M, __shfl_xor_sync(kFull, M, o));
-    }
-    for (int i = i0; i < n; i += 8) {
-        const float4 x = __ldcg(ml + slot_of(i) * kHeadRows + row);
-        L += x.z * part_weight(x.y, M);
-        weights[row * S::kMaxParts + i] = part_weight(x.x, Mo);
-    }
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) L += __shfl_xor_sync(kFull, L, o);
-    if (i0 == 0) sums[row] = make_float4(Mo, M, L, 0.0f);
-    __syncthreads();
-    for (int idx = threadIdx.x; idx < heads * (D / 4); idx += S::kThreads) {
-        const int r = idx / (D / 4);
-        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-        for (int i = 0; i < n; ++i) {
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(p.part) +
-                                    static_cast<size_t>(slot_of(i)) * (kHeadRows * D / 4) + idx);
-            const float w = weights[r * S::kMaxParts + i];
-            acc.x += w * x.x;
-            acc.y += w * x.y;
-            acc.z += w * x.z;
-            acc.w += w * x.w;
-        }
-        fin(r, (idx - r * (D / 4)) * 4, acc, sums[r]);
-    }
-    __syncthreads();
-}
-
 template <int D, bool kF16, bool kE4M3, bool kHalf, int kStages, int kCtas>
 __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendParams p, const int per_group, const int groups_per_kv) {
     using S = HeadsShape<D, kE4M3, kStages>;
@@ -118,23 +71,17 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
     constexpr int kSteps = D / 16, kOut = D / 8;
     constexpr float kLog2e = 1.4426950408889634f;
     extern __shared__ __align__(128) char smem[];
+    chain_release();   // the kernel that joins split rows may take its place
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane >> 2, t4 = lane & 3;
     const int groups = p.Hkv * groups_per_kv, G = p.Hq / p.Hkv;
 
-    const Share share = make_share<S::kThreads, S::kTile, S::kChunk>(p, groups, blockIdx.x, gridDim.x, reinterpret_cast<long long*>(smem + S::kScratch));
-    auto empty_rows = [&]() {   // requests without tokens
-        for (int r = blockIdx.x; r < p.R; r += gridDim.x)
-            if (clamped_len(p, r, false) == 0) {
-                uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + static_cast<size_t>(r) * p.Hq * D);
-                for (int i = tid; i < p.Hq * (D / 8); i += S::kThreads) o[i] = make_uint4(0, 0, 0, 0);
-                if (p.lse)
-                    for (int i = tid; i < p.Hq; i += S::kThreads) p.lse[static_cast<size_t>(r) * p.Hq + i] = -INFINITY;
-            }
-    };
-    if (share.u0 >= share.u1) {
-        empty_rows();
-        return;
-    }
+    Share& share = *reinterpret_cast<Share*>(smem + S::kShare);
+    if (!p.whole_rows)
+        make_share<S::kThreads, S::kTile, S::kChunk>(p, groups, blockIdx.x, reinterpret_cast<long long*>(smem + S::kScratch), &share);
+    int split = 0;   // parts of the row that this CTA begins and others end
+    Walk<S::kTile, S::kChunk> cw;
+    bool live = cw.start(p, share, groups, blockIdx.x);
+    bool fetching = live;
 
     char* const ring = smem + warp * (kStages * S::kSlot);
     const uint32_t ring32 = smem_u32(ring);
@@ -144,8 +91,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
     const bool one_page = (1 << p.page_shift) >= S::kChunk;   // a chunk lies in one page
 
     // ---- copies ----
-    Walk<S::kTile, S::kChunk> fw;
-    fw.start(p, share);
+    Walk<S::kTile, S::kChunk> fw = cw;
     int id = -1;
     auto look_up = [&]() {   // page of this lane's token in the chunk to come
         const int t = fw.span.base + (fw.tile * S::kWarps + warp) * S::kChunk + (one_page ? 0 : lane);
@@ -153,7 +99,23 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
         if (t < fw.span.end && (one_page || lane < S::kChunk))
             id = __ldg(p.table + static_cast<size_t>(fw.r) * p.max_pages + (t >> p.page_shift));
     };
+    // Queries of a row that begins: thread tid copies pieces tid % 8 + 8 i of head tid / 8 (and finds them there).
+    auto q_src = [&](const Walk<S::kTile, S::kChunk>& w, int* heads) {
+        const int hk = w.group / groups_per_kv, part = w.group - hk * groups_per_kv;
+        *heads = min(per_group, G - part * per_group);
+        return static_cast<const uint16_t*>(p.q) + w.r * p.q_row + (hk * G + part * per_group + (tid >> 3)) * p.q_head;
+    };
+    bool row_begins = true;
     auto fetch = [&](int stage) {
+        if (row_begins && p.q_aligned) {
+            int heads;
+            const uint16_t* const src = q_src(fw, &heads);
+            const bool in = (tid >> 3) < heads;
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i)
+                cp_async16(smem_u32(smem + S::kQ + stage * S::kQBytes + S::q_at(tid >> 3, i * 8 + (tid & 7))),
+                           in ? src + (i * 8 + (tid & 7)) * 8 : p.q, in);
+        }
         const int t0 = fw.span.base + (fw.tile * S::kWarps + warp) * S::kChunk, t = t0 + lane;
         const int hk = fw.group / groups_per_kv;
         const bool seen = lane < S::kChunk && t >= fw.span.begin && t < fw.span.end;
@@ -197,15 +159,13 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
             }
         }
     };
-    look_up();
-    long long fetched = share.u0;
+    if (fetching) look_up();
     auto fetch_next = [&](int stage) {
-        if (fetched < share.u1) {
+        if (fetching) {
             fetch(stage);
-            if (++fetched < share.u1) {
-                fw.next(p, groups);
-                look_up();
-            }
+            row_begins = fw.ends(p);
+            fetching = fw.next(p, groups);
+            if (fetching) look_up();
         }
         cp_commit();
     };
@@ -213,81 +173,82 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
     for (int s = 0; s < kStages; ++s) fetch_next(s);
 
     // ---- products ----
-    Walk<S::kTile, S::kChunk> cw;
-    cw.start(p, share);
     uint32_t qf[kQInRegs ? kSteps : 1][4];
     float o[kOut][4], m[2], mo[2], l[2], zs[2];
     int stage = 0, heads = 0, h0 = 0, began = -1;
-    const uint32_t q32 = smem_u32(smem + S::kQ);
+    const char* qs = smem + S::kQ;   // this row's queries
 
     auto q_frag = [&](uint32_t (&a)[4], int ks) {
         if (!kE4M3) {
-            ldsm4(a, q32 + S::q_at((lane & 7) + ((lane >> 3) & 1) * 8, ks * 2 + (lane >> 4)));
+            ldsm4(a, smem_u32(qs) + S::q_at((lane & 7) + ((lane >> 3) & 1) * 8, ks * 2 + (lane >> 4)));
         } else {
             // columns t4 16 + 4 (ks % 4) ... + 3 of 64-column block ks / 4: the order in which a lane finds its codes
             const int col = (ks >> 2) * 64 + t4 * 16 + (ks & 3) * 4;
-            const uint2 x = *reinterpret_cast<const uint2*>(smem + S::kQ + S::q_at(quad, col >> 3) + (col & 7) * 2);
-            const uint2 y = *reinterpret_cast<const uint2*>(smem + S::kQ + S::q_at(quad + 8, col >> 3) + (col & 7) * 2);
+            const uint2 x = *reinterpret_cast<const uint2*>(qs + S::q_at(quad, col >> 3) + (col & 7) * 2);
+            const uint2 y = *reinterpret_cast<const uint2*>(qs + S::q_at(quad + 8, col >> 3) + (col & 7) * 2);
             a[0] = x.x, a[1] = y.x, a[2] = x.y, a[3] = y.y;
         }
     };
 
-    for (long long u = share.u0; u < share.u1; ++u) {
+    while (live) {
+        cp_wait<kStages - 1>();
         if (began < 0) {   // a row of work begins: its queries
             began = cw.tile;
-            const int hk = cw.group / groups_per_kv, part = cw.group - hk * groups_per_kv;
-            h0 = hk * G + part * per_group;
-            heads = min(per_group, G - part * per_group);
+            const uint16_t* const src = q_src(cw, &heads);
+            h0 = cw.group / groups_per_kv * G + cw.group % groups_per_kv * per_group;
             const int row = tid >> 3, piece = tid & 7;
-            const uint16_t* const src = static_cast<const uint16_t*>(p.q) + cw.r * p.q_row + (h0 + row) * p.q_head;
-            uint4 x[D / 64];
-            float top = 0.0f;
+            char* const landed = smem + S::kQ + stage * S::kQBytes;
+            char* const kept = kQInRegs ? landed : smem + S::kQRow;
+            if (kE4M3 || !kQInRegs || !p.q_aligned) {
+                uint4 x[D / 64];
 #pragma unroll
-            for (int i = 0; i < D / 64; ++i) {
-                const int e = (i * 8 + piece) * 8;
-                x[i] = make_uint4(0, 0, 0, 0);
-                if (row < heads) {
+                for (int i = 0; i < D / 64; ++i) {
                     if (p.q_aligned) {
-                        x[i] = *reinterpret_cast<const uint4*>(src + e);
+                        x[i] = *reinterpret_cast<const uint4*>(landed + S::q_at(row, i * 8 + piece));
                     } else {
                         uint32_t w[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) w[j] = src[e + 2 * j] | static_cast<uint32_t>(src[e + 2 * j + 1]) << 16;
+                        for (int j = 0; j < 4; ++j) {
+                            const uint16_t* const e = src + (i * 8 + piece) * 8 + 2 * j;
+                            w[j] = row < heads ? e[0] | static_cast<uint32_t>(e[1]) << 16 : 0u;
+                        }
                         x[i] = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                 }
-            }
-            if (kE4M3) {
-                unsigned big = 0;   // |q| as integers order as the numbers do
+                if (kE4M3) {
+                    unsigned big = 0;   // |q| as integers order as the numbers do
 #pragma unroll
-                for (int i = 0; i < D / 64; ++i) {
-                    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                    for (int i = 0; i < D / 64; ++i) {
+                        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) big = max(big, max(w[j] << 16 & 0x7fffffffu, w[j] & 0x7fff0000u));
-                }
-#pragma unroll
-                for (int s = 1; s < 8; s <<= 1) big = max(big, __shfl_xor_sync(kFull, big, s));
-                const int e = big == 0 ? 0 : min(max(static_cast<int>(big >> 23) - 127, -126), 126);
-                const float inv = __uint_as_float(static_cast<unsigned>(127 - e) << 23);
-#pragma unroll
-                for (int i = 0; i < D / 64; ++i) {
-                    uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 y = unpack2<false>(w[j]);
-                        w[j] = pack2<true>(y.x * inv, y.y * inv);
+                        for (int j = 0; j < 4; ++j) big = max(big, max(w[j] << 16 & 0x7fffffffu, w[j] & 0x7fff0000u));
                     }
-                    x[i] = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-                top = __uint_as_float(static_cast<unsigned>(127 + e) << 23);
-                if (piece == 0) reinterpret_cast<float*>(smem + S::kQScale)[row] = top;
-            }
 #pragma unroll
-            for (int i = 0; i < D / 64; ++i) *reinterpret_cast<uint4*>(smem + S::kQ + S::q_at(row, i * 8 + piece)) = x[i];
+                    for (int s = 1; s < 8; s <<= 1) big = max(big, __shfl_xor_sync(kFull, big, s));
+                    const int e = big == 0 ? 0 : min(max(static_cast<int>(big >> 23) - 127, -126), 126);
+                    const float inv = __uint_as_float(static_cast<unsigned>(127 - e) << 23);
+#pragma unroll
+                    for (int i = 0; i < D / 64; ++i) {
+                        uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float2 y = unpack2<false>(w[j]);
+                            w[j] = pack2<true>(y.x * inv, y.y * inv);
+                        }
+                        x[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                    if (piece == 0)
+                        reinterpret_cast<float*>(smem + S::kQScale)[row] = __uint_as_float(static_cast<unsigned>(127 + e) << 23);
+                }
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) *reinterpret_cast<uint4*>(kept + S::q_at(row, i * 8 + piece)) = x[i];
+            }
             __syncthreads();
+            qs = kept;
             if (kQInRegs) {
 #pragma unroll
                 for (int ks = 0; ks < kSteps; ++ks) q_frag(qf[ks], ks);
+                __syncthreads();   // a warp ahead may have this buffer refilled
             }
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
@@ -301,8 +262,6 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
 #pragma unroll
                 for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
         }
-
-        cp_wait<kStages - 1>();
         __syncwarp();
         const uint32_t mask = masks[stage];
         const uint32_t kt = ring32 + stage * S::kSlot, vt = kt + S::kTensor;
@@ -448,8 +407,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
             }
         }
 
-        const bool row_ends = cw.tile == cw.span.tiles - 1;
-        if (row_ends || u + 1 == share.u1) {
+        if (cw.ends(p)) {
             // ---- the warps' parts of this row ----
             float* const mine = reinterpret_cast<float*>(ring + stage * S::kSlot);
             float4* const ml = reinterpret_cast<float4*>(smem + S::kMl);
@@ -487,10 +445,16 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
                 if (col == 0 && p.lse)
                     p.lse[out_row + row] = sums.z == 0.0f ? -INFINITY : (sums.y + log2f(sums.z)) * 0.6931471805599453f;
             };
-            const bool whole = began == 0 && row_ends;
-            const long long row_start = u - cw.tile;
-            const Joint j = whole ? Joint{0, 1} : joint_of(share.total, row_start, cw.span.tiles, gridDim.x);
-            const int me = static_cast<int>(blockIdx.x) - j.first, slot = part_slot(blockIdx.x, me == 0);
+            const bool whole = began == 0 && cw.tile == cw.span.tiles - 1;
+            int slot = 0;
+            if (!whole) {
+                const Joint j = joint_of(p, share, cw.left, cw.tile, cw.span.tiles);
+                slot = part_slot(blockIdx.x, j.first == static_cast<int>(blockIdx.x));
+                if (j.first == static_cast<int>(blockIdx.x)) {
+                    split = j.n;
+                    if (tid == 0) p.split[kKvWorkers + blockIdx.x] = cw.r * groups + cw.group;
+                }
+            }
             for (int idx = tid; idx < heads * (D / 4); idx += S::kThreads) {
                 const int row = idx / (D / 4), col = (idx - row * (D / 4)) * 4;
                 float4 x[S::kWarps];
@@ -512,31 +476,12 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
                     acc.z += c * v.z;
                     acc.w += c * v.w;
                 }
-                const float4 sums = make_float4(Mo, M, L, 0.0f);
+                const float4 sums = make_float4(Mo, M, L, L);
                 if (whole) {
                     finish(row, col, acc, sums);
                 } else {
                     reinterpret_cast<float4*>(p.part)[static_cast<size_t>(slot) * (kHeadRows * D / 4) + idx] = acc;
                     if (col == 0) reinterpret_cast<float4*>(p.part_ml)[slot * kHeadRows + row] = sums;
-                }
-            }
-            if (!whole) {
-                int* const flag = reinterpret_cast<int*>(smem + S::kScratch);
-                int* const join = p.join;
-                if (j.n <= kJoinFan) {
-                    if (arrive_last(join + j.first, j.n, flag)) join_parts<S, D>(p, smem, heads, j.first, 1, j.n, true, finish);
-                } else {
-                    const int g = me / kJoinFan, lead = j.first + g * kJoinFan, many = min(kJoinFan, j.n - g * kJoinFan);
-                    if (arrive_last(join + (g == 0 ? kKvWorkers : 2 * kKvWorkers) + lead, many, flag)) {
-                        const int to = part_slot(lead, g == 0);
-                        join_parts<S, D>(p, smem, heads, lead, 1, many, g == 0, [&](int row, int col, float4 acc, float4 sums) {
-                            reinterpret_cast<float4*>(p.part)[static_cast<size_t>(to) * (kHeadRows * D / 4) + row * (D / 4) + col / 4] = acc;
-                            if (col == 0) reinterpret_cast<float4*>(p.part_ml)[to * kHeadRows + row] = sums;
-                        });
-                        const int leads = (j.n + kJoinFan - 1) / kJoinFan;
-                        if (arrive_last(join + j.first, leads, flag))
-                            join_parts<S, D>(p, smem, heads, j.first, kJoinFan, leads, true, finish);
-                    }
                 }
             }
             began = -1;
@@ -545,21 +490,35 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
         __syncwarp();
         fetch_next(stage);
         stage = stage + 1 == kStages ? 0 : stage + 1;
-        if (u + 1 < share.u1) cw.next(p, groups);
+        live = cw.next(p, groups);
     }
-    empty_rows();
+    for (int r = blockIdx.x; r < p.R; r += p.workers)   // requests without tokens
+        if (clamped_len(p, r, true) == 0) {
+            uint4* out = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + static_cast<size_t>(r) * p.Hq * D);
+            for (int i = tid; i < p.Hq * (D / 8); i += S::kThreads) out[i] = make_uint4(0, 0, 0, 0);
+            if (p.lse)
+                for (int i = tid; i < p.Hq; i += S::kThreads) p.lse[static_cast<size_t>(r) * p.Hq + i] = -INFINITY;
+        }
+    if (!p.whole_rows && tid == 0) p.split[blockIdx.x] = split;
     cp_wait<0>();
 }
 
 template <int D, bool kF16, bool kE4M3, bool kHalf, int kStages, int kCtas>
-cudaError_t launch_heads(const KvAttendParams& p, int per_group, int groups_per_kv, cudaStream_t stream) {
+cudaError_t launch_heads(KvAttendParams p, int per_group, int groups_per_kv, cudaStream_t stream) {
     using S = HeadsShape<D, kE4M3, kStages>;
     auto* kernel = kv_heads_kernel<D, kF16, kE4M3, kHalf, kStages, kCtas>;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
     if (e != cudaSuccess) return e;
     const int ctas = device_sm_count() * kCtas;
-    kernel<<<ctas < kKvWorkers ? ctas : kKvWorkers, S::kThreads, S::kBytes, stream>>>(p, per_group, groups_per_kv);
-    return cudaGetLastError();
+    p.workers = ctas < kKvWorkers ? ctas : kKvWorkers;
+    p.whole_rows = (static_cast<long long>(p.max_pages) << p.page_shift) <= kWholeTiles * S::kTile;
+    if (p.whole_rows) {
+        const long long rows = static_cast<long long>(p.R) * p.Hkv * groups_per_kv;
+        if (rows < p.workers) p.workers = static_cast<int>(rows);
+    }
+    kernel<<<p.workers, S::kThreads, S::kBytes, stream>>>(p, per_group, groups_per_kv);
+    if ((e = cudaGetLastError()) != cudaSuccess || p.whole_rows) return e;
+    return launch_join<D, kF16>(p, JoinGeo{1, kHeadRows, per_group, p.Hq / p.Hkv, groups_per_kv}, stream);
 }
 
 // Heads of a group: G / ceil(G / 16), rounded up; up to 8 of them leave half of the products' rows free.

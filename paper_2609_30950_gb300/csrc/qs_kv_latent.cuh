@@ -39,14 +39,15 @@ constexpr float kLazyLatent = 8.0f;
 
 struct LatentGeo {
     int blocks;        // of 64 entries, the last may be half
-    int stages, smem, groups, per_group, workers;
+    int stages, smem, groups, per_group, columns, workers;
 };
 
 // Shared memory behind the tiles, the queries and p.
 struct LatentMisc {
     uint64_t full[kMaxStages], free[kMaxStages], sready[2], pready, drain;
     uint64_t mask[kMaxStages];
-    float top[4][64], topr[4][64], corr[64], ref[64], inv[64];
+    float top[4][64], topr[4][64], corr[64], inv[64];   // corr: the references at a row's end
+    Share share;
     uint32_t tmem;
     int abort;
 };
@@ -182,29 +183,29 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
         tc::mbar_fence_init();
         x.abort = 0;
     }
-    const Share share = make_share<kLatThreads, kLatTile, 1>(p, 1, worker, g.workers, reinterpret_cast<long long*>(x.top));
+    if (!p.whole_rows) make_share<kLatThreads, kLatTile, 1>(p, 1, worker, reinterpret_cast<long long*>(x.top), &x.share);
+    const Share& share = x.share;
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
     const uint32_t tmem = x.tmem;
-    const int n = static_cast<int>(share.u1 - share.u0);
     volatile int* const abort = &x.abort;
-    if (group == 0 && tid == 0 && n <= 0) p.split[worker] = 0;
+    W w;
+    bool live = w.start(p, share, 1, worker);
+    int split = 0;   // parts of the row that this CTA begins and others end
 
-    if (n > 0 && warp > kLatIssuer) {
+    if (live && warp > kLatIssuer) {
         // ---- copies ----
         const int pw = warp - kLatIssuer - 1, page_mask = (1 << p.page_shift) - 1;
-        W w;
-        w.start(p, share);
         auto look_up = [&]() {
             const int t = w.span.base + w.tile * kLatTile + pw * 16 + lane;
             return lane < 16 && t < w.span.end ? __ldg(p.table + static_cast<size_t>(w.r) * p.max_pages + (t >> p.page_shift)) : -1;
         };
         int id = look_up(), s = 0;
-        for (int i = 0; i < n; ++i) {
+        bool begins = true;
+        for (int i = 0; live; ++i) {
             bool ok = i < g.stages || role_wait(&x.free[s], (i / g.stages - 1) & 1, abort, p);
             const int r = w.r, t = w.span.base + w.tile * kLatTile + pw * 16 + lane;
-            const bool begins = i == 0 || w.tile == 0;
             const bool seen = lane < 16 && t < w.span.end, there = id >= 0 && id < p.n_pages;
             if (seen && !there) raise_status(p.status, QS_DEV_PAGES);
             const uint32_t on = __ballot_sync(kFull, seen && there) & 0xffffu;
@@ -215,14 +216,14 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 src[k] = static_cast<const char*>(p.k) + __shfl_sync(kFull, mine, k * 4 + row0) * (2 * p.dk) + seg * 16;
-            if (i + 1 < n) {
-                w.next(p, 1);
-                id = look_up();
-            }
+            const bool first = begins;
+            begins = w.ends(p);
+            live = w.next(p, 1);
+            if (live) id = look_up();
             // the queries of the row before are no longer read once S of its last tile is there
-            if (begins && i > 0) ok = ok && role_wait(&x.sready[(i - 1) & 1], ((i - 1) >> 1) & 1, abort, p);
+            if (first && i > 0) ok = ok && role_wait(&x.sready[(i - 1) & 1], ((i - 1) >> 1) & 1, abort, p);
             if (ok) {
-                if (begins) {
+                if (first) {
                     const uint16_t* const q = static_cast<const uint16_t*>(p.q) + r * p.q_row + h0 * p.q_head;
                     for (int b = 0; b < g.blocks; ++b)
                         for (int e = pw * 32 + lane; e < kN * 8; e += kLatCopiers * 32) {
@@ -257,15 +258,13 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
         }
         cp_commit();
         cp_wait<0>();
-    } else if (n > 0 && warp == kLatIssuer) {
+    } else if (live && warp == kLatIssuer) {
         // ---- products ----
         constexpr uint32_t idS = idesc_f16(kF16, 64, kN, false), idO = idesc_f16(kF16, 128, kN, true);
         const uint32_t lead = elect_lane(), tile_bytes = g.blocks * kBlockBytes;
         const uint32_t q32 = smem_u32(queries), p32 = smem_u32(probs), t32 = smem_u32(tiles);
         const uint64_t dq = desc_sw128(q32, 16, 1024), dp = desc_sw128(p32, 16, 1024);
         const int full_blocks = p.dk >> 6;
-        W w;
-        w.start(p, share);
         int ss = 0, so = 0;   // stages of the tiles whose S and whose O come next
         auto scores = [&](int i) {
             tc::fence_async_smem();   // the copies' writes, for the tensor core's reads
@@ -296,33 +295,33 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
         };
         // S runs one tile ahead of O where that tile is there, and never makes O wait for it: with two tiles in
         // flight the copy of the next one waits for O
-        int is = 0, full_phase = 0, idle = 0;
-        bool live = true;
-        for (int io = 0; io < n && live;) {
+        W ahead = w;
+        int is = 0, io = 0, full_phase = 0, idle = 0;   // tiles whose S and whose O have been issued
+        bool more = true, begins = true;
+        while (live) {
             bool did = false;
-            if (is < n && is <= io + 1 && warp_test(&x.full[ss], full_phase)) {
-                const int at = ss;
+            if (more && is <= io + 1 && warp_test(&x.full[ss], full_phase)) {
+                if (ss + 1 == g.stages) full_phase ^= 1;
                 scores(is++);
-                if (at + 1 == g.stages) full_phase ^= 1;
+                more = ahead.next(p, 1);
                 did = true;
             }
             if (io < is && warp_test(&x.pready, io & 1)) {
-                values(io == 0 || w.tile == 0);
-                if (++io < n) w.next(p, 1);
+                values(begins);
+                ++io;
+                begins = w.ends(p);
+                live = w.next(p, 1);
                 did = true;
             }
-            if (!did) {
-                if (++idle > p.wait_polls || *abort) {
-                    if (!*abort) raise_status(p.status, QS_DEV_TIMEOUT);
-                    *abort = 1;
-                    live = false;
-                }
-            } else {
-                idle = 0;
+            idle = did ? 0 : idle + 1;
+            if (idle > p.wait_polls || *abort) {
+                if (!*abort) raise_status(p.status, QS_DEV_TIMEOUT);
+                *abort = 1;
+                live = false;
             }
             live = __all_sync(kFull, live);
         }
-    } else if (n > 0) {
+    } else if (live && warp < kLatIssuer) {
         // ---- softmax ----
         const int quad = lane >> 2, t4 = lane & 3, sub = warp & 3, c0 = (warp >> 2) * (kN / 2);   // token quarter, first head
         const uint32_t tlane = tmem + (static_cast<uint32_t>(32 * sub) << 16);
@@ -330,13 +329,12 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
         const float zs = p.scale * kLog2e;
         // sums of p before and after its rounding
         float m[kPer], l[kPer], lr[kPer];
-        int prev = 0, s = 0, began = 0, split = 0;   // prev: stage of the tile before
+        int prev = 0, s = 0, began = 0;   // prev: stage of the tile before
+        bool begins = true;
         // k: head c0 + 8 (k / 2) + 2 t4 + k % 2, at tokens quad and quad + 8 of the quarter
         auto head = [&](int k) { return c0 + 8 * (k >> 1) + 2 * t4 + (k & 1); };
-        W w;
-        w.start(p, share);
-        for (int i = 0; i < n; ++i) {
-            const bool begins = i == 0 || w.tile == 0, row_ends = w.tile == w.span.tiles - 1, ends = row_ends || i + 1 == n;
+        for (int i = 0; live; ++i) {
+            const bool ends = w.ends(p);
             if (begins) {
                 began = w.tile;
 #pragma unroll
@@ -439,31 +437,30 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                     if (quad == 0) {
                         x.top[sub][h] = sum;
                         x.topr[sub][h] = sumr;
-                        if (sub == 0) x.ref[h] = m[k];
+                        if (sub == 0) x.corr[h] = m[k];
                     }
                 }
                 softmax_sync();
-                const bool whole = began == 0 && row_ends;
-                int slot = 0, parts = 0;
+                const bool whole = began == 0 && w.tile == w.span.tiles - 1;
+                int slot = 0;
                 if (!whole) {
-                    const Joint jt = joint_of(share.total, share.u0 + i - w.tile, w.span.tiles, g.workers);
-                    slot = part_slot(worker, jt.first == worker);
-                    if (jt.first == worker) parts = jt.n;
+                    const Joint j = joint_of(p, share, w.left, w.tile, w.span.tiles);
+                    slot = part_slot(worker, j.first == worker);
+                    if (j.first == worker) {
+                        split = j.n;
+                        if (group == 0 && tid == 0) p.split[kKvWorkers + worker] = w.r * g.groups;
+                    }
                 }
                 const size_t row = static_cast<size_t>(w.r) * p.Hq + h0;
                 const size_t prow = (static_cast<size_t>(slot) * g.groups + group) * kN;
                 if (tid < kN) {
-                    const float sum = x.top[0][tid] + x.top[1][tid] + x.top[2][tid] + x.top[3][tid], ref = x.ref[tid];
+                    const float sum = x.top[0][tid] + x.top[1][tid] + x.top[2][tid] + x.top[3][tid], ref = x.corr[tid];
                     const float sumr = x.topr[0][tid] + x.topr[1][tid] + x.topr[2][tid] + x.topr[3][tid];
                     x.inv[tid] = sumr == 0.0f ? 0.0f : 1.0f / sumr;
                     if (!whole)
-                        reinterpret_cast<float4*>(p.part_ml)[prow + tid] = make_float4(ref, sum, sumr, 0.0f);
+                        reinterpret_cast<float4*>(p.part_ml)[prow + tid] = make_float4(ref, ref, sum, sumr);
                     else if (p.lse && tid < heads)
                         p.lse[row + tid] = sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
-                }
-                if (parts) {   // the row that this CTA begins and others end
-                    split = parts;
-                    if (group == 0 && tid == 0) p.split[kKvWorkers + worker] = w.r;
                 }
                 softmax_sync();
                 role_wait(&x.free[s], (i / g.stages) & 1, abort, p);
@@ -488,13 +485,14 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
             }
             prev = s;
             s = s + 1 == g.stages ? 0 : s + 1;
-            if (i + 1 < n) w.next(p, 1);
+            begins = ends;
+            live = w.next(p, 1);
         }
-        if (group == 0 && tid == 0) p.split[worker] = split;
     }
+    if (!p.whole_rows && group == 0 && tid == 0) p.split[worker] = split;
     // requests without tokens
-    for (int r = worker; r < p.R; r += g.workers)
-        if (clamped_len(p, r, false) == 0) {
+    for (int r = worker; r < p.R; r += p.workers)
+        if (clamped_len(p, r, true) == 0) {
             uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + (static_cast<size_t>(r) * p.Hq + h0) * DV);
             for (int i = tid; i < heads * (DV / 8); i += kLatThreads) o[i] = make_uint4(0, 0, 0, 0);
             if (p.lse)
@@ -515,125 +513,15 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
     }
 }
 
-// Joins the rows that several CTAs share.  The CTA that begins a row has left its request and the number of
-// parts.  An item is one head of a row of many parts, whose parts the block's warps share out, or eight
-// heads of a row of few, one a warp: either way some dozen loads are in flight for each warp.
-constexpr int kJoinWarps = 8, kFewParts = 8;
-
-template <int DV, bool kF16>
-__global__ void __launch_bounds__(kJoinWarps * 32) kv_latent_join_kernel(const KvAttendParams p, const LatentGeo g, const int kN) {
-    __shared__ int s_parts[kKvWorkers], s_end[kKvWorkers];
-    __shared__ float4 s_acc[kJoinWarps][DV / 4];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    chain_wait();
-    for (int i = tid; i < g.workers; i += kJoinWarps * 32) s_parts[i] = __ldcg(p.split + i);
-    __syncthreads();
-    if (warp == 0) {
-        int before = 0;
-        for (int i0 = 0; i0 < g.workers; i0 += 32) {
-            const int n = i0 + lane < g.workers ? s_parts[i0 + lane] : 0;
-            int end = n < 2 ? 0 : g.groups * (n <= kFewParts ? (g.per_group + 7) / 8 : g.per_group);
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(kFull, end, o);
-                if (lane >= o) end += y;
-            }
-            if (i0 + lane < g.workers) s_end[i0 + lane] = before + end;
-            before += __shfl_sync(kFull, end, 31);
-        }
-    }
-    __syncthreads();
-    const int items = s_end[g.workers - 1];
-    const float4* const ml = reinterpret_cast<const float4*>(p.part_ml);   // reference, sums of p
-    for (int item = blockIdx.x; item < items; item += gridDim.x) {
-        int lo = 0;   // first worker whose items end behind this one
-        for (int k = g.workers; k > 0;) {
-            const int half = k >> 1;
-            if (s_end[lo + half] > item) {
-                k = half;
-            } else {
-                lo += half + 1;
-                k -= half + 1;
-            }
-        }
-        const int worker = lo, n = s_parts[worker], r = __ldcg(p.split + kKvWorkers + worker);
-        const bool few = n <= kFewParts;
-        const int per = few ? (g.per_group + 7) / 8 : g.per_group, rel = item - (worker > 0 ? s_end[worker - 1] : 0);
-        const int group = rel / per, h = few ? (rel - group * per) * 8 + warp : rel - group * per;
-        const bool mine = h < g.per_group && group * g.per_group + h < p.Hq;
-        const int i0 = few ? 0 : warp, step = few ? 1 : kJoinWarps;
-        auto at = [&](int i) { return (static_cast<size_t>(part_slot(worker + i, i == 0)) * g.groups + group) * kN + h; };
-        float M = -INFINITY, L = 0.0f, Lr = 0.0f;
-        float4 acc[DV / 128] = {};
-        if (mine) {
-            for (int i = lane; i < n; i += 32) M = fmaxf(M, __ldcg(ml + at(i)).x);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(kFull, M, o));
-            for (int i = lane; i < n; i += 32) {
-                const float4 y = __ldcg(ml + at(i));
-                L += y.y * part_weight(y.x, M);
-                Lr += y.z * part_weight(y.x, M);
-            }
-            L = warp_sum(L);
-            Lr = warp_sum(Lr);
-#pragma unroll 4
-            for (int i = i0; i < n; i += step) {
-                const float c = part_weight(__ldcg(ml + at(i)).x, M);
-                const float4* const src = reinterpret_cast<const float4*>(p.part + at(i) * DV) + lane;
-#pragma unroll
-                for (int k = 0; k < DV / 128; ++k) {
-                    const float4 v = __ldcg(src + k * 32);
-                    acc[k].x += c * v.x;
-                    acc[k].y += c * v.y;
-                    acc[k].z += c * v.z;
-                    acc[k].w += c * v.w;
-                }
-            }
-        }
-        const float inv = Lr == 0.0f ? 0.0f : 1.0f / Lr;
-        const size_t row = static_cast<size_t>(r) * p.Hq + group * g.per_group + h;
-        auto put = [&](int col, const float4& v) {
-            uint2 w;
-            w.x = pack2<kF16>(v.x * inv, v.y * inv);
-            w.y = pack2<kF16>(v.z * inv, v.w * inv);
-            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.o) + row * DV + col) = w;
-        };
-        if (few) {
-            if (mine)
-#pragma unroll
-                for (int k = 0; k < DV / 128; ++k) put(k * 128 + lane * 4, acc[k]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < DV / 128; ++k) s_acc[warp][k * 32 + lane] = acc[k];
-            __syncthreads();
-            if (mine && tid < DV / 4) {
-                float4 v = s_acc[0][tid];
-#pragma unroll
-                for (int w = 1; w < kJoinWarps; ++w) {
-                    const float4 y = s_acc[w][tid];
-                    v.x += y.x;
-                    v.y += y.y;
-                    v.z += y.z;
-                    v.w += y.w;
-                }
-                put(tid * 4, v);
-            }
-            __syncthreads();
-        }
-        if (mine && lane == 0 && (few || warp == 0) && p.lse)
-            p.lse[row] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
-    }
-}
-
 // Groups of at most 64 heads, products of 16, 32 or 64 columns; as many tiles in flight as fit beside the
 // queries, and two CTAs on an SM where each gets two.
-inline LatentGeo latent_geo(int Hq, int dk, int sms, int* cols) {
+inline LatentGeo latent_geo(int Hq, int dk, int sms) {
     if (sms > kKvSms) sms = kKvSms;
     LatentGeo g;
     g.groups = (Hq + 63) / 64;
     g.per_group = (Hq + g.groups - 1) / g.groups;
     const int N = g.per_group <= 16 ? 16 : g.per_group <= 32 ? 32 : 64;
-    *cols = N;
+    g.columns = N;
     g.blocks = (dk + 63) / 64;
     const int fixed = g.blocks * N * 128 + N * 128 + static_cast<int>(sizeof(LatentMisc)), tile = g.blocks * kBlockBytes;
     constexpr int kMost = 227 * 1024, kHalf = 113 * 1024;
@@ -648,23 +536,24 @@ inline LatentGeo latent_geo(int Hq, int dk, int sms, int* cols) {
 }
 
 template <int DV, int kN, bool kF16>
-cudaError_t launch_latent(const KvAttendParams& p, const LatentGeo& g, cudaStream_t stream) {
+cudaError_t launch_latent(KvAttendParams p, const LatentGeo& g, cudaStream_t stream) {
     auto* kernel = kv_latent_kernel<DV, kN, kF16>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, g.smem);
     if (e != cudaSuccess) return e;
-    kernel<<<g.workers * g.groups, kLatThreads, g.smem, stream>>>(p, g);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    const int grid = 2 * device_sm_count();
-    return launch_chained(kv_latent_join_kernel<DV, kF16>, grid, kJoinWarps * 32, 0, stream, true, p, g, kN);
+    p.workers = g.workers;
+    p.whole_rows = (static_cast<long long>(p.max_pages) << p.page_shift) <= kWholeTiles * kLatTile;
+    if (p.whole_rows && p.R < p.workers) p.workers = p.R;
+    kernel<<<p.workers * g.groups, kLatThreads, g.smem, stream>>>(p, g);
+    if ((e = cudaGetLastError()) != cudaSuccess || p.whole_rows) return e;
+    return launch_join<DV, kF16>(p, JoinGeo{g.groups, kN, g.per_group, p.Hq, g.groups}, stream);
 }
 
 template <int DV>
 cudaError_t launch_latent_of(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream) {
-    int N = 0;
-    const LatentGeo g = latent_geo(p.Hq, p.dk, device_sm_count(), &N);
+    const LatentGeo g = latent_geo(p.Hq, p.dk, device_sm_count());
     const bool f16 = c.dtype == QSTATE_KV_F16;
-    if (N == 16) return f16 ? launch_latent<DV, 16, true>(p, g, stream) : launch_latent<DV, 16, false>(p, g, stream);
-    if (N == 32) return f16 ? launch_latent<DV, 32, true>(p, g, stream) : launch_latent<DV, 32, false>(p, g, stream);
+    if (g.columns == 16) return f16 ? launch_latent<DV, 16, true>(p, g, stream) : launch_latent<DV, 16, false>(p, g, stream);
+    if (g.columns == 32) return f16 ? launch_latent<DV, 32, true>(p, g, stream) : launch_latent<DV, 32, false>(p, g, stream);
     return f16 ? launch_latent<DV, 64, true>(p, g, stream) : launch_latent<DV, 64, false>(p, g, stream);
 }
 

@@ -1,12 +1,16 @@
-// qs_kv_tiles.cuh -- what the attention kernels over the paged cache share: how the work is divided and
-// how the parts of a row are joined.
+// qs_kv_tiles.cuh -- what the attention kernels over the paged cache share: how the work is divided, how the
+// parts of a row are joined, and the instructions that they use.
 //
-// A row of work is one request and one group of its heads; its unit is a tile of tokens.  The units of all
-// rows, request after request, are dealt out evenly: CTA c of n takes a contiguous range of them,
-// so that a long row is split and short ones are strung together, whatever the lengths are, and no
-// length has to be known on the host.  A row that several CTAs share is joined by the last of them
-// to finish (a counter says who that is), in the order of the tokens: the sum does not depend on which it
-// was.
+// A row of work is one request and one group of its heads; its unit is a tile of tokens, and kRowUnits more
+// stand for what a row costs by itself (its queries, its end).  The units of all rows, request after
+// request, are dealt out evenly: worker c of n takes a contiguous range of them, so that a long row is
+// split and short ones are strung together, whatever the lengths are, and no length has to be known on
+// the host.  Parts of a row that several workers share go to memory, and a second
+// kernel, already placed and waiting when the first ends, joins them in the order of the tokens.  (Joined in
+// the first kernel by the last worker of a row, 25 parts of 8 KB took 23 us of one CTA's latencies.)
+// Where the table is so narrow that no row has more than kWholeTiles tiles, workers take whole rows in
+// turn instead: nothing to sum up over the requests first, nothing to join (one token of 40 cached:
+// 4.1 us against 6.9).
 #pragma once
 
 #include "qs_common.cuh"
@@ -37,31 +41,41 @@ __device__ __forceinline__ Span span_of(const KvAttendParams& p, int n) {
     return s;
 }
 
-// A CTA's share of the units.
+constexpr int kWholeTiles = 4;
+constexpr int kRowUnits = 1;
+
+// A worker's share of the units, [u0, u1), and where it is.  A worker goes through it from the start of its last
+// row (`turn`) to the end and then from u0 on: what it shares with the next worker comes first.
 struct Share {
     long long total;        // units of all rows
-    long long u0, u1;       // this CTA's
-    int r, group, tile;     // where u0 is
+    long long u0, u1;
+    int r, group, pos;      // where u0 is; tile t of a row is at pos kRowUnits + t
 };
 
-__device__ __forceinline__ long long share_start(long long total, int cta, int ctas) {
-    const long long q = total / ctas, rem = total - q * ctas;
-    return q * cta + (cta < rem ? cta : rem);
+__device__ __forceinline__ long long share_start(long long total, int worker, int workers) {
+    const long long q = total / workers, rem = total - q * workers;
+    return q * worker + (worker < rem ? worker : rem);
 }
-// CTA whose share holds unit u.
-__device__ __forceinline__ int share_owner(long long total, long long u, int ctas) {
-    const long long q = total / ctas, rem = total - q * ctas, cut = rem * (q + 1);
+// Worker whose share holds unit u.
+__device__ __forceinline__ int share_owner(long long total, long long u, int workers) {
+    const long long q = total / workers, rem = total - q * workers, cut = rem * (q + 1);
     return static_cast<int>(u < cut ? u / (q + 1) : rem + (u - cut) / q);
 }
 
-// All threads of the CTA; `groups` rows a request.  scratch: kThreads / 32 + 4 long longs of shared memory.
+__device__ __forceinline__ int row_units(int tiles) { return tiles > 0 ? tiles + kRowUnits : 0; }
+
+// All threads of the CTA; `groups` rows a request.  scratch: kThreads / 32 + 2 long longs of shared memory; *out too.
 template <int kThreads, int kTile, int kGrain>
-__device__ Share make_share(const KvAttendParams& p, int groups, int worker, int workers, long long* scratch) {
+__device__ __forceinline__ void make_share(const KvAttendParams& p, int groups, int worker, long long* scratch, Share* out) {
     constexpr int kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (p.R + kThreads - 1) / kThreads, r0 = min(p.R, tid * per), r1 = min(p.R, r0 + per);
     long long mine = 0;
-    for (int r = r0; r < r1; ++r) mine += span_of<kTile, kGrain>(p, clamped_len(p, r, blockIdx.x == 0)).tiles;
+    int tiles = 0;
+    for (int r = r0; r < r1; ++r) {
+        tiles = row_units(span_of<kTile, kGrain>(p, clamped_len(p, r, false)).tiles);
+        mine += tiles;
+    }
     long long before = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -73,93 +87,109 @@ __device__ Share make_share(const KvAttendParams& p, int groups, int worker, int
     long long all = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) before += scratch[w];
-        all += scratch[w];
+        const long long x = scratch[w];
+        if (w < warp) before += x;
+        all += x;
     }
     before -= mine;
-    Share s;
-    s.total = all * groups;
-    s.u0 = share_start(s.total, worker, workers);
-    s.u1 = share_start(s.total, worker + 1, workers);
-    long long* const found = scratch + kWarps;
+    const long long total = all * groups, u0 = share_start(total, worker, p.workers), u1 = share_start(total, worker + 1, p.workers);
+    if (tid == 0) {
+        out->total = total;
+        out->u0 = u0;
+        out->u1 = u1;
+    }
     const long long first = before * groups;
-    if (s.u0 < s.u1 && s.u0 >= first && s.u0 < first + mine * groups) {
-        long long at = s.u0 - first;
-        for (int r = r0; r < r1; ++r) {
-            const int tiles = span_of<kTile, kGrain>(p, clamped_len(p, r, false)).tiles;
-            if (at < static_cast<long long>(tiles) * groups) {
-                found[0] = r;
-                found[1] = at / tiles;
-                found[2] = at % tiles;
-                break;
+    if (u0 >= first && u0 < first + mine * groups) {
+        long long at = u0 - first;
+        int r = r0;
+        if (per > 1)
+            for (; r < r1; ++r) {
+                tiles = row_units(span_of<kTile, kGrain>(p, clamped_len(p, r, false)).tiles);
+                if (at < static_cast<long long>(tiles) * groups) break;
+                at -= static_cast<long long>(tiles) * groups;
             }
-            at -= static_cast<long long>(tiles) * groups;
-        }
+        const int group = static_cast<int>(at / tiles);
+        out->r = r;
+        out->group = group;
+        out->pos = static_cast<int>(at - static_cast<long long>(group) * tiles);
     }
     __syncthreads();
-    s.r = static_cast<int>(found[0]);
-    s.group = static_cast<int>(found[1]);
-    s.tile = static_cast<int>(found[2]);
-    return s;
 }
 
-// Walks the units of a share; rows without tiles are stepped over.
+// Walks the units of a worker: those of its share, or, with p.whole_rows, every p.workers-th row.  Rows without
+// tiles are stepped over.
 template <int kTile, int kGrain>
 struct Walk {
     int r, group, tile;
+    int left;      // units to the share's end, this one among them; whole rows: the row
     Span span;
 
-    __device__ __forceinline__ void start(const KvAttendParams& p, const Share& s) {
+    // false: no tile at all
+    __device__ __forceinline__ bool start(const KvAttendParams& p, const Share& s, int groups, int worker) {
+        tile = 0;
+        if (p.whole_rows) {
+            left = worker - p.workers;
+            return next_row(p, groups);
+        }
+        left = static_cast<int>(s.u1 - s.u0);
+        if (left <= 0) return false;
         r = s.r;
         group = s.group;
-        tile = s.tile;
+        tile = s.pos - kRowUnits;
         span = span_of<kTile, kGrain>(p, clamped_len(p, r, false));
+        if (tile < 0) {
+            left += tile;
+            tile = 0;
+        }
+        return left > 0;
     }
-    // to the next unit; the share must hold one
-    __device__ __forceinline__ void next(const KvAttendParams& p, int groups) {
-        if (++tile < span.tiles) return;
+    __device__ __forceinline__ bool next_row(const KvAttendParams& p, int groups) {
         tile = 0;
-        if (++group < groups) return;
+        do {
+            left += p.workers;
+            if (left >= p.R * groups) return false;
+            r = left / groups;
+            group = left - r * groups;
+            span = span_of<kTile, kGrain>(p, clamped_len(p, r, false));
+        } while (span.tiles == 0);
+        return true;
+    }
+    // to the next unit, if there is one
+    __device__ __forceinline__ bool next(const KvAttendParams& p, int groups) {
+        if (p.whole_rows) return ++tile < span.tiles || next_row(p, groups);
+        if (--left <= 0) return false;
+        if (++tile < span.tiles) return true;
+        tile = 0;
+        left -= kRowUnits;
+        if (left <= 0) return false;
+        if (++group < groups) return true;
         group = 0;
         do {
             span = span_of<kTile, kGrain>(p, clamped_len(p, ++r, false));
         } while (span.tiles == 0);
+        return true;
+    }
+    // Whether this is the last unit of its row here.
+    __device__ __forceinline__ bool ends(const KvAttendParams& p) const {
+        return tile == span.tiles - 1 || (!p.whole_rows && left == 1);
     }
 };
 
-// Contributors of a split row: CTAs first .. first + n - 1; the first holds its part in slot 1, the others
-// in slot 0 (a CTA has at most one row that began before its share and one that goes on behind it).
+// Workers that share a row: first .. first + n - 1; the first holds its part in slot 1, the others in slot 0 (a
+// worker has at most one row that began before its share and one that goes on behind it).
 struct Joint {
     int first, n;
 };
 
-__device__ __forceinline__ Joint joint_of(long long total, long long row_start, int tiles, int workers) {
+__device__ __forceinline__ Joint joint_of(const KvAttendParams& p, const Share& s, int left, int tile, int tiles) {
+    const long long start = s.u1 - left - tile;
     Joint j;
-    j.first = share_owner(total, row_start, workers);
-    j.n = share_owner(total, row_start + tiles - 1, workers) - j.first + 1;
+    j.first = share_owner(s.total, start, p.workers);
+    j.n = share_owner(s.total, start + tiles - 1, p.workers) - j.first + 1;
     return j;
 }
 
-// Parts that one CTA adds up at most; more contributors are joined in groups of so many first, each by the
-// last CTA of its group, then the groups' sums.  (One CTA reading all of 304 parts of 8 KB: about 20 us.)
-constexpr int kJoinFan = 16;
-
-__device__ __forceinline__ int part_slot(int cta, bool first) { return cta * 2 + (first ? 1 : 0); }
-
-// Counts this CTA in and tells whether it is the last of n.  What the CTA wrote before is visible to the last.
-__device__ __forceinline__ bool arrive_last(int* counter, int n, int* flag) {
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        const int last = atomicAdd(counter, 1) == n - 1;
-        if (last) *counter = 0;
-        *flag = last;
-    }
-    __syncthreads();
-    const bool last = *flag != 0;
-    if (last) __threadfence();
-    return last;
-}
+__device__ __forceinline__ int part_slot(int worker, bool first) { return worker * 2 + (first ? 1 : 0); }
 
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -225,6 +255,182 @@ __device__ __forceinline__ float max4(float x) {   // over the four lanes of a f
 __device__ __forceinline__ float sum4(float x) {
     x += __shfl_xor_sync(kFull, x, 1);
     return x + __shfl_xor_sync(kFull, x, 2);
+}
+
+// ---- joining the parts of split rows ------------------------------------------------------------------
+// A part: the sums of values [rows][DV], and for each row the references of values and of weights, the sum of
+// weights (for lse), and the sum that o is divided by.  The worker that begins a row has left the number of parts
+// and the row.  An item is one head of a row of many parts, whose parts the block's warps share out, or eight
+// heads of a row of few, one a warp: either way some dozen loads are in flight for each warp.
+struct JoinGeo {
+    int columns;         // CTAs a worker has, each with its own heads (latents), else 1
+    int rows;            // rows of a part
+    int per_group;       // heads of a group
+    int G, groups_per_kv;
+};
+constexpr int kJoinWarps = 8, kFewParts = 8;
+
+template <int DV, bool kF16>
+__global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const KvAttendParams p, const JoinGeo g) {
+    constexpr int kThreads = kJoinWarps * 32, kPer = (kKvWorkers + kThreads - 1) / kThreads;
+    constexpr int kPieces = DV / 128 > 0 ? DV / 128 : 1, kLanes = DV / 4 < 32 ? DV / 4 : 32;   // a lane's float4 of a row
+    constexpr int kBatch = DV >= 512 ? 4 : 8;                                                  // parts in flight for a warp
+    __shared__ int s_end[kKvWorkers], s_warp[kJoinWarps];
+    __shared__ float4 s_acc[kJoinWarps][DV / 4];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    chain_wait();
+    // items of each worker, summed up
+    int parts[kPer], mine_items = 0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const int w = tid * kPer + k;
+        parts[k] = w < p.workers ? __ldcg(p.split + w) : 0;
+    }
+    int ends[kPer];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        mine_items += parts[k] < 2 ? 0 : g.columns * (parts[k] <= kFewParts ? (g.per_group + 7) / 8 : g.per_group);
+        ends[k] = mine_items;
+    }
+    int before = mine_items;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(kFull, before, o);
+        if (lane >= o) before += y;
+    }
+    if (lane == 31) s_warp[warp] = before;
+    __syncthreads();
+    int items = 0;
+    before -= mine_items;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) {
+        if (w < warp) before += s_warp[w];
+        items += s_warp[w];
+    }
+    if (static_cast<int>(blockIdx.x) >= items) return;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k)
+        if (tid * kPer + k < kKvWorkers) s_end[tid * kPer + k] = before + ends[k];
+    __syncthreads();
+    const float4* const ml = reinterpret_cast<const float4*>(p.part_ml);
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        int worker = 0;   // the first whose items end behind this one
+        for (int k = p.workers; k > 0;) {
+            const int half = k >> 1;
+            if (s_end[worker + half] > item) {
+                k = half;
+            } else {
+                worker += half + 1;
+                k -= half + 1;
+            }
+        }
+        const int n = __ldcg(p.split + worker), row = __ldcg(p.split + kKvWorkers + worker);
+        const bool few = n <= kFewParts;
+        const int per = few ? (g.per_group + 7) / 8 : g.per_group, rel = item - (worker > 0 ? s_end[worker - 1] : 0);
+        const int column = rel / per, h = few ? (rel - column * per) * 8 + warp : rel - column * per;
+        // request and query head
+        const int groups = p.Hq / g.G * g.groups_per_kv, r = row / groups, group = row - r * groups + column;
+        const int kv = group / g.groups_per_kv, in_kv = (group - kv * g.groups_per_kv) * g.per_group + h;
+        const bool mine = h < g.per_group && in_kv < g.G;
+        const int i0 = few ? 0 : warp, step = few ? 1 : kJoinWarps;
+        auto at = [&](int i) { return (static_cast<size_t>(part_slot(worker + i, i == 0)) * g.columns + column) * g.rows + h; };
+        float Mo = -INFINITY, M = -INFINITY, L = 0.0f, Lo = 0.0f;
+        float4 acc[kPieces] = {};
+        float4 v[kBatch][kPieces];
+        float ref[kBatch];
+        auto load = [&](int from) {
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+                const int i = from + b * step;
+                ref[b] = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) v[b][k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (i < n) {
+                    ref[b] = __ldcg(p.part_ml + at(i) * 4);
+                    const float4* const src = reinterpret_cast<const float4*>(p.part + at(i) * DV) + lane;
+                    if (lane < kLanes)
+#pragma unroll
+                        for (int k = 0; k < kPieces; ++k) v[b][k] = __ldcg(src + k * 32);
+                }
+            }
+        };
+        if (mine) {
+            load(i0);
+            float4 y = make_float4(-INFINITY, -INFINITY, 0.0f, 0.0f);   // this lane's first part's
+            if (lane < n) y = __ldcg(ml + at(lane));
+            Mo = y.x;
+            M = y.y;
+            for (int i = lane + 32; i < n; i += 32) {
+                const float4 z = __ldcg(ml + at(i));
+                Mo = fmaxf(Mo, z.x);
+                M = fmaxf(M, z.y);
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                Mo = fmaxf(Mo, __shfl_xor_sync(kFull, Mo, o));
+                M = fmaxf(M, __shfl_xor_sync(kFull, M, o));
+            }
+            L = y.z * part_weight(y.y, M);
+            Lo = y.w * part_weight(y.y, M);
+            for (int i = lane + 32; i < n; i += 32) {
+                const float4 z = __ldcg(ml + at(i));
+                L += z.z * part_weight(z.y, M);
+                Lo += z.w * part_weight(z.y, M);
+            }
+            L = warp_sum(L);
+            Lo = warp_sum(Lo);
+            for (int i = i0; i < n; i += kBatch * step) {
+                if (i != i0) load(i);
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b) {
+                    const float c = part_weight(ref[b], Mo);
+#pragma unroll
+                    for (int k = 0; k < kPieces; ++k) {
+                        acc[k].x += c * v[b][k].x;
+                        acc[k].y += c * v[b][k].y;
+                        acc[k].z += c * v[b][k].z;
+                        acc[k].w += c * v[b][k].w;
+                    }
+                }
+            }
+        }
+        // values and weights have references of their own where values carry powers of two
+        const float inv = (Lo == 0.0f ? 0.0f : 1.0f / Lo) * (Mo == M ? 1.0f : exp2_fast(Mo - M));
+        const size_t out = static_cast<size_t>(r) * p.Hq + kv * g.G + in_kv;
+        auto put = [&](int piece, const float4& x) {
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.o) + out * DV + piece * 4) =
+                make_uint2(pack2<kF16>(x.x * inv, x.y * inv), pack2<kF16>(x.z * inv, x.w * inv));
+        };
+        if (few) {
+            if (mine && lane < kLanes)
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) put(k * 32 + lane, acc[k]);
+        } else {
+            if (lane < kLanes)
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) s_acc[warp][k * 32 + lane] = acc[k];
+            __syncthreads();
+            if (mine && tid < DV / 4) {
+                float4 x = s_acc[0][tid];
+#pragma unroll
+                for (int w = 1; w < kJoinWarps; ++w) {
+                    const float4 z = s_acc[w][tid];
+                    x.x += z.x;
+                    x.y += z.y;
+                    x.z += z.z;
+                    x.w += z.w;
+                }
+                put(tid, x);
+            }
+            __syncthreads();
+        }
+        if (mine && lane == 0 && (few || warp == 0) && p.lse) p.lse[out] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    }
+}
+
+template <int DV, bool kF16>
+cudaError_t launch_join(const KvAttendParams& p, const JoinGeo& g, cudaStream_t stream) {
+    return launch_chained(kv_join_kernel<DV, kF16>, 2 * device_sm_count(), kJoinWarps * 32, 0, stream, true, p, g);
 }
 
 }  // namespace kv
