@@ -138,6 +138,7 @@ struct KvPlanParams {
     const int32_t* n_new;
     int R, page_shift, n_pages, max_pages;
     int in_place;      // lens_out or free_out is the array that is read
+    int aligned;       // slot, pos and req can be written in 16 bytes
     int* ticket;
     int* status;
 };

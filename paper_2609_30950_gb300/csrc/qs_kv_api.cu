@@ -103,6 +103,7 @@ int qstate_kv_plan(const qstate_kv_cfg* cfg, const qstate_kv_pages* pages, const
     p.n_pages = cfg->n_pages;
     p.max_pages = cfg->max_pages;
     p.in_place = pages->lens_out == pages->lens || pages->free_out == pages->free_count;
+    p.aligned = aligned(slots->slot, 16) && aligned(slots->pos, 16) && aligned(slots->req, 16);
     p.ticket = static_cast<int*>(work) + kKvTicket;
     const cudaError_t e = launch_kv_plan(p, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? QSTATE_OK : cuda_fail(e, "page plan kernel");
