@@ -31,6 +31,11 @@ namespace kv {
 constexpr int kHeadRows = 16;
 constexpr float kLazy = 8.0f;
 
+// A word's codes 0, 1 and 2, 3 as pairs of f16.
+__device__ __forceinline__ void e4m3_cvt(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h;}" : "=r"(lo), "=r"(hi) : "r"(w));
+}
+
 template <int D, bool kE4M3, int kStages>
 struct HeadsShape {
     static constexpr int kWarps = 4, kThreads = kWarps * 32;
@@ -89,6 +94,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
     uint32_t* const masks = reinterpret_cast<uint32_t*>(smem + S::kMasks) + warp * kStages;
     const int page_mask = (1 << p.page_shift) - 1;
     const bool one_page = (1 << p.page_shift) >= S::kChunk;   // a chunk lies in one page
+    constexpr uint32_t kAllTokens = S::kChunk == 32 ? 0xffffffffu : (1u << (S::kChunk & 31)) - 1;
 
     // ---- copies ----
     Walk<S::kTile, S::kChunk> fw = cw;
@@ -130,12 +136,21 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
             const long long row0 = head_row + (t0 & page_mask);
             const char* const k = static_cast<const char*>(p.k) + row0 * S::kRow;
             const char* const v = static_cast<const char*>(p.v) + row0 * S::kRow;
+            if (mask == kAllTokens) {
 #pragma unroll
-            for (int i = 0; i < S::kChunk * S::kSeg / 32; ++i) {
-                const int e = i * 32 + lane, row = e / S::kSeg, seg = e % S::kSeg, to = S::at(row, seg);
-                const bool on = (mask >> row) & 1;
-                cp_async16(dst + to, on ? k + e * 16 : static_cast<const char*>(p.k), on);
-                cp_async16(dst + S::kTensor + to, on ? v + e * 16 : static_cast<const char*>(p.v), on);
+                for (int i = 0; i < S::kChunk * S::kSeg / 32; ++i) {
+                    const int e = i * 32 + lane, to = S::at(e / S::kSeg, e % S::kSeg);
+                    cp_async16(dst + to, k + e * 16);
+                    cp_async16(dst + S::kTensor + to, v + e * 16);
+                }
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < S::kChunk * S::kSeg / 32; ++i) {
+                    const int e = i * 32 + lane, row = e / S::kSeg, to = S::at(row, e % S::kSeg);
+                    const bool on = (mask >> row) & 1;
+                    cp_async16(dst + to, on ? k + e * 16 : static_cast<const char*>(p.k), on);
+                    cp_async16(dst + S::kTensor + to, on ? v + e * 16 : static_cast<const char*>(p.v), on);
+                }
             }
             if (kE4M3 && lane < 16) {
                 // exponents of four tokens a lane, keys' then values'; groups of four lie within a page of 4 and more
@@ -295,77 +310,94 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
                         for (int nt = 0; nt < 2; ++nt) {
                             const uint32_t c = s == 0 ? w[nt].x : s == 1 ? w[nt].y : s == 2 ? w[nt].z : w[nt].w;
                             uint32_t b0, b1;
-                            asm("{.reg .b16 lo, hi; mov.b32 {lo, hi}, %2; cvt.rn.f16x2.e4m3x2 %0, lo; cvt.rn.f16x2.e4m3x2 %1, hi;}"
-                                : "=r"(b0), "=r"(b1) : "r"(c));
+                            e4m3_cvt(c, b0, b1);
                             mma<true>(z[nt], kQInRegs ? qf[blk * 4 + s] : a, b0, b1);
                         }
                     }
                 }
             }
-            // scores in base 2; y also carries the values' powers
+            // scores in base 2 less their reference; y also carries the values' powers, which have one of their own
             float y[2][4];
+            constexpr int kRowSets = kHalf ? 1 : 2;
+            float mz[2], my[2];
+#pragma unroll
+            for (int r = 0; r < kRowSets; ++r) {
+                mz[r] = m[r] == -INFINITY ? 0.0f : m[r];
+                my[r] = mo[r] == -INFINITY ? 0.0f : mo[r];
+            }
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt) {
                 float ke[2] = {1.0f, 1.0f}, ve[2] = {0.0f, 0.0f};
                 if (kE4M3) {
                     const int tok = sb * 16 + nt * 8 + 2 * t4;
-                    const uint16_t kx = *reinterpret_cast<const uint16_t*>(exps + stage * 64 + tok);
-                    const uint16_t vx = *reinterpret_cast<const uint16_t*>(exps + stage * 64 + 32 + tok);
+                    const uint32_t kx = *reinterpret_cast<const uint16_t*>(exps + stage * 64 + tok);
+                    const uint32_t vx = *reinterpret_cast<const uint16_t*>(exps + stage * 64 + 32 + tok);
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const unsigned kj = (kx >> (8 * j)) & 255, vj = (vx >> (8 * j)) & 255;
-                        ke[j] = __uint_as_float(kj == 255 ? 0x7fffffffu : kj << 23);
-                        ve[j] = vj == 255 ? __uint_as_float(0x7fffffffu) : static_cast<float>(static_cast<int>(vj) - 127);
+                        // 2^(k - 127), and k - 127 as a number; 255, not finite, becomes NaN: its carry is a mantissa bit
+                        const uint32_t kj = (kx >> (8 * j)) & 255, vj = (vx >> (8 * j)) & 255;
+                        ke[j] = __uint_as_float(kj << 23 | (kj + 1) >> 8);
+                        ve[j] = vj == 255 ? __uint_as_float(0x7fffffffu) : __uint_as_float(0x4B000000u | vj) - 8388735.0f;
                     }
                 }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (kHalf && j >= 2) continue;
-                    float x = z[nt][j] * zs[j >> 1];
-                    if (kE4M3) x *= ke[j & 1];
-                    if (!((on >> (nt * 8 + 2 * t4 + (j & 1))) & 1)) x = -INFINITY;
-                    z[nt][j] = x;
-                    y[nt][j] = kE4M3 ? (x == -INFINITY ? x : x + ve[j & 1]) : x;
-                }
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int r = 0; r < kRowSets; ++r) {
+                        float& x = z[nt][2 * r + j];
+                        const float scale = kE4M3 ? zs[r] * ke[j] : zs[r];
+                        if (kE4M3) y[nt][2 * r + j] = fmaf(x, scale, ve[j] - my[r]);
+                        x = fmaf(x, scale, -mz[r]);
+                    }
+            }
+            if (on != 0xffffu) {
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (!((on >> (nt * 8 + 2 * t4 + (j & 1))) & 1)) z[nt][j] = y[nt][j] = -INFINITY;
             }
             // the references follow only what has outgrown them
             float top[2], topo[2];
             bool grown = false;
 #pragma unroll
-            for (int s = 0; s < (kHalf ? 1 : 2); ++s) {
-                top[s] = fmaxf(fmaxf(z[0][2 * s], z[0][2 * s + 1]), fmaxf(z[1][2 * s], z[1][2 * s + 1]));
-                grown = grown || top[s] > m[s] + kLazy;
-                if (kE4M3) {
-                    topo[s] = fmaxf(fmaxf(y[0][2 * s], y[0][2 * s + 1]), fmaxf(y[1][2 * s], y[1][2 * s + 1]));
-                    grown = grown || topo[s] > mo[s] + kLazy;
-                }
+            for (int r = 0; r < kRowSets; ++r) {
+                top[r] = fmaxf(fmaxf(z[0][2 * r], z[0][2 * r + 1]), fmaxf(z[1][2 * r], z[1][2 * r + 1]));
+                if (kE4M3) topo[r] = fmaxf(fmaxf(y[0][2 * r], y[0][2 * r + 1]), fmaxf(y[1][2 * r], y[1][2 * r + 1]));
+                grown = grown || (kE4M3 ? fmaxf(top[r], topo[r]) : top[r]) > (m[r] == -INFINITY ? -INFINITY : kLazy);
             }
             if (__any_sync(kFull, grown)) {
 #pragma unroll
-                for (int s = 0; s < (kHalf ? 1 : 2); ++s) {
-                    const float now = fmaxf(m[s], max4(top[s])), nowo = kE4M3 ? fmaxf(mo[s], max4(topo[s])) : now;
-                    l[s] *= part_weight(m[s], now);
-                    const float c = part_weight(mo[s], nowo);
-                    m[s] = now;
-                    mo[s] = nowo;
+                for (int r = 0; r < kRowSets; ++r) {
+                    const float now = fmaxf(m[r], mz[r] + max4(top[r])), nowo = kE4M3 ? fmaxf(mo[r], my[r] + max4(topo[r])) : now;
+                    l[r] *= part_weight(m[r], now);
+                    const float c = part_weight(mo[r], nowo);
+                    const float dz = (now == -INFINITY ? 0.0f : now) - mz[r], dy = (nowo == -INFINITY ? 0.0f : nowo) - my[r];
+                    m[r] = now;
+                    mo[r] = nowo;
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            z[nt][2 * r + j] -= dz;
+                            if (kE4M3) y[nt][2 * r + j] -= dy;
+                        }
 #pragma unroll
                     for (int i = 0; i < kOut; ++i) {
-                        o[i][2 * s] *= c;
-                        o[i][2 * s + 1] *= c;
+                        o[i][2 * r] *= c;
+                        o[i][2 * r + 1] *= c;
                         if (kHalf) o[i][2] *= c, o[i][3] *= c;
                     }
                 }
             }
             uint32_t hi[4], lo[4];
 #pragma unroll
-            for (int s = 0; s < (kHalf ? 1 : 2); ++s) {
-                const float mz = m[s] == -INFINITY ? 0.0f : m[s], my = mo[s] == -INFINITY ? 0.0f : mo[s];
+            for (int s = 0; s < kRowSets; ++s) {
 #pragma unroll
                 for (int nt = 0; nt < 2; ++nt) {
-                    const float p0 = exp2_fast(z[nt][2 * s] - mz), p1 = exp2_fast(z[nt][2 * s + 1] - mz);
+                    const float p0 = exp2_fast(z[nt][2 * s]), p1 = exp2_fast(z[nt][2 * s + 1]);
                     l[s] += p0 + p1;
-                    const float w0 = kE4M3 ? exp2_fast(y[nt][2 * s] - my) : p0;
-                    const float w1 = kE4M3 ? exp2_fast(y[nt][2 * s + 1] - my) : p1;
+                    const float w0 = kE4M3 ? exp2_fast(y[nt][2 * s]) : p0, w1 = kE4M3 ? exp2_fast(y[nt][2 * s + 1]) : p1;
                     const uint32_t h = pack2<kProd16>(w0, w1);
                     hi[2 * nt + s] = h;
                     if (!kE4M3) {
@@ -396,9 +428,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
                         uint32_t even[2], odd[2];
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
-                            const uint32_t w = __byte_perm(b[2 * s + j], 0, 0x3120);
-                            asm("{.reg .b16 lo, hi; mov.b32 {lo, hi}, %2; cvt.rn.f16x2.e4m3x2 %0, lo; cvt.rn.f16x2.e4m3x2 %1, hi;}"
-                                : "=r"(even[j]), "=r"(odd[j]) : "r"(w));
+                            e4m3_cvt(__byte_perm(b[2 * s + j], 0, 0x3120), even[j], odd[j]);
                         }
                         mma<true>(o[2 * (np + s)], hi, even[0], even[1]);
                         mma<true>(o[2 * (np + s) + 1], hi, odd[0], odd[1]);
