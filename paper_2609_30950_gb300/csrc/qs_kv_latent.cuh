@@ -14,7 +14,9 @@
 //   warps 0-7   softmax: 16 tokens and half of the heads each from S^T, p to shared memory in 16 bits; at
 //               a row's end o
 //   warp 8      issues the products
-//   warps 9-12  copy tiles (and, where a row begins, its queries) with cp.async, zeros for what is not seen
+//   warp 9      copies tiles, a box of the tensor map for each page and 64 entries; in parts, so that S need not
+//               wait for the whole of a tile
+//   warps 9-12  copy a row's queries, and tiles where pages are shorter than the swizzle's eight rows
 // As in the kernel for heads, the softmax reference follows the maximum only when that has outgrown it by
 // 2^8; all tokens of a row share one reference, so the eight warps vote.  p has 16 bits in the second product
 // and o is divided by the sum of the rounded p, so that the weights in use add up to one; lse comes from
@@ -23,6 +25,8 @@
 // read 147 KB of operands from shared memory for each tile, O with the remainder 49 KB more, and
 // shared memory, at 128 bytes a cycle, is what a tile of 74 KB waits for (105 us against 91 at 64 requests).
 #pragma once
+
+#include <cuda.h>   // CUtensorMap
 
 #include "qs_kv_tiles.cuh"
 #include "qs_tc.cuh"
@@ -35,16 +39,18 @@ constexpr int kLatSoftmax = 8, kLatIssuer = kLatSoftmax, kLatCopiers = 4;   // w
 constexpr int kLatThreads = (kLatSoftmax + 1 + kLatCopiers) * 32;
 constexpr int kBlockBytes = kLatTile * 128;   // 64 tokens x 64 entries
 constexpr int kMaxStages = 4;
+constexpr int kPartBlocks = 3, kMaxParts = 3;   // a tile is waited for in parts, so that S follows the copies
 constexpr float kLazyLatent = 8.0f;
 
 struct LatentGeo {
     int blocks;        // of 64 entries, the last may be half
     int stages, smem, groups, per_group, columns, workers;
+    int box;           // rows of a copy by the tensor map: a page, or a tile of it; 0: copies of 16 bytes
 };
 
 // Shared memory behind the tiles, the queries and p.
 struct LatentMisc {
-    uint64_t full[kMaxStages], free[kMaxStages], sready[2], pready, drain;
+    uint64_t full[kMaxStages][kMaxParts], free[kMaxStages], sready[2], qfull, qfree, pready, drain;
     uint64_t mask[kMaxStages];
     float top[4][64], topr[4][64], corr[64], inv[64];   // corr: the references at a row's end
     Share share;
@@ -107,6 +113,16 @@ __device__ __forceinline__ void tmem_ld_rows(uint32_t at, float (&v)[4 * N]) {
 #pragma unroll
     for (int i = 0; i < 4 * N; ++i) v[i] = __uint_as_float(r[i]);
 }
+// A box of the pool, 64 entries wide, to shared memory; its bytes count towards the barrier's phase.
+__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, int col, int row, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n" ::"r"(dst),
+        "l"(map), "r"(col), "r"(row), "r"(smem_u32(bar))
+        : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_expect(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void stmatrix4t(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d)
                  : "memory");
@@ -140,19 +156,23 @@ __device__ __forceinline__ bool softmax_any(bool x) {
 // Waits for a phase of a barrier; gives up after the limit, or at once where another role has.  Every role
 // runs to its end all the same (so that no one waits for a warp that left), without starting copies or
 // products any more.
+// Whole warps wait, and a warp's lanes agree on the answer.
 __device__ __forceinline__ bool role_wait(uint64_t* bar, uint32_t parity, volatile int* abort, const KvAttendParams& p) {
-    for (int it = 0; it < p.wait_polls; ++it) {
-        if (tc::mbar_try_wait(bar, parity)) return true;
-        if (*abort) return false;
+    bool ok = false, give_up = false;
+    for (int it = 0; it < p.wait_polls && !ok && !give_up; ++it) {
+        ok = tc::mbar_try_wait(bar, parity);
+        give_up = !ok && *abort;
     }
+    if (__all_sync(kFull, ok)) return true;
+    if (!*abort) raise_status(p.status, QS_DEV_TIMEOUT);
     *abort = 1;
-    raise_status(p.status, QS_DEV_TIMEOUT);
     return false;
 }
 
 template <int DV, int kN, bool kF16>
-__global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendParams p, const LatentGeo g) {
-    using W = Walk<kLatTile, 1>;
+__global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendParams p, const LatentGeo g,
+                                                                const __grid_constant__ CUtensorMap map) {
+    using W = Walk<kLatTile, kLatTile>;   // tiles start at multiples of a tile: a copy lies in one page
     constexpr int kOCols = DV / 128 * kN, kCols = kOCols + 2 * kN;
     constexpr int kAlloc = kCols <= 32 ? 32 : kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
     constexpr int kPer = kN / 8;   // heads a lane holds: 2 of each 8 of its warp's half
@@ -173,17 +193,19 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
     }
     if (tid == 0) {
         for (int s = 0; s < kMaxStages; ++s) {
-            tc::mbar_init(&x.full[s], kLatCopiers * 33);
+            for (int k = 0; k < kMaxParts; ++k) tc::mbar_init(&x.full[s][k], g.box ? 1 : kLatCopiers * 33);
             tc::mbar_init(&x.free[s], 1);
         }
         tc::mbar_init(&x.sready[0], 1);
         tc::mbar_init(&x.sready[1], 1);
+        tc::mbar_init(&x.qfull, kLatCopiers * 33);
+        tc::mbar_init(&x.qfree, 1);
         tc::mbar_init(&x.pready, kLatSoftmax);
         tc::mbar_init(&x.drain, 1);
         tc::mbar_fence_init();
         x.abort = 0;
     }
-    if (!p.whole_rows) make_share<kLatThreads, kLatTile, 1>(p, 1, worker, reinterpret_cast<long long*>(x.top), &x.share);
+    if (!p.whole_rows) make_share<kLatThreads, kLatTile, kLatTile>(p, 1, worker, reinterpret_cast<long long*>(x.top), &x.share);
     const Share& share = x.share;
     tc::fence_before_sync();
     __syncthreads();
@@ -193,67 +215,108 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
     W w;
     bool live = w.start(p, share, 1, worker);
     int split = 0;   // parts of the row that this CTA begins and others end
+    int copied = 0;  // tiles whose copies have been started
+    const int parts = (g.blocks + kPartBlocks - 1) / kPartBlocks;
 
     if (live && warp > kLatIssuer) {
         // ---- copies ----
         const int pw = warp - kLatIssuer - 1, page_mask = (1 << p.page_shift) - 1;
+        const int tokens = g.box ? g.box : 1;   // a lane looks a page up for so many
+        const int lanes = g.box ? kLatTile / g.box : 16, from = g.box ? 0 : pw * 16;
         auto look_up = [&]() {
-            const int t = w.span.base + w.tile * kLatTile + pw * 16 + lane;
-            return lane < 16 && t < w.span.end ? __ldg(p.table + static_cast<size_t>(w.r) * p.max_pages + (t >> p.page_shift)) : -1;
+            const int t = w.span.base + w.tile * kLatTile + from + lane * tokens;
+            return lane < lanes && t < w.span.end ? __ldg(p.table + static_cast<size_t>(w.r) * p.max_pages + (t >> p.page_shift)) : -1;
         };
-        int id = look_up(), s = 0;
+        int id = look_up(), s = 0, rows = 0;
         bool begins = true;
         for (int i = 0; live; ++i) {
-            bool ok = i < g.stages || role_wait(&x.free[s], (i / g.stages - 1) & 1, abort, p);
-            const int r = w.r, t = w.span.base + w.tile * kLatTile + pw * 16 + lane;
-            const bool seen = lane < 16 && t < w.span.end, there = id >= 0 && id < p.n_pages;
-            if (seen && !there) raise_status(p.status, QS_DEV_PAGES);
-            const uint32_t on = __ballot_sync(kFull, seen && there) & 0xffffu;
-            if (lane == 0) reinterpret_cast<volatile uint16_t*>(&x.mask[s])[pw] = static_cast<uint16_t>(on);
-            const long long mine = there && seen ? ((static_cast<long long>(id) << p.page_shift) + (t & page_mask)) : 0;
-            const char* src[4];
-            const int seg = lane & 7, row0 = lane >> 3;
+            bool ok = true;
+            const bool copier = !g.box || pw == 0;
+            if (copier && i >= g.stages) ok = role_wait(&x.free[s], (i / g.stages - 1) & 1, abort, p);
+            const int r = w.r, t = w.span.base + w.tile * kLatTile + from + lane * tokens;
+            // pages that hold nothing in the window are not looked at: they may have been given back
+            const bool wanted = lane < lanes && t < w.span.end && t + tokens > w.span.begin;
+            const bool there = wanted && id >= 0 && id < p.n_pages;
+            if (copier && wanted && !there) raise_status(p.status, QS_DEV_PAGES);
+            const long long row = there ? (static_cast<long long>(id) << p.page_shift) + (t & page_mask) : 0;
+            const uint32_t tile = smem_u32(tiles + s * g.blocks * kBlockBytes);
+            if (g.box && pw == 0) {
+                const int begin = w.span.begin - w.span.base - w.tile * kLatTile, end = w.span.end - w.span.base - w.tile * kLatTile;
+                // tokens that are seen: lanes take two each
+                uint64_t mask = 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                src[k] = static_cast<const char*>(p.k) + __shfl_sync(kFull, mine, k * 4 + row0) * (2 * p.dk) + seg * 16;
+                for (int k = 0; k < 2; ++k) {
+                    const int u = lane + 32 * k;
+                    const bool page_there = __shfl_sync(kFull, static_cast<int>(there), u / g.box) != 0;
+                    mask |= static_cast<uint64_t>(__ballot_sync(kFull, u >= begin && u < end && page_there)) << (32 * k);
+                }
+                const uint32_t boxes = __ballot_sync(kFull, there);
+                if (ok) {
+                    copied = i + 1;
+                    if (lane == 0) *reinterpret_cast<volatile uint64_t*>(&x.mask[s]) = mask;
+                    for (int k = 0; k < parts; ++k) {
+                        const int b0 = k * kPartBlocks, many = min(kPartBlocks, g.blocks - b0);
+                        if (lane == 0) mbar_arrive_expect(&x.full[s][k], __popc(boxes) * many * g.box * 128);
+                        __syncwarp();
+                        for (int j = lane; j < ((many * lanes + 31) & ~31); j += 32) {
+                            const int c = j % lanes, b = b0 + j / lanes;
+                            const int row_c = __shfl_sync(kFull, static_cast<int>(row), c);
+                            if (j < many * lanes && (boxes >> c) & 1)
+                                tma_box(tile + b * kBlockBytes + c * g.box * 128, &map, b * 64, row_c, &x.full[s][k]);
+                        }
+                    }
+                }
+            } else if (!g.box) {
+                const uint32_t on = __ballot_sync(kFull, there);
+                if (lane == 0) reinterpret_cast<volatile uint16_t*>(&x.mask[s])[pw] = static_cast<uint16_t>(on);
+                const char* src[4];
+                const int seg = lane & 7, row0 = lane >> 3;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    src[k] = static_cast<const char*>(p.k) + __shfl_sync(kFull, row, k * 4 + row0) * (2 * p.dk) + seg * 16;
+                const uint32_t to = tile + (from + row0) * 128;
+                for (int part = 0; part < parts; ++part) {
+                    for (int b = part * kPartBlocks; ok && b < min(g.blocks, (part + 1) * kPartBlocks); ++b)
+                        if (b * 64 + seg * 8 < p.dk) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const int u = k * 4 + row0;
+                                cp_async16(to + b * kBlockBytes + k * 512 + ((seg ^ (u & 7)) << 4), src[k] + b * 128, (on >> u) & 1);
+                            }
+                        }
+                    cp_async_arrive(&x.full[s][part]);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&x.full[s][part]);
+                }
+            }
             const bool first = begins;
             begins = w.ends(p);
             live = w.next(p, 1);
             if (live) id = look_up();
-            // the queries of the row before are no longer read once S of its last tile is there
-            if (first && i > 0) ok = ok && role_wait(&x.sready[(i - 1) & 1], ((i - 1) >> 1) & 1, abort, p);
-            if (ok) {
-                if (first) {
-                    const uint16_t* const q = static_cast<const uint16_t*>(p.q) + r * p.q_row + h0 * p.q_head;
-                    for (int b = 0; b < g.blocks; ++b)
-                        for (int e = pw * 32 + lane; e < kN * 8; e += kLatCopiers * 32) {
-                            const int h = e >> 3, sg = e & 7, col = b * 64 + sg * 8;
-                            const uint32_t to = smem_u32(queries + (b * kN + h) * 128 + ((sg ^ (h & 7)) << 4));
-                            if (p.q_aligned) {
-                                const bool in = h < heads && col < p.dk;
-                                cp_async16(to, in ? q + h * p.q_head + col : p.q, in);
-                            } else {
-                                uint16_t v[8];
+            if (first) {
+                // S of the row before is done with its queries
+                if (rows > 0 && !role_wait(&x.qfree, (rows - 1) & 1, abort, p)) ok = false;
+                ++rows;
+                const uint16_t* const q = static_cast<const uint16_t*>(p.q) + r * p.q_row + h0 * p.q_head;
+                for (int b = 0; ok && b < g.blocks; ++b)
+                    for (int e = pw * 32 + lane; e < kN * 8; e += kLatCopiers * 32) {
+                        const int h = e >> 3, sg = e & 7, col = b * 64 + sg * 8;
+                        const uint32_t to = smem_u32(queries + (b * kN + h) * 128 + ((sg ^ (h & 7)) << 4));
+                        if (p.q_aligned) {
+                            const bool in = h < heads && col < p.dk;
+                            cp_async16(to, in ? q + h * p.q_head + col : p.q, in);
+                        } else {
+                            uint16_t v[8];
 #pragma unroll
-                                for (int k = 0; k < 8; ++k) v[k] = h < heads && col < p.dk ? q[h * p.q_head + col + k] : 0;
-                                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v[0] | v[1] << 16),
-                                             "r"(v[2] | v[3] << 16), "r"(v[4] | v[5] << 16), "r"(v[6] | v[7] << 16) : "memory");
-                            }
-                        }
-                }
-                const uint32_t to = smem_u32(tiles + s * g.blocks * kBlockBytes) + (pw * 16 + row0) * 128;
-                for (int b = 0; b < g.blocks; ++b)
-                    if (b * 64 + seg * 8 < p.dk) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int row = k * 4 + row0;
-                            cp_async16(to + b * kBlockBytes + k * 512 + ((seg ^ (row & 7)) << 4), src[k] + b * 128, (on >> row) & 1);
+                            for (int k = 0; k < 8; ++k) v[k] = h < heads && col < p.dk ? q[h * p.q_head + col + k] : 0;
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v[0] | v[1] << 16),
+                                         "r"(v[2] | v[3] << 16), "r"(v[4] | v[5] << 16), "r"(v[6] | v[7] << 16) : "memory");
                         }
                     }
+                cp_async_arrive(&x.qfull);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&x.qfull);
             }
-            cp_async_arrive(&x.full[s]);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&x.full[s]);
             s = s + 1 == g.stages ? 0 : s + 1;
         }
         cp_commit();
@@ -264,23 +327,18 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
         const uint32_t lead = elect_lane(), tile_bytes = g.blocks * kBlockBytes;
         const uint32_t q32 = smem_u32(queries), p32 = smem_u32(probs), t32 = smem_u32(tiles);
         const uint64_t dq = desc_sw128(q32, 16, 1024), dp = desc_sw128(p32, 16, 1024);
-        const int full_blocks = p.dk >> 6;
         int ss = 0, so = 0;   // stages of the tiles whose S and whose O come next
-        auto scores = [&](int i) {
+        auto scores = [&](int i, int part) {
             tc::fence_async_smem();   // the copies' writes, for the tensor core's reads
             tc::fence_after_sync();
-            const uint64_t a = desc_sw128(t32 + ss * tile_bytes, 16, 1024);
             const uint32_t d = tmem + kOCols + (i & 1) * kN;
-            for (int b = 0; b < full_blocks; ++b)
+            for (int b = part * kPartBlocks; b < min(g.blocks, (part + 1) * kPartBlocks); ++b) {
+                const uint64_t a = desc_sw128(t32 + ss * tile_bytes + b * kBlockBytes, 16, 1024);
+                const bool half = b * 64 + 32 == p.dk;
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    mma_f16_ss(d, a + b * (kBlockBytes / 16) + k * 2, dq + b * (kN * 8) + k * 2, idS, b > 0 || k > 0, lead);
-            if (full_blocks < g.blocks)   // half a block
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    mma_f16_ss(d, a + full_blocks * (kBlockBytes / 16) + k * 2, dq + full_blocks * (kN * 8) + k * 2, idS, true, lead);
-            commit_by(&x.sready[i & 1], lead);
-            ss = ss + 1 == g.stages ? 0 : ss + 1;
+                    if (k < 2 || !half) mma_f16_ss(d, a + k * 2, dq + b * (kN * 8) + k * 2, idS, b > 0 || k > 0, lead);
+            }
         };
         auto values = [&](bool begins) {
             tc::fence_after_sync();
@@ -296,14 +354,23 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
         // S runs one tile ahead of O where that tile is there, and never makes O wait for it: with two tiles in
         // flight the copy of the next one waits for O
         W ahead = w;
-        int is = 0, io = 0, full_phase = 0, idle = 0;   // tiles whose S and whose O have been issued
-        bool more = true, begins = true;
+        int is = 0, part = 0, io = 0, full_phase = 0, q_phase = 0, idle = 0;   // tiles whose S and whose O have been issued
+        bool more = true, begins = true, row_begins = true;
         while (live) {
             bool did = false;
-            if (more && is <= io + 1 && warp_test(&x.full[ss], full_phase)) {
-                if (ss + 1 == g.stages) full_phase ^= 1;
-                scores(is++);
-                more = ahead.next(p, 1);
+            if (more && is <= io + 1 && warp_test(&x.full[ss][part], full_phase) && (!row_begins || warp_test(&x.qfull, q_phase))) {
+                if (row_begins) q_phase ^= 1;
+                row_begins = false;
+                scores(is, part);
+                if (++part == parts) {
+                    commit_by(&x.sready[is & 1], lead);
+                    ++is;
+                    part = 0;
+                    if (++ss == g.stages) ss = 0, full_phase ^= 1;
+                    row_begins = ahead.ends(p);
+                    if (row_begins) commit_by(&x.qfree, lead);
+                    more = ahead.next(p, 1);
+                }
                 did = true;
             }
             if (io < is && warp_test(&x.pready, io & 1)) {
@@ -340,12 +407,21 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
 #pragma unroll
                 for (int k = 0; k < kPer; ++k) m[k] = -INFINITY, l[k] = lr[k] = 0.0f;
             }
-            role_wait(&x.full[s], (i / g.stages) & 1, abort, p);
+            role_wait(&x.full[s][0], (i / g.stages) & 1, abort, p);
             role_wait(&x.sready[i & 1], (i >> 1) & 1, abort, p);
             tc::fence_after_sync();
             float z[2 * kPer];
             tmem_ld_rows<kN / 16>(tlane + kOCols + (i & 1) * kN + c0, z);
-            const uint32_t on = reinterpret_cast<volatile uint16_t*>(&x.mask[s])[sub];
+            const uint64_t seen = *reinterpret_cast<volatile uint64_t*>(&x.mask[s]);
+            const uint32_t on = static_cast<uint32_t>(seen >> (16 * sub)) & 0xffffu;
+            if (g.box && seen != ~0ull) {
+                // what a box brought beside the tokens that are seen, or left as it was, must not meet p = 0 as NaN
+                for (int u = warp; u < kLatTile; u += kLatSoftmax)
+                    if (!((seen >> u) & 1))
+                        for (int e = lane; e < DV / 8; e += 32)
+                            *reinterpret_cast<uint4*>(tiles + (s * g.blocks + (e >> 3)) * kBlockBytes + u * 128 + (e & 7) * 16) =
+                                make_uint4(0, 0, 0, 0);
+            }
             bool grown = false;
 #pragma unroll
             for (int k = 0; k < kPer; ++k) {
@@ -501,6 +577,9 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
 
     tc::fence_before_sync();
     __syncthreads();
+    if (*abort && warp == kLatIssuer + 1)   // copies by the tensor map may be under way: none may land in a CTA that has gone
+        for (int i = max(0, copied - g.stages); i < copied; ++i)
+            for (int k = 0; k < parts; ++k) tc::mbar_wait(&x.full[i % g.stages][k], (i / g.stages) & 1, kDefaultWaitPolls);
     if (warp == kLatIssuer) {
         if (*abort) {   // products may be under way: wait for them before tensor memory goes back
             const uint32_t lead = elect_lane();
@@ -512,6 +591,10 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
         tc::tmem_dealloc(tmem, kAlloc);
     }
 }
+
+// Map of the pool as rows of dk 16-bit entries, for boxes of 64 entries x `box` rows; false if the driver has no such
+// call or refuses (qs_kv_attend.cu).
+bool pool_map(CUtensorMap* map, const void* pool, int dk, long long rows, int box);
 
 // Groups of at most 64 heads, products of 16, 32 or 64 columns; as many tiles in flight as fit beside the
 // queries, and two CTAs on an SM where each gets two.
@@ -536,25 +619,29 @@ inline LatentGeo latent_geo(int Hq, int dk, int sms) {
 }
 
 template <int DV, int kN, bool kF16>
-cudaError_t launch_latent(KvAttendParams p, const LatentGeo& g, cudaStream_t stream) {
+cudaError_t launch_latent(KvAttendParams p, const LatentGeo& g, const CUtensorMap& map, cudaStream_t stream) {
     auto* kernel = kv_latent_kernel<DV, kN, kF16>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, g.smem);
     if (e != cudaSuccess) return e;
     p.workers = g.workers;
     p.whole_rows = (static_cast<long long>(p.max_pages) << p.page_shift) <= kWholeTiles * kLatTile;
     if (p.whole_rows && p.R < p.workers) p.workers = p.R;
-    kernel<<<p.workers * g.groups, kLatThreads, g.smem, stream>>>(p, g);
+    kernel<<<p.workers * g.groups, kLatThreads, g.smem, stream>>>(p, g, map);
     if ((e = cudaGetLastError()) != cudaSuccess || p.whole_rows) return e;
     return launch_join<DV, kF16>(p, JoinGeo{g.groups, kN, g.per_group, p.Hq, g.groups}, stream);
 }
 
 template <int DV>
 cudaError_t launch_latent_of(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream) {
-    const LatentGeo g = latent_geo(p.Hq, p.dk, device_sm_count());
+    LatentGeo g = latent_geo(p.Hq, p.dk, device_sm_count());
+    // boxes of eight rows and more keep the swizzle's groups of eight rows whole
+    CUtensorMap map = {};
+    g.box = c.page < 8 ? 0 : c.page < kLatTile ? c.page : kLatTile;
+    if (g.box && !pool_map(&map, p.k, p.dk, static_cast<long long>(c.n_pages) * c.page, g.box)) g.box = 0;
     const bool f16 = c.dtype == QSTATE_KV_F16;
-    if (g.columns == 16) return f16 ? launch_latent<DV, 16, true>(p, g, stream) : launch_latent<DV, 16, false>(p, g, stream);
-    if (g.columns == 32) return f16 ? launch_latent<DV, 32, true>(p, g, stream) : launch_latent<DV, 32, false>(p, g, stream);
-    return f16 ? launch_latent<DV, 64, true>(p, g, stream) : launch_latent<DV, 64, false>(p, g, stream);
+    if (g.columns == 16) return f16 ? launch_latent<DV, 16, true>(p, g, map, stream) : launch_latent<DV, 16, false>(p, g, map, stream);
+    if (g.columns == 32) return f16 ? launch_latent<DV, 32, true>(p, g, map, stream) : launch_latent<DV, 32, false>(p, g, map, stream);
+    return f16 ? launch_latent<DV, 64, true>(p, g, map, stream) : launch_latent<DV, 64, false>(p, g, map, stream);
 }
 
 }  // namespace kv

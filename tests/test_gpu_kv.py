@@ -351,6 +351,22 @@ def test_attend_passes_on_what_is_not_finite(qs):
     assert bool(((got - o).abs() <= do)[fine].all())
 
 
+@pytest.mark.parametrize("dk,dv,page", [(128, 128, 16), (576, 512, 32), (320, 256, 1)])
+def test_latent_waits_that_run_out_are_reported(qs, dk, dv, page):
+    """With no polls allowed the call gives up and says so; the next one is unaffected."""
+    b = ref.Batch(qs, [700, 90, 0, 64], 20, 1, dk, dv, page=page, latent=True)
+    qs.qstate_set_wait_limit(0)
+    try:
+        b.run(qs)
+        with pytest.raises(qs.QstateError) as e:
+            qs.qstate_check()
+        assert e.value.code == qs.QSTATE_ETIMEOUT
+    finally:
+        qs.qstate_set_wait_limit(-1)
+    b.run(qs)
+    b.check(qs)
+
+
 def test_a_step_in_a_captured_graph(qs):
     """plan, append and attend captured once and replayed token by token give what a growing cache gives."""
     R, Hq, Hkv, d, page, steps = 5, 8, 2, 64, 16, 40
