@@ -52,6 +52,7 @@ struct LatentGeo {
 struct LatentMisc {
     uint64_t full[kMaxStages][kMaxParts], free[kMaxStages], sready[2], qfull, qfree, pready, drain;
     uint64_t mask[kMaxStages];
+    uint32_t flags[kMaxStages];   // of the tile: 1 its row begins here, 2 it ends here, 4 it is the last
     float top[4][64], topr[4][64], corr[64], inv[64];   // corr: the references at a row's end
     Share share;
     uint32_t tmem;
@@ -65,18 +66,19 @@ __host__ __device__ constexpr uint32_t idesc_f16(bool f16, int M, int N, bool a_
     return (1u << 4) | ((f16 ? 0u : 1u) << 7) | ((f16 ? 0u : 1u) << 10) | ((a_m_major ? 1u : 0u) << 15) |
            (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
-// Operand in 128-byte rows with the 128-byte swizzle.  K-major: sbo between groups of 8 rows.  M-major: lbo
-// between blocks of 64 entries, sbo between groups of 8 of K.
-__device__ __forceinline__ uint64_t desc_sw128(uint32_t addr, uint32_t lbo, uint32_t sbo) {
-    return tc::smem_desc(addr, lbo, sbo) | (static_cast<uint64_t>(2u) << 61);
-}
+// Operands in 128-byte rows with the 128-byte swizzle.  K-major: 1024 bytes (sbo) between groups of 8 rows.  M-major:
+// lbo between blocks of 64 entries, 1024 (sbo) between groups of 8 of K.
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lbo) { return (addr >> 4) | (lbo >> 4) << 16; }
 // Executed by a whole warp in step, issued by the lane whose `lead` is not 0: descriptors then stay in uniform
 // registers (issued from a branch that one lane takes, each product took 85 cycles).
-__device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate, uint32_t lead) {
+// Descriptors differ in their low words only (start address and lbo; all of shared memory fits in them).
+template <uint32_t kHi>
+__device__ __forceinline__ void mma_f16_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, bool accumulate, uint32_t lead) {
     asm volatile(
-        "{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n"
-        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u), "r"(lead)
+        "{\n.reg .pred p, q;\n.reg .b64 a, b;\nmov.b64 a, {%1, %6};\nmov.b64 b, {%2, %6};\nsetp.ne.b32 p, %4, 0;\n"
+        "setp.ne.b32 q, %5, 0;\n@q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}\n" ::"r"(d),
+        "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate ? 1u : 0u), "r"(lead), "n"(kHi)
         : "memory");
 }
 __device__ __forceinline__ void commit_by(uint64_t* bar, uint32_t lead) {
@@ -113,11 +115,14 @@ __device__ __forceinline__ void tmem_ld_rows(uint32_t at, float (&v)[4 * N]) {
 #pragma unroll
     for (int i = 0; i < 4 * N; ++i) v[i] = __uint_as_float(r[i]);
 }
-// A box of the pool, 64 entries wide, to shared memory; its bytes count towards the barrier's phase.
-__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, int col, int row, uint64_t* bar) {
+// A box of the pool, 64 entries wide, to shared memory; its bytes count towards the barrier's phase.  Executed by a
+// warp in step and issued by its leading lane, as the products are (lanes with boxes of their own take turns of
+// some 200 cycles).
+__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, int col, int row, uint32_t bar, uint32_t lead) {
     asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n" ::"r"(dst),
-        "l"(map), "r"(col), "r"(row), "r"(smem_u32(bar))
+        "{\n.reg .pred q;\nsetp.ne.b32 q, %5, 0;\n"
+        "@q cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n}\n" ::"r"(dst),
+        "l"(map), "r"(col), "r"(row), "r"(bar), "r"(lead)
         : "memory");
 }
 __device__ __forceinline__ void mbar_arrive_expect(uint64_t* bar, uint32_t bytes) {
@@ -216,53 +221,64 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
     bool live = w.start(p, share, 1, worker);
     int split = 0;   // parts of the row that this CTA begins and others end
     int copied = 0;  // tiles whose copies have been started
-    const int parts = (g.blocks + kPartBlocks - 1) / kPartBlocks;
+    constexpr int kParts = (DV / 64 + kPartBlocks) / kPartBlocks;   // with or without a block behind the values
 
     if (live && warp > kLatIssuer) {
         // ---- copies ----
         const int pw = warp - kLatIssuer - 1, page_mask = (1 << p.page_shift) - 1;
         const int tokens = g.box ? g.box : 1;   // a lane looks a page up for so many
         const int lanes = g.box ? kLatTile / g.box : 16, from = g.box ? 0 : pw * 16;
-        auto look_up = [&]() {
-            const int t = w.span.base + w.tile * kLatTile + from + lane * tokens;
-            return lane < lanes && t < w.span.end ? __ldg(p.table + static_cast<size_t>(w.r) * p.max_pages + (t >> p.page_shift)) : -1;
+        auto look_up = [&](const W& at) {
+            const int t = at.span.base + at.tile * kLatTile + from + lane * tokens;
+            return lane < lanes && t < at.span.end ? __ldg(p.table + static_cast<size_t>(at.r) * p.max_pages + (t >> p.page_shift)) : -1;
         };
-        int id = look_up(), s = 0, rows = 0;
+        const uint32_t lead = elect_lane();
+        int id = look_up(w), s = 0, rows = 0;
         bool begins = true;
         for (int i = 0; live; ++i) {
             bool ok = true;
             const bool copier = !g.box || pw == 0;
-            if (copier && i >= g.stages) ok = role_wait(&x.free[s], (i / g.stages - 1) & 1, abort, p);
             const int r = w.r, t = w.span.base + w.tile * kLatTile + from + lane * tokens;
             // pages that hold nothing in the window are not looked at: they may have been given back
             const bool wanted = lane < lanes && t < w.span.end && t + tokens > w.span.begin;
             const bool there = wanted && id >= 0 && id < p.n_pages;
-            if (copier && wanted && !there) raise_status(p.status, QS_DEV_PAGES);
+            if ((!g.box || pw == 0) && wanted && !there) raise_status(p.status, QS_DEV_PAGES);
             const long long row = there ? (static_cast<long long>(id) << p.page_shift) + (t & page_mask) : 0;
             const uint32_t tile = smem_u32(tiles + s * g.blocks * kBlockBytes);
+            const bool first = begins;
+            begins = w.ends(p);
+            W after = w;
+            const bool more = after.next(p, 1);
+            uint64_t mask = 0;   // tokens that are seen: lanes take two each
             if (g.box && pw == 0) {
                 const int begin = w.span.begin - w.span.base - w.tile * kLatTile, end = w.span.end - w.span.base - w.tile * kLatTile;
-                // tokens that are seen: lanes take two each
-                uint64_t mask = 0;
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int u = lane + 32 * k;
                     const bool page_there = __shfl_sync(kFull, static_cast<int>(there), u / g.box) != 0;
                     mask |= static_cast<uint64_t>(__ballot_sync(kFull, u >= begin && u < end && page_there)) << (32 * k);
                 }
+            }
+            if (copier && i >= g.stages) ok = role_wait(&x.free[s], (i / g.stages - 1) & 1, abort, p);
+            if (pw == 0 && lane == 0 && ok)
+                *reinterpret_cast<volatile uint32_t*>(&x.flags[s]) = (first ? 1u : 0u) | (begins ? 2u : 0u) | (more ? 0u : 4u);
+            if (g.box && pw == 0) {
                 const uint32_t boxes = __ballot_sync(kFull, there);
                 if (ok) {
                     copied = i + 1;
                     if (lane == 0) *reinterpret_cast<volatile uint64_t*>(&x.mask[s]) = mask;
-                    for (int k = 0; k < parts; ++k) {
+                    for (int k = 0; k < kParts; ++k) {
                         const int b0 = k * kPartBlocks, many = min(kPartBlocks, g.blocks - b0);
                         if (lane == 0) mbar_arrive_expect(&x.full[s][k], __popc(boxes) * many * g.box * 128);
                         __syncwarp();
-                        for (int j = lane; j < ((many * lanes + 31) & ~31); j += 32) {
-                            const int c = j % lanes, b = b0 + j / lanes;
+                        const uint32_t bar = smem_u32(&x.full[s][k]);
+                        for (int c = 0; c < lanes; ++c) {
+                            if (!((boxes >> c) & 1)) continue;
                             const int row_c = __shfl_sync(kFull, static_cast<int>(row), c);
-                            if (j < many * lanes && (boxes >> c) & 1)
-                                tma_box(tile + b * kBlockBytes + c * g.box * 128, &map, b * 64, row_c, &x.full[s][k]);
+#pragma unroll
+                            for (int b = 0; b < kPartBlocks; ++b)
+                                if (b < many)
+                                    tma_box(tile + (b0 + b) * kBlockBytes + c * g.box * 128, &map, (b0 + b) * 64, row_c, bar, lead);
                         }
                     }
                 }
@@ -275,7 +291,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                 for (int k = 0; k < 4; ++k)
                     src[k] = static_cast<const char*>(p.k) + __shfl_sync(kFull, row, k * 4 + row0) * (2 * p.dk) + seg * 16;
                 const uint32_t to = tile + (from + row0) * 128;
-                for (int part = 0; part < parts; ++part) {
+                for (int part = 0; part < kParts; ++part) {
                     for (int b = part * kPartBlocks; ok && b < min(g.blocks, (part + 1) * kPartBlocks); ++b)
                         if (b * 64 + seg * 8 < p.dk) {
 #pragma unroll
@@ -289,10 +305,9 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                     if (lane == 0) mbar_arrive(&x.full[s][part]);
                 }
             }
-            const bool first = begins;
-            begins = w.ends(p);
-            live = w.next(p, 1);
-            if (live) id = look_up();
+            w = after;
+            live = more;
+            if (live) id = look_up(w);
             if (first) {
                 // S of the row before is done with its queries
                 if (rows > 0 && !role_wait(&x.qfree, (rows - 1) & 1, abort, p)) ok = false;
@@ -324,69 +339,82 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
     } else if (live && warp == kLatIssuer) {
         // ---- products ----
         constexpr uint32_t idS = idesc_f16(kF16, 64, kN, false), idO = idesc_f16(kF16, 128, kN, true);
+        constexpr int kMain = DV / 64;   // blocks of values; behind them a block, or half of one, or none
         const uint32_t lead = elect_lane(), tile_bytes = g.blocks * kBlockBytes;
-        const uint32_t q32 = smem_u32(queries), p32 = smem_u32(probs), t32 = smem_u32(tiles);
-        const uint64_t dq = desc_sw128(q32, 16, 1024), dp = desc_sw128(p32, 16, 1024);
+        const uint32_t t32 = smem_u32(tiles), dq = desc_lo(smem_u32(queries), 16), dp = desc_lo(smem_u32(probs), 16);
+        const int rope = (p.dk - DV) / 16;
         int ss = 0, so = 0;   // stages of the tiles whose S and whose O come next
+        auto block = [&](int b, uint32_t a0, uint32_t d, int steps) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k < steps)
+                    mma_f16_ss<kDescHi>(d, a0 + (b * kBlockBytes + k * 32) / 16, dq + (b * kN * 128 + k * 32) / 16, idS, b > 0 || k > 0, lead);
+        };
         auto scores = [&](int i, int part) {
             tc::fence_async_smem();   // the copies' writes, for the tensor core's reads
             tc::fence_after_sync();
-            const uint32_t d = tmem + kOCols + (i & 1) * kN;
-            for (int b = part * kPartBlocks; b < min(g.blocks, (part + 1) * kPartBlocks); ++b) {
-                const uint64_t a = desc_sw128(t32 + ss * tile_bytes + b * kBlockBytes, 16, 1024);
-                const bool half = b * 64 + 32 == p.dk;
+            const uint32_t d = tmem + kOCols + (i & 1) * kN, a0 = desc_lo(t32 + ss * tile_bytes, 16);
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (k < 2 || !half) mma_f16_ss(d, a + k * 2, dq + b * (kN * 8) + k * 2, idS, b > 0 || k > 0, lead);
-            }
+            for (int k = 0; k < kParts; ++k)
+                if (k == part)
+#pragma unroll
+                    for (int b = k * kPartBlocks; b < (k + 1) * kPartBlocks && b < kMain; ++b) block(b, a0, d, 4);
+            if (part == kParts - 1 && rope) block(kMain, a0, d, rope);
         };
         auto values = [&](bool begins) {
             tc::fence_after_sync();
-            const uint64_t a = desc_sw128(t32 + so * tile_bytes, kBlockBytes, 1024);
+            const uint32_t a0 = desc_lo(t32 + so * tile_bytes, kBlockBytes);
 #pragma unroll
             for (int c = 0; c < DV / 128; ++c)
 #pragma unroll
                 for (int k = 0; k < kLatTile / 16; ++k)
-                    mma_f16_ss(tmem + c * kN, a + c * (2 * kBlockBytes / 16) + k * (2048 / 16), dp + k * 2, idO, !begins || k > 0, lead);
+                    mma_f16_ss<kDescHi>(tmem + c * kN, a0 + (2 * c * kBlockBytes + k * 2048) / 16, dp + k * 2, idO, !begins || k > 0, lead);
             commit_by(&x.free[so], lead);
             so = so + 1 == g.stages ? 0 : so + 1;
         };
-        // S runs one tile ahead of O where that tile is there, and never makes O wait for it: with two tiles in
-        // flight the copy of the next one waits for O
-        W ahead = w;
+        // S runs one tile ahead of O, a part at a time as the parts come, and never makes O wait for it: with two
+        // tiles in flight the copy of the next one waits for O
         int is = 0, part = 0, io = 0, full_phase = 0, q_phase = 0, idle = 0;   // tiles whose S and whose O have been issued
-        bool more = true, begins = true, row_begins = true;
-        while (live) {
+        uint32_t now = 0, before = 0;   // flags of the tiles is and is - 1
+        bool more = true;
+        while (more || io < is) {
             bool did = false;
-            if (more && is <= io + 1 && warp_test(&x.full[ss][part], full_phase) && (!row_begins || warp_test(&x.qfull, q_phase))) {
-                if (row_begins) q_phase ^= 1;
-                row_begins = false;
+            if (io < is && warp_test(&x.pready, io & 1)) {
+                // the tile before the one whose S is under way, or has just been issued
+                values((io + 1 == is && part == 0 ? now : before) & 1);
+                ++io;
+                did = true;
+            }
+            bool part_there = more && is <= io + 1 && warp_test(&x.full[ss][part], full_phase);
+            if (part_there && part == 0) {
+                const uint32_t f = *reinterpret_cast<volatile uint32_t*>(&x.flags[ss]);
+                if ((f & 1) && !warp_test(&x.qfull, q_phase)) {
+                    part_there = false;
+                } else {
+                    q_phase ^= f & 1;
+                    before = now;
+                    now = f;
+                }
+            }
+            if (part_there) {
                 scores(is, part);
-                if (++part == parts) {
+                did = true;
+                if (++part == kParts) {
                     commit_by(&x.sready[is & 1], lead);
+                    if (now & 2) commit_by(&x.qfree, lead);
+                    more = !(now & 4);
                     ++is;
                     part = 0;
                     if (++ss == g.stages) ss = 0, full_phase ^= 1;
-                    row_begins = ahead.ends(p);
-                    if (row_begins) commit_by(&x.qfree, lead);
-                    more = ahead.next(p, 1);
                 }
-                did = true;
-            }
-            if (io < is && warp_test(&x.pready, io & 1)) {
-                values(begins);
-                ++io;
-                begins = w.ends(p);
-                live = w.next(p, 1);
-                did = true;
             }
             idle = did ? 0 : idle + 1;
             if (idle > p.wait_polls || *abort) {
                 if (!*abort) raise_status(p.status, QS_DEV_TIMEOUT);
                 *abort = 1;
-                live = false;
+                idle = p.wait_polls + 1;
             }
-            live = __all_sync(kFull, live);
+            if (__any_sync(kFull, idle > p.wait_polls)) break;
         }
     } else if (live && warp < kLatIssuer) {
         // ---- softmax ----
@@ -579,7 +607,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
     __syncthreads();
     if (*abort && warp == kLatIssuer + 1)   // copies by the tensor map may be under way: none may land in a CTA that has gone
         for (int i = max(0, copied - g.stages); i < copied; ++i)
-            for (int k = 0; k < parts; ++k) tc::mbar_wait(&x.full[i % g.stages][k], (i / g.stages) & 1, kDefaultWaitPolls);
+            for (int k = 0; k < kParts; ++k) tc::mbar_wait(&x.full[i % g.stages][k], (i / g.stages) & 1, kDefaultWaitPolls);
     if (warp == kLatIssuer) {
         if (*abort) {   // products may be under way: wait for them before tensor memory goes back
             const uint32_t lead = elect_lane();
