@@ -476,15 +476,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
                     p.lse[out_row + row] = sums.z == 0.0f ? -INFINITY : (sums.y + log2f(sums.z)) * 0.6931471805599453f;
             };
             const bool whole = began == 0 && cw.tile == cw.span.tiles - 1;
-            int slot = 0;
-            if (!whole) {
-                const Joint j = joint_of(p, share, cw.left, cw.tile, cw.span.tiles);
-                slot = part_slot(blockIdx.x, j.first == static_cast<int>(blockIdx.x));
-                if (j.first == static_cast<int>(blockIdx.x)) {
-                    split = j.n;
-                    if (tid == 0) p.split[kKvWorkers + blockIdx.x] = cw.r * groups + cw.group;
-                }
-            }
+            const int slot = part_slot(blockIdx.x, began == 0);
             for (int idx = tid; idx < heads * (D / 4); idx += S::kThreads) {
                 const int row = idx / (D / 4), col = (idx - row * (D / 4)) * 4;
                 float4 x[S::kWarps];
@@ -513,6 +505,10 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
                     reinterpret_cast<float4*>(p.part)[static_cast<size_t>(slot) * (kHeadRows * D / 4) + idx] = acc;
                     if (col == 0) reinterpret_cast<float4*>(p.part_ml)[slot * kHeadRows + row] = sums;
                 }
+            }
+            if (tid == 0 && !whole && began == 0) {
+                split = row_parts(p, share, blockIdx.x, cw.left, cw.tile, cw.span.tiles);
+                p.split[kKvWorkers + blockIdx.x] = cw.r * groups + cw.group;
             }
             began = -1;
             __syncthreads();   // parts and queries of the row are read

@@ -16,14 +16,14 @@
 //   warp 8      issues the products
 //   warp 9      copies tiles, a box of the tensor map for each page and 64 entries; in parts, so that S need not
 //               wait for the whole of a tile
-//   warps 9-12  copy a row's queries, and tiles where pages are shorter than the swizzle's eight rows
+//   warps 9-12  (10-12 where warp 9 copies boxes) copy a row's queries, and, 16 bytes at a time, tiles of short pages
 // As in the kernel for heads, the softmax reference follows the maximum only when that has outgrown it by
 // 2^8; all tokens of a row share one reference, so the eight warps vote.  p has 16 bits in the second product
 // and o is divided by the sum of the rounded p, so that the weights in use add up to one; lse comes from
 // the sum before rounding.  That leaves o with about 1.4 times the error of its own rounding.  Carrying the
 // remainder of p in a second product would cost a second pass over the tile: at 64 heads of 512 + 64, S and O
 // read 147 KB of operands from shared memory for each tile, O with the remainder 49 KB more, and
-// shared memory, at 128 bytes a cycle, is what a tile of 74 KB waits for (105 us against 91 at 64 requests).
+// shared memory, at 128 bytes a cycle, would bound the kernel before the cache's bytes do.
 #pragma once
 
 #include <cuda.h>   // CUtensorMap
@@ -125,6 +125,7 @@ __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, in
         "l"(map), "r"(col), "r"(row), "r"(bar), "r"(lead)
         : "memory");
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];\n" ::"l"(map) : "memory"); }
 __device__ __forceinline__ void mbar_arrive_expect(uint64_t* bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
@@ -185,13 +186,15 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
     extern __shared__ __align__(1024) char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     char* const tiles = smem;
-    char* const queries = tiles + g.stages * g.blocks * kBlockBytes;
-    char* const probs = queries + g.blocks * kN * 128;
+    char* const queries_at = tiles + g.stages * g.blocks * kBlockBytes;
+    char* const probs = queries_at + g.blocks * kN * 128;
     LatentMisc& x = *reinterpret_cast<LatentMisc*>(probs + kN * 128);
     const int worker = blockIdx.x / g.groups, group = blockIdx.x - worker * g.groups;
     const int h0 = group * g.per_group, heads = min(g.per_group, p.Hq - h0);
+    const int askers = g.box ? kLatCopiers - 1 : kLatCopiers;   // warps that copy queries
     chain_release();   // the kernel that joins split rows may take its place
 
+    if (g.box && warp == kLatIssuer + 1) prefetch_map(&map);
     if (warp == kLatIssuer) {
         tc::tmem_alloc(&x.tmem, kAlloc);
         tc::tmem_relinquish();
@@ -203,7 +206,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
         }
         tc::mbar_init(&x.sready[0], 1);
         tc::mbar_init(&x.sready[1], 1);
-        tc::mbar_init(&x.qfull, kLatCopiers * 33);
+        tc::mbar_init(&x.qfull, askers * 33);
         tc::mbar_init(&x.qfree, 1);
         tc::mbar_init(&x.pready, kLatSoftmax);
         tc::mbar_init(&x.drain, 1);
@@ -227,13 +230,43 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
         // ---- copies ----
         const int pw = warp - kLatIssuer - 1, page_mask = (1 << p.page_shift) - 1;
         const int tokens = g.box ? g.box : 1;   // a lane looks a page up for so many
-        const int lanes = g.box ? kLatTile / g.box : 16, from = g.box ? 0 : pw * 16;
+        const bool asks = !g.box || pw > 0;
+        const int lanes = !g.box ? 16 : pw == 0 ? kLatTile / g.box : 0, from = g.box ? 0 : pw * 16;
         auto look_up = [&](const W& at) {
             const int t = at.span.base + at.tile * kLatTile + from + lane * tokens;
             return lane < lanes && t < at.span.end ? __ldg(p.table + static_cast<size_t>(at.r) * p.max_pages + (t >> p.page_shift)) : -1;
         };
         const uint32_t lead = elect_lane();
-        int id = look_up(w), s = 0, rows = 0;
+        // a thread copies one of eight pieces of every block of its heads
+        auto queries = [&](int r) {
+            const int sg = lane & 7;
+            for (int h = (warp - kLatIssuer - 1 - kLatCopiers + askers) * 4 + (lane >> 3); h < kN; h += askers * 4) {
+                const uint16_t* const q = static_cast<const uint16_t*>(p.q) + r * p.q_row + (h0 + h) * p.q_head + sg * 8;
+                uint32_t to = smem_u32(queries_at + h * 128 + ((sg ^ (h & 7)) << 4));
+                for (int b = 0; b < g.blocks; ++b, to += kN * 128) {
+                    const bool in = h < heads && b * 64 + sg * 8 < p.dk;
+                    if (p.q_aligned) {
+                        cp_async16(to, in ? q + b * 64 : p.q, in);
+                    } else {
+                        uint16_t v[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) v[k] = in ? q[b * 64 + k] : 0;
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v[0] | v[1] << 16),
+                                     "r"(v[2] | v[3] << 16), "r"(v[4] | v[5] << 16), "r"(v[6] | v[7] << 16) : "memory");
+                    }
+                }
+            }
+        };
+        auto queries_done = [&]() {
+            cp_async_arrive(&x.qfull);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&x.qfull);
+        };
+        int id = look_up(w), s = 0, rows = 0;   // rows: that have waited for the queries of the one before
+        if (asks) {
+            queries(w.r);
+            queries_done();
+        }
         bool begins = true;
         for (int i = 0; live; ++i) {
             bool ok = true;
@@ -308,29 +341,11 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
             w = after;
             live = more;
             if (live) id = look_up(w);
-            if (first) {
+            if (first && i > 0 && asks) {
                 // S of the row before is done with its queries
-                if (rows > 0 && !role_wait(&x.qfree, (rows - 1) & 1, abort, p)) ok = false;
-                ++rows;
-                const uint16_t* const q = static_cast<const uint16_t*>(p.q) + r * p.q_row + h0 * p.q_head;
-                for (int b = 0; ok && b < g.blocks; ++b)
-                    for (int e = pw * 32 + lane; e < kN * 8; e += kLatCopiers * 32) {
-                        const int h = e >> 3, sg = e & 7, col = b * 64 + sg * 8;
-                        const uint32_t to = smem_u32(queries + (b * kN + h) * 128 + ((sg ^ (h & 7)) << 4));
-                        if (p.q_aligned) {
-                            const bool in = h < heads && col < p.dk;
-                            cp_async16(to, in ? q + h * p.q_head + col : p.q, in);
-                        } else {
-                            uint16_t v[8];
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) v[k] = h < heads && col < p.dk ? q[h * p.q_head + col + k] : 0;
-                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v[0] | v[1] << 16),
-                                         "r"(v[2] | v[3] << 16), "r"(v[4] | v[5] << 16), "r"(v[6] | v[7] << 16) : "memory");
-                        }
-                    }
-                cp_async_arrive(&x.qfull);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&x.qfull);
+                ok = role_wait(&x.qfree, rows++ & 1, abort, p);
+                if (ok) queries(r);
+                queries_done();
             }
             s = s + 1 == g.stages ? 0 : s + 1;
         }
@@ -341,7 +356,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
         constexpr uint32_t idS = idesc_f16(kF16, 64, kN, false), idO = idesc_f16(kF16, 128, kN, true);
         constexpr int kMain = DV / 64;   // blocks of values; behind them a block, or half of one, or none
         const uint32_t lead = elect_lane(), tile_bytes = g.blocks * kBlockBytes;
-        const uint32_t t32 = smem_u32(tiles), dq = desc_lo(smem_u32(queries), 16), dp = desc_lo(smem_u32(probs), 16);
+        const uint32_t t32 = smem_u32(tiles), dq = desc_lo(smem_u32(queries_at), 16), dp = desc_lo(smem_u32(probs), 16);
         const int rope = (p.dk - DV) / 16;
         int ss = 0, so = 0;   // stages of the tiles whose S and whose O come next
         auto block = [&](int b, uint32_t a0, uint32_t d, int steps) {
@@ -546,15 +561,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                 }
                 softmax_sync();
                 const bool whole = began == 0 && w.tile == w.span.tiles - 1;
-                int slot = 0;
-                if (!whole) {
-                    const Joint j = joint_of(p, share, w.left, w.tile, w.span.tiles);
-                    slot = part_slot(worker, j.first == worker);
-                    if (j.first == worker) {
-                        split = j.n;
-                        if (group == 0 && tid == 0) p.split[kKvWorkers + worker] = w.r * g.groups;
-                    }
-                }
+                const int slot = part_slot(worker, began == 0);
                 const size_t row = static_cast<size_t>(w.r) * p.Hq + h0;
                 const size_t prow = (static_cast<size_t>(slot) * g.groups + group) * kN;
                 if (tid < kN) {
@@ -586,6 +593,10 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                             if (hb + k < heads) o[k * DV] = v[k];
                     }
                 }
+                if (tid == 0 && !whole && began == 0) {
+                    split = row_parts(p, share, worker, w.left, w.tile, w.span.tiles);
+                    if (group == 0) p.split[kKvWorkers + worker] = w.r * g.groups;
+                }
             }
             prev = s;
             s = s + 1 == g.stages ? 0 : s + 1;
@@ -594,13 +605,14 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
         }
     }
     if (!p.whole_rows && group == 0 && tid == 0) p.split[worker] = split;
-    // requests without tokens
-    for (int r = worker; r < p.R; r += p.workers)
+    // requests without tokens, by the warps that are done first
+    const int ctid = tid - (kLatIssuer + 1) * 32;
+    for (int r = worker; ctid >= 0 && r < p.R; r += p.workers)
         if (clamped_len(p, r, true) == 0) {
             uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + (static_cast<size_t>(r) * p.Hq + h0) * DV);
-            for (int i = tid; i < heads * (DV / 8); i += kLatThreads) o[i] = make_uint4(0, 0, 0, 0);
+            for (int i = ctid; i < heads * (DV / 8); i += kLatCopiers * 32) o[i] = make_uint4(0, 0, 0, 0);
             if (p.lse)
-                for (int i = tid; i < heads; i += kLatThreads) p.lse[static_cast<size_t>(r) * p.Hq + h0 + i] = -INFINITY;
+                for (int i = ctid; i < heads; i += kLatCopiers * 32) p.lse[static_cast<size_t>(r) * p.Hq + h0 + i] = -INFINITY;
         }
 
     tc::fence_before_sync();
@@ -662,9 +674,13 @@ cudaError_t launch_latent(KvAttendParams p, const LatentGeo& g, const CUtensorMa
 template <int DV>
 cudaError_t launch_latent_of(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream) {
     LatentGeo g = latent_geo(p.Hq, p.dk, device_sm_count());
-    // boxes of eight rows and more keep the swizzle's groups of eight rows whole
+    // A box a page and 64 entries, from pages of 32 tokens on.  One lane issues them, some 100 cycles each, and
+    // shorter pages take so many that the copies of 16 bytes, which cost four warps' instructions but nothing
+    // a page, are faster (64 requests of 64 heads of 512 + 64, up to 8000 tokens: pages of 8 tokens 191 us by boxes, 107
+    // by 16 bytes; of 16 tokens 130 and 106; of 32 tokens 107 and 107; 64 requests of 16 heads of 128 + 64, up
+    // to 30000: 148 and 100, 111 and 99, 93 and 105).
     CUtensorMap map = {};
-    g.box = c.page < 8 ? 0 : c.page < kLatTile ? c.page : kLatTile;
+    g.box = c.page < 32 ? 0 : c.page < kLatTile ? c.page : kLatTile;
     if (g.box && !pool_map(&map, p.k, p.dk, static_cast<long long>(c.n_pages) * c.page, g.box)) g.box = 0;
     const bool f16 = c.dtype == QSTATE_KV_F16;
     if (g.columns == 16) return f16 ? launch_latent<DV, 16, true>(p, g, map, stream) : launch_latent<DV, 16, false>(p, g, map, stream);

@@ -175,21 +175,14 @@ struct Walk {
     }
 };
 
-// Workers that share a row: first .. first + n - 1; the first holds its part in slot 1, the others in slot 0 (a
-// worker has at most one row that began before its share and one that goes on behind it).
-struct Joint {
-    int first, n;
-};
-
-__device__ __forceinline__ Joint joint_of(const KvAttendParams& p, const Share& s, int left, int tile, int tiles) {
-    const long long start = s.u1 - left - tile;
-    Joint j;
-    j.first = share_owner(s.total, start, p.workers);
-    j.n = share_owner(s.total, start + tiles - 1, p.workers) - j.first + 1;
-    return j;
-}
-
+// A row that several workers share: the one that begins it holds its part in slot 1, the others in slot 0 (a worker has
+// at most one row that began before its share and one that goes on behind it).
 __device__ __forceinline__ int part_slot(int worker, bool first) { return worker * 2 + (first ? 1 : 0); }
+
+// Parts of a row whose tile `tile` is where the worker's share ends, for the worker that begins the row.
+__device__ __forceinline__ int row_parts(const KvAttendParams& p, const Share& s, int worker, int left, int tile, int tiles) {
+    return share_owner(s.total, s.u1 - left - tile + tiles - 1, p.workers) - worker + 1;
+}
 
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -264,7 +257,9 @@ __device__ __forceinline__ float sum4(float x) {
 // A part: the sums of values [rows][DV], and for each row the references of values and of weights, the sum of
 // weights (for lse), and the sum that o is divided by.  The worker that begins a row has left the number of parts
 // and the row.  An item is one head of a row of many parts, whose parts the block's warps share out, or eight
-// heads of a row of few, one a warp: either way some dozen loads are in flight for each warp.
+// heads of a row of few, one a warp: either way some dozen loads are in flight for each warp.  The kernel is a
+// chain of latencies (which row an item is of, its parts, their sum), so each step asks for all that it needs
+// at once.
 struct JoinGeo {
     int columns;         // CTAs a worker has, each with its own heads (latents), else 1
     int rows;            // rows of a part
@@ -273,23 +268,30 @@ struct JoinGeo {
 };
 constexpr int kJoinWarps = 8, kFewParts = 8;
 
+__device__ __forceinline__ float warp_top(float x) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(kFull, x, o));
+    return x;
+}
+
 template <int DV, bool kF16>
 __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const KvAttendParams p, const JoinGeo g) {
     constexpr int kThreads = kJoinWarps * 32, kPer = (kKvWorkers + kThreads - 1) / kThreads;
     constexpr int kPieces = DV / 128 > 0 ? DV / 128 : 1, kLanes = DV / 4 < 32 ? DV / 4 : 32;   // a lane's float4 of a row
     constexpr int kBatch = DV >= 512 ? 4 : 8;                                                  // parts in flight for a warp
-    __shared__ int s_end[kKvWorkers], s_warp[kJoinWarps];
-    __shared__ float4 s_acc[kJoinWarps][DV / 4];
+    __shared__ int s_warp[kJoinWarps];
+    __shared__ int4 s_item;
+    __shared__ float4 s_ml[kJoinWarps], s_acc[kJoinWarps][DV / 4];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     chain_wait();
     // items of each worker, summed up
-    int parts[kPer], mine_items = 0;
+    int parts[kPer], rows[kPer], ends[kPer], mine_items = 0;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
         const int w = tid * kPer + k;
         parts[k] = w < p.workers ? __ldcg(p.split + w) : 0;
+        rows[k] = w < p.workers ? __ldcg(p.split + kKvWorkers + w) : 0;
     }
-    int ends[kPer];
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
         mine_items += parts[k] < 2 ? 0 : g.columns * (parts[k] <= kFewParts ? (g.per_group + 7) / 8 : g.per_group);
@@ -310,97 +312,71 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const KvAttend
         if (w < warp) before += s_warp[w];
         items += s_warp[w];
     }
-    if (static_cast<int>(blockIdx.x) >= items) return;
-#pragma unroll
-    for (int k = 0; k < kPer; ++k)
-        if (tid * kPer + k < kKvWorkers) s_end[tid * kPer + k] = before + ends[k];
-    __syncthreads();
-    const float4* const ml = reinterpret_cast<const float4*>(p.part_ml);
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
-        int worker = 0;   // the first whose items end behind this one
-        for (int k = p.workers; k > 0;) {
-            const int half = k >> 1;
-            if (s_end[worker + half] > item) {
-                k = half;
-            } else {
-                worker += half + 1;
-                k -= half + 1;
-            }
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int rel = item - before - (k > 0 ? ends[k - 1] : 0);
+            if (rel >= 0 && item < before + ends[k]) s_item = make_int4(tid * kPer + k, parts[k], rows[k], rel);
         }
-        const int n = __ldcg(p.split + worker), row = __ldcg(p.split + kKvWorkers + worker);
+        __syncthreads();
+        const int worker = s_item.x, n = s_item.y, row = s_item.z, rel = s_item.w;
         const bool few = n <= kFewParts;
-        const int per = few ? (g.per_group + 7) / 8 : g.per_group, rel = item - (worker > 0 ? s_end[worker - 1] : 0);
+        const int per = few ? (g.per_group + 7) / 8 : g.per_group;
         const int column = rel / per, h = few ? (rel - column * per) * 8 + warp : rel - column * per;
         // request and query head
         const int groups = p.Hq / g.G * g.groups_per_kv, r = row / groups, group = row - r * groups + column;
         const int kv = group / g.groups_per_kv, in_kv = (group - kv * g.groups_per_kv) * g.per_group + h;
         const bool mine = h < g.per_group && in_kv < g.G;
-        const int i0 = few ? 0 : warp, step = few ? 1 : kJoinWarps;
-        auto at = [&](int i) { return (static_cast<size_t>(part_slot(worker + i, i == 0)) * g.columns + column) * g.rows + h; };
+        // this warp's parts: i0, i0 + step ...
+        const int i0 = few ? 0 : warp, step = few ? 1 : kJoinWarps, count = !mine ? 0 : few ? n : (n - warp + kJoinWarps - 1) / kJoinWarps;
+        auto at = [&](int j) {
+            const int i = i0 + j * step;
+            return (static_cast<size_t>(part_slot(worker + i, i == 0)) * g.columns + column) * g.rows + h;
+        };
         float Mo = -INFINITY, M = -INFINITY, L = 0.0f, Lo = 0.0f;
         float4 acc[kPieces] = {};
-        float4 v[kBatch][kPieces];
-        float ref[kBatch];
-        auto load = [&](int from) {
-#pragma unroll
-            for (int b = 0; b < kBatch; ++b) {
-                const int i = from + b * step;
-                ref[b] = -INFINITY;
-#pragma unroll
-                for (int k = 0; k < kPieces; ++k) v[b][k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                if (i < n) {
-                    ref[b] = __ldcg(p.part_ml + at(i) * 4);
-                    const float4* const src = reinterpret_cast<const float4*>(p.part + at(i) * DV) + lane;
-                    if (lane < kLanes)
-#pragma unroll
-                        for (int k = 0; k < kPieces; ++k) v[b][k] = __ldcg(src + k * 32);
-                }
-            }
-        };
-        if (mine) {
-            load(i0);
-            float4 y = make_float4(-INFINITY, -INFINITY, 0.0f, 0.0f);   // this lane's first part's
-            if (lane < n) y = __ldcg(ml + at(lane));
-            Mo = y.x;
-            M = y.y;
-            for (int i = lane + 32; i < n; i += 32) {
-                const float4 z = __ldcg(ml + at(i));
-                Mo = fmaxf(Mo, z.x);
-                M = fmaxf(M, z.y);
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                Mo = fmaxf(Mo, __shfl_xor_sync(kFull, Mo, o));
-                M = fmaxf(M, __shfl_xor_sync(kFull, M, o));
-            }
-            L = y.z * part_weight(y.y, M);
-            Lo = y.w * part_weight(y.y, M);
-            for (int i = lane + 32; i < n; i += 32) {
-                const float4 z = __ldcg(ml + at(i));
-                L += z.z * part_weight(z.y, M);
-                Lo += z.w * part_weight(z.y, M);
-            }
-            L = warp_sum(L);
-            Lo = warp_sum(Lo);
-            for (int i = i0; i < n; i += kBatch * step) {
-                if (i != i0) load(i);
+        for (int base = 0; base < count; base += 32) {
+            const int many = min(32, count - base);
+            float4 y = make_float4(-INFINITY, -INFINITY, 0.0f, 0.0f);   // a lane's part's
+            if (lane < many) y = __ldcg(reinterpret_cast<const float4*>(p.part_ml) + at(base + lane));
+            float c = 0.0f;
+            for (int j = 0; j < many; j += kBatch) {
+                float4 v[kBatch][kPieces];
 #pragma unroll
                 for (int b = 0; b < kBatch; ++b) {
-                    const float c = part_weight(ref[b], Mo);
+                    const float4* const src = reinterpret_cast<const float4*>(p.part + at(base + j + b) * DV) + lane;
+#pragma unroll
+                    for (int k = 0; k < kPieces; ++k)
+                        v[b][k] = j + b < many && lane < kLanes ? __ldcg(src + k * 32) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                }
+                if (j == 0) {
+                    const float to = fmaxf(Mo, warp_top(y.x)), tm = fmaxf(M, warp_top(y.y));
+                    const float co = part_weight(Mo, to), cm = part_weight(M, tm), cy = part_weight(y.y, tm);
+                    L = L * cm + warp_sum(y.z * cy);
+                    Lo = Lo * cm + warp_sum(y.w * cy);
+                    Mo = to;
+                    M = tm;
+                    c = part_weight(y.x, to);
+#pragma unroll
+                    for (int k = 0; k < kPieces; ++k) acc[k] = make_float4(acc[k].x * co, acc[k].y * co, acc[k].z * co, acc[k].w * co);
+                }
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b) {
+                    const float cb = __shfl_sync(kFull, c, j + b);
 #pragma unroll
                     for (int k = 0; k < kPieces; ++k) {
-                        acc[k].x += c * v[b][k].x;
-                        acc[k].y += c * v[b][k].y;
-                        acc[k].z += c * v[b][k].z;
-                        acc[k].w += c * v[b][k].w;
+                        acc[k].x += cb * v[b][k].x;
+                        acc[k].y += cb * v[b][k].y;
+                        acc[k].z += cb * v[b][k].z;
+                        acc[k].w += cb * v[b][k].w;
                     }
                 }
             }
         }
-        // values and weights have references of their own where values carry powers of two
-        const float inv = (Lo == 0.0f ? 0.0f : 1.0f / Lo) * (Mo == M ? 1.0f : exp2_fast(Mo - M));
         const size_t out = static_cast<size_t>(r) * p.Hq + kv * g.G + in_kv;
+        // values and weights have references of their own where values carry powers of two
         auto put = [&](int piece, const float4& x) {
+            const float inv = (Lo == 0.0f ? 0.0f : 1.0f / Lo) * (Mo == M ? 1.0f : exp2_fast(Mo - M));
             *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.o) + out * DV + piece * 4) =
                 make_uint2(pack2<kF16>(x.x * inv, x.y * inv), pack2<kF16>(x.z * inv, x.w * inv));
         };
@@ -412,22 +388,33 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const KvAttend
             if (lane < kLanes)
 #pragma unroll
                 for (int k = 0; k < kPieces; ++k) s_acc[warp][k * 32 + lane] = acc[k];
+            if (lane == 0) s_ml[warp] = make_float4(Mo, M, L, Lo);
             __syncthreads();
-            if (mine && tid < DV / 4) {
-                float4 x = s_acc[0][tid];
+            Mo = M = -INFINITY;
+            L = Lo = 0.0f;
+            float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-                for (int w = 1; w < kJoinWarps; ++w) {
-                    const float4 z = s_acc[w][tid];
-                    x.x += z.x;
-                    x.y += z.y;
-                    x.z += z.z;
-                    x.w += z.w;
+            for (int w = 0; w < kJoinWarps; ++w) {
+                Mo = fmaxf(Mo, s_ml[w].x);
+                M = fmaxf(M, s_ml[w].y);
+            }
+            if (mine && tid < DV / 4) {
+#pragma unroll
+                for (int w = 0; w < kJoinWarps; ++w) {
+                    const float4 z = s_acc[w][tid], y = s_ml[w];
+                    const float co = part_weight(y.x, Mo), cm = part_weight(y.y, M);
+                    L += y.z * cm;
+                    Lo += y.w * cm;
+                    x.x += co * z.x;
+                    x.y += co * z.y;
+                    x.z += co * z.z;
+                    x.w += co * z.w;
                 }
                 put(tid, x);
             }
-            __syncthreads();
         }
         if (mine && lane == 0 && (few || warp == 0) && p.lse) p.lse[out] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+        __syncthreads();
     }
 }
 
