@@ -43,8 +43,9 @@ extern "C" {
 #define QSTATE_ECUDA 3   /* a CUDA runtime call failed (message in qstate_last_error)          */
 #define QSTATE_EDEVICE 4 /* a kernel reported an inconsistent device-side layout or input, or
                             the device was marked unusable (see qstate_check)                 */
-#define QSTATE_ETIMEOUT 5 /* a bounded device-side wait gave up (chunked form: a tensor-core
-                             product did not signal completion within the wait limit)         */
+#define QSTATE_ETIMEOUT 5 /* a bounded device-side wait gave up (chunked form and attention over
+                             latents: a tensor-core product, or a copy for one, did not signal
+                             completion within the wait limit)                                */
 
 /* ---- configuration enums ---------------------------------------------------------------- */
 #define QSTATE_DECAY_ROW 0   /* one rate per key row (KDA, Sec. 1)                            */
@@ -382,7 +383,7 @@ int qstate_kv_attend(const qstate_kv_cfg* cfg, const qstate_kv_cache* cache, con
                      void* work, void* stream);
 
 /* Synchronise `stream`, read and clear the device status word.  QSTATE_OK; QSTATE_ETIMEOUT if a
- * bounded wait of the chunked form gave up (the call's results are not valid; the kernel still
+ * bounded wait of the chunked form or of qstate_kv_attend over latents gave up (the call's results are not valid; the kernel still
  * waited for its products before freeing tensor memory, so later calls are unaffected);
  * otherwise QSTATE_EDEVICE with the reasons in qstate_last_error().  If even that last wait
  * gave up, tensor memory may have been freed under products in flight: the device is then
@@ -390,8 +391,8 @@ int qstate_kv_attend(const qstate_kv_cfg* cfg, const qstate_kv_cache* cache, con
  * QSTATE_EDEVICE for the rest of the process. */
 int qstate_check(void* stream);
 
-/* Limit, in polls of the mbarrier, of the chunked form's waits for its tensor-core products in
- * the calls that follow (process-wide; read when a call is enqueued).  polls >= 0 sets it; 0
+/* Limit, in polls of the mbarrier, of the waits of the chunked form and of qstate_kv_attend over
+ * latents for their tensor-core products in the calls that follow (process-wide; read when a call is enqueued).  polls >= 0 sets it; 0
  * gives up at the first wait without polling (the products still complete, the results of
  * that call are invalid and qstate_check reports QSTATE_ETIMEOUT): a way to exercise the
  * timeout path without a faulty kernel.  polls < 0 restores the default (2^24 polls, far

@@ -267,9 +267,8 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
             queries(w.r);
             queries_done();
         }
-        bool begins = true;
+        bool begins = true, ok = true;   // ok: no wait has been given up
         for (int i = 0; live; ++i) {
-            bool ok = true;
             const bool copier = !g.box || pw == 0;
             const int r = w.r, t = w.span.base + w.tile * kLatTile + from + lane * tokens;
             // pages that hold nothing in the window are not looked at: they may have been given back
@@ -292,7 +291,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                     mask |= static_cast<uint64_t>(__ballot_sync(kFull, u >= begin && u < end && page_there)) << (32 * k);
                 }
             }
-            if (copier && i >= g.stages) ok = role_wait(&x.free[s], (i / g.stages - 1) & 1, abort, p);
+            if (copier && i >= g.stages) ok = ok && role_wait(&x.free[s], (i / g.stages - 1) & 1, abort, p);
             if (pw == 0 && lane == 0 && ok)
                 *reinterpret_cast<volatile uint32_t*>(&x.flags[s]) = (first ? 1u : 0u) | (begins ? 2u : 0u) | (more ? 0u : 4u);
             if (g.box && pw == 0) {
@@ -343,7 +342,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
             if (live) id = look_up(w);
             if (first && i > 0 && asks) {
                 // S of the row before is done with its queries
-                ok = role_wait(&x.qfree, rows++ & 1, abort, p);
+                ok = ok && role_wait(&x.qfree, rows++ & 1, abort, p);
                 if (ok) queries(r);
                 queries_done();
             }
