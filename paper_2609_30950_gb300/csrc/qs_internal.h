@@ -100,6 +100,9 @@ struct AllocParams {
 // each; one-prompt prefill 811 -> 730 us).  The chains of a partitioned scan launch without it:
 // CTAs that wait in one chain would hold SMs that another chain's work fills (KDA prefill, 2 chains:
 // 1243 us with it, 1226 us without; KDA decode, 4 chains: 1442 against 1440 us).
+// The paged cache's kernels all launch with it, so what the one before wrote (lengths, tables, slots) is read by
+// ordinary loads (a step of a plan, 12 appends and 12 attentions for 4 requests of 100 tokens, in a graph:
+// 86 us without, 76 with).
 template <class... P, class... A>
 cudaError_t launch_chained(void (*kern)(P...), int grid, int threads, size_t smem, cudaStream_t stream, bool early,
                            A... args) {

@@ -35,6 +35,7 @@ template <int kEntries, int kLanes>
 __global__ void __launch_bounds__(kThreads) kv_copy_kernel(const KvAppendParams p, const int head_shift) {
     using Vec = typename std::conditional<kEntries == 8, uint4, uint16_t>::type;
     constexpr int kSteps = 4;
+    chain_wait();
     const long long t = static_cast<long long>(blockIdx.x) * TokenLanes<kLanes>::kTokens + threadIdx.x / kLanes;
     const int part = threadIdx.x % kLanes;
     if (t >= p.T) return;
@@ -70,6 +71,7 @@ __global__ void __launch_bounds__(kThreads) kv_copy_kernel(const KvAppendParams 
 template <int D, bool kAligned, int kLanes>
 __global__ void __launch_bounds__(kThreads) kv_quant_kernel(const KvAppendParams p) {
     constexpr int kVec = D / 16;
+    chain_wait();
     const long long t = static_cast<long long>(blockIdx.x) * TokenLanes<kLanes>::kTokens + threadIdx.x / kLanes;
     const int part = threadIdx.x % kLanes;
     int slot = t < p.T ? p.slot[t] : -1;
@@ -131,29 +133,24 @@ template <int kLanes>
 unsigned token_blocks(int T) { return (static_cast<unsigned>(T) + TokenLanes<kLanes>::kTokens - 1) / TokenLanes<kLanes>::kTokens; }
 
 template <int D>
-void launch_quant(bool aligned, const KvAppendParams& p, cudaStream_t stream) {
+cudaError_t launch_quant(bool aligned, const KvAppendParams& p, cudaStream_t stream) {
     constexpr int kFew = D / 16 > 8 ? D / 16 : 8;   // lanes of a token of one or two heads
     const bool few = p.Hkv * (D / 16) <= kFew;
-    if (few && aligned)
-        kv_quant_kernel<D, true, kFew><<<token_blocks<kFew>(p.T), kThreads, 0, stream>>>(p);
-    else if (few)
-        kv_quant_kernel<D, false, kFew><<<token_blocks<kFew>(p.T), kThreads, 0, stream>>>(p);
-    else if (aligned)
-        kv_quant_kernel<D, true, 32><<<token_blocks<32>(p.T), kThreads, 0, stream>>>(p);
-    else
-        kv_quant_kernel<D, false, 32><<<token_blocks<32>(p.T), kThreads, 0, stream>>>(p);
+    if (few && aligned) return launch_chained(kv_quant_kernel<D, true, kFew>, token_blocks<kFew>(p.T), kThreads, 0, stream, true, p);
+    if (few) return launch_chained(kv_quant_kernel<D, false, kFew>, token_blocks<kFew>(p.T), kThreads, 0, stream, true, p);
+    if (aligned) return launch_chained(kv_quant_kernel<D, true, 32>, token_blocks<32>(p.T), kThreads, 0, stream, true, p);
+    return launch_chained(kv_quant_kernel<D, false, 32>, token_blocks<32>(p.T), kThreads, 0, stream, true, p);
 }
 
 template <int kEntries>
-void launch_copy(const KvAppendParams& p, cudaStream_t stream) {
+cudaError_t launch_copy(const KvAppendParams& p, cudaStream_t stream) {
     // entries of a head as a power of two of steps; one head needs none
     int shift = 30;
     if (p.Hkv > 1)
         for (shift = 0; (kEntries << shift) < p.d[0];) ++shift;
     if (p.Hkv * p.d[0] / kEntries <= 8)
-        kv_copy_kernel<kEntries, 8><<<token_blocks<8>(p.T), kThreads, 0, stream>>>(p, shift);
-    else
-        kv_copy_kernel<kEntries, 32><<<token_blocks<32>(p.T), kThreads, 0, stream>>>(p, shift);
+        return launch_chained(kv_copy_kernel<kEntries, 8>, token_blocks<8>(p.T), kThreads, 0, stream, true, p, shift);
+    return launch_chained(kv_copy_kernel<kEntries, 32>, token_blocks<32>(p.T), kThreads, 0, stream, true, p, shift);
 }
 
 }  // namespace
@@ -164,15 +161,10 @@ cudaError_t launch_kv_append(const qstate_kv_cfg& c, const KvAppendParams& p, cu
         aligned = aligned && reinterpret_cast<uintptr_t>(p.src[x]) % 16 == 0 && p.row[x] % 8 == 0 &&
                   (p.head[x] % 8 == 0 || p.Hkv == 1);
     if (c.store == QSTATE_KV_E4M3) {
-        if (p.d[0] == 64) launch_quant<64>(aligned, p, stream);
-        else if (p.d[0] == 128) launch_quant<128>(aligned, p, stream);
-        else launch_quant<256>(aligned, p, stream);
-    } else if (aligned) {
-        launch_copy<8>(p, stream);
-    } else {
-        launch_copy<1>(p, stream);
+        if (p.d[0] == 64) return launch_quant<64>(aligned, p, stream);
+        return p.d[0] == 128 ? launch_quant<128>(aligned, p, stream) : launch_quant<256>(aligned, p, stream);
     }
-    return cudaGetLastError();
+    return aligned ? launch_copy<8>(p, stream) : launch_copy<1>(p, stream);
 }
 
 }  // namespace qs

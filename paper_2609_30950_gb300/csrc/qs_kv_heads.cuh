@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
     constexpr int kSteps = D / 16, kOut = D / 8;
     constexpr float kLog2e = 1.4426950408889634f;
     extern __shared__ __align__(128) char smem[];
-    chain_release();   // the kernel that joins split rows may take its place
+    chain_wait();   // and the kernel that joins split rows may take its place
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane >> 2, t4 = lane & 3;
     const int groups = p.Hkv * groups_per_kv, G = p.Hq / p.Hkv;
 
@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
         const int t = fw.span.base + (fw.tile * S::kWarps + warp) * S::kChunk + (one_page ? 0 : lane);
         id = -1;
         if (t < fw.span.end && (one_page || lane < S::kChunk))
-            id = __ldg(p.table + static_cast<size_t>(fw.r) * p.max_pages + (t >> p.page_shift));
+            id = p.table[static_cast<size_t>(fw.r) * p.max_pages + (t >> p.page_shift)];
     };
     // Queries of a row that begins: thread tid copies pieces tid % 8 + 8 i of head tid / 8 (and finds them there).
     auto q_src = [&](const Walk<S::kTile, S::kChunk>& w, int* heads) {
@@ -542,8 +542,8 @@ cudaError_t launch_heads(KvAttendParams p, int per_group, int groups_per_kv, cud
         const long long rows = static_cast<long long>(p.R) * p.Hkv * groups_per_kv;
         if (rows < p.workers) p.workers = static_cast<int>(rows);
     }
-    kernel<<<p.workers, S::kThreads, S::kBytes, stream>>>(p, per_group, groups_per_kv);
-    if ((e = cudaGetLastError()) != cudaSuccess || p.whole_rows) return e;
+    e = launch_chained(kernel, p.workers, S::kThreads, S::kBytes, stream, true, p, per_group, groups_per_kv);
+    if (e != cudaSuccess || p.whole_rows) return e;
     return launch_join<D, kF16>(p, JoinGeo{1, kHeadRows, per_group, p.Hq / p.Hkv, groups_per_kv}, stream);
 }
 

@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
     const int worker = blockIdx.x / g.groups, group = blockIdx.x - worker * g.groups;
     const int h0 = group * g.per_group, heads = min(g.per_group, p.Hq - h0);
     const int askers = g.box ? kLatCopiers - 1 : kLatCopiers;   // warps that copy queries
-    chain_release();   // the kernel that joins split rows may take its place
+    chain_wait();   // and the kernel that joins split rows may take its place
 
     if (g.box && warp == kLatIssuer + 1) prefetch_map(&map);
     if (warp == kLatIssuer) {
@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
         const int lanes = !g.box ? 16 : pw == 0 ? kLatTile / g.box : 0, from = g.box ? 0 : pw * 16;
         auto look_up = [&](const W& at) {
             const int t = at.span.base + at.tile * kLatTile + from + lane * tokens;
-            return lane < lanes && t < at.span.end ? __ldg(p.table + static_cast<size_t>(at.r) * p.max_pages + (t >> p.page_shift)) : -1;
+            return lane < lanes && t < at.span.end ? p.table[static_cast<size_t>(at.r) * p.max_pages + (t >> p.page_shift)] : -1;
         };
         const uint32_t lead = elect_lane();
         // a thread copies one of eight pieces of every block of its heads
@@ -665,8 +665,8 @@ cudaError_t launch_latent(KvAttendParams p, const LatentGeo& g, const CUtensorMa
     p.workers = g.workers;
     p.whole_rows = (static_cast<long long>(p.max_pages) << p.page_shift) <= kWholeTiles * kLatTile;
     if (p.whole_rows && p.R < p.workers) p.workers = p.R;
-    kernel<<<p.workers * g.groups, kLatThreads, g.smem, stream>>>(p, g, map);
-    if ((e = cudaGetLastError()) != cudaSuccess || p.whole_rows) return e;
+    e = launch_chained(kernel, p.workers * g.groups, kLatThreads, g.smem, stream, true, p, g, map);
+    if (e != cudaSuccess || p.whole_rows) return e;
     return launch_join<DV, kF16>(p, JoinGeo{g.groups, kN, g.per_group, p.Hq, g.groups}, stream);
 }
 

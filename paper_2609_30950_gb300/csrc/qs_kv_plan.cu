@@ -67,6 +67,7 @@ __device__ __forceinline__ int first_above(const unsigned* ends, int n, unsigned
 template <int kRows>
 __global__ void __launch_bounds__(256) kv_plan_kernel(const KvPlanParams p) {
     extern __shared__ int smem[];
+    chain_wait();
     __shared__ unsigned sums[4][32];
     __shared__ unsigned s_granted;
     __shared__ int s_last;
@@ -264,8 +265,7 @@ cudaError_t launch_kv_plan(const KvPlanParams& p, cudaStream_t stream) {
     long long grid = (threads + kThreads - 1) / kThreads;
     if (grid < 4) grid = 4;
     if (grid > kMostPerSm * device_sm_count()) grid = kMostPerSm * device_sm_count();
-    kernel<<<static_cast<int>(grid), kThreads, smem, stream>>>(p);
-    return cudaGetLastError();
+    return launch_chained(kernel, static_cast<int>(grid), kThreads, smem, stream, true, p);
 }
 
 }  // namespace qs

@@ -24,7 +24,7 @@ struct Span {
 };
 
 __device__ __forceinline__ int clamped_len(const KvAttendParams& p, int r, bool report) {
-    const int n = __ldg(p.lens + r);
+    const int n = p.lens[r];
     const long long most = static_cast<long long>(p.max_pages) << p.page_shift;
     if (n >= 0 && n <= most) return n;
     if (report) raise_status(p.status, QS_DEV_PAGES);
