@@ -8,7 +8,7 @@
 #include <cstring>
 #include <mutex>
 
-#include "qs_internal.h"
+#include "qs_kv.h"
 
 namespace qs {
 cudaError_t launch_step_128x128(const qstate_cfg&, int, int, const StepParams&, cudaStream_t);

@@ -2,7 +2,7 @@
 #include <cmath>
 #include <cstring>
 
-#include "qs_internal.h"
+#include "qs_kv.h"
 
 using namespace qs;
 

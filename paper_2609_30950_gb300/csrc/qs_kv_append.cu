@@ -11,6 +11,7 @@
 #include <type_traits>
 
 #include "qs_common.cuh"
+#include "qs_kv.h"
 
 namespace qs {
 namespace {

@@ -14,6 +14,7 @@
 // round: the list is written at [free, new height) and read at [new height, free), the table is
 // written behind a request's old pages and read in front of them.
 #include "qs_common.cuh"
+#include "qs_kv.h"
 
 namespace qs {
 namespace {

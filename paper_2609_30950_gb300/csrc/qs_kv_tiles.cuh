@@ -14,6 +14,7 @@
 #pragma once
 
 #include "qs_common.cuh"
+#include "qs_kv.h"
 
 namespace qs {
 namespace kv {
