@@ -315,7 +315,7 @@ typedef struct qstate_kv_cfg {
 } qstate_kv_cfg;
 
 /* One layer's cache (device): k (n_pages, Hkv, page, dk), v (n_pages, Hkv, page, dv), 16-byte
- * aligned; v is NULL for LATENT.  k_exp and v_exp, (n_pages, Hkv, page) bytes, for E4M3 only.
+ * aligned; v is NULL for LATENT.  k_exp and v_exp, (n_pages, Hkv, page) bytes, 4-byte aligned, for E4M3 only.
  * What lies behind a request's last token is never used, whatever its bits. */
 typedef struct qstate_kv_cache {
     void* k;

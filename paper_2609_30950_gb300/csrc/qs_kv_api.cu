@@ -53,6 +53,8 @@ int check_cache(const qstate_kv_cfg* c, const qstate_kv_cache* cache) {
         return fail(QSTATE_EINVAL, "exponents belong to an e4m3 cache, and only to one");
     if (!aligned(cache->k, 16) || !aligned(cache->v, 16))
         return fail(QSTATE_EINVAL, "the cache must be 16-byte aligned");
+    if (!aligned(cache->k_exp, 4) || !aligned(cache->v_exp, 4))
+        return fail(QSTATE_EINVAL, "exponents must be 4-byte aligned");
     return QSTATE_OK;
 }
 

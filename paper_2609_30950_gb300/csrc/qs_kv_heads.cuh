@@ -160,15 +160,21 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
             }
         } else {
             const long long mine = head_row + (t & page_mask);   // row of the pool that this lane's token is
-#pragma unroll 2
+            const long long mine_at = mine * S::kRow;
+#pragma unroll 4
             for (int i = 0; i < S::kChunk * S::kSeg / 32; ++i) {
                 const int e = i * 32 + lane, row = e / S::kSeg, seg = e % S::kSeg, to = S::at(row, seg);
                 const bool on = (mask >> row) & 1;
-                const long long at = __shfl_sync(kFull, mine, row) * S::kRow + seg * 16;
+                const long long at = __shfl_sync(kFull, mine_at, row) + seg * 16;
                 cp_async16(dst + to, static_cast<const char*>(p.k) + (on ? at : 0), on);
                 cp_async16(dst + S::kTensor + to, static_cast<const char*>(p.v) + (on ? at : 0), on);
             }
-            if (kE4M3 && seen && there) {
+            if (kE4M3 && p.page_shift >= 2) {
+                const int g = lane & 7;
+                const long long four = __shfl_sync(kFull, mine, 4 * g);   // in one page
+                if (lane < 16 && ((mask >> (4 * g)) & 15))
+                    cp_async4(smem_u32(exps + stage * 64 + lane * 4), (lane < 8 ? p.k_exp : p.v_exp) + four);
+            } else if (kE4M3 && seen && there) {
                 exps[stage * 64 + lane] = p.k_exp[mine];
                 exps[stage * 64 + 32 + lane] = p.v_exp[mine];
             }

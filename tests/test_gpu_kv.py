@@ -406,3 +406,12 @@ def test_a_step_in_a_captured_graph(qs):
     mag = torch.einsum("rhgt,trhd->rhgd", w, V.abs()).reshape(R, Hq, d)
     assert bool(((o.double().cpu() - want).abs() <= 2.0 ** -9 * want.abs() + (2.0 ** -8 + 2.0 ** -13) * mag).all())
     assert math.isfinite(float(lse.sum()))
+
+
+@pytest.mark.parametrize("window", [0, 45])
+@pytest.mark.parametrize("page", [1, 2, 4, 8, 16, 32])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_codes_over_pages_shorter_than_a_chunk(qs, d, page, window):
+    b = ref.Batch(qs, EDGES, 10, 2, d, page=page, e4m3=True, window=window, seed=page + d, spread=2.0)
+    b.run(qs)
+    b.check(qs)

@@ -104,3 +104,12 @@ def test_reference_codes_are_the_nearest():
     assert torch.equal((codes - y).abs(), (y[..., None] - raw).abs().amin(-1))
     big = y.abs().amax(-1)
     assert bool(((big > 224) | (big == 0)).all())   # one power lower would not do
+
+
+def test_exponents_that_are_not_aligned_are_refused(q):
+    """The attention reads exponents four at a time."""
+    L, c, r = q._lib, config(q, store=q.KV_E4M3), ct.byref
+    for cache in (q._KvCache(A, A, A + 2, A), q._KvCache(A, A, A, A + 1)):
+        assert L.qstate_kv_attend(r(c._c), r(cache), A, 1024, 128, A, A, 1, A, None, A, None) == q.QSTATE_EINVAL
+        assert b"exponents" in L.qstate_last_error()
+        assert L.qstate_kv_append(r(c._c), r(cache), A, 256, 128, A, 256, 128, A, 1, None) == q.QSTATE_EINVAL
