@@ -37,7 +37,7 @@ KvPartBytes kv_part_bytes(const qstate_kv_cfg& c) {
     if (c.kind == QSTATE_KV_HEADS)
         return {static_cast<size_t>(kKvWorkers) * 2 * 16 * c.dv * sizeof(float),
                 static_cast<size_t>(kKvWorkers) * 2 * 16 * 16, split};
-    const kv::LatentGeo g = kv::latent_geo(c.Hq, c.dk, kKvSms);
+    const kv::LatentGeo g = kv::latent_geo(c.Hq, c.dk, c.dv, kKvSms);
     const size_t rows = static_cast<size_t>(g.workers) * g.groups * 2 * g.columns;
     return {rows * c.dv * sizeof(float), rows * 16, split};
 }

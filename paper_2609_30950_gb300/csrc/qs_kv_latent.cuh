@@ -48,6 +48,10 @@ struct LatentGeo {
     int box;           // rows of a copy by the tensor map: a page, or a tile of it; 0: copies of 16 bytes
 };
 
+// CTAs an SM that the kernel's registers are held to: two where shared memory has room for two with two tiles each.  (64 heads of
+// 128 + 0, 0.3 GB: 166 us with one, 127 with two.)
+__host__ __device__ constexpr int latent_ctas(int dv, int columns) { return dv == 128 || (dv == 256 && columns < 64) ? 2 : 1; }
+
 // Shared memory behind the tiles, the queries and p.
 struct LatentMisc {
     uint64_t full[kMaxStages][kMaxParts], free[kMaxStages], sready[2], qfull, qfree, pready, drain;
@@ -143,13 +147,29 @@ __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
 __device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];\n" ::"r"(smem_u32(bar)) : "memory");
 }
-// Whether a phase of a barrier is complete, for the whole warp alike and without waiting.
+// Whether a phase of a barrier is complete, for the whole warp alike; one lane looks for all.  (With this and phases that
+// are kept, not divided out of the tile's number, 64 requests of 64 heads of 128 + 0, up to 36000 tokens, took 166 us for
+// 191.)
+__device__ __forceinline__ bool warp_look(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p, q;\nsetp.eq.u32 q, %3, 0;\nsetp.ne.u32 p, %3, %3;\n"
+        "@q mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(threadIdx.x & 31) : "memory");
+    const bool done = __any_sync(kFull, ok != 0);
+    __syncwarp();   // what the phase's arrivals made visible to one lane is there for all
+    return done;
+}
+// The same without waiting a while in hardware.
 __device__ __forceinline__ bool warp_test(uint64_t* bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
-        "{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
-    return __all_sync(kFull, ok != 0);
+        "{\n.reg .pred p, q;\nsetp.eq.u32 q, %3, 0;\nsetp.ne.u32 p, %3, %3;\n"
+        "@q mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(threadIdx.x & 31) : "memory");
+    const bool done = __any_sync(kFull, ok != 0);
+    __syncwarp();   // what the phase's arrivals made visible to one lane is there for all
+    return done;
 }
 __device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;\n" ::: "memory"); }
 __device__ __forceinline__ bool softmax_any(bool x) {
@@ -164,19 +184,17 @@ __device__ __forceinline__ bool softmax_any(bool x) {
 // products any more.
 // Whole warps wait, and a warp's lanes agree on the answer.
 __device__ __forceinline__ bool role_wait(uint64_t* bar, uint32_t parity, volatile int* abort, const KvAttendParams& p) {
-    bool ok = false, give_up = false;
-    for (int it = 0; it < p.wait_polls && !ok && !give_up; ++it) {
-        ok = tc::mbar_try_wait(bar, parity);
-        give_up = !ok && *abort;
+    for (int it = 0; it < p.wait_polls; ++it) {
+        if (warp_look(bar, parity)) return true;
+        if (__any_sync(kFull, *abort)) break;
     }
-    if (__all_sync(kFull, ok)) return true;
     if (!*abort) raise_status(p.status, QS_DEV_TIMEOUT);
     *abort = 1;
     return false;
 }
 
 template <int DV, int kN, bool kF16>
-__global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendParams p, const LatentGeo g,
+__global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_kernel(const KvAttendParams p, const LatentGeo g,
                                                                 const __grid_constant__ CUtensorMap map) {
     using W = Walk<kLatTile, kLatTile>;   // tiles start at multiples of a tile: a copy lies in one page
     constexpr int kOCols = DV / 128 * kN, kCols = kOCols + 2 * kN;
@@ -262,7 +280,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
             __syncwarp();
             if (lane == 0) mbar_arrive(&x.qfull);
         };
-        int id = look_up(w), s = 0, rows = 0;   // rows: that have waited for the queries of the one before
+        int id = look_up(w), s = 0, phase = 0, rows = 0;   // rows: that have waited for the queries of the one before
         if (asks) {
             queries(w.r);
             queries_done();
@@ -291,7 +309,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                     mask |= static_cast<uint64_t>(__ballot_sync(kFull, u >= begin && u < end && page_there)) << (32 * k);
                 }
             }
-            if (copier && i >= g.stages) ok = ok && role_wait(&x.free[s], (i / g.stages - 1) & 1, abort, p);
+            if (copier && i >= g.stages) ok = ok && role_wait(&x.free[s], phase ^ 1, abort, p);
             if (pw == 0 && lane == 0 && ok)
                 *reinterpret_cast<volatile uint32_t*>(&x.flags[s]) = (first ? 1u : 0u) | (begins ? 2u : 0u) | (more ? 0u : 4u);
             if (g.box && pw == 0) {
@@ -346,7 +364,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                 if (ok) queries(r);
                 queries_done();
             }
-            s = s + 1 == g.stages ? 0 : s + 1;
+            if (++s == g.stages) s = 0, phase ^= 1;
         }
         cp_commit();
         cp_wait<0>();
@@ -440,7 +458,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
         const float zs = p.scale * kLog2e;
         // sums of p before and after its rounding
         float m[kPer], l[kPer], lr[kPer];
-        int prev = 0, s = 0, began = 0;   // prev: stage of the tile before
+        int prev = 0, prev_phase = 0, s = 0, phase = 0, began = 0;   // prev: stage of the tile before
         bool begins = true;
         // k: head c0 + 8 (k / 2) + 2 t4 + k % 2, at tokens quad and quad + 8 of the quarter
         auto head = [&](int k) { return c0 + 8 * (k >> 1) + 2 * t4 + (k & 1); };
@@ -451,7 +469,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
 #pragma unroll
                 for (int k = 0; k < kPer; ++k) m[k] = -INFINITY, l[k] = lr[k] = 0.0f;
             }
-            role_wait(&x.full[s][0], (i / g.stages) & 1, abort, p);
+            role_wait(&x.full[s][0], phase, abort, p);
             role_wait(&x.sready[i & 1], (i >> 1) & 1, abort, p);
             tc::fence_after_sync();
             float z[2 * kPer];
@@ -475,7 +493,6 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                 b = (on >> (quad + 8)) & 1 ? b * zs : -INFINITY;
                 grown = grown || fmaxf(a, b) > m[k] + kLazyLatent;
             }
-            const uint32_t prev_parity = i > 0 ? ((i - 1) / g.stages) & 1 : 0;
             if (softmax_any(grown)) {
 #pragma unroll
                 for (int k = 0; k < kPer; ++k) {
@@ -497,7 +514,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                 }
                 softmax_sync();
                 if (!begins) {
-                    role_wait(&x.free[prev], prev_parity, abort, p);   // the products so far are in
+                    role_wait(&x.free[prev], prev_phase, abort, p);   // the products so far are in
                     tc::fence_after_sync();
 #pragma unroll 1
                     for (int c = (warp >> 2) * 16; c < kOCols; c += 32) {
@@ -527,7 +544,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                 lr[j & ~1] += r.x;
                 lr[j | 1] += r.y;
             }
-            if (i > 0) role_wait(&x.free[prev], prev_parity, abort, p);   // p of the tile before has been read
+            if (i > 0) role_wait(&x.free[prev], prev_phase, abort, p);   // p of the tile before has been read
             if constexpr (kN == 16) {
                 const int h = c0 + (lane & 7), chunk = sub * 2 + ((lane >> 3) & 1);
                 stmatrix2t(p32 + h * 128 + ((chunk ^ (h & 7)) << 4), pk[0], pk[1]);
@@ -575,7 +592,7 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                         p.lse[row + tid] = sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
                 }
                 softmax_sync();
-                role_wait(&x.free[s], (i / g.stages) & 1, abort, p);
+                role_wait(&x.free[s], phase, abort, p);
                 tc::fence_after_sync();
 #pragma unroll 1
                 for (int c = (warp >> 2) * 16; c < kOCols; c += 32) {
@@ -600,7 +617,8 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
                 }
             }
             prev = s;
-            s = s + 1 == g.stages ? 0 : s + 1;
+            prev_phase = phase;
+            if (++s == g.stages) s = 0, phase ^= 1;
             begins = ends;
             live = w.next(p, 1);
         }
@@ -638,8 +656,8 @@ __global__ void __launch_bounds__(kLatThreads) kv_latent_kernel(const KvAttendPa
 bool pool_map(CUtensorMap* map, const void* pool, int dk, long long rows, int box);
 
 // Groups of at most 64 heads, products of 16, 32 or 64 columns; as many tiles in flight as fit beside the
-// queries, and two CTAs on an SM where each gets two.
-inline LatentGeo latent_geo(int Hq, int dk, int sms) {
+// queries, and two CTAs on an SM where the kernel is made for it.
+inline LatentGeo latent_geo(int Hq, int dk, int dv, int sms) {
     if (sms > kKvSms) sms = kKvSms;
     LatentGeo g;
     g.groups = (Hq + 63) / 64;
@@ -649,7 +667,7 @@ inline LatentGeo latent_geo(int Hq, int dk, int sms) {
     g.blocks = (dk + 63) / 64;
     const int fixed = g.blocks * N * 128 + N * 128 + static_cast<int>(sizeof(LatentMisc)), tile = g.blocks * kBlockBytes;
     constexpr int kMost = 227 * 1024, kHalf = 113 * 1024;
-    const int limit = fixed + 2 * tile <= kHalf ? kHalf : kMost;
+    const int limit = latent_ctas(dv, N) == 2 && fixed + 2 * tile <= kHalf ? kHalf : kMost;
     g.stages = (limit - fixed) / tile;
     if (g.stages > kMaxStages) g.stages = kMaxStages;
     g.smem = fixed + g.stages * tile;
@@ -674,7 +692,7 @@ cudaError_t launch_latent(KvAttendParams p, const LatentGeo& g, const CUtensorMa
 
 template <int DV>
 cudaError_t launch_latent_of(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream) {
-    LatentGeo g = latent_geo(p.Hq, p.dk, device_sm_count());
+    LatentGeo g = latent_geo(p.Hq, p.dk, DV, device_sm_count());
     // A box a page and 64 entries, from pages of 32 tokens on.  One lane issues them, some 100 cycles each, and
     // shorter pages take so many that the copies of 16 bytes, which cost four warps' instructions but nothing
     // a page, are faster (64 requests of 64 heads of 512 + 64, up to 8000 tokens: pages of 8 tokens 191 us by boxes, 107
