@@ -14,9 +14,9 @@
 //   warps 0-7   softmax: 16 tokens and half of the heads each from S^T, p to shared memory in 16 bits; at
 //               a row's end o
 //   warp 8      issues the products
-//   warp 9      copies tiles, a box of the tensor map for each page and 64 entries; in parts, so that S need not
-//               wait for the whole of a tile
-//   warps 9-12  (10-12 where warp 9 copies boxes) copy a row's queries, and, 16 bytes at a time, tiles of short pages
+//   warp 9      copies tiles that lie in one page, a box of the tensor map for each 64 entries; in parts, so that S need
+//               not wait for the whole of a tile
+//   warps 9-12  (10-12 where warp 9 copies boxes) copy a row's queries, and, 16 bytes at a time, tiles of shorter pages
 // As in the kernel for heads, the softmax reference follows the maximum only when that has outgrown it by
 // 2^8; all tokens of a row share one reference, so the eight warps vote.  p has 16 bits in the second product
 // and o is divided by the sum of the rounded p, so that the weights in use add up to one; lse comes from
@@ -45,7 +45,7 @@ constexpr float kLazyLatent = 8.0f;
 struct LatentGeo {
     int blocks;        // of 64 entries, the last may be half
     int stages, smem, groups, per_group, columns, workers;
-    int box;           // rows of a copy by the tensor map: a page, or a tile of it; 0: copies of 16 bytes
+    bool boxes;        // a tile lies in one page and is copied by the tensor map
 };
 
 // CTAs an SM that the kernel's registers are held to: two where shared memory has room for two with two tiles each.  (64 heads of
@@ -209,17 +209,17 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
     LatentMisc& x = *reinterpret_cast<LatentMisc*>(probs + kN * 128);
     const int worker = blockIdx.x / g.groups, group = blockIdx.x - worker * g.groups;
     const int h0 = group * g.per_group, heads = min(g.per_group, p.Hq - h0);
-    const int askers = g.box ? kLatCopiers - 1 : kLatCopiers;   // warps that copy queries
+    const int askers = g.boxes ? kLatCopiers - 1 : kLatCopiers;   // warps that copy queries
     chain_wait();   // and the kernel that joins split rows may take its place
 
-    if (g.box && warp == kLatIssuer + 1) prefetch_map(&map);
+    if (g.boxes && warp == kLatIssuer + 1) prefetch_map(&map);
     if (warp == kLatIssuer) {
         tc::tmem_alloc(&x.tmem, kAlloc);
         tc::tmem_relinquish();
     }
     if (tid == 0) {
         for (int s = 0; s < kMaxStages; ++s) {
-            for (int k = 0; k < kMaxParts; ++k) tc::mbar_init(&x.full[s][k], g.box ? 1 : kLatCopiers * 33);
+            for (int k = 0; k < kMaxParts; ++k) tc::mbar_init(&x.full[s][k], g.boxes ? 1 : kLatCopiers * 33);
             tc::mbar_init(&x.free[s], 1);
         }
         tc::mbar_init(&x.sready[0], 1);
@@ -247,12 +247,13 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
     if (live && warp > kLatIssuer) {
         // ---- copies ----
         const int pw = warp - kLatIssuer - 1, page_mask = (1 << p.page_shift) - 1;
-        const int tokens = g.box ? g.box : 1;   // a lane looks a page up for so many
-        const bool asks = !g.box || pw > 0;
-        const int lanes = !g.box ? 16 : pw == 0 ? kLatTile / g.box : 0, from = g.box ? 0 : pw * 16;
+        const bool asks = !g.boxes || pw > 0, copier = !g.boxes || pw == 0;
+        // of a tile's tokens, the one whose page a lane looks up, and those that are with it
+        const int from = g.boxes ? 0 : pw * 16 + lane, tokens = g.boxes ? kLatTile : 1;
+        const bool looks = copier && (g.boxes || lane < 16);
         auto look_up = [&](const W& at) {
-            const int t = at.span.base + at.tile * kLatTile + from + lane * tokens;
-            return lane < lanes && t < at.span.end ? p.table[static_cast<size_t>(at.r) * p.max_pages + (t >> p.page_shift)] : -1;
+            const int t = at.span.base + at.tile * kLatTile + from;
+            return looks && t < at.span.end ? p.table[static_cast<size_t>(at.r) * p.max_pages + (t >> p.page_shift)] : -1;
         };
         const uint32_t lead = elect_lane();
         // a thread copies one of eight pieces of every block of its heads
@@ -287,12 +288,11 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
         }
         bool begins = true, ok = true;   // ok: no wait has been given up
         for (int i = 0; live; ++i) {
-            const bool copier = !g.box || pw == 0;
-            const int r = w.r, t = w.span.base + w.tile * kLatTile + from + lane * tokens;
+            const int r = w.r, t = w.span.base + w.tile * kLatTile + from;
             // pages that hold nothing in the window are not looked at: they may have been given back
-            const bool wanted = lane < lanes && t < w.span.end && t + tokens > w.span.begin;
+            const bool wanted = looks && t < w.span.end && t + tokens > w.span.begin;
             const bool there = wanted && id >= 0 && id < p.n_pages;
-            if ((!g.box || pw == 0) && wanted && !there) raise_status(p.status, QS_DEV_PAGES);
+            if (wanted && !there) raise_status(p.status, QS_DEV_PAGES);
             const long long row = there ? (static_cast<long long>(id) << p.page_shift) + (t & page_mask) : 0;
             const uint32_t tile = smem_u32(tiles + s * g.blocks * kBlockBytes);
             const bool first = begins;
@@ -300,39 +300,33 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
             W after = w;
             const bool more = after.next(p, 1);
             uint64_t mask = 0;   // tokens that are seen: lanes take two each
-            if (g.box && pw == 0) {
+            if (g.boxes) {
                 const int begin = w.span.begin - w.span.base - w.tile * kLatTile, end = w.span.end - w.span.base - w.tile * kLatTile;
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int u = lane + 32 * k;
-                    const bool page_there = __shfl_sync(kFull, static_cast<int>(there), u / g.box) != 0;
-                    mask |= static_cast<uint64_t>(__ballot_sync(kFull, u >= begin && u < end && page_there)) << (32 * k);
+                    mask |= static_cast<uint64_t>(__ballot_sync(kFull, u >= begin && u < end && there)) << (32 * k);
                 }
             }
             if (copier && i >= g.stages) ok = ok && role_wait(&x.free[s], phase ^ 1, abort, p);
             if (pw == 0 && lane == 0 && ok)
                 *reinterpret_cast<volatile uint32_t*>(&x.flags[s]) = (first ? 1u : 0u) | (begins ? 2u : 0u) | (more ? 0u : 4u);
-            if (g.box && pw == 0) {
-                const uint32_t boxes = __ballot_sync(kFull, there);
-                if (ok) {
+            if (g.boxes) {
+                if (copier && ok) {
                     copied = i + 1;
                     if (lane == 0) *reinterpret_cast<volatile uint64_t*>(&x.mask[s]) = mask;
                     for (int k = 0; k < kParts; ++k) {
                         const int b0 = k * kPartBlocks, many = min(kPartBlocks, g.blocks - b0);
-                        if (lane == 0) mbar_arrive_expect(&x.full[s][k], __popc(boxes) * many * g.box * 128);
+                        if (lane == 0) mbar_arrive_expect(&x.full[s][k], there ? many * kBlockBytes : 0);
                         __syncwarp();
                         const uint32_t bar = smem_u32(&x.full[s][k]);
-                        for (int c = 0; c < lanes; ++c) {
-                            if (!((boxes >> c) & 1)) continue;
-                            const int row_c = __shfl_sync(kFull, static_cast<int>(row), c);
 #pragma unroll
-                            for (int b = 0; b < kPartBlocks; ++b)
-                                if (b < many)
-                                    tma_box(tile + (b0 + b) * kBlockBytes + c * g.box * 128, &map, (b0 + b) * 64, row_c, bar, lead);
-                        }
+                        for (int b = 0; b < kPartBlocks; ++b)
+                            if (there && b < many)
+                                tma_box(tile + (b0 + b) * kBlockBytes, &map, (b0 + b) * 64, static_cast<int>(row), bar, lead);
                     }
                 }
-            } else if (!g.box) {
+            } else {
                 const uint32_t on = __ballot_sync(kFull, there);
                 if (lane == 0) reinterpret_cast<volatile uint16_t*>(&x.mask[s])[pw] = static_cast<uint16_t>(on);
                 const char* src[4];
@@ -340,7 +334,7 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                     src[k] = static_cast<const char*>(p.k) + __shfl_sync(kFull, row, k * 4 + row0) * (2 * p.dk) + seg * 16;
-                const uint32_t to = tile + (from + row0) * 128;
+                const uint32_t to = tile + (pw * 16 + row0) * 128;
                 for (int part = 0; part < kParts; ++part) {
                     for (int b = part * kPartBlocks; ok && b < min(g.blocks, (part + 1) * kPartBlocks); ++b)
                         if (b * 64 + seg * 8 < p.dk) {
@@ -476,7 +470,7 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
             tmem_ld_rows<kN / 16>(tlane + kOCols + (i & 1) * kN + c0, z);
             const uint64_t seen = *reinterpret_cast<volatile uint64_t*>(&x.mask[s]);
             const uint32_t on = static_cast<uint32_t>(seen >> (16 * sub)) & 0xffffu;
-            if (g.box && seen != ~0ull) {
+            if (g.boxes && seen != ~0ull) {
                 // what a box brought beside the tokens that are seen, or left as it was, must not meet p = 0 as NaN
                 for (int u = warp; u < kLatTile; u += kLatSoftmax)
                     if (!((seen >> u) & 1))
@@ -651,9 +645,9 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
     }
 }
 
-// Map of the pool as rows of dk 16-bit entries, for boxes of 64 entries x `box` rows; false if the driver has no such
+// Map of the pool as rows of dk 16-bit entries, for boxes of 64 entries x 64 rows; false if the driver has no such
 // call or refuses (qs_kv_attend.cu).
-bool pool_map(CUtensorMap* map, const void* pool, int dk, long long rows, int box);
+bool pool_map(CUtensorMap* map, const void* pool, int dk, long long rows);
 
 // Groups of at most 64 heads, products of 16, 32 or 64 columns; as many tiles in flight as fit beside the
 // queries, and two CTAs on an SM where the kernel is made for it.
@@ -693,14 +687,13 @@ cudaError_t launch_latent(KvAttendParams p, const LatentGeo& g, const CUtensorMa
 template <int DV>
 cudaError_t launch_latent_of(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream) {
     LatentGeo g = latent_geo(p.Hq, p.dk, DV, device_sm_count());
-    // A box a page and 64 entries, from pages of 32 tokens on.  One lane issues them, some 100 cycles each, and
-    // shorter pages take so many that the copies of 16 bytes, which cost four warps' instructions but nothing
-    // a page, are faster (64 requests of 64 heads of 512 + 64, up to 8000 tokens: pages of 8 tokens 191 us by boxes, 107
-    // by 16 bytes; of 16 tokens 130 and 106; of 32 tokens 107 and 107; 64 requests of 16 heads of 128 + 64, up
-    // to 30000: 148 and 100, 111 and 99, 93 and 105).
+    // Boxes where a page holds a whole tile: nine of them for 512 + 64.  One lane issues them, some 100 cycles each, so that with
+    // shorter pages the copies of 16 bytes, which cost four warps' instructions but nothing a page, are the faster ones
+    // or near (64 requests, heads and latents: pages of 32 tokens by boxes and by 16 bytes, then pages of 64: 64 of 512 + 64
+    // 95.8, 92.3, then 91.9 and 92.0 us; 64 of 256 + 64 68.4, 59.8, then 58.0 and 59.7; 16 of 128 + 64 87.2, 89.0, then 75.5
+    // and 89.0; at pages of 8 the first took 191 by boxes, 107 by 16 bytes).
     CUtensorMap map = {};
-    g.box = c.page < 32 ? 0 : c.page < kLatTile ? c.page : kLatTile;
-    if (g.box && !pool_map(&map, p.k, p.dk, static_cast<long long>(c.n_pages) * c.page, g.box)) g.box = 0;
+    g.boxes = c.page >= kLatTile && pool_map(&map, p.k, p.dk, static_cast<long long>(c.n_pages) * c.page);
     const bool f16 = c.dtype == QSTATE_KV_F16;
     if (g.columns == 16) return f16 ? launch_latent<DV, 16, true>(p, g, map, stream) : launch_latent<DV, 16, false>(p, g, map, stream);
     if (g.columns == 32) return f16 ? launch_latent<DV, 32, true>(p, g, map, stream) : launch_latent<DV, 32, false>(p, g, map, stream);
