@@ -60,7 +60,9 @@ struct LatentMisc {
     uint64_t full[kMaxStages][kMaxParts], free[kMaxStages], sready[2], qfull, qfree, pready, drain;
     uint64_t mask[kMaxStages];
     uint32_t flags[kMaxStages];   // of the tile: 1 its row begins here, 2 it ends here, 4 it is the last
-    float top[4][64], topr[4][64], corr[64], inv[64];   // corr: the references at a row's end
+    float top[4][64], topr[4][64];
+    float corr[64];   // what O's sums are multiplied by; warps read it at their own pace until the next vote
+    float inv[64];    // at a row's end its references, then what o is multiplied by
     Share share;
     uint32_t tmem;
     int abort;
@@ -571,7 +573,7 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
                     if (quad == 0) {
                         x.top[sub][h] = sum;
                         x.topr[sub][h] = sumr;
-                        if (sub == 0) x.corr[h] = m[k];
+                        if (sub == 0) x.inv[h] = m[k];
                     }
                 }
                 softmax_sync();
@@ -580,7 +582,7 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
                 const size_t row = static_cast<size_t>(w.r) * p.Hq + h0;
                 const size_t prow = (static_cast<size_t>(slot) * g.groups + group) * kN;
                 if (tid < kN) {
-                    const float sum = x.top[0][tid] + x.top[1][tid] + x.top[2][tid] + x.top[3][tid], ref = x.corr[tid];
+                    const float sum = x.top[0][tid] + x.top[1][tid] + x.top[2][tid] + x.top[3][tid], ref = x.inv[tid];
                     const float sumr = x.topr[0][tid] + x.topr[1][tid] + x.topr[2][tid] + x.topr[3][tid];
                     x.inv[tid] = sumr == 0.0f ? 0.0f : 1.0f / sumr;
                     if (!whole)
