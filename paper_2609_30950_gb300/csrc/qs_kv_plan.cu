@@ -256,8 +256,11 @@ cudaError_t launch_kv_plan(const KvPlanParams& p, cudaStream_t stream) {
     // a row or so for each request the look-ups would follow one another (256 requests: 6.8 us against 4.6).
     const bool many = p.slots.T > 16LL * p.R;
     auto* const kernel = many ? kv_plan_kernel<4> : kv_plan_kernel<1>;
-    if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    // 48 KB without asking count the kernel's own arrays (some 500 bytes) too.  The limit is the kernel's, not the
+    // call's: every call sets the same one, so that none takes it away from another thread's between its two steps.
+    constexpr int kAsk = 40 * 1024, kMost = 5 * sizeof(int) * kKvMaxRequests;
+    if (smem > kAsk) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
         if (e != cudaSuccess) return e;
     }
     // CTAs of 8 warps, four at least: a decode step's few rows, and the pages that ended requests give back, are
