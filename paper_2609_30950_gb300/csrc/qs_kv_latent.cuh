@@ -42,6 +42,7 @@ constexpr int kLatSoftmax = 8, kLatIssuer = kLatSoftmax, kLatCopiers = 4;   // w
 constexpr int kLatThreads = (kLatSoftmax + 1 + kLatCopiers) * 32;
 constexpr int kBlockBytes = kLatTile * 128;   // 64 tokens x 64 entries
 constexpr int kMaxStages = 4;
+constexpr int kLatSmem = 227 * 1024;   // shared memory of an SM's only CTA
 constexpr int kPartBlocks = 3, kMaxParts = 3;   // a tile is waited for in parts, so that S follows the copies
 constexpr float kLazyLatent = 8.0f;
 
@@ -68,7 +69,7 @@ struct LatentMisc {
     int abort;
 };
 // two tiles of the widest latents stand beside 64 heads' queries and p
-static_assert(2 * 9 * kBlockBytes + 9 * 64 * 128 + 64 * 128 + sizeof(LatentMisc) <= 227 * 1024, "shared memory of an SM");
+static_assert(2 * 9 * kBlockBytes + 9 * 64 * 128 + 64 * 128 + sizeof(LatentMisc) <= kLatSmem, "shared memory of an SM");
 
 // Products of 16-bit types, FP32 sums: M x N, A optionally M-major.
 __host__ __device__ constexpr uint32_t idesc_f16(bool f16, int M, int N, bool a_m_major) {
@@ -665,8 +666,8 @@ inline LatentGeo latent_geo(int Hq, int dk, int dv, int sms) {
     g.columns = N;
     g.blocks = (dk + 63) / 64;
     const int fixed = g.blocks * N * 128 + N * 128 + static_cast<int>(sizeof(LatentMisc)), tile = g.blocks * kBlockBytes;
-    constexpr int kMost = 227 * 1024, kHalf = 113 * 1024;
-    const int limit = latent_ctas(dv, N) == 2 && fixed + 2 * tile <= kHalf ? kHalf : kMost;
+    constexpr int kHalf = 113 * 1024;
+    const int limit = latent_ctas(dv, N) == 2 && fixed + 2 * tile <= kHalf ? kHalf : kLatSmem;
     g.stages = (limit - fixed) / tile;
     if (g.stages > kMaxStages) g.stages = kMaxStages;
     g.smem = fixed + g.stages * tile;
@@ -679,7 +680,9 @@ inline LatentGeo latent_geo(int Hq, int dk, int dv, int sms) {
 template <int DV, int kN, bool kF16>
 cudaError_t launch_latent(KvAttendParams p, const LatentGeo& g, const CUtensorMap& map, cudaStream_t stream) {
     auto* kernel = kv_latent_kernel<DV, kN, kF16>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, g.smem);
+    // The limit is the kernel's, and layers of other widths share the kernel: all of an SM for every call, so that none
+    // takes it away from another thread's between its two steps.
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLatSmem);
     if (e != cudaSuccess) return e;
     p.workers = g.workers;
     p.whole_rows = (static_cast<long long>(p.max_pages) << p.page_shift) <= kWholeTiles * kLatTile;

@@ -8,6 +8,8 @@ import threading
 import pytest
 import torch
 
+import kv_reference as ref
+
 pytestmark = pytest.mark.gpu
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -58,6 +60,15 @@ def at_once(calls, seconds=4.0):
         t.join()
     torch.cuda.synchronize()
     return errors
+
+
+def test_layers_of_different_widths_from_several_threads(qs):
+    batches = [ref.Batch(qs, [40, 3], 64, 1, dk, 128, page=64, latent=True, seed=dk) for dk in (128, 160, 192)]
+    torch.cuda.synchronize()
+    errors = at_once([lambda s, b=b: b.run(qs, stream=s) for b in batches])
+    assert not errors, errors[0]
+    for b in batches:
+        b.check(qs)
 
 
 def test_plans_of_different_sizes_from_several_threads(qs):
