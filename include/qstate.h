@@ -299,8 +299,8 @@ int qstate_scan_fp32(const qstate_cfg* cfg, float* S, const qstate_inputs* x, in
 #define QSTATE_KV_E4M3 1    /* the cache holds 8-bit floats (4 exponent bits, 3 mantissa bits) times
                                2^(e - 127), e a byte for each token and head: the smallest power with
                                |x| <= 448 * 2^(e - 127), so that only the rounding of the codes (to
-                               nearest, ties to even) loses anything.  e = 255: the vector was not
-                               finite and reads as NaN.  HEADS and BF16 only                    */
+                               nearest, ties to even) loses anything; 127 for a vector of zeros.  e = 255:
+                               the vector was not finite and reads as NaN.  HEADS and BF16 only  */
 
 typedef struct qstate_kv_cfg {
     int32_t kind;            /* QSTATE_KV_HEADS or QSTATE_KV_LATENT                            */

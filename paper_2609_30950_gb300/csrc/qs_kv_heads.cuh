@@ -325,6 +325,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
                     }
                 }
             }
+            bool unit = false;   // values with the power 2^0
             // scores in base 2 less their reference; y also carries the values' powers, which have one of their own
             float y[2][4];
             constexpr int kRowSets = kHalf ? 1 : 2;
@@ -346,6 +347,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
                         // 2^(k - 127), and k - 127 as a number; 255, not finite, becomes NaN: its carry is a mantissa bit
                         const uint32_t kj = (kx >> (8 * j)) & 255, vj = (vx >> (8 * j)) & 255;
                         ke[j] = __uint_as_float(kj << 23 | (kj + 1) >> 8);
+                        unit = unit || vj == 127;
                         ve[j] = vj == 255 ? __uint_as_float(0x7fffffffu) : __uint_as_float(0x4B000000u | vj) - 8388735.0f;
                     }
                 }
@@ -368,14 +370,39 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
             }
             // the references follow only what has outgrown them
             float top[2], topo[2];
-            bool grown = false;
+            bool grown;
+            auto compare = [&]() {
+                grown = false;
 #pragma unroll
-            for (int r = 0; r < kRowSets; ++r) {
-                top[r] = fmaxf(fmaxf(z[0][2 * r], z[0][2 * r + 1]), fmaxf(z[1][2 * r], z[1][2 * r + 1]));
-                if (kE4M3) topo[r] = fmaxf(fmaxf(y[0][2 * r], y[0][2 * r + 1]), fmaxf(y[1][2 * r], y[1][2 * r + 1]));
-                grown = grown || (kE4M3 ? fmaxf(top[r], topo[r]) : top[r]) > (m[r] == -INFINITY ? -INFINITY : kLazy);
+                for (int r = 0; r < kRowSets; ++r) {
+                    top[r] = fmaxf(fmaxf(z[0][2 * r], z[0][2 * r + 1]), fmaxf(z[1][2 * r], z[1][2 * r + 1]));
+                    if (kE4M3) topo[r] = fmaxf(fmaxf(y[0][2 * r], y[0][2 * r + 1]), fmaxf(y[1][2 * r], y[1][2 * r + 1]));
+                    grown = grown || (kE4M3 ? fmaxf(top[r], topo[r]) : top[r]) > (m[r] == -INFINITY ? -INFINITY : kLazy);
+                }
+            };
+            compare();
+            bool follow = __any_sync(kFull, grown || unit);
+            if (kE4M3 && follow) {
+                if (__any_sync(kFull, unit)) {
+                    // Zeros have that power too, however small the values beside them are: it is no measure of them, and
+                    // what they add is nothing.
+                    uint32_t any = 0;
+#pragma unroll 1
+                    for (int seg = 0; seg < S::kSeg; ++seg) {
+                        const uint4 w = *reinterpret_cast<const uint4*>(kb + S::kTensor + S::at(sb * 16 + (lane & 15), seg));
+                        any |= w.x | w.y | w.z | w.w;
+                    }
+                    const uint32_t zeros = __ballot_sync(kFull, (any & 0x7f7f7f7fu) == 0);
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if ((zeros >> (nt * 8 + 2 * t4 + (j & 1))) & 1) y[nt][j] = -INFINITY;
+                    compare();
+                }
+                follow = __any_sync(kFull, grown);
             }
-            if (__any_sync(kFull, grown)) {
+            if (follow) {
 #pragma unroll
                 for (int r = 0; r < kRowSets; ++r) {
                     const float now = fmaxf(m[r], mz[r] + max4(top[r])), nowo = kE4M3 ? fmaxf(mo[r], my[r] + max4(topo[r])) : now;
