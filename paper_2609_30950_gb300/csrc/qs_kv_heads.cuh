@@ -18,6 +18,11 @@
 //  - p goes into the second product as hi + lo of two 16-bit values: one alone would add as much
 //    error as the rounding of o itself.  With up to 8 heads lo takes the rows that are left over,
 //    at no cost.
+//  - products in f16 (f16 layers and e4m3): f16 ends at 2^-24, so a weight of the reference enters as 2^7, and
+//    where the largest of a block of 16 tokens is under 2^-16 of it, the values' reference goes down to that one (o's sums
+//    are FP32 and have room above), at most 2^48 under the highest it was.  Otherwise what lies far under one large
+//    weight would be lost beside it, and where that one's value is zero it is all there is.  In a block a weight loses at most
+//    2^-16 of the largest there.  (256 requests of 32 heads 172 us with and without; e4m3 above 150 against 145.)
 //  - e4m3: codes are exact in f16, so both products run in f16.  q is scaled by a power of two for
 //    each head first (its entries under 2^-14 of the largest lose bits of 2^-25 of it, as sums in 32
 //    bits do); the keys' powers multiply the scores, and the values' powers are added to them in
@@ -33,6 +38,9 @@ namespace kv {
 
 constexpr int kHeadRows = 16;
 constexpr float kLazy = 8.0f;
+// Products in f16: a weight of the reference enters as 2^kLift, one of 2^kLazy more as 2^15; the reference goes down to a
+// block's largest where that is under 2^-kFar of it, but not under 2^-kDeep of the highest it was.
+constexpr float kLift = 7.0f, kFar = 16.0f, kDeep = 48.0f;
 
 // A word's codes 0, 1 and 2, 3 as pairs of f16.
 __device__ __forceinline__ void e4m3_cvt(uint32_t w, uint32_t& lo, uint32_t& hi) {
@@ -198,7 +206,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
 
     // ---- products ----
     uint32_t qf[kQInRegs ? kSteps : 1][4];
-    float o[kOut][4], m[2], mo[2], l[2], zs[2];
+    float o[kOut][4], m[2], mo[2], l[2], zs[2], high[2];   // high: e4m3, the highest mo so far
     int stage = 0, heads = 0, h0 = 0, began = -1;
     const char* qs = smem + S::kQ;   // this row's queries
 
@@ -276,7 +284,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
             }
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                m[s] = mo[s] = -INFINITY;
+                m[s] = mo[s] = high[s] = -INFINITY;
                 l[s] = 0.0f;
                 zs[s] = p.scale * kLog2e;
                 if (kE4M3) zs[s] *= reinterpret_cast<const float*>(smem + S::kQScale)[quad + 8 * s];
@@ -368,21 +376,27 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
                     for (int j = 0; j < 4; ++j)
                         if (!((on >> (nt * 8 + 2 * t4 + (j & 1))) & 1)) z[nt][j] = y[nt][j] = -INFINITY;
             }
-            // the references follow only what has outgrown them
+            // The references follow only what has outgrown them, or, in f16, what they stand far above: a row of whose
+            // four lanes none is near.  A lane with nothing near is rare enough to look closer.
             float top[2], topo[2];
-            bool grown;
+            bool grown, apart;
             auto compare = [&]() {
-                grown = false;
+                grown = apart = false;
 #pragma unroll
                 for (int r = 0; r < kRowSets; ++r) {
                     top[r] = fmaxf(fmaxf(z[0][2 * r], z[0][2 * r + 1]), fmaxf(z[1][2 * r], z[1][2 * r + 1]));
                     if (kE4M3) topo[r] = fmaxf(fmaxf(y[0][2 * r], y[0][2 * r + 1]), fmaxf(y[1][2 * r], y[1][2 * r + 1]));
-                    grown = grown || (kE4M3 ? fmaxf(top[r], topo[r]) : top[r]) > (m[r] == -INFINITY ? -INFINITY : kLazy);
+                    if (kF16) topo[r] = top[r] + (mz[r] - my[r]);
+                    if (!kF16) grown = grown || top[r] > (m[r] == -INFINITY ? -INFINITY : kLazy);
+                    if (kProd16) {
+                        grown = grown || topo[r] > (mo[r] == -INFINITY ? -INFINITY : kLift + kLazy);
+                        apart = apart || topo[r] < kLift - kFar;
+                    }
                 }
             };
             compare();
-            bool follow = __any_sync(kFull, grown || unit);
-            if (kE4M3 && follow) {
+            bool follow = __any_sync(kFull, grown || apart || unit);
+            if (kProd16 && follow) {
                 if (__any_sync(kFull, unit)) {
                     // Zeros have that power too, however small the values beside them are: it is no measure of them, and
                     // what they add is nothing.
@@ -401,16 +415,34 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
                     compare();
                 }
                 follow = __any_sync(kFull, grown);
+#pragma unroll
+                for (int r = 0; r < kRowSets; ++r) {
+                    const bool deep = kE4M3 ? mo[r] <= high[r] - kDeep : mz[r] - my[r] > kLift + kDeep - 0.5f;
+                    uint32_t near = __ballot_sync(kFull, topo[r] >= kLift - kFar || deep);
+                    near |= near >> 1;
+                    follow = follow || (~(near | near >> 2) & 0x11111111u) != 0;
+                }
             }
             if (follow) {
 #pragma unroll
                 for (int r = 0; r < kRowSets; ++r) {
-                    const float now = fmaxf(m[r], mz[r] + max4(top[r])), nowo = kE4M3 ? fmaxf(mo[r], my[r] + max4(topo[r])) : now;
+                    const float now = fmaxf(m[r], mz[r] + max4(top[r]));
+                    float nowo = now;
+                    if (kProd16) {
+                        const float t = max4(topo[r]);
+                        const bool moves = t > kLift + kLazy || t < kLift - kFar || mo[r] == -INFINITY;
+                        nowo = mo[r];
+                        if (moves && t > -INFINITY) nowo = fmaxf(my[r] + t - kLift, kE4M3 ? high[r] - kDeep : now - kLift - kDeep);
+                        high[r] = fmaxf(high[r], nowo);
+                    }
                     l[r] *= part_weight(m[r], now);
                     const float c = part_weight(mo[r], nowo);
-                    const float dz = (now == -INFINITY ? 0.0f : now) - mz[r], dy = (nowo == -INFINITY ? 0.0f : nowo) - my[r];
+                    const float mzr = now == -INFINITY ? 0.0f : now, myr = nowo == -INFINITY ? 0.0f : nowo;
+                    const float dz = mzr - mz[r], dy = myr - my[r];
                     m[r] = now;
                     mo[r] = nowo;
+                    mz[r] = mzr;
+                    my[r] = myr;
 #pragma unroll
                     for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
@@ -429,11 +461,12 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
             uint32_t hi[4], lo[4];
 #pragma unroll
             for (int s = 0; s < kRowSets; ++s) {
+                const float lift = kF16 ? exp2_fast(mz[s] - my[s]) : 1.0f;
 #pragma unroll
                 for (int nt = 0; nt < 2; ++nt) {
                     const float p0 = exp2_fast(z[nt][2 * s]), p1 = exp2_fast(z[nt][2 * s + 1]);
                     l[s] += p0 + p1;
-                    const float w0 = kE4M3 ? exp2_fast(y[nt][2 * s]) : p0, w1 = kE4M3 ? exp2_fast(y[nt][2 * s + 1]) : p1;
+                    const float w0 = kE4M3 ? exp2_fast(y[nt][2 * s]) : p0 * lift, w1 = kE4M3 ? exp2_fast(y[nt][2 * s + 1]) : p1 * lift;
                     const uint32_t h = pack2<kProd16>(w0, w1);
                     hi[2 * nt + s] = h;
                     if (!kE4M3) {
@@ -503,7 +536,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
             auto finish = [&](int row, int col, float4 acc, float4 sums) {
                 // sums: references of values and weights, sum of weights
                 const float inv = sums.z == 0.0f ? 0.0f : 1.0f / sums.z;
-                const float c = kE4M3 && sums.x != sums.y ? inv * exp2_fast(sums.x - sums.y) : inv;
+                const float c = kProd16 && sums.x != sums.y ? inv * exp2_fast(sums.x - sums.y) : inv;
                 uint2 w;
                 w.x = pack2<kF16>(acc.x * c, acc.y * c);
                 w.y = pack2<kF16>(acc.z * c, acc.w * c);

@@ -1,5 +1,6 @@
-"""Attention over the paged cache where much of a row's weight lies on tokens whose values are zero: o comes from the
-others alone, and has to be as exact as any other o."""
+"""Attention over the paged cache where most of a row's weight lies on tokens whose values are zero (the first token of
+many models): what is left of o comes from weights that are tiny beside the largest one, and has to be as exact as any
+other o."""
 import math
 
 import pytest
@@ -84,6 +85,61 @@ def check(qs, b, kind, dtype):
         assert bool((err <= bound).all()), f"request {r} of {n}: {float((err / bound).max()):.3g} bounds, o {float(o.abs().max()):.3g}"
         lse = lse.reshape(-1)
         assert bool(((gl[r] - lse).abs() <= 2.0 ** -19 + n * 2.0 ** -24 + lse.abs() * 2.0 ** -22).all())
+
+
+KINDS = [("heads", "bf16"), ("heads", "f16"), ("e4m3", "bf16"), ("latent", "bf16")]
+LENS = [6000 - 37 * r for r in range(40)]   # some tens of tiles a CTA
+
+
+def sink(place, above):
+    def score(r, n):
+        x = 0.5 * torch.sin(torch.arange(n) * 1.7 + r)
+        x[{"first": 0, "middle": n // 2, "last": n - 1}[place]] = above
+        return x
+    return score
+
+
+@pytest.mark.parametrize("above", [9.0, 17.0, 17.375, 24.0, 36.0])
+@pytest.mark.parametrize("place", ["first", "middle", "last"])
+@pytest.mark.parametrize("kind,dtype", KINDS)
+def test_a_sink_without_a_value(qs, kind, dtype, place, above):
+    # f16 holds o itself down to 2^-24: its values are larger where little of them is left
+    value = 1.0 if dtype == "bf16" or above < 20 else 8192.0
+    b = scored(qs, kind, dtype, LENS, sink(place, above), value=value, seed=int(above))
+    b.run(qs)
+    check(qs, b, kind, dtype)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d", [(1, 1, 64), (10, 1, 128), (16, 1, 256), (40, 2, 64)])
+@pytest.mark.parametrize("kind,dtype", [("heads", "f16"), ("e4m3", "bf16")])
+def test_a_sink_without_a_value_for_other_heads(qs, kind, dtype, Hq, Hkv, d):
+    b = scored(qs, kind, dtype, LENS[:20] + [70, 33, 2], sink("first", 19.0), Hq=Hq, Hkv=Hkv, d=d, seed=d)
+    b.run(qs)
+    check(qs, b, kind, dtype)
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS)
+def test_scores_that_fall_by_hundreds_after_a_sink(qs, kind, dtype):
+    """A row whose weights fall without end: the reference does not follow for ever, and nothing overflows."""
+    def score(r, n):
+        x = -torch.arange(n) * (0.0625 * (1 + r % 3))
+        x[0] = 30.0
+        return x.clamp(min=-440.0)
+    b = scored(qs, kind, dtype, LENS, score, value=64.0)
+    b.run(qs)
+    check(qs, b, kind, dtype)
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS)
+def test_many_sinks_without_values(qs, kind, dtype):
+    """Every 200th token: the reference goes up and down all along a row."""
+    def score(r, n):
+        x = 0.5 * torch.sin(torch.arange(n) * 1.7 + r)
+        x[r % 200::200] = 20.0
+        return x
+    b = scored(qs, kind, dtype, LENS, score, value=1.0 if dtype == "bf16" else 512.0)
+    b.run(qs)
+    check(qs, b, kind, dtype)
 
 
 @pytest.mark.parametrize("value", [2.0 ** -60, 2.0 ** -20, 2.0 ** -9, 180.0])
