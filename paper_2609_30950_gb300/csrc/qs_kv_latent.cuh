@@ -18,7 +18,10 @@
 //               not wait for the whole of a tile
 //   warps 9-12  (10-12 where warp 9 copies boxes) copy a row's queries, and, 16 bytes at a time, tiles of shorter pages
 // As in the kernel for heads, the softmax reference follows the maximum only when that has outgrown it by
-// 2^8; all tokens of a row share one reference, so the eight warps vote.  p has 16 bits in the second product
+// 2^8; all tokens of a row share one reference, so the eight warps vote.  In f16, which ends at 2^-24, a weight of the
+// reference is 2^7, and the reference also goes down, to a tile whose largest weight is under 2^-16 of it: what
+// lies far under one large weight would otherwise be lost beside it, and where that one's value is zero it is all
+// there is (f16, 64 heads: 512 + 64 93 us with it, 91 without; 128 + 0 143 and 127, 256 + 64 95 and 93).  p has 16 bits in the second product
 // and o is divided by the sum of the rounded p, so that the weights in use add up to one; lse comes from
 // the sum before rounding.  That leaves o with about 1.4 times the error of its own rounding.  Carrying the
 // remainder of p in a second product would cost a second pass over the tile: at 64 heads of 512 + 64, S
@@ -45,6 +48,9 @@ constexpr int kMaxStages = 4;
 constexpr int kLatSmem = 227 * 1024;   // shared memory of an SM's only CTA
 constexpr int kPartBlocks = 3, kMaxParts = 3;   // a tile is waited for in parts, so that S follows the copies
 constexpr float kLazyLatent = 8.0f;
+// f16: a weight of the reference is 2^kLiftLatent; the reference goes down where a tile's largest weight is under
+// 2^-kFarLatent of it, but not under 2^-kDeepLatent of the highest it was.
+constexpr float kLiftLatent = 7.0f, kFarLatent = 16.0f, kDeepLatent = 48.0f;
 
 struct LatentGeo {
     int blocks;        // of 64 entries, the last may be half
@@ -61,7 +67,9 @@ struct LatentMisc {
     uint64_t full[kMaxStages][kMaxParts], free[kMaxStages], sready[2], qfull, qfree, pready, drain;
     uint64_t mask[kMaxStages];
     uint32_t flags[kMaxStages];   // of the tile: 1 its row begins here, 2 it ends here, 4 it is the last
-    float top[4][64], topr[4][64];
+    float top[4][64];
+    float topr[4][64];   // f16, within a row: in the first the highest references so far
+    alignas(16) uint32_t near[2][kLatSoftmax];   // f16: of a tile, heads with a weight of some size, a bit each
     float corr[64];   // what O's sums are multiplied by; warps read it at their own pace until the next vote
     float inv[64];    // at a row's end its references, then what o is multiplied by
     Share share;
@@ -459,6 +467,8 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
         // sums of p before and after its rounding
         float m[kPer], l[kPer], lr[kPer];
         int prev = 0, prev_phase = 0, s = 0, phase = 0, began = 0;   // prev: stage of the tile before
+        constexpr uint32_t kHeads = 0xffffffffu >> (32 - 4 * kPer);   // bits of a warp's heads
+        constexpr float kAbove = kF16 ? kLazyLatent + kLiftLatent : kLazyLatent, kBelow = kLiftLatent - kFarLatent;
         bool begins = true;
         // k: head c0 + 8 (k / 2) + 2 t4 + k % 2, at tokens quad and quad + 8 of the quarter
         auto head = [&](int k) { return c0 + 8 * (k >> 1) + 2 * t4 + (k & 1); };
@@ -467,7 +477,10 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
             if (begins) {
                 began = w.tile;
 #pragma unroll
-                for (int k = 0; k < kPer; ++k) m[k] = -INFINITY, l[k] = lr[k] = 0.0f;
+                for (int k = 0; k < kPer; ++k) {
+                    m[k] = -INFINITY, l[k] = lr[k] = 0.0f;
+                    if (kF16 && sub == 0 && quad == 0) x.topr[0][head(k)] = -INFINITY;
+                }
             }
             role_wait(&x.full[s][0], phase, abort, p);
             role_wait(&x.sready[i & 1], (i >> 1) & 1, abort, p);
@@ -485,15 +498,26 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
                                 make_uint4(0, 0, 0, 0);
             }
             bool grown = false;
+            uint32_t near = 0;   // f16: heads with a weight of some size among this lane's tokens
 #pragma unroll
             for (int k = 0; k < kPer; ++k) {
                 float& a = z[4 * (k >> 1) + (k & 1)];
                 float& b = z[4 * (k >> 1) + (k & 1) + 2];
                 a = (on >> quad) & 1 ? a * zs : -INFINITY;
                 b = (on >> (quad + 8)) & 1 ? b * zs : -INFINITY;
-                grown = grown || fmaxf(a, b) > m[k] + kLazyLatent;
+                grown = grown || fmaxf(a, b) > m[k] + kAbove;
+                if (kF16 && fmaxf(a, b) >= m[k] + kBelow) near |= 1u << k;
             }
-            if (softmax_any(grown)) {
+            if (kF16) {   // or among this warp's, for the other warps
+                const uint32_t all = __reduce_or_sync(kFull, near << (kPer * t4));
+                if (lane == 0) x.near[i & 1][warp] = all;
+            }
+            bool follow = softmax_any(grown);
+            if (kF16) {   // heads without one in the tile
+                const uint4 a = *reinterpret_cast<const uint4*>(x.near[i & 1]), b = *reinterpret_cast<const uint4*>(x.near[i & 1] + 4);
+                follow = follow || (a.x | a.y | a.z | a.w) != kHeads || (b.x | b.y | b.z | b.w) != kHeads;
+            }
+            if (follow) {
 #pragma unroll
                 for (int k = 0; k < kPer; ++k) {
                     float top = fmaxf(z[4 * (k >> 1) + (k & 1)], z[4 * (k >> 1) + (k & 1) + 2]);
@@ -502,18 +526,28 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
                     if (quad == 0) x.top[sub][head(k)] = top;
                 }
                 softmax_sync();
+                bool moved = false;
 #pragma unroll
                 for (int k = 0; k < kPer; ++k) {
                     const int h = head(k);
-                    const float now = fmaxf(fmaxf(fmaxf(x.top[0][h], x.top[1][h]), fmaxf(x.top[2][h], x.top[3][h])), m[k]);
+                    const float top = fmaxf(fmaxf(x.top[0][h], x.top[1][h]), fmaxf(x.top[2][h], x.top[3][h]));
+                    float now = fmaxf(top, m[k]);
+                    if (kF16) {
+                        now = fmaxf(m[k], top - kLiftLatent);
+                        if (top < m[k] + kBelow && top > -INFINITY) now = fmaxf(top - kLiftLatent, x.topr[0][h] - kDeepLatent);
+                    }
+                    moved = moved || now != m[k];
                     const float c = part_weight(m[k], now);
                     l[k] *= c;
                     lr[k] *= c;
                     m[k] = now;
                     if (sub == 0 && quad == 0) x.corr[h] = c;
                 }
-                softmax_sync();
-                if (!begins) {
+                moved = softmax_any(moved);
+                if (kF16 && sub == 0 && quad == 0)
+#pragma unroll
+                    for (int k = 0; k < kPer; ++k) x.topr[0][head(k)] = fmaxf(x.topr[0][head(k)], m[k]);
+                if (moved && !begins) {
                     role_wait(&x.free[prev], prev_phase, abort, p);   // the products so far are in
                     tc::fence_after_sync();
 #pragma unroll 1
@@ -589,7 +623,7 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
                     if (!whole)
                         reinterpret_cast<float4*>(p.part_ml)[prow + tid] = make_float4(ref, ref, sum, sumr);
                     else if (p.lse && tid < heads)
-                        p.lse[row + tid] = sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
+                        p.lse[row + tid] = log_sum(ref, sum);
                 }
                 softmax_sync();
                 role_wait(&x.free[s], phase, abort, p);

@@ -193,6 +193,15 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // Weight of a part whose reference is m in a sum whose reference is M; nothing at all has m = -inf.
 __device__ __forceinline__ float part_weight(float m, float M) { return m == -INFINITY ? 0.0f : exp2_fast(m - M); }
 
+// log of a sum of 2^z against the reference ref; the sum's exponent goes to the reference, so that log2f adds nothing to
+// the rounding of the result.
+__device__ __forceinline__ float log_sum(float ref, float sum) {
+    if (sum == 0.0f) return -INFINITY;
+    int e = 0;
+    const float f = frexpf(sum, &e);   // infinities and NaN stay what they are
+    return (ref + static_cast<float>(e) + log2f(f)) * 0.6931471805599453f;
+}
+
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool on) {
@@ -414,7 +423,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const KvAttend
                 put(tid, x);
             }
         }
-        if (mine && lane == 0 && (few || warp == 0) && p.lse) p.lse[out] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+        if (mine && lane == 0 && (few || warp == 0) && p.lse) p.lse[out] = log_sum(M, L);
         __syncthreads();
     }
 }

@@ -87,7 +87,7 @@ def check(qs, b, kind, dtype):
         assert bool(((gl[r] - lse).abs() <= 2.0 ** -19 + n * 2.0 ** -24 + lse.abs() * 2.0 ** -22).all())
 
 
-KINDS = [("heads", "bf16"), ("heads", "f16"), ("e4m3", "bf16"), ("latent", "bf16")]
+KINDS = [("heads", "bf16"), ("heads", "f16"), ("e4m3", "bf16"), ("latent", "bf16"), ("latent", "f16")]
 LENS = [6000 - 37 * r for r in range(40)]   # some tens of tiles a CTA
 
 
