@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes as ct
 import os
-from dataclasses import dataclass, field
+from dataclasses import dataclass, field, fields
 
 from . import build as _build
 
@@ -434,6 +434,13 @@ def qstate_scan_partition_count(cfg: Config, x: Inputs, stats: Stats) -> int:
 # ---- paged cache of attention layers -------------------------------------------------------------
 # Descriptions and tensors of these calls stay the same from step to step, so their structures are made
 # once, with the frozen object that holds them.
+class _Kept:
+    """Copies (copy, deepcopy, pickle) are made again from the fields, so that their addresses are their own."""
+
+    def __reduce__(self):
+        return type(self), tuple(getattr(self, f.name) for f in fields(self))
+
+
 def _keep(obj, struct=None, **more):
     """Keeps a structure, its address and whatever else belongs to a frozen object."""
     if struct is not None:
@@ -443,7 +450,7 @@ def _keep(obj, struct=None, **more):
 
 
 @dataclass(frozen=True)
-class KvConfig:
+class KvConfig(_Kept):
     """One attention layer's paged cache (mirrors ``qstate_kv_cfg``).  A description for
     qstate_kv_plan alone needs page, n_pages and max_pages only."""
     page: int
@@ -485,7 +492,7 @@ def _sized(t, name, n):
 
 
 @dataclass(frozen=True)
-class KvCache:
+class KvCache(_Kept):
     """One layer's cache (device tensors, caller-owned): k (n_pages, Hkv, page, dk), v (n_pages, Hkv, page, dv)
     or None for latents, and for e4m3 the exponent bytes (n_pages, Hkv, page).  The tensors keep their storage
     for as long as the object is in use; so do those of KvPages and KvSlots."""
@@ -528,7 +535,7 @@ def new_kv_cache(cfg: KvConfig, device="cuda") -> KvCache:
 
 
 @dataclass(frozen=True)
-class KvPages:
+class KvPages(_Kept):
     """Who holds which page: table (R, max_pages), lens (R), free_list (n_pages), free_count (1), int32."""
     table: object
     lens: object
@@ -552,7 +559,7 @@ def new_kv_pages(cfg: KvConfig, R: int, device="cuda") -> KvPages:
 
 
 @dataclass(frozen=True)
-class KvSlots:
+class KvSlots(_Kept):
     """A step's tokens, as qstate_kv_plan lays them out: cu (R + 1), slot, pos, req (T; pos and req may
     be None), int32, and ok (R), uint8."""
     cu: object

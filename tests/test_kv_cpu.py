@@ -1,6 +1,8 @@
 """Refusals and sizes of the paged cache's calls, on the CPU: placeholder device addresses, which every call
 here refuses before anything could read them."""
+import copy
 import ctypes as ct
+import io
 
 import pytest
 import torch
@@ -113,3 +115,44 @@ def test_exponents_that_are_not_aligned_are_refused(q):
         assert L.qstate_kv_attend(r(c._c), r(cache), A, 1024, 128, A, A, 1, A, None, A, None) == q.QSTATE_EINVAL
         assert b"exponents" in L.qstate_last_error()
         assert L.qstate_kv_append(r(c._c), r(cache), A, 256, 128, A, 256, 128, A, 1, None) == q.QSTATE_EINVAL
+
+
+def copies(x):
+    yield copy.copy(x)
+    yield copy.deepcopy(x)
+    file = io.BytesIO()
+    torch.save(x, file)   # pickles, tensors of every type among it
+    file.seek(0)
+    yield torch.load(file, weights_only=False)
+
+
+def test_copies_of_a_description_stand_by_themselves(q):
+    """The calls pass a description's address on: a copy has to have one of its own."""
+    c = config(q, window=7)
+    for d in copies(c):
+        assert d == c and d._at != c._at and d._at == ct.addressof(d._c)
+        seen = q._KvCfg.from_address(d._at)
+        assert [getattr(seen, n) for n, _ in q._KvCfg._fields_] == [getattr(c._c, n) for n, _ in q._KvCfg._fields_]
+        q.kv_validate(d)
+
+
+def test_copies_of_tensors_holders_point_to_their_own_tensors(q, monkeypatch):
+    monkeypatch.setattr(q, "_ptr", lambda t: t.data_ptr())   # host tensors stand for device ones
+    c = config(q, store=q.KV_E4M3)
+    i32 = lambda *n: torch.zeros(*n, dtype=torch.int32)  # noqa: E731
+    fp8 = lambda: torch.zeros(10, 2, 16, 128).to(torch.float8_e4m3fn)  # noqa: E731
+    u8 = lambda *n: torch.zeros(*n, dtype=torch.uint8)  # noqa: E731
+    cache = q.KvCache(fp8(), fp8(), u8(10, 2, 16), u8(10, 2, 16))
+    cache._check(c)
+    pages, slots = q.KvPages(i32(3, 4), i32(3), i32(10), i32(1)), q.KvSlots(i32(4), i32(5), i32(5), None, u8(3))
+    for d in copies(pages):
+        assert d._args == [t.data_ptr() for t in (d.table, d.lens, d.free_list, d.free_count)] and d.R == 3
+    for x, names in ((cache, ("k", "v", "k_exp", "v_exp")), (slots, ("cu", "slot", "pos", "req", "ok"))):
+        for d in copies(x):
+            assert d._at == ct.addressof(d._c) != x._at
+            for n in names:
+                t = getattr(d, n)
+                assert getattr(d._c, n) == (None if t is None else t.data_ptr())
+    deep = copy.deepcopy(pages)
+    deep.lens.fill_(5)
+    assert not bool(pages.lens.any()) and deep._args[1] == deep.lens.data_ptr() != pages._args[1]
