@@ -353,7 +353,9 @@ typedef struct qstate_kv_slots {
 
 /* Bytes of one layer's k (or, with v != 0, its v; 0 for LATENT) array, and of the work space: 256-byte
  * aligned device memory, zeroed once after it is made, left zeroed where that matters by every call.
- * One work space serves any number of layers and calls in stream order, not two streams at once. */
+ * One work space serves any number of layers and calls in stream order, not two streams at once.  A
+ * description of the pool alone (page, n_pages, max_pages; Hq = Hkv = dk = dv = 0) has the work space of
+ * qstate_kv_plan. */
 size_t qstate_kv_cache_bytes(const qstate_kv_cfg* cfg, int32_t v);
 size_t qstate_kv_work_bytes(const qstate_kv_cfg* cfg);
 int qstate_kv_validate(const qstate_kv_cfg* cfg);

@@ -586,8 +586,10 @@ def new_kv_slots(R: int, T: int, device="cuda") -> KvSlots:
 def new_kv_work(cfg: KvConfig, device="cuda"):
     """Work space of a layer's calls (zeroed); serves any number of calls in stream order."""
     import torch
-    kv_validate(cfg)
-    return torch.zeros(int(_lib_or_raise().qstate_kv_work_bytes(ct.byref(cfg._c))), dtype=torch.uint8, device=device)
+    n = int(_lib_or_raise().qstate_kv_work_bytes(ct.byref(cfg._c)))
+    if n == 0:
+        kv_validate(cfg)
+    return torch.zeros(n, dtype=torch.uint8, device=device)
 
 
 def _work(cfg, work):

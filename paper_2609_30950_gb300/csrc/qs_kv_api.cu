@@ -78,6 +78,7 @@ size_t qstate_kv_cache_bytes(const qstate_kv_cfg* cfg, int32_t v) {
 }
 
 size_t qstate_kv_work_bytes(const qstate_kv_cfg* cfg) {
+    if (cfg && !cfg->Hq && !cfg->Hkv && !cfg->dk && !cfg->dv) return check_pool(cfg) ? 0 : kKvHeadBytes;   // no layer: the plan's
     if (check_cfg(cfg)) return 0;
     const KvPartBytes b = kv_part_bytes(*cfg);
     return kKvHeadBytes + b.sums + b.ml + b.split;

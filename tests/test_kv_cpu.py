@@ -156,3 +156,16 @@ def test_copies_of_tensors_holders_point_to_their_own_tensors(q, monkeypatch):
     deep = copy.deepcopy(pages)
     deep.lens.fill_(5)
     assert not bool(pages.lens.any()) and deep._args[1] == deep.lens.data_ptr() != pages._args[1]
+
+
+def test_a_pool_alone_has_the_plans_work_space(q):
+    """The plan takes a description of which page, n_pages and max_pages alone are set, and so does its work space."""
+    bytes_of = lambda **kw: q._lib.qstate_kv_work_bytes(ct.byref(q._KvCfg(**kw)))  # noqa: E731
+    layer = q._lib.qstate_kv_work_bytes(ct.byref(config(q)._c))
+    assert 4096 <= bytes_of(page=16, n_pages=10, max_pages=4) <= layer
+    assert bytes_of(page=16, n_pages=10) == bytes_of(page=3, n_pages=10, max_pages=4) == 0
+    assert bytes_of(page=16, n_pages=10, max_pages=4, dk=128) == 0   # an unfinished layer
+    pool = q.KvConfig(page=16, n_pages=10, max_pages=4, Hq=0, Hkv=0, dk=0, dv=0)
+    assert q.new_kv_work(pool, device="cpu").numel() >= 4096
+    with pytest.raises(q.QstateError):
+        q.new_kv_work(q.KvConfig(page=3, n_pages=10, max_pages=4, Hq=0, Hkv=0, dk=0, dv=0), device="cpu")
