@@ -45,6 +45,10 @@ int check_cfg(const qstate_kv_cfg* c) {
 
 bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
+// Arrays of 32-bit entries; NULL counts as aligned.
+template <class... P>
+bool words(const P*... p) { return (aligned(p, 4) && ...); }
+
 int check_cache(const qstate_kv_cfg* c, const qstate_kv_cache* cache) {
     const bool heads = c->kind == QSTATE_KV_HEADS, e4m3 = c->store == QSTATE_KV_E4M3;
     if (!cache || !cache->k || (heads && !cache->v)) return fail(QSTATE_EINVAL, "null cache pointer");
@@ -94,6 +98,9 @@ int qstate_kv_plan(const qstate_kv_cfg* cfg, const qstate_kv_pages* pages, const
     if (R > 0 && (!n_new || !pages->table || !pages->lens || !pages->lens_out || !slots->ok))
         return fail(QSTATE_EINVAL, "null pointer");
     if (slots->T < 0 || (slots->T > 0 && !slots->slot)) return fail(QSTATE_EINVAL, "bad rows");
+    if (!words(pages->table, pages->lens, pages->lens_out, pages->free_list, pages->free_count, pages->free_out, n_new,
+               slots->cu, slots->slot, slots->pos, slots->req))
+        return fail(QSTATE_EINVAL, "arrays of 32-bit entries must be 4-byte aligned");
     if (!aligned(work, 256)) return fail(QSTATE_EINVAL, "the work space must be 256-byte aligned");
     KvPlanParams p;
     std::memset(&p, 0, sizeof(p));
@@ -122,6 +129,7 @@ int qstate_kv_append(const qstate_kv_cfg* cfg, const qstate_kv_cache* cache, con
     if (T == 0) return QSTATE_OK;
     if (!heads && v) return fail(QSTATE_EINVAL, "latent attention has no separate values");
     if (!k || !slot || (heads && !v)) return fail(QSTATE_EINVAL, "null pointer");
+    if (!words(slot)) return fail(QSTATE_EINVAL, "slots must be 4-byte aligned");
     if (!aligned(k, 2) || (heads && !aligned(v, 2))) return fail(QSTATE_EINVAL, "keys and values must be 2-byte aligned");
     KvAppendParams p;
     std::memset(&p, 0, sizeof(p));
@@ -157,6 +165,7 @@ int qstate_kv_attend(const qstate_kv_cfg* cfg, const qstate_kv_cache* cache, con
     if (R == 0) return QSTATE_OK;
     if (!q || !table || !lens || !o || !work) return fail(QSTATE_EINVAL, "null pointer");
     if (!aligned(q, 2)) return fail(QSTATE_EINVAL, "q must be 2-byte aligned");
+    if (!words(table, lens, lse)) return fail(QSTATE_EINVAL, "arrays of 32-bit entries must be 4-byte aligned");
     if (!aligned(o, 16)) return fail(QSTATE_EINVAL, "o must be 16-byte aligned");
     if (!aligned(work, 256)) return fail(QSTATE_EINVAL, "the work space must be 256-byte aligned");
     KvAttendParams p;

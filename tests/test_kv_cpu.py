@@ -169,3 +169,19 @@ def test_a_pool_alone_has_the_plans_work_space(q):
     assert q.new_kv_work(pool, device="cpu").numel() >= 4096
     with pytest.raises(q.QstateError):
         q.new_kv_work(q.KvConfig(page=3, n_pages=10, max_pages=4, Hq=0, Hkv=0, dk=0, dv=0), device="cpu")
+
+
+def test_arrays_of_words_that_are_not_aligned_are_refused(q):
+    L, c, r = q._lib, config(q), ct.byref
+    cache = q._KvCache(A, A, None, None)
+    for i in range(3):
+        at = [A + 2 * (i == j) for j in range(3)]   # table, lens, lse
+        assert L.qstate_kv_attend(r(c._c), r(cache), A, 1024, 128, at[0], at[1], 1, A, at[2], A, None) == q.QSTATE_EINVAL
+        assert b"4-byte" in L.qstate_last_error()
+    assert L.qstate_kv_append(r(c._c), r(cache), A, 256, 128, A, 256, 128, A + 1, 1, None) == q.QSTATE_EINVAL
+    assert b"4-byte" in L.qstate_last_error()
+    for i in range(11):
+        at = [A + 2 * (i == j) for j in range(11)]
+        pages, slots = q._KvPages(*at[:6]), q._KvSlots(*at[6:10], A, 1)
+        assert L.qstate_kv_plan(r(c._c), r(pages), at[10], 1, r(slots), A, None) == q.QSTATE_EINVAL
+        assert b"4-byte" in L.qstate_last_error()
