@@ -224,12 +224,13 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
     const int worker = blockIdx.x / g.groups, group = blockIdx.x - worker * g.groups;
     const int h0 = group * g.per_group, heads = min(g.per_group, p.Hq - h0);
     const int askers = g.boxes ? kLatCopiers - 1 : kLatCopiers;   // warps that copy queries
-    chain_wait();   // and the kernel that joins split rows may take its place
+    chain_enter();
 
     if (g.boxes && warp == kLatIssuer + 1) prefetch_map(&map);
     if (warp == kLatIssuer) {
         tc::tmem_alloc(&x.tmem, kAlloc);
         tc::tmem_relinquish();
+        chain_release();   // the kernel that joins split rows may take its place; one with tensor memory no sooner
     }
     if (tid == 0) {
         for (int s = 0; s < kMaxStages; ++s) {
