@@ -307,7 +307,7 @@ typedef struct qstate_kv_cfg {
     int32_t Hq, Hkv, dk, dv; /* 1 <= Hq <= 1024                                                */
     int32_t page;            /* tokens of a page: a power of two, 1 to 1024                    */
     int32_t n_pages;         /* pages of the pool; n_pages * page < 2^31                        */
-    int32_t max_pages;       /* columns of the block table; max_pages * page < 2^31             */
+    int32_t max_pages;       /* columns of the block table; max_pages * page <= 2^31 - 1024      */
     int32_t dtype;           /* QSTATE_KV_BF16 or QSTATE_KV_F16                                 */
     int32_t store;           /* QSTATE_KV_16 or QSTATE_KV_E4M3                                  */
     int32_t window;          /* last tokens that are seen; 0: all                              */

@@ -14,8 +14,9 @@ int check_pool(const qstate_kv_cfg* c) {
         return fail(QSTATE_EINVAL, "page must be a power of two in [1, 1024], got %d", c->page);
     if (c->n_pages < 1 || static_cast<long long>(c->n_pages) * c->page > 0x7fffffffLL)
         return fail(QSTATE_EINVAL, "need n_pages >= 1 and n_pages * page < 2^31");
-    if (c->max_pages < 1 || static_cast<long long>(c->max_pages) * c->page > 0x7fffffffLL)
-        return fail(QSTATE_EINVAL, "need max_pages >= 1 and max_pages * page < 2^31");
+    // the last tile of a request's tokens ends within 32 bits
+    if (c->max_pages < 1 || static_cast<long long>(c->max_pages) * c->page > 0x80000000LL - 1024)
+        return fail(QSTATE_EINVAL, "need max_pages >= 1 and max_pages * page <= 2^31 - 1024");
     return QSTATE_OK;
 }
 

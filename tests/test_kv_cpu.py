@@ -185,3 +185,12 @@ def test_arrays_of_words_that_are_not_aligned_are_refused(q):
         pages, slots = q._KvPages(*at[:6]), q._KvSlots(*at[6:10], A, 1)
         assert L.qstate_kv_plan(r(c._c), r(pages), at[10], 1, r(slots), A, None) == q.QSTATE_EINVAL
         assert b"4-byte" in L.qstate_last_error()
+
+
+def test_the_last_tile_of_the_longest_request_ends_within_32_bits(q):
+    """Tiles have up to 128 tokens: with 2^31 - 1 tokens the places behind the last one would be negative numbers."""
+    for page, columns in ((1, 2 ** 31 - 1), (1, 2 ** 31 - 1023), (64, 2 ** 25 - 15), (64, 2 ** 25 - 1)):
+        with pytest.raises(q.QstateError):
+            q.kv_validate(config(q, page=page, max_pages=columns))
+    for page, columns in ((1, 2 ** 31 - 1024), (64, 2 ** 25 - 16), (1024, 2 ** 21 - 1)):
+        q.kv_validate(config(q, page=page, max_pages=columns))
