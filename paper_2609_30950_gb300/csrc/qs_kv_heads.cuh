@@ -24,8 +24,8 @@
 //    weight would be lost beside it, and where that one's value is zero it is all there is.  In a block a weight loses at most
 //    2^-16 of the largest there.  (256 requests of 32 heads 172 us with and without; e4m3 above 150 against 145.)
 //  - e4m3: codes are exact in f16, so both products run in f16.  q is scaled by a power of two for
-//    each head first (its entries under 2^-14 of the largest lose bits of 2^-25 of it, as sums in 32
-//    bits do); the keys' powers multiply the scores, and the values' powers are added to them in
+//    each head first: entries over 2^-14 of the head's largest are exact, smaller ones are off by up to 2^-25 of the
+//    largest (a score notices only where keys are next to nothing at q's largest entries); the keys' powers multiply the scores, and the values' powers are added to them in
 //    base 2, with a reference of their own, so that p times the power stays in f16's range.
 #pragma once
 

@@ -23,8 +23,8 @@
 // lies far under one large weight would otherwise be lost beside it, and where that one's value is zero it is all
 // there is (f16, 64 heads: 512 + 64 93 us with it, 91 without; 128 + 0 143 and 127, 256 + 64 95 and 93).  p has 16 bits in the second product
 // and o is divided by the sum of the rounded p, so that the weights in use add up to one; lse comes from
-// the sum before rounding.  That leaves o with about 1.4 times the error of its own rounding.  Carrying the
-// remainder of p in a second product would cost a second pass over the tile: at 64 heads of 512 + 64, S
+// the sum before rounding.  That leaves o with 1.04 to 1.14 times the error of the same in 32 bits, rounded once
+// (measured over the cases).  Carrying the remainder of p in a second product would cost a second pass over the tile: at 64 heads of 512 + 64, S
 // reads 147 KB of operands from shared memory for each tile, at 128 bytes a cycle, O 98 KB and the remainder 98 KB
 // more (105 us against 102 when it was tried, before the steps that made it 92).
 // What bounds it: with 64 heads of 512 + 64, room for two tiles, whose copies, S, softmax and O follow one another (0.31 GB
@@ -304,7 +304,8 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
         bool begins = true, ok = true;   // ok: no wait has been given up
         for (int i = 0; live; ++i) {
             const int r = w.r, t = w.span.base + w.tile * kLatTile + from;
-            // pages that hold nothing in the window are not looked at: they may have been given back
+            // pages that hold nothing in the window are not looked at (a program with tables of its own may have taken
+            // them back)
             const bool wanted = looks && t < w.span.end && t + tokens > w.span.begin;
             const bool there = wanted && id >= 0 && id < p.n_pages;
             if (wanted && !there) raise_status(p.status, QS_DEV_PAGES);

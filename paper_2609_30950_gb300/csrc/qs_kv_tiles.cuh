@@ -45,8 +45,8 @@ __device__ __forceinline__ Span span_of(const KvAttendParams& p, int n) {
 constexpr int kWholeTiles = 4;
 constexpr int kRowUnits = 1;
 
-// A worker's share of the units, [u0, u1), and where it is.  A worker goes through it from the start of its last
-// row (`turn`) to the end and then from u0 on: what it shares with the next worker comes first.
+// A worker's share of the units, [u0, u1), and where it begins.  A worker goes through it from u0 to u1, in the order
+// of rows and tokens, so the parts of a split row belong to workers in a row, in the order of its tokens.
 struct Share {
     long long total;        // units of all rows
     long long u0, u1;
