@@ -28,7 +28,7 @@
 // reads 147 KB of operands from shared memory for each tile, at 128 bytes a cycle, O 98 KB and the remainder 98 KB
 // more (105 us against 102 when it was tried, before the steps that made it 92).
 // What bounds it: with 64 heads of 512 + 64, room for two tiles, whose copies, S, softmax and O follow one another (0.31 GB
-// in 92 us, 49 % of the copy rate; 16 heads 72); with latents of 128 or 256, where three and four tiles fit, the softmax's
+// in 93 us, 49 % of the copy rate; 16 heads 72); with latents of 128 or 256, where three and four tiles fit, the softmax's
 // chain (64 heads of 128 + 0: 127 us for 0.3 GB; 16 heads of 128 + 64 57, 77 %).
 #pragma once
 
