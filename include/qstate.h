@@ -43,8 +43,8 @@ extern "C" {
 #define QSTATE_ECUDA 3   /* a CUDA runtime call failed (message in qstate_last_error)          */
 #define QSTATE_EDEVICE 4 /* a kernel reported an inconsistent device-side layout or input, or
                             the device was marked unusable (see qstate_check)                 */
-#define QSTATE_ETIMEOUT 5 /* a bounded device-side wait gave up (chunked form and attention over
-                             latents: a tensor-core product, or a copy for one, did not signal
+#define QSTATE_ETIMEOUT 5 /* a bounded device-side wait gave up (chunked form, attention over
+                             latents or over shared tokens: a tensor-core product, or a copy for one, did not signal
                              completion within the wait limit)                                */
 
 /* ---- configuration enums ---------------------------------------------------------------- */
@@ -282,6 +282,12 @@ int qstate_scan_fp32(const qstate_cfg* cfg, float* S, const qstate_inputs* x, in
  *   qstate_kv_plan    block table, slots of the step's new tokens, free list   (once a step)
  *   qstate_kv_append  the new tokens' keys and values into their slots          (each layer)
  *   qstate_kv_attend  one new token of each request against its pages           (each layer)
+ * and where requests begin alike (samples of one prompt, beams, users behind one system prompt)
+ *   qstate_kv_fork    requests take over the first tokens of others: pages held together
+ *   qstate_kv_compact pages move to the pool's low end
+ *   qstate_kv_copy    the pages that these two moved, before the next append     (each layer)
+ *   qstate_kv_group   which requests share their first tokens                    (once a step and kind of layer)
+ *   qstate_kv_attend_shared  the attention, shared tokens read once for all      (each layer)
  * With n cached tokens of a request (the new one among them, so append before attend),
  * z_t = scale q.k_t and t in [max(0, n - window), n) (window = 0: [0, n)):
  *   lse = log sum_t e^{z_t},   o = sum_t e^{z_t - lse} v_t.
@@ -384,8 +390,73 @@ int qstate_kv_attend(const qstate_kv_cfg* cfg, const qstate_kv_cache* cache, con
                      int64_t q_head, const int32_t* table, const int32_t* lens, int32_t R, void* o, float* lse,
                      void* work, void* stream);
 
+/* ---- requests that hold pages together ----
+ * others (n_pages, device, int32): how many requests hold a page beside the first; 0 for a page that one or nobody
+ * holds, so zeros to begin with.  Where requests share pages they end by qstate_kv_fork (qstate_kv_plan would give their
+ * pages back whoever else holds them); qstate_kv_plan gives them new pages, and qstate_kv_append writes, as before: a page that
+ * is not full has one holder. */
+
+/* Pages to copy (device): page src[i] to page dst[i], -1 in both where there is nothing to copy; n entries each. */
+typedef struct qstate_kv_moves {
+    int32_t* src;
+    int32_t* dst;
+    int32_t n;
+} qstate_kv_moves;
+
+/* Bytes of the work space of qstate_kv_fork and qstate_kv_compact for R requests: 256-byte aligned device memory, zeroed once
+ * after it is made, left zeroed where that matters by every call.  It serves any number of calls in stream order, of no
+ * more requests than R, not two streams at once.  Only page, n_pages and max_pages of cfg matter, here and in both calls. */
+size_t qstate_kv_pages_work_bytes(const qstate_kv_cfg* cfg, int32_t R);
+
+/* Request r (of 0 <= R <= 8192) takes over the first tokens of request parent[r], as that one stands before the call: all of
+ * them, or keep[r] where that is not negative and less (keep may be NULL).  parent[r] = r: it goes on (with fewer tokens, gives
+ * the pages behind them back); parent[r] < 0: it ends.  Pages that its tokens fill are held together with whoever has them.
+ * The page that its last token lies in without filling it has to be its own: it goes on with its parent's where nobody else
+ * is left with that (others 0 before the call, no request taking over all of it, and of several that might the parent itself, else
+ * the first); otherwise it gets a page from the free list's top and moves->src[r], dst[r] say what to copy, before the next append (-1, -1
+ * without, and in entries behind R; n >= R).  If the list, as it is before the call, has no page left for it, it is refused: ok[r]
+ * (R bytes) is 0 and it ends; requests are served in their order.  Pages that nobody holds any more go back on the list, in the order of
+ * the last request that held them and of its pages.  The table is changed in place, columns behind a request's pages
+ * stay; lens_out and free_out may be lens and free_count.  Page ids outside the pool, lengths outside the table and
+ * parents of R and more (which count as the request itself) set the device status. */
+int qstate_kv_fork(const qstate_kv_cfg* cfg, const qstate_kv_pages* pages, int32_t* others, const int32_t* parent,
+                   const int32_t* keep, int32_t R, const qstate_kv_moves* moves, uint8_t* ok, void* work, void* stream);
+
+/* Moves pages that requests hold, by table and lens, in front of page `limit` (1 to n_pages): the i-th held page from `limit` on
+ * goes to the i-th page in front of it that nobody holds, ids ascending, up to moves->n of them (-1, -1 in the entries that
+ * are left); left (may be NULL) receives how many held pages are still behind.  table_out (R x max_pages) receives the requests' pages,
+ * columns behind them stay; it may be the table itself, or another, so that the old one serves until the copies are
+ * done.  The free list becomes the pages in front of `limit` that nobody holds then, the lowest on top: with limit = n_pages every page that
+ * no request holds.  others (may be NULL) moves along.  lens_out is not used; free_out may be free_count. */
+int qstate_kv_compact(const qstate_kv_cfg* cfg, const qstate_kv_pages* pages, int32_t* others, int32_t R, int32_t limit,
+                      const qstate_kv_moves* moves, int32_t* left, int32_t* table_out, void* work, void* stream);
+
+/* Copies whole pages of one layer's cache, of every kind and store.  No page is source and destination at once, or
+ * destination twice.  Entries with a negative page are skipped; pages outside the pool are skipped and set the device status. */
+int qstate_kv_copy(const qstate_kv_cfg* cfg, const qstate_kv_cache* cache, const qstate_kv_moves* moves, void* stream);
+
+/* Bytes of what qstate_kv_group leaves for qstate_kv_attend_shared (16-byte aligned device memory; zeros: nothing shared),
+ * and of the latter's work space (256-byte aligned, zeroed once), for R requests; 0 for LATENT, whose heads share what they
+ * read already. */
+size_t qstate_kv_group_bytes(const qstate_kv_cfg* cfg, int32_t R);
+size_t qstate_kv_shared_work_bytes(const qstate_kv_cfg* cfg, int32_t R);
+
+/* Which of R requests share their first tokens: group g of N (0 <= N <= R) is the requests [start[g], start[g + 1]) (start: N + 1,
+ * not falling, within [0, R]), whose first common[g] tokens are the same.  Requests outside all groups, those with fewer tokens and
+ * those whose window begins behind token 0 read theirs by themselves, and so does a group that only one could share in.  Made from lens (R) as
+ * they are at the attention, for layers of one Hq, Hkv, dk and window.  A start outside its bounds or a number of tokens
+ * outside the table sets the device status, and nothing (or that group) is shared. */
+int qstate_kv_group(const qstate_kv_cfg* cfg, const int32_t* lens, int32_t R, const int32_t* start, const int32_t* common, int32_t N,
+                    void* groups, void* stream);
+
+/* qstate_kv_attend (HEADS), a group's common tokens read once, through the table of the first request that shares in
+ * them.  The results are those of qstate_kv_attend up to FP32 rounding and one rounding of the weights to 16 bits. */
+int qstate_kv_attend_shared(const qstate_kv_cfg* cfg, const qstate_kv_cache* cache, const void* q, int64_t q_row,
+                            int64_t q_head, const int32_t* table, const int32_t* lens, int32_t R, const void* groups, void* o,
+                            float* lse, void* work, void* stream);
+
 /* Synchronise `stream`, read and clear the device status word.  QSTATE_OK; QSTATE_ETIMEOUT if a
- * bounded wait of the chunked form or of qstate_kv_attend over latents gave up (the call's results are not valid; the kernel still
+ * bounded wait of the chunked form, of qstate_kv_attend over latents or of qstate_kv_attend_shared gave up (the call's results are not valid; the kernel still
  * waited for its products before freeing tensor memory, so later calls are unaffected);
  * otherwise QSTATE_EDEVICE with the reasons in qstate_last_error().  If even that last wait
  * gave up, tensor memory may have been freed under products in flight: the device is then
@@ -393,8 +464,8 @@ int qstate_kv_attend(const qstate_kv_cfg* cfg, const qstate_kv_cache* cache, con
  * QSTATE_EDEVICE for the rest of the process. */
 int qstate_check(void* stream);
 
-/* Limit, in polls of the mbarrier, of the waits of the chunked form and of qstate_kv_attend over
- * latents for their tensor-core products in the calls that follow (process-wide; read when a call is enqueued).  polls >= 0 sets it; 0
+/* Limit, in polls of the mbarrier, of the waits of the chunked form, of qstate_kv_attend over
+ * latents and of qstate_kv_attend_shared for their tensor-core products in the calls that follow (process-wide; read when a call is enqueued).  polls >= 0 sets it; 0
  * gives up at the first wait without polling (the products still complete, the results of
  * that call are invalid and qstate_check reports QSTATE_ETIMEOUT): a way to exercise the
  * timeout path without a faulty kernel.  polls < 0 restores the default (2^24 polls, far

@@ -81,13 +81,19 @@ class _KvSlots(ct.Structure):
                 ("ok", ct.c_void_p), ("T", ct.c_int32)]
 
 
+class _KvMoves(ct.Structure):
+    _fields_ = [("src", ct.c_void_p), ("dst", ct.c_void_p), ("n", ct.c_int32)]
+
+
 EXPORTS = ["qstate_validate", "qstate_region_bytes", "qstate_units", "qstate_scale_groups",
            "qstate_bits_per_element", "qstate_init", "qstate_alloc_bits", "qstate_pack",
            "qstate_unpack", "qstate_quant_decay", "qstate_quant_decay_noalloc", "qstate_step",
            "qstate_scan", "qstate_scan_host",
            "qstate_scan_fp32", "qstate_check", "qstate_set_wait_limit", "qstate_set_scan_partitions",
            "qstate_scan_partition_count", "qstate_last_error", "qstate_kv_validate", "qstate_kv_cache_bytes",
-           "qstate_kv_work_bytes", "qstate_kv_plan", "qstate_kv_append", "qstate_kv_attend"]
+           "qstate_kv_work_bytes", "qstate_kv_plan", "qstate_kv_append", "qstate_kv_attend",
+           "qstate_kv_pages_work_bytes", "qstate_kv_fork", "qstate_kv_compact", "qstate_kv_copy",
+           "qstate_kv_group_bytes", "qstate_kv_shared_work_bytes", "qstate_kv_group", "qstate_kv_attend_shared"]
 
 _lib = None
 
@@ -146,10 +152,19 @@ def load(path: str | None = None, build_if_missing: bool = False):
     L.qstate_kv_plan.argtypes = [P, P, P, I32, P, P, P]
     L.qstate_kv_append.argtypes = [P, P, P, I64, I64, P, I64, I64, P, I32, P]
     L.qstate_kv_attend.argtypes = [P, P, P, I64, I64, P, P, I32, P, P, P, P]
+    for name in ("qstate_kv_pages_work_bytes", "qstate_kv_group_bytes", "qstate_kv_shared_work_bytes"):
+        getattr(L, name).argtypes = [KC, I32]
+        getattr(L, name).restype = ct.c_size_t
+    L.qstate_kv_fork.argtypes = [P, P, P, P, P, I32, P, P, P, P]
+    L.qstate_kv_compact.argtypes = [P, P, P, I32, I32, P, P, P, P, P]
+    L.qstate_kv_copy.argtypes = [P, P, P, P]
+    L.qstate_kv_group.argtypes = [P, P, I32, P, P, I32, P, P]
+    L.qstate_kv_attend_shared.argtypes = [P, P, P, I64, I64, P, P, I32, P, P, P, P, P]
     for name in EXPORTS:
         if name not in ("qstate_region_bytes", "qstate_units", "qstate_scale_groups",
                         "qstate_bits_per_element", "qstate_last_error", "qstate_kv_cache_bytes",
-                        "qstate_kv_work_bytes"):
+                        "qstate_kv_work_bytes", "qstate_kv_pages_work_bytes", "qstate_kv_group_bytes",
+                        "qstate_kv_shared_work_bytes"):
             getattr(L, name).restype = ct.c_int
     _lib = L
     return L
@@ -685,5 +700,191 @@ def qstate_kv_attend(cfg: KvConfig, cache: KvCache, q, table, lens, o, lse, work
     rc = (_lib or load()).qstate_kv_attend(cfg._at, cache._at, q.data_ptr(), qr, qh, table.data_ptr(), lens.data_ptr(), R,
                                            o.data_ptr(), sums, _work(cfg, work),
                                            _current_stream() if stream is None else stream.cuda_stream)
+    if rc:
+        _check(rc)
+
+
+# ---- requests that hold pages together ---------------------------------------------------------------
+@dataclass(frozen=True)
+class KvMoves(_Kept):
+    """Pages to copy, src[i] to dst[i] (int32, one length; -1 in both where there is nothing to copy)."""
+    src: object
+    dst: object
+
+    def __post_init__(self):
+        import torch
+        at = [_typed(getattr(self, n), n, torch.int32) for n in ("src", "dst")]
+        _sized(self.dst, "dst", self.src.numel())
+        _keep(self, _KvMoves(*at, self.src.numel()), n=self.src.numel())
+
+
+def new_kv_moves(n: int, device="cuda") -> KvMoves:
+    import torch
+    return KvMoves(*(torch.full((n,), -1, dtype=torch.int32, device=device) for _ in range(2)))
+
+
+@dataclass(frozen=True)
+class KvGroups(_Kept):
+    """What qstate_kv_group leaves for qstate_kv_attend_shared, for R requests."""
+    data: object
+    R: int
+
+    def __post_init__(self):
+        import torch
+        _keep(self, _at=_typed(self.data, "data", torch.uint8), _fits=None)
+
+    def _check(self, cfg):
+        """The memory is enough for the description; looked at once for each description."""
+        need = _bytes("qstate_kv_group_bytes", cfg, self.R)
+        if self.data.numel() < need:
+            raise ValueError(f"groups of {self.R} requests need {need} bytes")
+        _keep(self, _fits=cfg)
+
+
+def _bytes(name, cfg, R):
+    lib = _lib_or_raise()
+    n = int(getattr(lib, name)(ct.byref(cfg._c), R))
+    if n == 0:
+        raise QstateError(QSTATE_EINVAL, lib.qstate_last_error().decode())
+    return n
+
+
+def new_kv_groups(cfg: KvConfig, R: int, device="cuda") -> KvGroups:
+    import torch
+    return KvGroups(torch.zeros(_bytes("qstate_kv_group_bytes", cfg, R), dtype=torch.uint8, device=device), R)
+
+
+def new_kv_pages_work(cfg: KvConfig, R: int, device="cuda"):
+    """Work space of qstate_kv_fork and qstate_kv_compact for up to R requests (zeroed)."""
+    import torch
+    return torch.zeros(_bytes("qstate_kv_pages_work_bytes", cfg, R), dtype=torch.uint8, device=device)
+
+
+def new_kv_shared_work(cfg: KvConfig, R: int, device="cuda"):
+    """Work space of qstate_kv_attend_shared for up to R requests (zeroed); serves qstate_kv_attend too."""
+    import torch
+    return torch.zeros(_bytes("qstate_kv_shared_work_bytes", cfg, R), dtype=torch.uint8, device=device)
+
+
+def _work_of(name, cfg, work, R):
+    """The address of a work space for R requests; its size is looked at once for each description and R."""
+    if getattr(work, "_kv_fits_R", None) != (name, R) or getattr(work, "_kv_fits_cfg", None) is not cfg:
+        need = _bytes(name, cfg, R)
+        if work.numel() * work.element_size() < need:
+            raise ValueError(f"the work space needs {need} bytes")
+        _ptr(work)
+        work._kv_fits_R, work._kv_fits_cfg = (name, R), cfg
+    return work.data_ptr()
+
+
+def _ints(t, name, n, none=False):
+    """Address of n int32 (None stays None where it may be)."""
+    import torch
+    if t is None and none:
+        return None
+    if t is None or t.dtype is not torch.int32 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+        _refuse(name, f"{n} int32")
+    return t.data_ptr()
+
+
+def _pages_struct(cfg, pages, lens_out, free_out):
+    R = pages.R
+    if pages._sizes != (R * cfg.max_pages, cfg.n_pages):
+        raise ValueError(f"table must have {R} x {cfg.max_pages} entries and free_list {cfg.n_pages}")
+    table, lens, free_list, free = pages._args
+    return _KvPages(table, lens, lens if lens_out is None else _ints(lens_out, "lens_out", R), free_list, free,
+                    free if free_out is None else _ints(free_out, "free_out", 1))
+
+
+def qstate_kv_fork(cfg: KvConfig, pages: KvPages, others, parent, keep, moves: KvMoves, ok, work, lens_out=None, free_out=None,
+                   stream=None) -> None:
+    """Requests take over the first keep[r] tokens of request parent[r] (see include/qstate.h): others (n_pages), parent
+    (R), keep (R, or None for all tokens), int32, ok (R), uint8, moves of R entries or more.  The new lengths and free
+    count go to lens_out and free_out, in place without them."""
+    import torch
+    R = pages.R
+    c = _pages_struct(cfg, pages, lens_out, free_out)
+    if ok.dtype is not torch.uint8 or ok.numel() != R or not ok.is_cuda or not ok.is_contiguous():
+        _refuse("ok", f"{R} uint8")
+    if moves.n < R:
+        raise ValueError(f"moves must have {R} entries or more, got {moves.n}")
+    rc = (_lib or load()).qstate_kv_fork(cfg._at, ct.addressof(c), _ints(others, "others", cfg.n_pages), _ints(parent, "parent", R),
+                                         _ints(keep, "keep", R, none=True), R, moves._at, ok.data_ptr(),
+                                         _work_of("qstate_kv_pages_work_bytes", cfg, work, R),
+                                         _current_stream() if stream is None else stream.cuda_stream)
+    if rc:
+        _check(rc)
+
+
+def qstate_kv_compact(cfg: KvConfig, pages: KvPages, others, limit: int, moves: KvMoves, left, work, table_out=None,
+                      free_out=None, stream=None) -> None:
+    """Held pages from `limit` on move in front of it (see include/qstate.h): others (n_pages) and left (1), int32,
+    may be None.  The new table and free count go to table_out and free_out, in place without them."""
+    R = pages.R
+    c = _pages_struct(cfg, pages, None, free_out)
+    to = c.table if table_out is None else _ints(table_out, "table_out", R * cfg.max_pages)
+    rc = (_lib or load()).qstate_kv_compact(cfg._at, ct.addressof(c), _ints(others, "others", cfg.n_pages, none=True), R, limit,
+                                            moves._at, _ints(left, "left", 1, none=True), to,
+                                            _work_of("qstate_kv_pages_work_bytes", cfg, work, R),
+                                            _current_stream() if stream is None else stream.cuda_stream)
+    if rc:
+        _check(rc)
+
+
+def qstate_kv_copy(cfg: KvConfig, cache: KvCache, moves: KvMoves, stream=None) -> None:
+    """Copies the pages of `moves` in one layer's cache."""
+    if cache._fits is not cfg:
+        cache._check(cfg)
+    rc = (_lib or load()).qstate_kv_copy(cfg._at, cache._at, moves._at, _current_stream() if stream is None else stream.cuda_stream)
+    if rc:
+        _check(rc)
+
+
+def qstate_kv_group(cfg: KvConfig, lens, start, common, groups: KvGroups, stream=None) -> None:
+    """Which requests share their first tokens (see include/qstate.h): lens (R), start (N + 1), common (N), int32."""
+    if groups._fits is not cfg:
+        groups._check(cfg)
+    N = common.numel()
+    rc = (_lib or load()).qstate_kv_group(cfg._at, _ints(lens, "lens", groups.R), groups.R, _ints(start, "start", N + 1),
+                                          _ints(common, "common", N), N, groups._at,
+                                          _current_stream() if stream is None else stream.cuda_stream)
+    if rc:
+        _check(rc)
+
+
+def _attend_args(cfg, cache, q, table, lens, o, lse):
+    """What an attention takes, looked at: q's strides, requests, lse's address."""
+    if cache._fits is not cfg:
+        cache._check(cfg)
+    R, H, dtype, i32 = lens.numel(), cfg.Hq, cfg.torch_dtype, cfg._i32
+    if q.dtype is not dtype or q.shape != (R, H, cfg.dk) or q.stride(2) != 1 or not q.is_cuda:
+        _refuse_rows("q", cfg, R, H, cfg.dk)
+    qr, qh, _ = q.stride()
+    if lens.dtype is not i32 or not lens.is_cuda or not lens.is_contiguous():
+        _refuse("lens", "int32")
+    if table.dtype is not i32 or table.numel() != R * cfg.max_pages or not table.is_cuda or not table.is_contiguous():
+        _refuse("table", f"{R} x {cfg.max_pages} int32")
+    if o.dtype is not dtype or o.numel() != R * H * cfg.dv or not o.is_cuda or not o.is_contiguous():
+        _refuse("o", f"{R} x {H} x {cfg.dv} {dtype}")
+    sums = None
+    if lse is not None:
+        if lse.dtype is not cfg._f32 or lse.numel() != R * H or not lse.is_cuda or not lse.is_contiguous():
+            _refuse("lse", f"{R} x {H} float32")
+        sums = lse.data_ptr()
+    return qr, qh, R, sums
+
+
+def qstate_kv_attend_shared(cfg: KvConfig, cache: KvCache, q, table, lens, groups: KvGroups, o, lse, work, stream=None) -> None:
+    """qstate_kv_attend with the groups' common tokens read once for all of their requests; `groups` as qstate_kv_group
+    left them for these lengths."""
+    qr, qh, R, sums = _attend_args(cfg, cache, q, table, lens, o, lse)
+    if groups._fits is not cfg:
+        groups._check(cfg)
+    if groups.R != R:
+        raise ValueError(f"groups were made for {groups.R} requests, got {R}")
+    rc = (_lib or load()).qstate_kv_attend_shared(cfg._at, cache._at, q.data_ptr(), qr, qh, table.data_ptr(), lens.data_ptr(), R,
+                                                  groups._at, o.data_ptr(), sums,
+                                                  _work_of("qstate_kv_shared_work_bytes", cfg, work, R),
+                                                  _current_stream() if stream is None else stream.cuda_stream)
     if rc:
         _check(rc)

@@ -63,6 +63,100 @@ struct KvAttendParams {
     int q_aligned;   // q can be read in 16 bytes
     int wait_polls;  // limit of the latent kernel's waits for copies and products
     int* status;
+    // ---- requests that share their first tokens; null and unused without ----
+    const int4* shared;      // of each request: tokens that it leaves to its group, the group's first block, blocks of a
+                             // key head, the request's first row
+    const int* groups;       // the groups (KvGroup)
+    float* store;            // unsplit rows of a request's own tokens: sums, and references and weights
+    float4* store_ml;
+    int2* dir;               // of each row of work: the worker that begins it (-1: unsplit, in the store), its parts
+    float* pre_part;         // the same of the groups' blocks of rows
+    float4* pre_ml;
+    float* pre_store;
+    float4* pre_store_ml;
+    int2* pre_dir;
+};
+
+// Tokens of a tile, and rows (requests' heads) of a block, in the attention over tokens that requests share.
+constexpr int kv_shared_tile(int d) { return d == 256 ? 64 : 128; }
+constexpr int kv_shared_rows(int d) { return d == 256 ? 128 : 256; }
+constexpr int kSharedRowUnits = 2;   // tiles that a block of rows costs by itself: its queries, its end
+
+// What qstate_kv_group leaves behind: a head, the requests' records, the groups that share anything.
+struct KvGroupHead {
+    int groups;              // that share
+    int R, Hq, Hkv, tile, rows;
+    long long units;         // of all blocks
+};
+struct KvGroup {
+    int first, rows;         // its first request; requests times query heads of a key head
+    int owner, tokens;       // the request whose pages are read, how many tokens
+    int blocks, block0;      // blocks of rows of a key head; index of its first block
+    long long unit0;         // units of the groups before it
+};
+constexpr int kKvGroupHeadBytes = 256;
+static_assert(sizeof(KvGroupHead) <= kKvGroupHeadBytes && sizeof(KvGroup) == 32, "layout");
+inline int kv_most_groups(int R) { return R / 2 + 1; }
+// Blocks of rows of at most R / 2 groups over R requests.
+inline long long kv_most_blocks(const qstate_kv_cfg& c, int R) {
+    return c.Hkv * (static_cast<long long>(R) * (c.Hq / c.Hkv) / kv_shared_rows(c.dk) + kv_most_groups(R));
+}
+
+struct KvGroupParams {
+    const int32_t* lens;
+    const int32_t* start;
+    const int32_t* common;
+    int N, R, G, Hkv, tile, rows, window;
+    long long most;          // tokens of a table's row
+    KvGroupHead head;        // host: what the head is to say, but for sums
+    KvGroupHead* out;
+    int4* shared;
+    KvGroup* groups;
+    int* status;
+};
+
+struct KvForkParams {
+    qstate_kv_pages pages;
+    qstate_kv_moves moves;
+    int32_t* others;
+    const int32_t* parent;
+    const int32_t* keep;
+    uint8_t* ok;
+    int R, page_shift, n_pages, max_pages;
+    int parts, chunk;        // of a request's columns: warps that share them, columns of each
+    int* head;               // work space: entries of the list below the pages that come back
+    int4* rec;
+    int* count;              // pages of a part that come back
+    int* owner;              // of each page: the last request that held it, plus 1; zeros between calls
+    int* stage;              // the new rows
+    int* status;
+};
+
+constexpr int kCompactSpan = 32768;   // pages that a CTA ranks
+struct KvCompactParams {
+    qstate_kv_pages pages;
+    qstate_kv_moves moves;
+    int32_t* others;
+    int32_t* table_out;
+    int32_t* left;
+    int R, limit, page_shift, n_pages, max_pages;
+    int parts, chunk;
+    int* head;               // work space: pages that move
+    uint32_t* used;          // a bit for each page; zeros between calls
+    int2* spans;
+    int* rank;
+    int* status;
+};
+
+struct KvCopyParams {
+    const int32_t* src;
+    const int32_t* dst;
+    int n, n_pages, tensors;
+    void* data[4];           // k, v and their exponents
+    long long bytes[4];      // of a page
+    int width[4];            // of a load
+    int pieces[4], pieces_all;
+    int* status;
 };
 
 cudaError_t launch_kv_plan(const KvPlanParams& p, cudaStream_t stream);
@@ -74,6 +168,14 @@ cudaError_t launch_kv_latent_512(const qstate_kv_cfg& c, const KvAttendParams& p
 cudaError_t launch_kv_heads_64(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
 cudaError_t launch_kv_heads_128(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
 cudaError_t launch_kv_heads_256(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
+cudaError_t launch_kv_shared_64(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
+cudaError_t launch_kv_shared_128(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
+cudaError_t launch_kv_shared_256(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
+cudaError_t launch_kv_group(const KvGroupParams& p, cudaStream_t stream);
+cudaError_t launch_kv_fork(const KvForkParams& p, cudaStream_t stream);
+cudaError_t launch_kv_compact(const KvCompactParams& p, cudaStream_t stream);
+cudaError_t launch_kv_copy(KvCopyParams p, cudaStream_t stream);
+int kv_column_parts(int R, int max_pages);
 // partial results that an attention launch may use: bytes of sums, of references and weights, of the list of
 // split rows
 struct KvPartBytes {

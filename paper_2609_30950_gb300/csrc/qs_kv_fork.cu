@@ -1,0 +1,348 @@
+// qs_kv_fork.cu -- requests take over the first tokens of others: tables, holders of each page, free list, copies.
+//
+// Request r takes over the first m_r tokens of request p = parent_r as they stand before the call, m_r = min(n_p, keep_r).
+// Of p's pages it holds the first w = floor(m / page) whole; where m ends inside a page (a cut), that one is to be written
+// by r alone.  With h(x) = others(x) + 1 holders of a page before the call:
+//     longest_p = max of w over the requests that take over from p
+//     r may go on with the page it is cut in where w = longest_p and h = 1 (no one else is left with it whole);
+//     one does, p itself if it may, else the first; every other cut takes a page from the list's top, in request order:
+//     (inclusive prefix sum of cuts)_r <= free, or r is refused
+//     h'(x) = h(x) - (requests whose old pages have x) + (requests whose new pages have x)
+//     pages with h' = 0 come back, in the order of the last request that held them and of its pages.
+// Four steps, each of which needs all of the one before: who gets what (one CTA: R <= 8192, prefix sums and two reductions
+// in shared memory); counts of holders and the new rows, to the work space (atomic sums of whole numbers: any order gives the same, and
+// a maximum that says who held a page last); pages that come back, counted; their places, and the rows in place.
+// A chain of latencies: one cluster whose CTAs meet at its barrier where tables are short, a launch a step else.
+#include "qs_common.cuh"
+#include "qs_kv.h"
+
+namespace qs {
+namespace {
+
+constexpr int kForkThreads = 1024, kForkWarps = kForkThreads / 32, kForkCluster = 8;
+constexpr int kNoTail = -1, kBadTail = -2;
+
+// Record of a request: parent, old pages, whole pages (bit 31: the tail is fresh), tail page.
+__device__ __forceinline__ int whole_of(const int4& rec) { return rec.z & 0x7fffffff; }
+__device__ __forceinline__ bool fresh_of(const int4& rec) { return rec.z < 0; }
+// First old column that the request leaves.
+__device__ __forceinline__ int leaves_from(const int4& rec, int r) {
+    return rec.x == r ? whole_of(rec) + (rec.w >= 0 && !fresh_of(rec) ? 1 : 0) : 0;
+}
+__device__ __forceinline__ bool changes(const int4& rec, int r) {
+    return rec.x != r || fresh_of(rec) || rec.w == kBadTail || rec.y != whole_of(rec) + (rec.w >= 0 ? 1 : 0);
+}
+
+// Inclusive prefix sum of x over the CTA's threads; all of them in `all`.
+__device__ __forceinline__ int block_sum(int x, int& all, int* sums) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(kFull, x, o);
+        if (lane >= o) x += y;
+    }
+    if (lane == 31) sums[warp] = x;
+    __syncthreads();
+    int w = lane < warps ? sums[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(kFull, w, o);
+        if (lane >= o) w += y;
+    }
+    all = __shfl_sync(kFull, w, 31);
+    const int before = __shfl_sync(kFull, w, (warp + 31) & 31);
+    __syncthreads();
+    return x + (warp ? before : 0);
+}
+
+// Who gets what.  kPer: requests a thread.  smem: 2 R ints.
+template <int kPer>
+__device__ void fork_decide(const KvForkParams& p, int* smem, int* sums) {
+    int* const longest = smem;
+    unsigned* const best = reinterpret_cast<unsigned*>(smem + p.R);
+    const int tid = threadIdx.x, R = p.R, sh = p.page_shift;
+    const long long most = static_cast<long long>(p.max_pages) << sh;
+    auto length = [&](int r) {
+        const int n = __ldcg(p.pages.lens + r);
+        if (n >= 0 && n <= most) return n;
+        raise_status(p.status, QS_DEV_PAGES);
+        return n < 0 ? 0 : static_cast<int>(most);
+    };
+    int free_n = __ldcg(p.pages.free_count);
+    for (int r = tid; r < R; r += kForkThreads) longest[r] = 0, best[r] = 0xffffffffu;
+    int par[kPer], n[kPer], m[kPer];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const int r = k * kForkThreads + tid;
+        par[k] = -1;
+        n[k] = m[k] = 0;
+        if (r >= R) continue;
+        par[k] = __ldcg(p.parent + r);
+        const int keep = p.keep ? __ldcg(p.keep + r) : -1;
+        n[k] = length(r);
+        if (par[k] >= R) {
+            raise_status(p.status, QS_DEV_PAGES);
+            par[k] = r;
+        }
+        if (par[k] < 0) continue;
+        m[k] = par[k] == r ? n[k] : length(par[k]);
+        if (keep >= 0 && keep < m[k]) m[k] = keep;
+    }
+    if (free_n < 0 || free_n > p.n_pages) {
+        if (tid == 0) raise_status(p.status, QS_DEV_PAGES);
+        free_n = min(max(free_n, 0), p.n_pages);
+    }
+    __syncthreads();
+    int tail[kPer];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        tail[k] = kNoTail;
+        if (par[k] < 0) continue;
+        const int whole = m[k] >> sh;
+        if (whole) atomicMax(longest + par[k], whole);
+        if (m[k] & ((1 << sh) - 1)) tail[k] = __ldcg(p.pages.table + static_cast<size_t>(par[k]) * p.max_pages + whole);
+        if (tail[k] >= p.n_pages || tail[k] < kNoTail || (tail[k] == kNoTail && (m[k] & ((1 << sh) - 1)))) {
+            raise_status(p.status, QS_DEV_PAGES);
+            tail[k] = kBadTail;
+        }
+    }
+    __syncthreads();
+    bool could[kPer];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const int r = k * kForkThreads + tid;
+        could[k] = tail[k] >= 0 && (m[k] >> sh) == longest[par[k]] && __ldcg(p.others + tail[k]) == 0;
+        if (could[k]) atomicMin(best + par[k], r == par[k] ? 0u : static_cast<unsigned>(r) + 1u);
+    }
+    __syncthreads();
+    int asked = 0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        if (k * kForkThreads >= R) break;
+        const int r = k * kForkThreads + tid;
+        const bool need = tail[k] >= 0 && !(could[k] && best[par[k]] == (r == par[k] ? 0u : static_cast<unsigned>(r) + 1u));
+        int all;
+        const int end = asked + block_sum(need, all, sums);
+        asked += all;
+        if (r >= R) continue;
+        const bool ok = !need || end <= free_n;
+        int src = -1, dst = -1, whole = m[k] >> sh;
+        if (need && ok) {
+            src = tail[k];
+            dst = __ldcg(p.pages.free_list + free_n - end);
+            if (dst < 0 || dst >= p.n_pages) {
+                raise_status(p.status, QS_DEV_PAGES);
+                src = dst = -1;
+                tail[k] = kBadTail;
+            } else {
+                tail[k] = dst;
+            }
+        }
+        if (!ok) {
+            m[k] = whole = 0;
+            par[k] = -1;
+            tail[k] = kNoTail;
+        }
+        const int pages = static_cast<int>((static_cast<unsigned>(n[k]) + (1u << sh) - 1) >> sh);
+        p.rec[r] = make_int4(par[k], pages, whole | (dst >= 0 ? static_cast<int>(0x80000000u) : 0), tail[k]);
+        p.pages.lens_out[r] = m[k];
+        p.ok[r] = ok;
+        p.moves.src[r] = src;
+        p.moves.dst[r] = dst;
+    }
+    for (int r = R + tid; r < p.moves.n; r += kForkThreads) p.moves.src[r] = p.moves.dst[r] = -1;
+    if (tid == 0) p.head[0] = free_n - min(asked, free_n);
+}
+
+// The steps over pages: a warp takes one of `parts` parts of a request's columns.
+template <class F>
+__device__ __forceinline__ void each_part(const KvForkParams& p, int worker, int workers, F f) {
+    const int items = p.R * p.parts;
+    for (int item = worker; item < items; item += workers) {
+        const int r = item / p.parts, c0 = (item - r * p.parts) * p.chunk;
+        const int4 rec = __ldcg(p.rec + r);
+        if (changes(rec, r)) f(item, r, rec, c0, c0 + p.chunk);
+    }
+}
+
+__device__ void fork_count_holders(const KvForkParams& p, int worker, int workers) {
+    const int lane = threadIdx.x & 31;
+    each_part(p, worker, workers, [&](int, int r, const int4& rec, int c0, int c1) {
+        const int32_t* const mine = p.pages.table + static_cast<size_t>(r) * p.max_pages;
+        const int whole = whole_of(rec);
+        if (rec.x >= 0 && rec.x != r) {
+            const int32_t* const from = p.pages.table + static_cast<size_t>(rec.x) * p.max_pages;
+#pragma unroll 4
+            for (int c = c0 + lane; c < min(c1, whole); c += 32) {
+                const int x = __ldcg(from + c);
+                p.stage[static_cast<size_t>(r) * p.max_pages + c] = x;
+                if (x >= 0 && x < p.n_pages)
+                    atomicAdd(p.others + x, 1);
+                else
+                    raise_status(p.status, QS_DEV_PAGES);
+            }
+        }
+        // the tail that is kept under a new name, and a fresh one (see fork_count_back)
+        if (lane == 0 && whole >= c0 && whole < c1 && rec.w >= 0 && (rec.x != r || fresh_of(rec))) atomicAdd(p.others + rec.w, 1);
+#pragma unroll 4
+        for (int c = max(c0, leaves_from(rec, r)) + lane; c < min(c1, rec.y); c += 32) {
+            const int x = __ldcg(mine + c);
+            if (x >= 0 && x < p.n_pages) {
+                atomicAdd(p.others + x, -1);
+                atomicMax(p.owner + x, r + 1);
+            } else {
+                raise_status(p.status, QS_DEV_PAGES);
+            }
+        }
+    });
+}
+
+// Whether request r is the last that held the page in this column, and whether it comes back.
+__device__ __forceinline__ bool last_holder(const KvForkParams& p, int r, int c, int c1, int& x, bool& back) {
+    back = false;
+    if (c >= c1) return false;
+    x = __ldcg(p.pages.table + static_cast<size_t>(r) * p.max_pages + c);
+    if (x < 0 || x >= p.n_pages) return false;
+    const int who = __ldcg(p.owner + x), others = __ldcg(p.others + x);
+    back = who == r + 1 && others == -1;
+    return who == r + 1;
+}
+
+__device__ void fork_count_back(const KvForkParams& p, int worker, int workers) {
+    const int lane = threadIdx.x & 31;
+    for (int i = worker * 32 + lane; i < p.R * p.parts; i += workers * 32) {
+        const int r = i / p.parts;
+        if (!changes(__ldcg(p.rec + r), r)) p.count[i] = 0;
+    }
+    each_part(p, worker, workers, [&](int item, int r, const int4& rec, int c0, int c1) {
+        int n = 0;
+#pragma unroll 4
+        for (int c = max(c0, leaves_from(rec, r)) + lane; c < min(c1, rec.y); c += 32) {
+            int x;
+            bool back;
+            last_holder(p, r, c, min(c1, rec.y), x, back);
+            n += back;
+        }
+        n = __reduce_add_sync(kFull, n);
+        if (lane == 0) p.count[item] = n;
+        // A fresh page has one holder now, so nobody beside it.  (One that was on the list although a request held it, and that
+        // this request leaves now, does not come back: it has just been given out.)
+        const int whole = whole_of(rec);
+        if (lane == 0 && whole >= c0 && whole < c1 && fresh_of(rec) && __ldcg(p.owner + rec.w) == 0) atomicAdd(p.others + rec.w, -1);
+    });
+}
+
+// smem: R parts ints.
+__device__ void fork_place(const KvForkParams& p, int cta, int ctas, int* smem, int* sums) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, items = p.R * p.parts;
+    const int base = __ldcg(p.head);
+    int total = 0;
+    for (int i0 = 0; i0 < items; i0 += kForkThreads) {
+        const int i = i0 + threadIdx.x, n = i < items ? __ldcg(p.count + i) : 0;
+        int all;
+        const int end = block_sum(n, all, sums);
+        if (i < items) smem[i] = total + end - n;
+        total += all;
+    }
+    __syncthreads();
+    if (cta == 0 && threadIdx.x == 0) p.pages.free_out[0] = min(base + total, p.n_pages);
+    each_part(p, cta * kForkWarps + warp, ctas * kForkWarps, [&](int item, int r, const int4& rec, int c0, int c1) {
+        int32_t* const mine = p.pages.table + static_cast<size_t>(r) * p.max_pages;
+        const int end = min(c1, rec.y), whole = whole_of(rec);
+        int at = base + smem[item];
+        for (int c = max(c0, leaves_from(rec, r)); c < end; c += 32) {
+            int x = -1;
+            bool back;
+            const bool last = last_holder(p, r, c + lane, end, x, back);
+            const unsigned mask = __ballot_sync(kFull, back);
+            if (back) {
+                const int to = at + __popc(mask & ((1u << lane) - 1));
+                if (to < p.n_pages)
+                    p.pages.free_list[to] = x;
+                else
+                    raise_status(p.status, QS_DEV_PAGES);
+                p.others[x] = 0;
+            }
+            if (last) p.owner[x] = 0;
+            at += __popc(mask);
+        }
+        __syncwarp();   // the old pages of these columns are read
+        if (rec.x >= 0 && rec.x != r)
+#pragma unroll 4
+            for (int c = c0 + lane; c < min(c1, whole); c += 32) mine[c] = __ldcg(p.stage + static_cast<size_t>(r) * p.max_pages + c);
+        if (lane == 0 && whole >= c0 && whole < c1 && rec.w != kNoTail) mine[whole] = rec.w >= 0 ? rec.w : -1;
+    });
+}
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+}
+
+// All four steps; CTAs of one cluster.
+template <int kPer>
+__global__ void __cluster_dims__(kForkCluster, 1, 1) __launch_bounds__(kForkThreads) kv_fork_kernel(const KvForkParams p) {
+    extern __shared__ int smem[];
+    __shared__ int sums[32];
+    chain_wait();
+    const int worker = blockIdx.x * kForkWarps + (threadIdx.x >> 5), workers = kForkCluster * kForkWarps;
+    if (blockIdx.x == 0) fork_decide<kPer>(p, smem, sums);
+    cluster_sync();
+    fork_count_holders(p, worker, workers);
+    cluster_sync();
+    fork_count_back(p, worker, workers);
+    cluster_sync();
+    fork_place(p, blockIdx.x, kForkCluster, smem, sums);
+}
+
+// One step.
+template <int kPer>
+__global__ void __launch_bounds__(kForkThreads) kv_fork_step_kernel(const KvForkParams p, const int step) {
+    extern __shared__ int smem[];
+    __shared__ int sums[32];
+    chain_wait();
+    const int worker = blockIdx.x * kForkWarps + (threadIdx.x >> 5), workers = gridDim.x * kForkWarps;
+    if (step == 0)
+        fork_decide<kPer>(p, smem, sums);
+    else if (step == 1)
+        fork_count_holders(p, worker, workers);
+    else if (step == 2)
+        fork_count_back(p, worker, workers);
+    else
+        fork_place(p, blockIdx.x, gridDim.x, smem, sums);
+}
+
+template <int kPer>
+cudaError_t launch_fork(const KvForkParams& p, bool cluster, cudaStream_t stream) {
+    // The limit is the kernel's, not the call's: every call sets the same one.
+    constexpr int kMost = 2 * sizeof(int) * kKvMaxRequests;
+    const size_t decide = 2 * sizeof(int) * static_cast<size_t>(p.R), place = sizeof(int) * static_cast<size_t>(p.R) * p.parts;
+    const size_t both = decide > place ? decide : place;
+    if (cluster) {
+        const cudaError_t e = cudaFuncSetAttribute(kv_fork_kernel<kPer>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+        if (e != cudaSuccess) return e;
+        return launch_chained(kv_fork_kernel<kPer>, kForkCluster, kForkThreads, both, stream, true, p);
+    }
+    cudaError_t e = cudaFuncSetAttribute(kv_fork_step_kernel<kPer>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+    const int need = (p.R * p.parts + kForkWarps - 1) / kForkWarps, most = 2 * device_sm_count();
+    const int grid = need < 1 ? 1 : need < most ? need : most;
+    for (int step = 0; step < 4 && e == cudaSuccess; ++step)
+        e = launch_chained(kv_fork_step_kernel<kPer>, step == 0 ? 1 : grid, kForkThreads, step == 0 ? decide : step == 3 ? place : 0,
+                           stream, true, p, step);
+    return e;
+}
+
+}  // namespace
+
+// Parts of a request's columns, a power of two with R parts <= kKvMaxRequests, of 128 columns or more.
+int kv_column_parts(int R, int max_pages) {
+    int parts = 1;
+    while (2LL * parts * (R < 1 ? 1 : R) <= kKvMaxRequests && 2LL * parts * 128 <= max_pages) parts *= 2;
+    return parts;
+}
+
+cudaError_t launch_kv_fork(const KvForkParams& p, cudaStream_t stream) {
+    const bool cluster = static_cast<long long>(p.R) * p.max_pages <= 1 << 19;
+    return p.R <= kForkThreads ? launch_fork<1>(p, cluster, stream) : launch_fork<kKvMaxRequests / kForkThreads>(p, cluster, stream);
+}
+
+}  // namespace qs

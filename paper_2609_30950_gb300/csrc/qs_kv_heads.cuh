@@ -31,7 +31,7 @@
 
 #include <cuda_bf16.h>
 
-#include "qs_kv_tiles.cuh"
+#include "qs_kv_join.cuh"
 
 namespace qs {
 namespace kv {
@@ -79,7 +79,9 @@ struct HeadsShape {
     }
 };
 
-template <int D, bool kF16, bool kE4M3, bool kHalf, int kStages, int kCtas>
+// kShared: requests leave the tokens that they share to another kernel, and what they make of the others goes to memory, to be
+// joined with that kernel's part.
+template <int D, bool kF16, bool kE4M3, bool kHalf, int kStages, int kCtas, bool kShared>
 __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendParams p, const int per_group, const int groups_per_kv) {
     using S = HeadsShape<D, kE4M3, kStages>;
     constexpr bool kProd16 = kF16 || kE4M3;         // products in f16
@@ -93,9 +95,9 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
 
     Share& share = *reinterpret_cast<Share*>(smem + S::kShare);
     if (!p.whole_rows)
-        make_share<S::kThreads, S::kTile, S::kChunk>(p, groups, blockIdx.x, reinterpret_cast<long long*>(smem + S::kScratch), &share);
+        make_share<S::kThreads, S::kTile, S::kChunk, kShared>(p, groups, blockIdx.x, reinterpret_cast<long long*>(smem + S::kScratch), &share);
     int split = 0;   // parts of the row that this CTA begins and others end
-    Walk<S::kTile, S::kChunk> cw;
+    Walk<S::kTile, S::kChunk, kShared> cw;
     bool live = cw.start(p, share, groups, blockIdx.x);
     bool fetching = live;
 
@@ -108,7 +110,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
     constexpr uint32_t kAllTokens = S::kChunk == 32 ? 0xffffffffu : (1u << (S::kChunk & 31)) - 1;
 
     // ---- copies ----
-    Walk<S::kTile, S::kChunk> fw = cw;
+    Walk<S::kTile, S::kChunk, kShared> fw = cw;
     int id = -1;
     auto look_up = [&]() {   // page of this lane's token in the chunk to come
         const int t = fw.span.base + (fw.tile * S::kWarps + warp) * S::kChunk + (one_page ? 0 : lane);
@@ -117,7 +119,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
             id = p.table[static_cast<size_t>(fw.r) * p.max_pages + (t >> p.page_shift)];
     };
     // Queries of a row that begins: thread tid copies pieces tid % 8 + 8 i of head tid / 8 (and finds them there).
-    auto q_src = [&](const Walk<S::kTile, S::kChunk>& w, int* heads) {
+    auto q_src = [&](const Walk<S::kTile, S::kChunk, kShared>& w, int* heads) {
         const int hk = w.group / groups_per_kv, part = w.group - hk * groups_per_kv;
         *heads = min(per_group, G - part * per_group);
         return static_cast<const uint16_t*>(p.q) + w.r * p.q_row + (hk * G + part * per_group + (tid >> 3)) * p.q_head;
@@ -534,6 +536,11 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
             const float* const all = reinterpret_cast<const float*>(smem + stage * S::kSlot);
             const size_t out_row = static_cast<size_t>(cw.r) * p.Hq + h0;
             auto finish = [&](int row, int col, float4 acc, float4 sums) {
+                if (kShared) {
+                    reinterpret_cast<float4*>(p.store)[((out_row + row) * D + col) / 4] = acc;
+                    if (col == 0) p.store_ml[out_row + row] = sums;
+                    return;
+                }
                 // sums: references of values and weights, sum of weights
                 const float inv = sums.z == 0.0f ? 0.0f : 1.0f / sums.z;
                 const float c = kProd16 && sums.x != sums.y ? inv * exp2_fast(sums.x - sums.y) : inv;
@@ -575,7 +582,11 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
                     if (col == 0) reinterpret_cast<float4*>(p.part_ml)[slot * kHeadRows + row] = sums;
                 }
             }
-            if (tid == 0 && !whole && began == 0) {
+            if (kShared && tid == 0 && began == 0)
+                p.dir[static_cast<size_t>(cw.r) * groups + cw.group] =
+                    whole ? make_int2(-1, 1)
+                          : make_int2(blockIdx.x, row_parts(p, share, blockIdx.x, cw.left, cw.tile, cw.span.tiles));
+            if (!kShared && tid == 0 && !whole && began == 0) {
                 split = row_parts(p, share, blockIdx.x, cw.left, cw.tile, cw.span.tiles);
                 p.split[kKvWorkers + blockIdx.x] = cw.r * groups + cw.group;
             }
@@ -588,20 +599,20 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
         live = cw.next(p, groups);
     }
     for (int r = blockIdx.x; r < p.R; r += p.workers)   // requests without tokens
-        if (clamped_len(p, r, true) == 0) {
+        if (clamped_len(p, r, true) == 0 && !kShared) {
             uint4* out = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.o) + static_cast<size_t>(r) * p.Hq * D);
             for (int i = tid; i < p.Hq * (D / 8); i += S::kThreads) out[i] = make_uint4(0, 0, 0, 0);
             if (p.lse)
                 for (int i = tid; i < p.Hq; i += S::kThreads) p.lse[static_cast<size_t>(r) * p.Hq + i] = -INFINITY;
         }
-    if (!p.whole_rows && tid == 0) p.split[blockIdx.x] = split;
+    if (!kShared && !p.whole_rows && tid == 0) p.split[blockIdx.x] = split;
     cp_wait<0>();
 }
 
-template <int D, bool kF16, bool kE4M3, bool kHalf, int kStages, int kCtas>
+template <int D, bool kF16, bool kE4M3, bool kHalf, int kStages, int kCtas, bool kShared>
 cudaError_t launch_heads(KvAttendParams p, int per_group, int groups_per_kv, cudaStream_t stream) {
     using S = HeadsShape<D, kE4M3, kStages>;
-    auto* kernel = kv_heads_kernel<D, kF16, kE4M3, kHalf, kStages, kCtas>;
+    auto* kernel = kv_heads_kernel<D, kF16, kE4M3, kHalf, kStages, kCtas, kShared>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
     if (e != cudaSuccess) return e;
     const int ctas = device_sm_count() * kCtas;
@@ -612,16 +623,21 @@ cudaError_t launch_heads(KvAttendParams p, int per_group, int groups_per_kv, cud
         if (rows < p.workers) p.workers = static_cast<int>(rows);
     }
     e = launch_chained(kernel, p.workers, S::kThreads, S::kBytes, stream, true, p, per_group, groups_per_kv);
-    if (e != cudaSuccess || p.whole_rows) return e;
-    return launch_join<D, kF16>(p, JoinGeo{1, kHeadRows, per_group, p.Hq / p.Hkv, groups_per_kv}, stream);
+    if (e != cudaSuccess || (p.whole_rows && !kShared)) return e;
+    const JoinGeo geo{1, kHeadRows, per_group, p.Hq / p.Hkv, groups_per_kv};
+    if constexpr (kShared) return launch_join_shared<D, kF16>(p, geo, stream);
+    return launch_join<D, kF16>(p, geo, stream);
 }
 
 // Heads of a group: G / ceil(G / 16), rounded up; up to 8 of them leave half of the products' rows free.
 template <int D, bool kF16, bool kE4M3, int kStages, int kCtas>
 cudaError_t launch_heads_of(const KvAttendParams& p, cudaStream_t stream) {
     const int G = p.Hq / p.Hkv, n = (G + kHeadRows - 1) / kHeadRows, per = (G + n - 1) / n;
-    return per <= 8 ? launch_heads<D, kF16, kE4M3, true, kStages, kCtas>(p, per, n, stream)
-                    : launch_heads<D, kF16, kE4M3, false, kStages, kCtas>(p, per, n, stream);
+    if (p.shared)
+        return per <= 8 ? launch_heads<D, kF16, kE4M3, true, kStages, kCtas, true>(p, per, n, stream)
+                        : launch_heads<D, kF16, kE4M3, false, kStages, kCtas, true>(p, per, n, stream);
+    return per <= 8 ? launch_heads<D, kF16, kE4M3, true, kStages, kCtas, false>(p, per, n, stream)
+                    : launch_heads<D, kF16, kE4M3, false, kStages, kCtas, false>(p, per, n, stream);
 }
 
 }  // namespace kv

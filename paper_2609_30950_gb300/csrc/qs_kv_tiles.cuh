@@ -32,13 +32,15 @@ __device__ __forceinline__ int clamped_len(const KvAttendParams& p, int r, bool 
     return n < 0 ? 0 : static_cast<int>(most);
 }
 
-template <int kTile, int kGrain>
-__device__ __forceinline__ Span span_of(const KvAttendParams& p, int n) {
+// kShared: without the tokens that request r shares with others, which another kernel reads.
+template <int kTile, int kGrain, bool kShared>
+__device__ __forceinline__ Span span_of(const KvAttendParams& p, int r, int n) {
     Span s;
     s.end = n;
     s.begin = p.window > 0 && n > p.window ? n - p.window : 0;
+    if (kShared) s.begin = min(max(s.begin, p.shared[r].x), n);
     s.base = s.begin & ~(kGrain - 1);
-    s.tiles = (n - s.base + kTile - 1) / kTile;
+    s.tiles = kShared && s.begin == n ? 0 : (n - s.base + kTile - 1) / kTile;
     return s;
 }
 
@@ -66,7 +68,7 @@ __device__ __forceinline__ int share_owner(long long total, long long u, int wor
 __device__ __forceinline__ int row_units(int tiles) { return tiles > 0 ? tiles + kRowUnits : 0; }
 
 // All threads of the CTA; `groups` rows a request.  scratch: kThreads / 32 + 2 long longs of shared memory; *out too.
-template <int kThreads, int kTile, int kGrain>
+template <int kThreads, int kTile, int kGrain, bool kShared = false>
 __device__ __forceinline__ void make_share(const KvAttendParams& p, int groups, int worker, long long* scratch, Share* out) {
     constexpr int kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -74,7 +76,7 @@ __device__ __forceinline__ void make_share(const KvAttendParams& p, int groups, 
     long long mine = 0;
     int tiles = 0;
     for (int r = r0; r < r1; ++r) {
-        tiles = row_units(span_of<kTile, kGrain>(p, clamped_len(p, r, false)).tiles);
+        tiles = row_units(span_of<kTile, kGrain, kShared>(p, r, clamped_len(p, r, false)).tiles);
         mine += tiles;
     }
     long long before = mine;
@@ -105,7 +107,7 @@ __device__ __forceinline__ void make_share(const KvAttendParams& p, int groups, 
         int r = r0;
         if (per > 1)
             for (; r < r1; ++r) {
-                tiles = row_units(span_of<kTile, kGrain>(p, clamped_len(p, r, false)).tiles);
+                tiles = row_units(span_of<kTile, kGrain, kShared>(p, r, clamped_len(p, r, false)).tiles);
                 if (at < static_cast<long long>(tiles) * groups) break;
                 at -= static_cast<long long>(tiles) * groups;
             }
@@ -119,7 +121,7 @@ __device__ __forceinline__ void make_share(const KvAttendParams& p, int groups, 
 
 // Walks the units of a worker: those of its share, or, with p.whole_rows, every p.workers-th row.  Rows without
 // tiles are stepped over.
-template <int kTile, int kGrain>
+template <int kTile, int kGrain, bool kShared = false>
 struct Walk {
     int r, group, tile;
     int left;      // units to the share's end, this one among them; whole rows: the row
@@ -137,7 +139,7 @@ struct Walk {
         r = s.r;
         group = s.group;
         tile = s.pos - kRowUnits;
-        span = span_of<kTile, kGrain>(p, clamped_len(p, r, false));
+        span = span_of<kTile, kGrain, kShared>(p, r, clamped_len(p, r, false));
         if (tile < 0) {
             left += tile;
             tile = 0;
@@ -151,7 +153,7 @@ struct Walk {
             if (left >= p.R * groups) return false;
             r = left / groups;
             group = left - r * groups;
-            span = span_of<kTile, kGrain>(p, clamped_len(p, r, false));
+            span = span_of<kTile, kGrain, kShared>(p, r, clamped_len(p, r, false));
         } while (span.tiles == 0);
         return true;
     }
@@ -166,7 +168,8 @@ struct Walk {
         if (++group < groups) return true;
         group = 0;
         do {
-            span = span_of<kTile, kGrain>(p, clamped_len(p, ++r, false));
+            ++r;
+            span = span_of<kTile, kGrain, kShared>(p, r, clamped_len(p, r, false));
         } while (span.tiles == 0);
         return true;
     }
