@@ -102,8 +102,8 @@ SharedWork shared_work(const qstate_kv_cfg& c, int R) {
     w.part = w.dir + whole(rows * sizeof(int2));
     w.part_ml = w.part + slots * d * sizeof(float);
     w.pre_store = w.part_ml + slots * sizeof(float4);
-    w.pre_store_ml = w.pre_store + whole(rows * d * sizeof(float));
-    w.pre_dir = w.pre_store_ml + whole(rows * sizeof(float4));
+    w.pre_store_ml = w.pre_store + whole(2 * rows * d * sizeof(float));   // two streams
+    w.pre_dir = w.pre_store_ml + whole(2 * rows * sizeof(float4));
     w.all = w.pre_dir + whole(static_cast<size_t>(kv_most_blocks(c, R)) * sizeof(int2));
     return w;
 }

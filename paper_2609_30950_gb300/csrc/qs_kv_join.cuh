@@ -12,29 +12,28 @@ namespace qs {
 namespace kv {
 
 struct PartList {
-    const float* sums;       // of the first part
+    const float* sums;       // rows of D
     const float4* ml;
-    size_t step, step1;      // floats between parts (from the second on), and from the first to the second
-    size_t ml_step, ml_step1;
-    int n;
+    size_t row, step, step1; // the first part's row; rows between parts (from the second on), and from the first to the second
+    size_t pair;             // rows between the two streams of a part
+    int n, streams;
 };
 
 // The parts of a row: unsplit in the store, or in slots of `rows` rows from `worker` on.
-template <int D>
 __device__ __forceinline__ PartList part_list(int2 dir, const float* store, const float4* store_ml, size_t out_row, const float* part,
                                               const float4* part_ml, int rows, int row) {
-    if (dir.x < 0) return {store + out_row * D, store_ml + out_row, 0, 0, 0, 0, 1};
-    const size_t first = static_cast<size_t>(part_slot(dir.x, true)) * rows + row;
+    if (dir.x < 0) return {store, store_ml, out_row, 0, 0, 0, 1, 1};
     // the first is in slot 2 worker + 1, part i behind it in slot 2 (worker + i)
-    return {part + first * D, part_ml + first, static_cast<size_t>(2) * rows * D, static_cast<size_t>(rows) * D,
-            static_cast<size_t>(2) * rows, static_cast<size_t>(rows), dir.y};
+    return {part, part_ml, static_cast<size_t>(part_slot(dir.x, true)) * rows + row, 2 * static_cast<size_t>(rows),
+            static_cast<size_t>(rows), 0, dir.y, 1};
 }
-template <int D>
-__device__ __forceinline__ const float* sums_at(const PartList& p, int i) {
-    return i == 0 ? p.sums : p.sums + p.step1 + (i - 1) * p.step;
-}
-__device__ __forceinline__ const float4* ml_at(const PartList& p, int i) {
-    return i == 0 ? p.ml : p.ml + p.ml_step1 + (i - 1) * p.ml_step;
+__device__ __forceinline__ size_t part_row(const PartList& p, int i) {
+    size_t at = p.row;
+    if (p.streams == 2) {
+        at += (i & 1) * p.pair;
+        i >>= 1;
+    }
+    return i == 0 ? at : at + p.step1 + (i - 1) * p.step;
 }
 
 template <int D, bool kF16, int kWarpsPer>
@@ -54,11 +53,19 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_shared_kernel(const K
         const int group = kv * g.groups_per_kv + in_kv / g.per_group, at = rec.w + in_kv;
         PartList own{}, pre{};
         if (mine && begin < n)
-            own = part_list<D>(__ldcg(p.dir + static_cast<size_t>(r) * groups + group), p.store, p.store_ml, row, p.part,
+            own = part_list(__ldcg(p.dir + static_cast<size_t>(r) * groups + group), p.store, p.store_ml, row, p.part,
                                reinterpret_cast<const float4*>(p.part_ml), g.rows, in_kv % g.per_group);
-        if (mine && rec.x > 0)
-            pre = part_list<D>(__ldcg(p.pre_dir + rec.y + kv * rec.z + at / kv_shared_rows(D)), p.pre_store, p.pre_store_ml, row, p.pre_part,
-                               p.pre_ml, kv_shared_rows(D), at % kv_shared_rows(D));
+        if (mine && rec.x > 0) {
+            int2 dir = __ldcg(p.pre_dir + rec.y + kv * rec.z + at / kv_shared_rows(D));
+            const bool pair = dir.y < 0;   // two streams of one half
+            dir.y = abs(dir.y);
+            pre = part_list(dir, p.pre_store, p.pre_store_ml, row, p.pre_part, p.pre_ml, kv_shared_rows(D), at % kv_shared_rows(D));
+            if (pair) {
+                pre.streams = 2;
+                pre.n *= 2;
+                pre.pair = dir.x < 0 ? static_cast<size_t>(rows) : 128;
+            }
+        }
         const int first = warp % kWarpsPer, all = own.n + pre.n, count = all > first ? (all - first + kWarpsPer - 1) / kWarpsPer : 0;
         float Mo = -INFINITY, M = -INFINITY, L = 0.0f, Lo = 0.0f;
         float4 acc[kPieces] = {};
@@ -67,7 +74,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_shared_kernel(const K
             float4 y = make_float4(-INFINITY, -INFINITY, 0.0f, 0.0f);   // a lane's part's
             if (lane < many) {
                 const int i = first + (base + lane) * kWarpsPer;
-                y = __ldcg(i < pre.n ? ml_at(pre, i) : ml_at(own, i - pre.n));
+                y = __ldcg(i < pre.n ? pre.ml + part_row(pre, i) : own.ml + part_row(own, i - pre.n));
             }
             float c = 0.0f;
             for (int j = 0; j < many; j += kBatch) {
@@ -76,7 +83,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_shared_kernel(const K
                 for (int b = 0; b < kBatch; ++b) {
                     const int i = first + (base + j + b) * kWarpsPer;
                     const bool on = j + b < many && lane < kLanes;
-                    const float4* const src = reinterpret_cast<const float4*>(i < pre.n ? sums_at<D>(pre, i) : sums_at<D>(own, i - pre.n)) + lane;
+                    const float4* const src =
+                        reinterpret_cast<const float4*>(i < pre.n ? pre.sums + part_row(pre, i) * D : own.sums + part_row(own, i - pre.n) * D) + lane;
 #pragma unroll
                     for (int k = 0; k < kPieces; ++k) v[b][k] = on ? __ldcg(src + k * 32) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 }
@@ -93,7 +101,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_shared_kernel(const K
                 }
 #pragma unroll
                 for (int b = 0; b < kBatch; ++b) {
-                    const float cb = __shfl_sync(kFull, c, j + b);
+                    const float cb = __shfl_sync(kFull, c, j + b), ref = __shfl_sync(kFull, y.x, j + b);
+                    if (ref == -INFINITY) continue;   // no token, and no sums
 #pragma unroll
                     for (int k = 0; k < kPieces; ++k) {
                         acc[k].x += cb * v[b][k].x;

@@ -9,11 +9,12 @@
 // the cache's bytes, that bound it, and below that one pass over the bytes.  Both products run on the tensor cores:
 //     S [128 rows x tokens] = Q K^T     Q and K in shared memory, entries contiguous (K-major)
 //     O [128 rows x d]     += P V       P in tensor memory over S itself, V in shared memory, entries contiguous (N-major)
-//   warps 0-3, 4-7  softmax: a row each, of the block's first and second 128 rows (at 256 entries only the first, whose S has two
-//                   buffers instead)
-//   warp 8          issues the products
-//   warps 9-12      copy queries, keys and values, 16 bytes at a time (e4m3: eight warps, which turn codes into bf16 on the way,
-//                   exactly: a code has 4 bits and its power of two is one of the type's)
+//   warps 0-3, 4-7  softmax: a row each, of the block's first and second 128 rows; of a block with no second half, of its even and
+//                   odd tiles, which make a part each (at 256 entries there is room for one O only: warps 0-3, and two buffers of S)
+//   warps 8 and 9   issue S and O: each waits for nothing but what its next product needs, and a stream's O runs while the other one's
+//                   softmax does
+//   warps 10-13     copy queries, keys and values, 16 bytes at a time (e4m3: they turn codes into bf16 on the way, exactly: a code has
+//                   4 bits and its power of two is one of the type's)
 // The units of all blocks (a tile; kSharedRowUnits more for the block itself) are dealt out evenly, as the rows' are in
 // qs_kv_tiles.cuh: a block that several CTAs share leaves a part from each.
 // The reference m follows the maximum only when that has outgrown it by 2^8.  In f16, which ends at 2^-24, a weight of the
@@ -29,7 +30,7 @@ namespace kv {
 
 constexpr int kMaxRing = 8, kMaskRing = 8;
 
-template <int D, bool kE4M3>
+template <int D>
 struct SharedShape {
     static constexpr int kTile = kv_shared_tile(D), kRows = kv_shared_rows(D), kM = kRows / 128;
     static constexpr int kBuffers = kM == 1 ? 2 : 1;                  // of S
@@ -39,30 +40,33 @@ struct SharedShape {
     static constexpr int kQBlock = 128 * 128, kQTile = kBlocks * kQBlock;
     static constexpr int kStages = D == 64 ? 8 : 5;
     static constexpr int kRing = kM * kQTile, kMisc = kRing + kStages * kTensor;
-    static constexpr int kSoftmax = 4 * kM, kIssuer = kSoftmax, kCopiers = kE4M3 ? 8 : 4;
-    static constexpr int kThreads = (kSoftmax + 1 + kCopiers) * 32;
+    static constexpr int kSoftmax = 4 * kM, kIssuer = kSoftmax, kCopiers = 4;
+    static constexpr int kThreads = (kSoftmax + 2 + kCopiers) * 32;
+    // S, P and O of a stream's job n are waited for at barriers of its buffer, whose next phase needs all who wait for this one:
+    // a parity tells neighbouring phases apart only.
+    static __device__ __forceinline__ int phase(int n) { return (kBuffers == 2 ? n >> 1 : n) & 1; }
     static constexpr int kOCol = kM * kBuffers * kTile;               // columns of tensor memory in front of O
     static_assert(kStages <= kMaxRing && kOCol + kM * D <= 512, "tensor memory");
     static constexpr int kWarpTokens = kTile / kCopiers;
 };
 
 struct SharedMisc {
-    uint64_t full[kMaxRing], free[kMaxRing], seen[kMaskRing], sready[2], pready[2], odone[2], qfull, qfree, drain;
-    uint32_t mask[kMaskRing][4];
+    uint64_t full[kMaxRing], free[kMaxRing], sgo[2], sready[2], pready[2], odone[2], qfull, qfree, drain;
+    alignas(16) uint32_t mask[kMaskRing][4];   // tokens of a tile that are there
     uint32_t tmem;
     int abort;
 };
 
-// Walks a worker's units.
-struct SharedWalk {
-    int e, hb, tile, tiles;      // group, key head and block of rows in one, tile
-    int left;
+// A worker's units, part after part: a part is the worker's tiles of one block of rows.
+struct SharedPart {
     KvGroup g;
+    int e, hb, tile, count, tiles;   // group; key head and block of rows in one; first tile and how many; the block's
+    int left;                        // units from the first tile to the share's end
 
     __device__ __forceinline__ void load(const KvGroup* groups, int index, int kTile) {
         e = index;
         const int4* const src = reinterpret_cast<const int4*>(groups + index);
-        int4 a = __ldcg(src), b = __ldcg(src + 1);
+        const int4 a = __ldcg(src), b = __ldcg(src + 1);
         g.first = a.x, g.rows = a.y, g.owner = a.z, g.tokens = a.w;
         g.blocks = b.x, g.block0 = b.y;
         g.unit0 = static_cast<long long>(static_cast<unsigned>(b.z)) | static_cast<long long>(b.w) << 32;
@@ -91,22 +95,23 @@ struct SharedWalk {
             left += tile;
             tile = 0;
         }
+        count = min(tiles - tile, left);
         return left > 0;
     }
     __device__ __forceinline__ bool next(const KvGroup* groups, int Hkv, int kTile) {
-        if (--left <= 0) return false;
-        if (++tile < tiles) return true;
-        tile = 0;
-        left -= kSharedRowUnits;
+        left -= count + kSharedRowUnits;
         if (left <= 0) return false;
-        if (++hb < g.blocks * Hkv) return true;
-        hb = 0;
-        load(groups, e + 1, kTile);
+        tile = 0;
+        if (++hb == g.blocks * Hkv) {
+            hb = 0;
+            load(groups, e + 1, kTile);
+        }
+        count = min(tiles, left);
         return true;
     }
-    __device__ __forceinline__ bool ends() const { return tile == tiles - 1 || left == 1; }
     __device__ __forceinline__ int kv() const { return hb / g.blocks; }
-    __device__ __forceinline__ int block() const { return hb % g.blocks; }
+    __device__ __forceinline__ int row0(int kRows) const { return hb % g.blocks * kRows; }
+    __device__ __forceinline__ bool whole() const { return count == tiles; }
 };
 
 // D [128 x N] (+)= A [128 x 16] B, A in tensor memory (two entries a column).  As mma_f16_ss: a whole warp in step.
@@ -118,20 +123,26 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint32_t b_lo
         "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate ? 1u : 0u), "r"(lead), "n"(kHi)
         : "memory");
 }
-// 32 columns of a lane's row.
-__device__ __forceinline__ void tmem_ld32(uint32_t at, float (&v)[32]) {
-    uint32_t r[32];
+// Columns of a lane's row.
+__device__ __forceinline__ void tmem_ld64(uint32_t at, float (&v)[64]) {
+    uint32_t r[64];
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
-        "tcgen05.wait::ld.sync.aligned;\n"
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+        "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,"
+        "%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,"
+        "%57,%58,%59,%60,%61,%62,%63"
+        "}, [%64];\ntcgen05.wait::ld.sync.aligned;\n"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
           "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
           "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
-          "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+          "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]),
+          "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]),
+          "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]),
+          "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]),
+          "=r"(r[63])
         : "r"(at) : "memory");
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
 }
 __device__ __forceinline__ void tmem_st16u(uint32_t at, const uint32_t (&r)[16]) {
     asm volatile(
@@ -145,8 +156,8 @@ __device__ __forceinline__ void st_shared16(uint32_t at, uint32_t a, uint32_t b,
 }
 
 template <int D, bool kF16, bool kE4M3>
-__global__ void __launch_bounds__(SharedShape<D, kE4M3>::kThreads, 1) kv_shared_kernel(const KvAttendParams p) {
-    using S = SharedShape<D, kE4M3>;
+__global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(const KvAttendParams p) {
+    using S = SharedShape<D>;
     constexpr int kTile = S::kTile, kM = S::kM, kAlloc = 512;
     constexpr float kLog2e = 1.4426950408889634f;
     extern __shared__ __align__(1024) char smem[];
@@ -165,15 +176,15 @@ __global__ void __launch_bounds__(SharedShape<D, kE4M3>::kThreads, 1) kv_shared_
             tc::mbar_init(&x.full[s], S::kCopiers * (kE4M3 ? 1 : 33));
             tc::mbar_init(&x.free[s], 1);
         }
-        for (int s = 0; s < kMaskRing; ++s) tc::mbar_init(&x.seen[s], S::kCopiers);
         for (int m = 0; m < 2; ++m) {
+            tc::mbar_init(&x.sgo[m], 1);
             tc::mbar_init(&x.sready[m], 1);
             tc::mbar_init(&x.pready[m], 4);
             tc::mbar_init(&x.odone[m], 1);
         }
         tc::mbar_init(&x.qfull, S::kCopiers * 33);
         tc::mbar_init(&x.qfree, 1);
-        tc::mbar_init(&x.drain, 1);
+        tc::mbar_init(&x.drain, 2);
         tc::mbar_fence_init();
         x.abort = 0;
     }
@@ -193,24 +204,28 @@ __global__ void __launch_bounds__(SharedShape<D, kE4M3>::kThreads, 1) kv_shared_
     const uint32_t tmem = x.tmem;
     volatile int* const abort = &x.abort;
     const int G = p.Hq / p.Hkv;
-    SharedWalk w;
-    bool live = fits && head.groups > 0 && w.start(head, groups, worker, p.workers, kTile);
+    SharedPart w;
+    const bool live = fits && head.groups > 0 && w.start(head, groups, worker, p.workers, kTile);
+    // Streams have their own S, P, O and softmax warps.  They are a block's halves (`two`), or, where it has one half, the part's
+    // even and odd tiles.
+    auto two_halves = [&](int rows) { return kM == 2 && rows > 128; };
+    auto stream_of = [&](int t) { return kM == 2 ? t & 1 : 0; };   // of a part's tile where there is one half
 
-    if (live && warp > S::kIssuer) {
+    if (live && warp > S::kIssuer + 1) {
         // ---- copies ----
-        const int pw = warp - S::kIssuer - 1, page_mask = (1 << p.page_shift) - 1;
-        auto look_up = [&](const SharedWalk& at) {
-            const int t = at.tile * kTile + pw * S::kWarpTokens + lane;
-            return lane < S::kWarpTokens && t < at.g.tokens ? __ldcg(p.table + static_cast<size_t>(at.g.owner) * p.max_pages + (t >> p.page_shift)) : -1;
+        const int pw = warp - S::kIssuer - 2, page_mask = (1 << p.page_shift) - 1;
+        auto look_up = [&](int tile) {
+            const int t = tile * kTile + pw * S::kWarpTokens + lane;
+            return lane < S::kWarpTokens && t < w.g.tokens ? __ldcg(p.table + static_cast<size_t>(w.g.owner) * p.max_pages + (t >> p.page_shift)) : -1;
         };
         // a thread copies one of eight pieces of every block of its rows
-        auto queries = [&](const SharedWalk& at) {
-            const int sg = lane & 7, h0 = at.kv() * G, i0 = at.block() * S::kRows;
-            const int rows = min(S::kRows, at.g.rows - i0);
+        auto queries = [&]() {
+            const int sg = lane & 7, h0 = w.kv() * G, i0 = w.row0(S::kRows);
+            const int rows = min(S::kRows, w.g.rows - i0);
             for (int i = pw * 4 + (lane >> 3); i < S::kRows; i += S::kCopiers * 4) {
                 const bool in = i < rows;
                 const int at_row = i0 + i, member = in ? at_row / G : 0;
-                const uint16_t* const q = static_cast<const uint16_t*>(p.q) + (at.g.first + member) * p.q_row +
+                const uint16_t* const q = static_cast<const uint16_t*>(p.q) + (w.g.first + member) * p.q_row +
                                           (in ? h0 + at_row - member * G : 0) * p.q_head + sg * 8;
                 uint32_t to = smem_u32(smem + (i >> 7) * S::kQTile + (i & 127) * 128 + ((sg ^ (i & 7)) << 4));
                 for (int b = 0; b < S::kBlocks; ++b, to += S::kQBlock) {
@@ -228,36 +243,32 @@ __global__ void __launch_bounds__(SharedShape<D, kE4M3>::kThreads, 1) kv_shared_
             __syncwarp();
             if (lane == 0) mbar_arrive(&x.qfull);
         };
-        int id = look_up(w), s = 0, phase = 0, blocks = 0, used = 0;   // blocks: of rows, whose queries have been asked for
-        bool begins = true, ok = true;                                 // ok: no wait has been given up
-        for (int i = 0; live; ++i) {
-            if (begins) {
-                if (blocks > 0) ok = ok && role_wait(&x.qfree, (blocks - 1) & 1, abort, p);   // S of the block before is done
-                if (ok)
-                    queries(w);
-                else {
-                    cp_async_arrive(&x.qfull);
-                    if (lane == 0) mbar_arrive(&x.qfull);
-                }
-                ++blocks;
+        int s = 0, phase = 0, parts = 0, used = 0, i = 0;
+        bool ok = true, more = true;   // ok: no wait has been given up
+        while (more) {
+            int id = look_up(w.tile);
+            if (parts > 0) ok = ok && role_wait(&x.qfree, (parts - 1) & 1, abort, p);   // S of the part before is done
+            if (ok) {
+                queries();
+            } else {
+                cp_async_arrive(&x.qfull);
+                if (lane == 0) mbar_arrive(&x.qfull);
             }
-            begins = w.ends();
-            const int t = w.tile * kTile + pw * S::kWarpTokens + lane;
+            ++parts;
+            const int kv_head = w.kv();
+            for (int c = 0; c < w.count; ++c, ++i) {
+            const int t = (w.tile + c) * kTile + pw * S::kWarpTokens + lane;
             const bool wanted = lane < S::kWarpTokens && t < w.g.tokens, there = wanted && id >= 0 && id < p.n_pages;
             if (wanted && !there) raise_status(p.status, QS_DEV_PAGES);
             const uint32_t on = __ballot_sync(kFull, there);
             if (lane == 0) {
                 if (S::kWarpTokens == 32)
                     *reinterpret_cast<volatile uint32_t*>(&x.mask[i % kMaskRing][pw]) = on;
-                else if (S::kWarpTokens == 16)
-                    reinterpret_cast<volatile uint16_t*>(x.mask[i % kMaskRing])[pw] = static_cast<uint16_t>(on);
                 else
-                    reinterpret_cast<volatile uint8_t*>(x.mask[i % kMaskRing])[pw] = static_cast<uint8_t>(on);
-                mbar_arrive(&x.seen[i % kMaskRing]);
+                    reinterpret_cast<volatile uint16_t*>(x.mask[i % kMaskRing])[pw] = static_cast<uint16_t>(on);
             }
-            const long long row = there ? ((static_cast<long long>(id) * p.Hkv + w.kv()) << p.page_shift) + (t & page_mask) : 0;
-            live = w.next(groups, p.Hkv, kTile);
-            if (live) id = look_up(w);
+            const long long row = there ? ((static_cast<long long>(id) * p.Hkv + kv_head) << p.page_shift) + (t & page_mask) : 0;
+            if (c + 1 < w.count) id = look_up(w.tile + c + 1);
 #pragma unroll 1
             for (int kv = 0; kv < 2; ++kv) {
                 const char* const pool = static_cast<const char*>(kv ? p.v : p.k);
@@ -324,137 +335,130 @@ __global__ void __launch_bounds__(SharedShape<D, kE4M3>::kThreads, 1) kv_shared_
                 ++used;
                 if (++s == S::kStages) s = 0, phase ^= 1;
             }
+            }
+            more = w.next(groups, p.Hkv, kTile);
         }
         cp_commit();
         cp_wait<0>();
     } else if (live && warp == S::kIssuer) {
-        // ---- products ----
-        constexpr uint32_t idS = idesc_f16(kF16, 128, kTile, false), idO = idesc_f16(kF16, 128, D, false) | 1u << 16;
-        const uint32_t lead = elect_lane();
-        const uint32_t dq = desc_lo(smem_u32(smem), 16), ring = smem_u32(smem + S::kRing);
-        int s = 0, phase = 0;           // ring
-        int done[2] = {0, 0};           // tiles of either half whose S has been issued
-        int blocks = 0;
-        bool ok = true, begins = true;
-        auto advance = [&]() {
-            if (++s == S::kStages) s = 0, phase ^= 1;
-        };
-        auto wait = [&](uint64_t* bar, uint32_t parity) { ok = ok && role_wait(bar, parity, abort, p); };
-        auto scores = [&](int m, uint32_t k_at) {   // of the half's next tile
-            const int n = done[m]++, buffer = kM == 2 ? m : n & 1;
-            const int before = n - S::kBuffers;     // its tile that had this buffer: p has been read
-            if (before >= 0) wait(&x.odone[m], before & 1);
-            if (!ok) return;
-            tc::fence_after_sync();
-            const uint32_t b0 = desc_lo(k_at, 16), a0 = dq + m * (S::kQTile / 16);
+        // ---- S ----
+        // A scale below zero is taken as S = -Q K^T (bit 13: A negated)
+        const uint32_t id = idesc_f16(kF16, 128, kTile, false) | (p.scale < 0.0f ? 1u << 13 : 0u);
+        const uint32_t lead = elect_lane(), dq = desc_lo(smem_u32(smem), 16), ring = desc_lo(smem_u32(smem + S::kRing), 16);
+        int s = 0, phase = 0, parts = 0, n0 = 0, n1 = 0;   // n: jobs of a stream that have been issued
+        bool ok = true, more = true;
+        while (more && ok) {
+            const bool two = two_halves(min(S::kRows, w.g.rows - w.row0(S::kRows)));
+            ok = role_wait(&x.qfull, parts++ & 1, abort, p);
+            for (int c = 0; c < w.count && ok; ++c) {
+                ok = role_wait(&x.full[s], phase, abort, p);
+                for (int h = two ? 0 : stream_of(c), end = two ? 2 : h + 1; h < end && ok; ++h) {
+                    const int n = h ? n1 : n0, buffer = kM == 2 ? h : n & 1;
+                    if (n >= S::kBuffers) ok = role_wait(&x.odone[buffer], S::phase(n - S::kBuffers), abort, p);   // p before has been read
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive(&x.sgo[buffer]);   // the tile's mask is there
+                    tc::fence_async_smem();                       // the copies' writes, for the tensor core's reads
+                    tc::fence_after_sync();
+                    const uint32_t d = tmem + buffer * kTile, a0 = dq + (two ? h : 0) * (S::kQTile / 16), b0 = ring + s * (S::kTensor / 16);
 #pragma unroll
-            for (int b = 0; b < S::kBlocks; ++b)
+                    for (int b = 0; b < S::kBlocks; ++b)
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    mma_f16_ss<kDescHi>(tmem + buffer * kTile, a0 + (b * S::kQBlock + k * 32) / 16, b0 + (b * S::kBlock + k * 32) / 16, idS,
-                                        b > 0 || k > 0, lead);
-            commit_by(&x.sready[buffer], lead);
-        };
-        auto values = [&](int m, int n, uint32_t v_at, bool first) {   // of the half's tile n
-            const int buffer = kM == 2 ? m : n & 1;
-            wait(&x.pready[buffer], (S::kBuffers == 2 ? n >> 1 : n) & 1);
-            if (!ok) return;
-            tc::fence_after_sync();
-            const uint32_t b0 = desc_lo(v_at, S::kBlock);
-#pragma unroll
-            for (int k = 0; k < kTile / 16; ++k)
-                mma_f16_ts<kDescHi>(tmem + S::kOCol + m * D, tmem + buffer * kTile + k * 8, b0 + k * 128, idO, !first || k > 0, lead);
-            commit_by(&x.odone[m], lead);
-        };
-        // keys of the walk's tile: S of both halves
-        auto keys = [&]() {
-            const bool two = kM == 2 && w.g.rows - w.block() * S::kRows > 128;
-            if (begins) wait(&x.qfull, blocks++ & 1);
-            wait(&x.full[s], phase);
-            if (ok) tc::fence_async_smem();   // the copies' writes, for the tensor core's reads
-            const uint32_t at = ring + s * S::kTensor;
-            scores(0, at);
-            if (two) scores(1, at);
-            if (ok) {
+                        for (int k = 0; k < 4; ++k)
+                            mma_f16_ss<kDescHi>(d, a0 + (b * S::kQBlock + k * 32) / 16, b0 + (b * S::kBlock + k * 32) / 16, id, b > 0 || k > 0, lead);
+                    commit_by(&x.sready[buffer], lead);
+                    (h ? n1 : n0) = n + 1;
+                }
+                if (!ok) break;
                 commit_by(&x.free[s], lead);
-                if (w.ends()) commit_by(&x.qfree, lead);
+                if (c == w.count - 1) commit_by(&x.qfree, lead);
+                s += 2;
+                if (s >= S::kStages) s -= S::kStages, phase ^= 1;
             }
-            advance();
-            return two;
-        };
-        bool two = keys();
-        while (live && ok) {
-            // keys of the next tile go in front of this one's values in the ring's order, behind them where S has one buffer
-            const bool first = begins, ends = w.ends(), now = two;
-            const int n0 = done[0] - 1, n1 = done[1] - 1;
-            const int sv = s, pv = phase;
-            auto products = [&]() {
-                wait(&x.full[sv], pv);
-                if (ok) tc::fence_async_smem();
-                const uint32_t at = ring + sv * S::kTensor;
-                values(0, n0, at, first);
-                if (now) values(1, n1, at, first);
-                if (ok) commit_by(&x.free[sv], lead);
-            };
-            advance();
-            if (S::kBuffers == 1) products();
-            begins = ends;
-            live = w.next(groups, p.Hkv, kTile);
-            if (live) two = keys();
-            if (S::kBuffers == 2) products();
+            more = w.next(groups, p.Hkv, kTile);
+        }
+    } else if (live && warp == S::kIssuer + 1) {
+        // ---- O ----
+        constexpr uint32_t id = idesc_f16(kF16, 128, D, false) | 1u << 16;   // B N-major
+        const uint32_t lead = elect_lane(), ring = desc_lo(smem_u32(smem + S::kRing), S::kBlock);
+        int s = 1, phase = 0, n0 = 0, n1 = 0;
+        bool ok = true, more = true;
+        while (more && ok) {
+            const bool two = two_halves(min(S::kRows, w.g.rows - w.row0(S::kRows)));
+            for (int c = 0; c < w.count && ok; ++c) {
+                ok = role_wait(&x.full[s], phase, abort, p);
+                for (int h = two ? 0 : stream_of(c), end = two ? 2 : h + 1; h < end && ok; ++h) {
+                    const int n = h ? n1 : n0, buffer = kM == 2 ? h : n & 1;
+                    ok = role_wait(&x.pready[buffer], S::phase(n), abort, p);
+                    if (!ok) break;
+                    tc::fence_async_smem();
+                    tc::fence_after_sync();
+                    const uint32_t d = tmem + S::kOCol + h * D, a0 = tmem + buffer * kTile + kTile / 2, b0 = ring + s * (S::kTensor / 16);
+                    const bool first = c < (two ? 1 : kM);   // of the stream's in this part
+#pragma unroll
+                    for (int k = 0; k < kTile / 16; ++k) mma_f16_ts<kDescHi>(d, a0 + k * 8, b0 + k * 128, id, !first || k > 0, lead);
+                    commit_by(&x.odone[buffer], lead);
+                    (h ? n1 : n0) = n + 1;
+                }
+                if (!ok) break;
+                commit_by(&x.free[s], lead);
+                s += 2;
+                if (s >= S::kStages) s -= S::kStages, phase ^= 1;
+            }
+            more = w.next(groups, p.Hkv, kTile);
         }
     } else if (live && warp < S::kSoftmax) {
         // ---- softmax ----
-        const int m_half = warp >> 2, row = (warp & 3) * 32 + lane;   // of the half
+        const int stream = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t tlane = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16);
-        const uint32_t o_at = tlane + S::kOCol + m_half * D;
-        const float zs = p.scale * kLog2e;
+        const uint32_t o_at = tlane + S::kOCol + stream * D;
+        // S carries the scale's sign; a scale of zero as next to nothing, so that the -inf of tokens that are not seen stays
+        const float zs = fmaxf(fabsf(p.scale) * kLog2e, 0x1p-126f);
         constexpr float kAbove = kF16 ? kLazyLatent + kLiftLatent : kLazyLatent, kBelow = kLiftLatent - kFarLatent;
         float m = -INFINITY, high = -INFINITY, l = 0.0f, lr = 0.0f;   // reference, the highest so far, sums of p and of rounded p
-        bool begins = true;
-        int began = 0, n = 0;   // n: tiles of this half
-        for (int i = 0; live; ++i) {
-            const int i0 = w.block() * S::kRows, rows = min(S::kRows, w.g.rows - i0) - m_half * 128;
-            const bool ends = w.ends();
-            if (begins) {
-                began = w.tile;
-                m = high = -INFINITY;
-                l = lr = 0.0f;
-            }
-            if (rows > 0) {
-                const int buffer = kM == 2 ? m_half : n & 1;
+        int n = 0, i = 0;   // the stream's jobs, all tiles
+        for (bool more = true; more;) {
+            const int i0 = w.row0(S::kRows), rows = min(S::kRows, w.g.rows - i0);
+            const bool two = two_halves(rows);
+            bool any = false;   // the stream has had a tile of this part
+            m = high = -INFINITY;
+            l = lr = 0.0f;
+            for (int c = 0; c < w.count; ++c, ++i) {
+                if (!two && stream_of(c) != stream) continue;
+                const int buffer = kM == 2 ? stream : n & 1;
                 const uint32_t s_at = tlane + buffer * kTile;
-                role_wait(&x.sready[buffer], (S::kBuffers == 2 ? n >> 1 : n) & 1, abort, p);
-                // behind the scores: a half that stepped over blocks may be rounds ahead of the masks
-                role_wait(&x.seen[i % kMaskRing], (i / kMaskRing) & 1, abort, p);
-                uint32_t on[kTile / 32];
-                bool all = true;
-#pragma unroll
-                for (int k = 0; k < kTile / 32; ++k) {
-                    on[k] = *reinterpret_cast<volatile uint32_t*>(&x.mask[i % kMaskRing][k]);
-                    all = all && on[k] == kFull;
-                }
+                role_wait(&x.sgo[buffer], S::phase(n), abort, p);
+                const uint4 seen = *reinterpret_cast<const uint4*>(x.mask[i % kMaskRing]);
+                role_wait(&x.sready[buffer], S::phase(n), abort, p);
                 tc::fence_after_sync();
-                // the largest score
-                float top = -INFINITY;
+                if ((seen.x & seen.y & (kTile > 64 ? seen.z & seen.w : kFull)) != kFull)
+#pragma unroll 1
+                for (int k = 0; k < kTile / 32; ++k) {   // scores of tokens that are not there
+                    const uint32_t on = x.mask[i % kMaskRing][k];
+                    if (on == kFull) continue;
+#pragma unroll 1
+                    for (int j = 0; j < 32; j += 16) {
+                        float z[16];
+                        tc::tmem_ld16(s_at + k * 32 + j, z);
 #pragma unroll
-                for (int k = 0; k < kTile / 32; ++k) {
-                    float z[32];
-                    tmem_ld32(s_at + k * 32, z);
-                    if (!all)
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) z[j] = (on[k] >> j) & 1 ? z[j] * zs : -INFINITY;
-                    float a = -INFINITY, b = -INFINITY;
-                    if (all && zs < 0.0f) {
-#pragma unroll
-                        for (int j = 0; j < 32; j += 2) a = fmaxf(a, -z[j]), b = fmaxf(b, -z[j + 1]);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; j += 2) a = fmaxf(a, z[j]), b = fmaxf(b, z[j + 1]);
+                        for (int e = 0; e < 16; ++e) z[e] = (on >> (j + e)) & 1 ? z[e] : -INFINITY;
+                        tc::tmem_st16(s_at + k * 32 + j, z);
                     }
-                    a = fmaxf(a, b);
-                    top = fmaxf(top, all ? a * fabsf(zs) : a);
+                    tc::wait_st();
                 }
+                // 64 tokens at a time; the last ones stay for what follows
+                float z[64], top = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < kTile; k += 64) {
+                    tmem_ld64(s_at + k, z);
+                    float a = top, b = -INFINITY;
+#pragma unroll
+                    for (int j = 0; j < 64; j += 4) {
+                        a = fmaxf(fmaxf(a, z[j]), z[j + 1]);
+                        b = fmaxf(fmaxf(b, z[j + 2]), z[j + 3]);
+                    }
+                    top = fmaxf(a, b);
+                }
+                top *= zs;
                 float now = m;
                 if (kF16) {
                     if (top > m + kAbove || m == -INFINITY) now = fmaxf(m, top - kLiftLatent);
@@ -468,8 +472,8 @@ __global__ void __launch_bounds__(SharedShape<D, kE4M3>::kThreads, 1) kv_shared_
                     l *= c;
                     lr *= c;
                     m = now;
-                    if (!begins) {
-                        role_wait(&x.odone[m_half], (n - 1) & 1, abort, p);   // the products so far are in
+                    if (any) {
+                        role_wait(&x.odone[kM == 2 ? stream : buffer ^ 1], S::phase(n - 1), abort, p);   // the products so far are in
                         tc::fence_after_sync();
 #pragma unroll 1
                         for (int k = 0; k < D; k += 16) {
@@ -484,76 +488,73 @@ __global__ void __launch_bounds__(SharedShape<D, kE4M3>::kThreads, 1) kv_shared_
                 const float mz = m == -INFINITY ? 0.0f : m;
                 const float2 zs2 = make_float2(zs, zs), mz2 = make_float2(-mz, -mz);
                 float2 ls = make_float2(0.0f, 0.0f), lrs = ls;
+                // P of the last tokens over the second half of S, whose scores are in registers, then the others'
 #pragma unroll
-                for (int k = 0; k < kTile / 32; ++k) {
-                    float z[32];
-                    tmem_ld32(s_at + k * 32, z);
-                    uint32_t w16[16];
+                for (int k = kTile - 64; k >= 0; k -= 64) {
+                    if (k < kTile - 64) tmem_ld64(s_at + k, z);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        float2 y = __ffma2_rn(make_float2(z[2 * j], z[2 * j + 1]), zs2, mz2);
-                        if (!all) {
-                            y.x = (on[k] >> (2 * j)) & 1 ? y.x : -INFINITY;
-                            y.y = (on[k] >> (2 * j + 1)) & 1 ? y.y : -INFINITY;
+                    for (int part = 0; part < 64; part += 32) {
+                        uint32_t w16[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            float2 y = __ffma2_rn(make_float2(z[part + 2 * j], z[part + 2 * j + 1]), zs2, mz2);
+                            y.x = exp2_fast(y.x);
+                            y.y = exp2_fast(y.y);
+                            ls = __fadd2_rn(ls, y);
+                            w16[j] = pack2<kF16>(y.x, y.y);
+                            lrs = __fadd2_rn(lrs, unpack2<kF16>(w16[j]));
                         }
-                        y.x = exp2_fast(y.x);
-                        y.y = exp2_fast(y.y);
-                        ls = __fadd2_rn(ls, y);
-                        w16[j] = pack2<kF16>(y.x, y.y);
-                        lrs = __fadd2_rn(lrs, unpack2<kF16>(w16[j]));
+                        tmem_st16u(s_at + kTile / 2 + (k + part) / 2, w16);
                     }
-                    tmem_st16u(s_at + k * 16, w16);   // over scores that have been read
                 }
                 l += ls.x + ls.y;
                 lr += lrs.x + lrs.y;
                 tc::wait_st();
-                // With two buffers the products of the tile before may be under way still: its phase is waited for while this
-                // tile's cannot be over, for the wait below tells neighbouring phases apart only.
-                if (S::kBuffers == 2 && ends && n > 0) role_wait(&x.odone[m_half], (n - 1) & 1, abort, p);
                 tc::fence_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&x.pready[buffer]);
-                if (ends) {
-                    // ---- the part's end ----
-                    role_wait(&x.odone[m_half], n & 1, abort, p);
-                    tc::fence_after_sync();
-                    const bool whole = began == 0 && w.tile == w.tiles - 1;
-                    const size_t slot_row = static_cast<size_t>(part_slot(worker, began == 0)) * S::kRows + m_half * 128 + row;
-                    const int at_row = i0 + m_half * 128 + row, member = at_row / G;
-                    const size_t out_row = static_cast<size_t>(w.g.first + member) * p.Hq + w.kv() * G + at_row - member * G;
-                    float* const to = whole ? p.pre_store + out_row * D : p.pre_part + slot_row * D;
-                    if (row < rows) (whole ? p.pre_store_ml[out_row] : p.pre_ml[slot_row]) = make_float4(m, m, l, lr);
+                any = true;
+                ++n;
+            }
+            // ---- the part's end ----
+            {
+                if (any) role_wait(&x.odone[kM == 2 ? stream : (n - 1) & 1], S::phase(n - 1), abort, p);
+                tc::fence_after_sync();
+                const bool whole = w.whole();
+                const int at = two ? stream * 128 + row : row, at_row = i0 + at, member = at_row / G;   // of the block, of the group
+                const size_t out_row = static_cast<size_t>(w.g.first + member) * p.Hq + w.kv() * G + at_row - member * G;
+                const size_t to_row = whole ? (two ? 0 : static_cast<size_t>(stream) * p.R * p.Hq) + out_row
+                                            : static_cast<size_t>(part_slot(worker, w.tile == 0)) * S::kRows + stream * 128 + row;
+                if (at < rows) (whole ? p.pre_store_ml : p.pre_ml)[to_row] = make_float4(m, m, l, lr);
+                if (any) {
+                    float* const to = (whole ? p.pre_store : p.pre_part) + to_row * D;
 #pragma unroll 1
                     for (int k = 0; k < D; k += 16) {
                         float v[16];
                         tc::tmem_ld16(o_at + k, v);
-                        if (row < rows)
+                        if (at < rows)
 #pragma unroll
                             for (int j = 0; j < 16; j += 4)
                                 *reinterpret_cast<float4*>(to + k + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
                     }
-                    if (tid == 0 && began == 0) {
-                        const long long last = w.g.unit0 + static_cast<long long>(w.hb + 1) * (w.tiles + kSharedRowUnits) - 1;
-                        p.pre_dir[w.g.block0 + w.hb] =
-                            whole ? make_int2(-1, 1) : make_int2(worker, share_owner(head.units, last, p.workers) - worker + 1);
-                    }
-                    tc::fence_before_sync();
                 }
-                ++n;
+                if (tid == 0 && w.tile == 0) {
+                    const long long last = w.g.unit0 + static_cast<long long>(w.hb + 1) * (w.tiles + kSharedRowUnits) - 1;
+                    const int parts = whole ? 1 : share_owner(head.units, last, p.workers) - worker + 1;
+                    p.pre_dir[w.g.block0 + w.hb] = make_int2(whole ? -1 : worker, kM == 2 && !two ? -parts : parts);
+                }
+                tc::fence_before_sync();
             }
-            begins = ends;
-            live = w.next(groups, p.Hkv, kTile);
+            more = w.next(groups, p.Hkv, kTile);
         }
     }
 
     tc::fence_before_sync();
     __syncthreads();
+    if (*abort && (warp == S::kIssuer || warp == S::kIssuer + 1)) commit_by(&x.drain, elect_lane());   // of the products that it issued
     if (warp == S::kIssuer) {
-        if (*abort) {   // products may be under way: wait for them before tensor memory goes back
-            const uint32_t lead = elect_lane();
-            commit_by(&x.drain, lead);
-            if (lead && !tc::mbar_wait(&x.drain, 0, kDefaultWaitPolls)) raise_status(p.status, QS_DEV_TEARDOWN);
-        }
+        // products may be under way: wait for them before tensor memory goes back
+        if (*abort && lane == 0 && !tc::mbar_wait(&x.drain, 0, kDefaultWaitPolls)) raise_status(p.status, QS_DEV_TEARDOWN);
         __syncwarp();
         tc::fence_after_sync();
         tc::tmem_dealloc(tmem, kAlloc);
@@ -562,7 +563,7 @@ __global__ void __launch_bounds__(SharedShape<D, kE4M3>::kThreads, 1) kv_shared_
 
 template <int D, bool kF16, bool kE4M3>
 cudaError_t launch_shared(KvAttendParams p, cudaStream_t stream) {
-    using S = SharedShape<D, kE4M3>;
+    using S = SharedShape<D>;
     constexpr int kBytes = S::kMisc + sizeof(SharedMisc);
     static_assert(kBytes <= kLatSmem, "shared memory of an SM");
     const cudaError_t e = cudaFuncSetAttribute(kv_shared_kernel<D, kF16, kE4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
