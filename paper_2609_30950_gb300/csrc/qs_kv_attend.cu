@@ -7,7 +7,7 @@ namespace qs {
 namespace kv {
 
 // The driver's call comes through the runtime: the library does not link the driver library.
-bool pool_map(CUtensorMap* map, const void* pool, int dk, long long rows) {
+bool pool_map(CUtensorMap* map, const void* pool, int dk, long long rows, int box_rows) {
     using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -22,7 +22,7 @@ bool pool_map(CUtensorMap* map, const void* pool, int dk, long long rows) {
     });
     if (!encode) return false;
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(dk), static_cast<cuuint64_t>(rows)}, strides[1] = {2ull * dk};
-    const cuuint32_t shape[2] = {64, kLatTile}, steps[2] = {1, 1};
+    const cuuint32_t shape[2] = {64, static_cast<cuuint32_t>(box_rows)}, steps[2] = {1, 1};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void*>(pool), dims, strides, shape, steps,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;

@@ -687,9 +687,9 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
     }
 }
 
-// Map of the pool as rows of dk 16-bit entries, for boxes of 64 entries x 64 rows; false if the driver has no such
+// Map of the pool as rows of dk 16-bit entries, for boxes of 64 entries x box_rows; false if the driver has no such
 // call or refuses (qs_kv_attend.cu).
-bool pool_map(CUtensorMap* map, const void* pool, int dk, long long rows);
+bool pool_map(CUtensorMap* map, const void* pool, int dk, long long rows, int box_rows);
 
 // Groups of at most 64 heads, products of 16, 32 or 64 columns; as many tiles in flight as fit beside the
 // queries, and two CTAs on an SM where the kernel is made for it.
@@ -737,7 +737,7 @@ cudaError_t launch_latent_of(const qstate_kv_cfg& c, const KvAttendParams& p, cu
     // 95.8, 92.3, then 91.9 and 92.0 us; 64 of 256 + 64 68.4, 59.8, then 58.0 and 59.7; 16 of 128 + 64 87.2, 89.0, then 75.5
     // and 89.0; at pages of 8 the first took 191 by boxes, 107 by 16 bytes).
     CUtensorMap map = {};
-    g.boxes = c.page >= kLatTile && pool_map(&map, p.k, p.dk, static_cast<long long>(c.n_pages) * c.page);
+    g.boxes = c.page >= kLatTile && pool_map(&map, p.k, p.dk, static_cast<long long>(c.n_pages) * c.page, kLatTile);
     const bool f16 = c.dtype == QSTATE_KV_F16;
     if (g.columns == 16) return f16 ? launch_latent<DV, 16, true>(p, g, map, stream) : launch_latent<DV, 16, false>(p, g, map, stream);
     if (g.columns == 32) return f16 ? launch_latent<DV, 32, true>(p, g, map, stream) : launch_latent<DV, 32, false>(p, g, map, stream);

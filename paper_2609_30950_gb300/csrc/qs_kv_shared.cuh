@@ -9,11 +9,11 @@
 // the cache's bytes, that bound it, and below that one pass over the bytes.  Both products run on the tensor cores:
 //     S [128 rows x tokens] = Q K^T     Q and K in shared memory, entries contiguous (K-major)
 //     O [128 rows x d]     += P V       P in tensor memory over S itself, V in shared memory, entries contiguous (N-major)
-//   warps 0-3, 4-7  softmax: a row each, of the block's first and second 128 rows; of a block with no second half, of its even and
+//   warps 0-3, 4-7  copy queries, softmax: a row each, of the block's first and second 128 rows; of a block with no second half, of its even and
 //                   odd tiles, which make a part each (at 256 entries there is room for one O only: warps 0-3, and two buffers of S)
 //   warps 8 and 9   issue S and O: each waits for nothing but what its next product needs, and a stream's O runs while the other one's
 //                   softmax does
-//   warps 10-13     copy queries, keys and values, 16 bytes at a time (e4m3: they turn codes into bf16 on the way, exactly: a code has
+//   warps 10-13     copy keys and values, 16 bytes at a time (e4m3: they turn codes into bf16 on the way, exactly: a code has
 //                   4 bits and its power of two is one of the type's)
 // The units of all blocks (a tile; kSharedRowUnits more for the block itself) are dealt out evenly, as the rows' are in
 // qs_kv_tiles.cuh: a block that several CTAs share leaves a part from each.
@@ -53,6 +53,7 @@ struct SharedShape {
 struct SharedMisc {
     uint64_t full[kMaxRing], free[kMaxRing], sgo[2], sready[2], pready[2], odone[2], qfull, qfree, drain;
     alignas(16) uint32_t mask[kMaskRing][4];   // tokens of a tile that are there
+    int started[4];              // tensors that each copying warp has arrived for
     uint32_t tmem;
     int abort;
 };
@@ -156,13 +157,16 @@ __device__ __forceinline__ void st_shared16(uint32_t at, uint32_t a, uint32_t b,
 }
 
 template <int D, bool kF16, bool kE4M3>
-__global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(const KvAttendParams p) {
+__global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(const KvAttendParams p, const int box_rows,
+                                                                                const __grid_constant__ CUtensorMap k_map,
+                                                                                const __grid_constant__ CUtensorMap v_map) {
     using S = SharedShape<D>;
     constexpr int kTile = S::kTile, kM = S::kM, kAlloc = 512;
     constexpr float kLog2e = 1.4426950408889634f;
     extern __shared__ __align__(1024) char smem[];
     SharedMisc& x = *reinterpret_cast<SharedMisc*>(smem + S::kMisc);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, worker = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 31, worker = blockIdx.x;
+    const int warp = __shfl_sync(kFull, tid >> 5, 0);   // the same for a warp, as the compiler can see
     const KvGroupHead* const head_at = reinterpret_cast<const KvGroupHead*>(p.groups);
     const KvGroup* const groups = reinterpret_cast<const KvGroup*>(reinterpret_cast<const char*>(p.groups) + kKvGroupHeadBytes);
     chain_enter();
@@ -173,7 +177,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
     }
     if (tid == 0) {
         for (int s = 0; s < S::kStages; ++s) {
-            tc::mbar_init(&x.full[s], S::kCopiers * (kE4M3 ? 1 : 33));
+            tc::mbar_init(&x.full[s], S::kCopiers * (kE4M3 || box_rows ? 1 : 33));
             tc::mbar_init(&x.free[s], 1);
         }
         for (int m = 0; m < 2; ++m) {
@@ -182,11 +186,16 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
             tc::mbar_init(&x.pready[m], 4);
             tc::mbar_init(&x.odone[m], 1);
         }
-        tc::mbar_init(&x.qfull, S::kCopiers * 33);
+        tc::mbar_init(&x.qfull, S::kSoftmax * 33);
         tc::mbar_init(&x.qfree, 1);
         tc::mbar_init(&x.drain, 2);
         tc::mbar_fence_init();
         x.abort = 0;
+        for (int c = 0; c < S::kCopiers; ++c) x.started[c] = 0;
+    }
+    if (!kE4M3 && box_rows && warp == S::kIssuer + 2) {
+        prefetch_map(&k_map);
+        prefetch_map(&v_map);
     }
     KvGroupHead head;
     head.groups = __ldcg(&head_at->groups);
@@ -208,6 +217,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
     const bool live = fits && head.groups > 0 && w.start(head, groups, worker, p.workers, kTile);
     // Streams have their own S, P, O and softmax warps.  They are a block's halves (`two`), or, where it has one half, the part's
     // even and odd tiles.
+    const bool fences = !kE4M3 && !box_rows;   // copies by cp.async, whose writes the product's issuer makes visible to the tensor core
     auto two_halves = [&](int rows) { return kM == 2 && rows > 128; };
     auto stream_of = [&](int t) { return kM == 2 ? t & 1 : 0; };   // of a part's tile where there is one half
 
@@ -218,126 +228,115 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
             const int t = tile * kTile + pw * S::kWarpTokens + lane;
             return lane < S::kWarpTokens && t < w.g.tokens ? __ldcg(p.table + static_cast<size_t>(w.g.owner) * p.max_pages + (t >> p.page_shift)) : -1;
         };
-        // a thread copies one of eight pieces of every block of its rows
-        auto queries = [&]() {
-            const int sg = lane & 7, h0 = w.kv() * G, i0 = w.row0(S::kRows);
-            const int rows = min(S::kRows, w.g.rows - i0);
-            for (int i = pw * 4 + (lane >> 3); i < S::kRows; i += S::kCopiers * 4) {
-                const bool in = i < rows;
-                const int at_row = i0 + i, member = in ? at_row / G : 0;
-                const uint16_t* const q = static_cast<const uint16_t*>(p.q) + (w.g.first + member) * p.q_row +
-                                          (in ? h0 + at_row - member * G : 0) * p.q_head + sg * 8;
-                uint32_t to = smem_u32(smem + (i >> 7) * S::kQTile + (i & 127) * 128 + ((sg ^ (i & 7)) << 4));
-                for (int b = 0; b < S::kBlocks; ++b, to += S::kQBlock) {
-                    if (p.q_aligned) {
-                        cp_async16(to, in ? q + b * 64 : p.q, in);
-                    } else {
-                        uint16_t v[8];
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) v[k] = in ? q[b * 64 + k] : 0;
-                        st_shared16(to, v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
-                    }
-                }
-            }
-            cp_async_arrive(&x.qfull);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&x.qfull);
-        };
-        int s = 0, phase = 0, parts = 0, used = 0, i = 0;
+        const uint32_t lead = elect_lane();
+        int s = 0, phase = 0, used = 0;
         bool ok = true, more = true;   // ok: no wait has been given up
-        while (more) {
+        while (more && ok) {
             int id = look_up(w.tile);
-            if (parts > 0) ok = ok && role_wait(&x.qfree, (parts - 1) & 1, abort, p);   // S of the part before is done
-            if (ok) {
-                queries();
-            } else {
-                cp_async_arrive(&x.qfull);
-                if (lane == 0) mbar_arrive(&x.qfull);
-            }
-            ++parts;
             const int kv_head = w.kv();
-            for (int c = 0; c < w.count; ++c, ++i) {
-            const int t = (w.tile + c) * kTile + pw * S::kWarpTokens + lane;
-            const bool wanted = lane < S::kWarpTokens && t < w.g.tokens, there = wanted && id >= 0 && id < p.n_pages;
-            if (wanted && !there) raise_status(p.status, QS_DEV_PAGES);
-            const uint32_t on = __ballot_sync(kFull, there);
-            if (lane == 0) {
-                if (S::kWarpTokens == 32)
-                    *reinterpret_cast<volatile uint32_t*>(&x.mask[i % kMaskRing][pw]) = on;
-                else
-                    reinterpret_cast<volatile uint16_t*>(x.mask[i % kMaskRing])[pw] = static_cast<uint16_t>(on);
-            }
-            const long long row = there ? ((static_cast<long long>(id) * p.Hkv + kv_head) << p.page_shift) + (t & page_mask) : 0;
-            if (c + 1 < w.count) id = look_up(w.tile + c + 1);
-#pragma unroll 1
-            for (int kv = 0; kv < 2; ++kv) {
-                const char* const pool = static_cast<const char*>(kv ? p.v : p.k);
-                const uint32_t stage = smem_u32(smem + S::kRing + s * S::kTensor);
-                if constexpr (!kE4M3) {
-                    if (used >= S::kStages) ok = ok && role_wait(&x.free[s], phase ^ 1, abort, p);
-                    const int sg = lane & 7, row0 = lane >> 3;
-                    if (ok)
-#pragma unroll
-                        for (int k = 0; k < S::kWarpTokens / 4; ++k) {
-                            const int u = k * 4 + row0;
-                            const char* const src = pool + __shfl_sync(kFull, row, u) * (2 * D) + sg * 16;
-                            const bool seen = (on >> u) & 1;
-                            const uint32_t to = stage + (pw * S::kWarpTokens + u) * 128 + ((sg ^ (u & 7)) << 4);
-#pragma unroll
-                            for (int b = 0; b < S::kBlocks; ++b) cp_async16(to + b * S::kBlock, src + b * 128, seen);
-                        }
-                    cp_async_arrive(&x.full[s]);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&x.full[s]);
-                } else {
-                    // 16 codes a lane and load, all of a tile's in flight; D / 16 lanes take a token
-                    constexpr int kLanes = D / 16, kLoads = S::kWarpTokens * kLanes / 32;
-                    const uint8_t* const exps = kv ? p.v_exp : p.k_exp;
-                    const int sg = lane % kLanes, row0 = lane / kLanes;
-                    uint4 codes[kLoads];
-                    const int power = there ? __ldcg(exps + row) : 127;
-#pragma unroll
-                    for (int k = 0; k < kLoads; ++k) {
-                        const int u = k * (32 / kLanes) + row0;
-                        const char* const src = pool + __shfl_sync(kFull, row, u) * D + sg * 16;
-                        codes[k] = (on >> u) & 1 ? __ldcg(reinterpret_cast<const uint4*>(src)) : make_uint4(0, 0, 0, 0);
-                    }
-                    if (used >= S::kStages) ok = ok && role_wait(&x.free[s], phase ^ 1, abort, p);
-#pragma unroll
-                    for (int k = 0; k < kLoads; ++k) {
-                        const int u = k * (32 / kLanes) + row0;
-                        const unsigned e = __shfl_sync(kFull, power, u);
-                        // 2^(e - 127); 0 is the type's lowest power (2^-127, not a normal number), 255 NaN
-                        const float two = e == 255 ? __uint_as_float(0x7fffffffu) : e ? __uint_as_float(e << 23) : 0x1p-127f;
-                        const uint32_t c[4] = {codes[k].x, codes[k].y, codes[k].z, codes[k].w};
-                        uint32_t y[8];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            uint32_t lo, hi;
-                            asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h;}"
-                                : "=r"(lo), "=r"(hi) : "r"(c[j]));
-                            const float2 a = unpack2<true>(lo), b = unpack2<true>(hi);
-                            y[2 * j] = pack2<false>(a.x * two, a.y * two);
-                            y[2 * j + 1] = pack2<false>(b.x * two, b.y * two);
-                        }
-                        // entries 16 sg ...: pieces 2 (sg % 4) and the next of block sg / 4
-                        const int token = pw * S::kWarpTokens + u, piece = (sg & 3) * 2;
-                        const uint32_t to = stage + (sg >> 2) * S::kBlock + token * 128;
-                        if (ok) {
-                            st_shared16(to + ((piece ^ (token & 7)) << 4), y[0], y[1], y[2], y[3]);
-                            st_shared16(to + (((piece + 1) ^ (token & 7)) << 4), y[4], y[5], y[6], y[7]);
-                        }
-                    }
-                    tc::fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&x.full[s]);
+            for (int c = 0; c < w.count && ok; ++c) {
+                const int t = (w.tile + c) * kTile + pw * S::kWarpTokens + lane;
+                const bool wanted = lane < S::kWarpTokens && t < w.g.tokens, there = wanted && id >= 0 && id < p.n_pages;
+                if (wanted && !there) raise_status(p.status, QS_DEV_PAGES);
+                const uint32_t on = __ballot_sync(kFull, there);
+                uint32_t* const mask = x.mask[(used >> 1) % kMaskRing];
+                if (lane == 0) {
+                    if (S::kWarpTokens == 32)
+                        *reinterpret_cast<volatile uint32_t*>(mask + pw) = on;
+                    else
+                        reinterpret_cast<volatile uint16_t*>(mask)[pw] = static_cast<uint16_t>(on);
                 }
-                ++used;
-                if (++s == S::kStages) s = 0, phase ^= 1;
-            }
+                const bool whole = on == (S::kWarpTokens == 32 ? kFull : (1u << (S::kWarpTokens & 31)) - 1);
+                const long long row = there ? ((static_cast<long long>(id) * p.Hkv + kv_head) << p.page_shift) + (t & page_mask) : 0;
+                if (c + 1 < w.count) id = look_up(w.tile + c + 1);
+#pragma unroll 1
+                for (int kv = 0; kv < 2 && ok; ++kv) {
+                    const char* const pool = static_cast<const char*>(kv ? p.v : p.k);
+                    const uint32_t stage = smem_u32(smem + S::kRing + s * S::kTensor) + pw * S::kWarpTokens * 128;   // the warp's tokens
+                    if constexpr (!kE4M3) {
+                        if (used >= S::kStages) ok = role_wait(&x.free[s], phase ^ 1, abort, p);
+                        if (!ok) break;
+                        if (box_rows && whole) {
+                            if (lane == 0) mbar_arrive_expect(&x.full[s], S::kWarpTokens * D * 2);
+                            __syncwarp();
+                            const uint32_t bar = smem_u32(&x.full[s]);
+                            for (int u = 0; u < S::kWarpTokens; u += box_rows) {
+                                const int at = static_cast<int>(__shfl_sync(kFull, row, u));
+#pragma unroll
+                                for (int b = 0; b < S::kBlocks; ++b)
+                                    tma_box(stage + b * S::kBlock + u * 128, kv ? &v_map : &k_map, b * 64, at, bar, lead);
+                            }
+                        } else {
+                            // 16 bytes a lane; zeros in place of what is not there
+                            const int sg = lane & 7, row0 = lane >> 3;
+#pragma unroll
+                            for (int k = 0; k < S::kWarpTokens / 4; ++k) {
+                                const int u = k * 4 + row0;
+                                const char* const src = pool + __shfl_sync(kFull, row, u) * (2 * D) + sg * 16;
+                                const bool seen = (on >> u) & 1;
+                                const uint32_t to = stage + u * 128 + ((sg ^ (u & 7)) << 4);
+#pragma unroll
+                                for (int b = 0; b < S::kBlocks; ++b) cp_async16(to + b * S::kBlock, src + b * 128, seen);
+                            }
+                            if (box_rows) {   // one arrival a warp: the ends of what is shared only
+                                cp_commit();
+                                cp_wait<0>();
+                                tc::fence_async_smem();
+                            } else {
+                                cp_async_arrive(&x.full[s]);
+                            }
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&x.full[s]);
+                        }
+                    } else {
+                        // 16 codes a lane and load, all of a tensor's in flight; D / 16 lanes take a token
+                        constexpr int kLanes = D / 16, kLoads = S::kWarpTokens * kLanes / 32;
+                        const uint8_t* const exps = kv ? p.v_exp : p.k_exp;
+                        const int sg = lane % kLanes, row0 = lane / kLanes;
+                        uint4 codes[kLoads];
+                        const int power = there ? __ldcg(exps + row) : 127;
+#pragma unroll
+                        for (int k = 0; k < kLoads; ++k) {
+                            const int u = k * (32 / kLanes) + row0;
+                            const char* const src = pool + __shfl_sync(kFull, row, u) * D + sg * 16;
+                            codes[k] = (on >> u) & 1 ? __ldcg(reinterpret_cast<const uint4*>(src)) : make_uint4(0, 0, 0, 0);
+                        }
+                        if (used >= S::kStages) ok = role_wait(&x.free[s], phase ^ 1, abort, p);
+                        if (!ok) break;
+#pragma unroll
+                        for (int k = 0; k < kLoads; ++k) {
+                            const int u = k * (32 / kLanes) + row0;
+                            const unsigned e = __shfl_sync(kFull, power, u);
+                            // 2^(e - 127); 0 is the type's lowest power (2^-127, not a normal number), 255 NaN
+                            const float two = e == 255 ? __uint_as_float(0x7fffffffu) : e ? __uint_as_float(e << 23) : 0x1p-127f;
+                            const uint32_t w4[4] = {codes[k].x, codes[k].y, codes[k].z, codes[k].w};
+                            uint32_t y[8];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                uint32_t lo, hi;
+                                asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h;}"
+                                    : "=r"(lo), "=r"(hi) : "r"(w4[j]));
+                                const float2 a = unpack2<true>(lo), b = unpack2<true>(hi);
+                                y[2 * j] = pack2<false>(a.x * two, a.y * two);
+                                y[2 * j + 1] = pack2<false>(b.x * two, b.y * two);
+                            }
+                            // entries 16 sg ...: pieces 2 (sg % 4) and the next of block sg / 4
+                            const int piece = (sg & 3) * 2;
+                            const uint32_t to = stage + (sg >> 2) * S::kBlock + u * 128;
+                            st_shared16(to + ((piece ^ (u & 7)) << 4), y[0], y[1], y[2], y[3]);
+                            st_shared16(to + (((piece + 1) ^ (u & 7)) << 4), y[4], y[5], y[6], y[7]);
+                        }
+                        tc::fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&x.full[s]);
+                    }
+                    ++used;
+                    if (++s == S::kStages) s = 0, phase ^= 1;
+                }
             }
             more = w.next(groups, p.Hkv, kTile);
         }
+        if (lane == 0) x.started[pw] = used;
         cp_commit();
         cp_wait<0>();
     } else if (live && warp == S::kIssuer) {
@@ -350,14 +349,15 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
         while (more && ok) {
             const bool two = two_halves(min(S::kRows, w.g.rows - w.row0(S::kRows)));
             ok = role_wait(&x.qfull, parts++ & 1, abort, p);
+            tc::fence_async_smem();   // the copies' writes, for the tensor core's reads
             for (int c = 0; c < w.count && ok; ++c) {
                 ok = role_wait(&x.full[s], phase, abort, p);
+                if (fences) tc::fence_async_smem();
                 for (int h = two ? 0 : stream_of(c), end = two ? 2 : h + 1; h < end && ok; ++h) {
                     const int n = h ? n1 : n0, buffer = kM == 2 ? h : n & 1;
                     if (n >= S::kBuffers) ok = role_wait(&x.odone[buffer], S::phase(n - S::kBuffers), abort, p);   // p before has been read
                     if (!ok) break;
                     if (lane == 0) mbar_arrive(&x.sgo[buffer]);   // the tile's mask is there
-                    tc::fence_async_smem();                       // the copies' writes, for the tensor core's reads
                     tc::fence_after_sync();
                     const uint32_t d = tmem + buffer * kTile, a0 = dq + (two ? h : 0) * (S::kQTile / 16), b0 = ring + s * (S::kTensor / 16);
 #pragma unroll
@@ -386,11 +386,11 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
             const bool two = two_halves(min(S::kRows, w.g.rows - w.row0(S::kRows)));
             for (int c = 0; c < w.count && ok; ++c) {
                 ok = role_wait(&x.full[s], phase, abort, p);
+                if (fences) tc::fence_async_smem();
                 for (int h = two ? 0 : stream_of(c), end = two ? 2 : h + 1; h < end && ok; ++h) {
                     const int n = h ? n1 : n0, buffer = kM == 2 ? h : n & 1;
                     ok = role_wait(&x.pready[buffer], S::phase(n), abort, p);
                     if (!ok) break;
-                    tc::fence_async_smem();
                     tc::fence_after_sync();
                     const uint32_t d = tmem + S::kOCol + h * D, a0 = tmem + buffer * kTile + kTile / 2, b0 = ring + s * (S::kTensor / 16);
                     const bool first = c < (two ? 1 : kM);   // of the stream's in this part
@@ -415,7 +415,40 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
         const float zs = fmaxf(fabsf(p.scale) * kLog2e, 0x1p-126f);
         constexpr float kAbove = kF16 ? kLazyLatent + kLiftLatent : kLazyLatent, kBelow = kLiftLatent - kFarLatent;
         float m = -INFINITY, high = -INFINITY, l = 0.0f, lr = 0.0f;   // reference, the highest so far, sums of p and of rounded p
-        int n = 0, i = 0;   // the stream's jobs, all tiles
+        // Queries of w's block, this warp's 32 rows: a lane looks up a row, eight lanes copy it.
+        auto queries = [&]() {
+            const int i0 = w.row0(S::kRows), rows = min(S::kRows, w.g.rows - i0), first = stream * 128 + (warp & 3) * 32, sg = lane & 7;
+            const bool in = first + lane < rows;
+            const int at_row = i0 + first + lane, member = in ? at_row / G : 0;
+            const uint16_t* const mine = static_cast<const uint16_t*>(p.q) + (w.g.first + member) * p.q_row +
+                                         (in ? w.kv() * G + at_row - member * G : 0) * p.q_head;
+            const uint32_t to = smem_u32(smem + stream * S::kQTile);
+            if (first < rows)
+#pragma unroll 2
+                for (int k = 0; k < 8; ++k) {
+                    const int u = k * 4 + (lane >> 3), at = (warp & 3) * 32 + u;
+                    const uint16_t* const q =
+                        reinterpret_cast<const uint16_t*>(__shfl_sync(kFull, reinterpret_cast<unsigned long long>(mine), u)) + sg * 8;
+                    const bool on = first + u < rows;
+#pragma unroll
+                    for (int b = 0; b < S::kBlocks; ++b) {
+                        const uint32_t piece = to + b * S::kQBlock + at * 128 + ((sg ^ (at & 7)) << 4);
+                        if (p.q_aligned) {
+                            cp_async16(piece, on ? q + b * 64 : p.q, on);
+                        } else {
+                            uint16_t v[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] = on ? q[b * 64 + e] : 0;
+                            st_shared16(piece, v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+                        }
+                    }
+                }
+            cp_async_arrive(&x.qfull);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&x.qfull);
+        };
+        queries();
+        int n = 0, i = 0, parts = 0;   // the stream's jobs, all tiles
         for (bool more = true; more;) {
             const int i0 = w.row0(S::kRows), rows = min(S::kRows, w.g.rows - i0);
             const bool two = two_halves(rows);
@@ -517,40 +550,65 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                 ++n;
             }
             // ---- the part's end ----
-            {
-                if (any) role_wait(&x.odone[kM == 2 ? stream : (n - 1) & 1], S::phase(n - 1), abort, p);
-                tc::fence_after_sync();
-                const bool whole = w.whole();
-                const int at = two ? stream * 128 + row : row, at_row = i0 + at, member = at_row / G;   // of the block, of the group
-                const size_t out_row = static_cast<size_t>(w.g.first + member) * p.Hq + w.kv() * G + at_row - member * G;
-                const size_t to_row = whole ? (two ? 0 : static_cast<size_t>(stream) * p.R * p.Hq) + out_row
-                                            : static_cast<size_t>(part_slot(worker, w.tile == 0)) * S::kRows + stream * 128 + row;
-                if (at < rows) (whole ? p.pre_store_ml : p.pre_ml)[to_row] = make_float4(m, m, l, lr);
-                if (any) {
-                    float* const to = (whole ? p.pre_store : p.pre_part) + to_row * D;
-#pragma unroll 1
-                    for (int k = 0; k < D; k += 16) {
-                        float v[16];
-                        tc::tmem_ld16(o_at + k, v);
-                        if (at < rows)
-#pragma unroll
-                            for (int j = 0; j < 16; j += 4)
-                                *reinterpret_cast<float4*>(to + k + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-                    }
-                }
-                if (tid == 0 && w.tile == 0) {
-                    const long long last = w.g.unit0 + static_cast<long long>(w.hb + 1) * (w.tiles + kSharedRowUnits) - 1;
-                    const int parts = whole ? 1 : share_owner(head.units, last, p.workers) - worker + 1;
-                    p.pre_dir[w.g.block0 + w.hb] = make_int2(whole ? -1 : worker, kM == 2 && !two ? -parts : parts);
-                }
-                tc::fence_before_sync();
-            }
+            const SharedPart was = w;
             more = w.next(groups, p.Hkv, kTile);
+            if (more) {
+                role_wait(&x.qfree, parts++ & 1, abort, p);   // S of this part is done with its queries
+                queries();
+            }
+            if (any) role_wait(&x.odone[kM == 2 ? stream : (n - 1) & 1], S::phase(n - 1), abort, p);
+            tc::fence_after_sync();
+            const bool whole = was.whole();
+            const int at = two ? stream * 128 + row : row, at_row = i0 + at, member = at_row / G;   // of the block, of the group
+            const size_t slot = part_slot(worker, was.tile == 0);
+            const size_t out_row = (two ? 0 : static_cast<size_t>(stream) * p.R * p.Hq) +
+                                   static_cast<size_t>(was.g.first + member) * p.Hq + was.kv() * G + at_row - member * G;
+            if (at < rows) {
+                if (whole)
+                    p.pre_store_ml[out_row] = make_float4(m, m, l, lr);
+                else
+                    p.pre_ml[slot * S::kRows + stream * 128 + row] = make_float4(m, m, l, lr);
+            }
+            if (any) {
+                // a part's sums lie column by column: 32 lanes' rows side by side
+                float4* const to = whole ? reinterpret_cast<float4*>(p.pre_store) + out_row * (D / 4)
+                                         : reinterpret_cast<float4*>(p.pre_part) + slot * (S::kRows * (D / 4)) + stream * 128 + row;
+                const int column = whole ? 1 : S::kRows;
+#pragma unroll 1
+                for (int k = 0; k < D; k += 16) {
+                    float v[16];
+                    tc::tmem_ld16(o_at + k, v);
+                    if (at < rows)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            to[(k / 4 + j) * column] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                }
+            }
+            if (tid == 0 && was.tile == 0) {
+                const long long last = was.g.unit0 + static_cast<long long>(was.hb + 1) * (was.tiles + kSharedRowUnits) - 1;
+                const int many = whole ? 1 : share_owner(head.units, last, p.workers) - worker + 1;
+                p.pre_dir[was.g.block0 + was.hb] = make_int2(whole ? -1 : worker, kM == 2 && !two ? -many : many);
+            }
+            tc::fence_before_sync();
         }
+        cp_commit();
+        cp_wait<0>();
     }
 
     tc::fence_before_sync();
     __syncthreads();
+    if (!kE4M3 && box_rows && *abort && warp > S::kIssuer + 1) {
+        // Boxes may be under way: none may land in a CTA that has gone.  A warp that gave up earlier than others arrives for
+        // the tensors that those have begun.
+        const int pw = warp - S::kIssuer - 2;
+        int most = 0;
+        for (int c = 0; c < S::kCopiers; ++c) most = max(most, x.started[c]);
+        if (lane == 0) {
+            for (int k = x.started[pw]; k < most; ++k) mbar_arrive(&x.full[k % S::kStages]);
+            for (int k = max(0, most - S::kStages); k < most; ++k) tc::mbar_wait(&x.full[k % S::kStages], (k / S::kStages) & 1, kDefaultWaitPolls);
+        }
+        __syncwarp();
+    }
     if (*abort && (warp == S::kIssuer || warp == S::kIssuer + 1)) commit_by(&x.drain, elect_lane());   // of the products that it issued
     if (warp == S::kIssuer) {
         // products may be under way: wait for them before tensor memory goes back
@@ -562,7 +620,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
 }
 
 template <int D, bool kF16, bool kE4M3>
-cudaError_t launch_shared(KvAttendParams p, cudaStream_t stream) {
+cudaError_t launch_shared(const qstate_kv_cfg& c, KvAttendParams p, cudaStream_t stream) {
     using S = SharedShape<D>;
     constexpr int kBytes = S::kMisc + sizeof(SharedMisc);
     static_assert(kBytes <= kLatSmem, "shared memory of an SM");
@@ -570,13 +628,22 @@ cudaError_t launch_shared(KvAttendParams p, cudaStream_t stream) {
     if (e != cudaSuccess) return e;
     const int sms = device_sm_count();
     p.workers = sms < kKvSms ? sms : kKvSms;
-    return launch_chained(kv_shared_kernel<D, kF16, kE4M3>, p.workers, S::kThreads, kBytes, stream, true, p);
+    // Boxes of a page's tokens, as many as a warp copies at most: whole groups of eight rows of the swizzle, and rows of the pool
+    // that 31 bits number.
+    CUtensorMap k_map = {}, v_map = {};
+    int box_rows = 0;
+    const long long rows = static_cast<long long>(c.n_pages) * c.Hkv * c.page;
+    if (!kE4M3 && c.page >= 8 && rows <= 0x7fffffffLL) {
+        box_rows = c.page < S::kWarpTokens ? c.page : S::kWarpTokens;
+        if (!pool_map(&k_map, p.k, D, rows, box_rows) || !pool_map(&v_map, p.v, D, rows, box_rows)) box_rows = 0;
+    }
+    return launch_chained(kv_shared_kernel<D, kF16, kE4M3>, p.workers, S::kThreads, kBytes, stream, true, p, box_rows, k_map, v_map);
 }
 
 template <int D>
 cudaError_t launch_shared_of(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream) {
-    if (c.store == QSTATE_KV_E4M3) return launch_shared<D, false, true>(p, stream);
-    return c.dtype == QSTATE_KV_F16 ? launch_shared<D, true, false>(p, stream) : launch_shared<D, false, false>(p, stream);
+    if (c.store == QSTATE_KV_E4M3) return launch_shared<D, false, true>(c, p, stream);
+    return c.dtype == QSTATE_KV_F16 ? launch_shared<D, true, false>(c, p, stream) : launch_shared<D, false, false>(c, p, stream);
 }
 
 }  // namespace kv
