@@ -78,9 +78,9 @@ struct KvAttendParams {
 };
 
 // Tokens of a tile, and rows (requests' heads) of a block, in the attention over tokens that requests share.
-constexpr int kv_shared_tile(int d) { return d == 256 ? 64 : 128; }
+constexpr int kSharedTile = 64;
 constexpr int kv_shared_rows(int d) { return d == 256 ? 128 : 256; }
-constexpr int kSharedRowUnits = 2;   // tiles that a block of rows costs by itself: its queries, its end
+constexpr int kSharedRowUnits = 4;   // tiles that a block of rows costs by itself: its queries, its end
 
 // What qstate_kv_group leaves behind: a head, the requests' records, the groups that share anything.
 struct KvGroupHead {

@@ -393,7 +393,7 @@ int qstate_kv_group(const qstate_kv_cfg* cfg, const int32_t* lens, int32_t R, co
     p.R = R;
     p.G = cfg->Hq / cfg->Hkv;
     p.Hkv = cfg->Hkv;
-    p.tile = kv_shared_tile(cfg->dk);
+    p.tile = kSharedTile;
     p.rows = kv_shared_rows(cfg->dk);
     p.window = cfg->window;
     p.most = static_cast<long long>(cfg->max_pages) * cfg->page;

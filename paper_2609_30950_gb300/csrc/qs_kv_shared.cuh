@@ -28,31 +28,33 @@
 namespace qs {
 namespace kv {
 
-constexpr int kMaxRing = 8, kMaskRing = 8;
+constexpr int kMaxRing = 16, kMaskRing = 16;
 
 template <int D>
 struct SharedShape {
-    static constexpr int kTile = kv_shared_tile(D), kRows = kv_shared_rows(D), kM = kRows / 128;
-    static constexpr int kBuffers = kM == 1 ? 2 : 1;                  // of S
+    static constexpr int kTile = kSharedTile, kRows = kv_shared_rows(D), kM = kRows / 128;
+    static constexpr int kBuffers = 2;                                // of S, for each stream
     static constexpr int kBlocks = D / 64;                            // of 64 entries
     static constexpr int kTensor = kTile * D * 2;                     // bytes of a tile's keys
     static constexpr int kBlock = kTile * 128;                        // and of a block of them
     static constexpr int kQBlock = 128 * 128, kQTile = kBlocks * kQBlock;
-    static constexpr int kStages = D == 64 ? 8 : 5;
+    static constexpr int kStages = D == 64 ? 16 : D == 128 ? 10 : 5;
     static constexpr int kRing = kM * kQTile, kMisc = kRing + kStages * kTensor;
     static constexpr int kSoftmax = 4 * kM, kIssuer = kSoftmax, kCopiers = 4;
     static constexpr int kThreads = (kSoftmax + 2 + kCopiers) * 32;
     // S, P and O of a stream's job n are waited for at barriers of its buffer, whose next phase needs all who wait for this one:
     // a parity tells neighbouring phases apart only.
-    static __device__ __forceinline__ int phase(int n) { return (kBuffers == 2 ? n >> 1 : n) & 1; }
+    static __device__ __forceinline__ int buffer(int stream, int n) { return stream * kBuffers + (n & 1); }
+    static __device__ __forceinline__ int phase(int n) { return (n >> 1) & 1; }
     static constexpr int kOCol = kM * kBuffers * kTile;               // columns of tensor memory in front of O
-    static_assert(kStages <= kMaxRing && kOCol + kM * D <= 512, "tensor memory");
+    static_assert(kStages <= kMaxRing && kOCol + kM * D <= 512, "barriers, tensor memory");
     static constexpr int kWarpTokens = kTile / kCopiers;
+    static_assert(kWarpTokens == 16, "16 bits of a mask");
 };
 
 struct SharedMisc {
-    uint64_t full[kMaxRing], free[kMaxRing], sgo[2], sready[2], pready[2], odone[2], qfull, qfree, drain;
-    alignas(16) uint32_t mask[kMaskRing][4];   // tokens of a tile that are there
+    uint64_t full[kMaxRing], free[kMaxRing], sready[4], pready[4], odone[4], qfull, qfree, drain;
+    alignas(8) uint32_t mask[kMaskRing][2];   // tokens of a tile that are there
     int started[4];              // tensors that each copying warp has arrived for
     uint32_t tmem;
     int abort;
@@ -156,6 +158,27 @@ __device__ __forceinline__ void st_shared16(uint32_t at, uint32_t a, uint32_t b,
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
+// A role's wait has given up, or another role's has: every role ends, without starting copies or products any more.
+static __device__ __noinline__ void give_up(volatile int* abort, int* status) {
+    if (!*abort) raise_status(status, QS_DEV_TIMEOUT);
+    *abort = 1;
+}
+// Waits for a phase of a barrier, all lanes of a warp alike, until the limit or until a role has given up.  Few instructions
+// where the phase is over: the roles' loops take turns in the instruction cache, and what they take is what they wait for
+// (80 clocks against 400 of role_wait's, in the issuing warps).
+__device__ __forceinline__ bool phase_wait(uint64_t* bar, uint32_t parity, volatile int* abort, const KvAttendParams& p) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p, q;\n.reg .u32 n, a;\nmov.u32 %0, 1;\nmov.u32 n, 0;\nWAIT:\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n@p bra DONE;\n"
+        "ld.volatile.shared.u32 a, [%3];\nadd.u32 n, n, 1;\nsetp.ge.u32 q, n, %4;\nsetp.ne.or.u32 q, a, 0, q;\n@!q bra WAIT;\n"
+        "mov.u32 %0, 0;\nDONE:\n}\n"
+        : "=&r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(smem_u32(const_cast<int*>(abort))), "r"(p.wait_polls) : "memory");
+    if (__all_sync(kFull, ok != 0)) return true;
+    give_up(abort, p.status);
+    return false;
+}
+
 template <int D, bool kF16, bool kE4M3>
 __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(const KvAttendParams p, const int box_rows,
                                                                                 const __grid_constant__ CUtensorMap k_map,
@@ -180,9 +203,8 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
             tc::mbar_init(&x.full[s], S::kCopiers * (kE4M3 || box_rows ? 1 : 33));
             tc::mbar_init(&x.free[s], 1);
         }
-        for (int m = 0; m < 2; ++m) {
-            tc::mbar_init(&x.sgo[m], 1);
-            tc::mbar_init(&x.sready[m], 1);
+        for (int m = 0; m < 4; ++m) {
+            tc::mbar_init(&x.sready[m], 2);   // the product, and its tile's mask
             tc::mbar_init(&x.pready[m], 4);
             tc::mbar_init(&x.odone[m], 1);
         }
@@ -210,11 +232,13 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
-    const uint32_t tmem = x.tmem;
+    const uint32_t tmem = __shfl_sync(kFull, x.tmem, 0);
     volatile int* const abort = &x.abort;
     const int G = p.Hq / p.Hkv;
     SharedPart w;
-    const bool live = fits && head.groups > 0 && w.start(head, groups, worker, p.workers, kTile);
+    // a limit of no polls gives up at the first wait
+    if (fits && head.groups > 0 && p.wait_polls == 0 && tid == 0) raise_status(p.status, QS_DEV_TIMEOUT);
+    const bool live = fits && head.groups > 0 && p.wait_polls > 0 && w.start(head, groups, worker, p.workers, kTile);
     // Streams have their own S, P, O and softmax warps.  They are a block's halves (`two`), or, where it has one half, the part's
     // even and odd tiles.
     const bool fences = !kE4M3 && !box_rows;   // copies by cp.async, whose writes the product's issuer makes visible to the tensor core
@@ -240,13 +264,8 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                 if (wanted && !there) raise_status(p.status, QS_DEV_PAGES);
                 const uint32_t on = __ballot_sync(kFull, there);
                 uint32_t* const mask = x.mask[(used >> 1) % kMaskRing];
-                if (lane == 0) {
-                    if (S::kWarpTokens == 32)
-                        *reinterpret_cast<volatile uint32_t*>(mask + pw) = on;
-                    else
-                        reinterpret_cast<volatile uint16_t*>(mask)[pw] = static_cast<uint16_t>(on);
-                }
-                const bool whole = on == (S::kWarpTokens == 32 ? kFull : (1u << (S::kWarpTokens & 31)) - 1);
+                if (lane == 0) reinterpret_cast<volatile uint16_t*>(mask)[pw] = static_cast<uint16_t>(on);
+                const bool whole = on == (1u << S::kWarpTokens) - 1;
                 const long long row = there ? ((static_cast<long long>(id) * p.Hkv + kv_head) << p.page_shift) + (t & page_mask) : 0;
                 if (c + 1 < w.count) id = look_up(w.tile + c + 1);
 #pragma unroll 1
@@ -254,7 +273,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                     const char* const pool = static_cast<const char*>(kv ? p.v : p.k);
                     const uint32_t stage = smem_u32(smem + S::kRing + s * S::kTensor) + pw * S::kWarpTokens * 128;   // the warp's tokens
                     if constexpr (!kE4M3) {
-                        if (used >= S::kStages) ok = role_wait(&x.free[s], phase ^ 1, abort, p);
+                        if (used >= S::kStages) ok = phase_wait(&x.free[s], phase ^ 1, abort, p);
                         if (!ok) break;
                         if (box_rows && whole) {
                             if (lane == 0) mbar_arrive_expect(&x.full[s], S::kWarpTokens * D * 2);
@@ -301,7 +320,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                             const char* const src = pool + __shfl_sync(kFull, row, u) * D + sg * 16;
                             codes[k] = (on >> u) & 1 ? __ldcg(reinterpret_cast<const uint4*>(src)) : make_uint4(0, 0, 0, 0);
                         }
-                        if (used >= S::kStages) ok = role_wait(&x.free[s], phase ^ 1, abort, p);
+                        if (used >= S::kStages) ok = phase_wait(&x.free[s], phase ^ 1, abort, p);
                         if (!ok) break;
 #pragma unroll
                         for (int k = 0; k < kLoads; ++k) {
@@ -348,23 +367,24 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
         bool ok = true, more = true;
         while (more && ok) {
             const bool two = two_halves(min(S::kRows, w.g.rows - w.row0(S::kRows)));
-            ok = role_wait(&x.qfull, parts++ & 1, abort, p);
+            ok = phase_wait(&x.qfull, parts++ & 1, abort, p);
             tc::fence_async_smem();   // the copies' writes, for the tensor core's reads
             for (int c = 0; c < w.count && ok; ++c) {
-                ok = role_wait(&x.full[s], phase, abort, p);
+                ok = phase_wait(&x.full[s], phase, abort, p);
                 if (fences) tc::fence_async_smem();
+#pragma unroll 1
                 for (int h = two ? 0 : stream_of(c), end = two ? 2 : h + 1; h < end && ok; ++h) {
-                    const int n = h ? n1 : n0, buffer = kM == 2 ? h : n & 1;
-                    if (n >= S::kBuffers) ok = role_wait(&x.odone[buffer], S::phase(n - S::kBuffers), abort, p);   // p before has been read
+                    const int n = h ? n1 : n0, buffer = S::buffer(h, n);
+                    if (n >= S::kBuffers) ok = phase_wait(&x.odone[buffer], S::phase(n - S::kBuffers), abort, p);   // p before has been read
                     if (!ok) break;
-                    if (lane == 0) mbar_arrive(&x.sgo[buffer]);   // the tile's mask is there
+                    if (lane == 0) mbar_arrive(&x.sready[buffer]);   // the tile's mask is there
                     tc::fence_after_sync();
-                    const uint32_t d = tmem + buffer * kTile, a0 = dq + (two ? h : 0) * (S::kQTile / 16), b0 = ring + s * (S::kTensor / 16);
+                    const uint32_t d = tmem + buffer * kTile;
+                    uint32_t a0 = dq + (two ? h : 0) * (S::kQTile / 16), b0 = ring + s * (S::kTensor / 16);
+#pragma unroll 1
+                    for (int b = 0; b < S::kBlocks; ++b, a0 += S::kQBlock / 16, b0 += S::kBlock / 16)
 #pragma unroll
-                    for (int b = 0; b < S::kBlocks; ++b)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            mma_f16_ss<kDescHi>(d, a0 + (b * S::kQBlock + k * 32) / 16, b0 + (b * S::kBlock + k * 32) / 16, id, b > 0 || k > 0, lead);
+                        for (int k = 0; k < 4; ++k) mma_f16_ss<kDescHi>(d, a0 + 2 * k, b0 + 2 * k, id, b > 0 || k > 0, lead);
                     commit_by(&x.sready[buffer], lead);
                     (h ? n1 : n0) = n + 1;
                 }
@@ -385,14 +405,15 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
         while (more && ok) {
             const bool two = two_halves(min(S::kRows, w.g.rows - w.row0(S::kRows)));
             for (int c = 0; c < w.count && ok; ++c) {
-                ok = role_wait(&x.full[s], phase, abort, p);
+                ok = phase_wait(&x.full[s], phase, abort, p);
                 if (fences) tc::fence_async_smem();
+#pragma unroll 1
                 for (int h = two ? 0 : stream_of(c), end = two ? 2 : h + 1; h < end && ok; ++h) {
-                    const int n = h ? n1 : n0, buffer = kM == 2 ? h : n & 1;
-                    ok = role_wait(&x.pready[buffer], S::phase(n), abort, p);
+                    const int n = h ? n1 : n0, buffer = S::buffer(h, n);
+                    ok = phase_wait(&x.pready[buffer], S::phase(n), abort, p);
                     if (!ok) break;
                     tc::fence_after_sync();
-                    const uint32_t d = tmem + S::kOCol + h * D, a0 = tmem + buffer * kTile + kTile / 2, b0 = ring + s * (S::kTensor / 16);
+                    const uint32_t d = tmem + S::kOCol + h * D, a0 = tmem + buffer * kTile, b0 = ring + s * (S::kTensor / 16);
                     const bool first = c < (two ? 1 : kM);   // of the stream's in this part
 #pragma unroll
                     for (int k = 0; k < kTile / 16; ++k) mma_f16_ts<kDescHi>(d, a0 + k * 8, b0 + k * 128, id, !first || k > 0, lead);
@@ -457,13 +478,12 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
             l = lr = 0.0f;
             for (int c = 0; c < w.count; ++c, ++i) {
                 if (!two && stream_of(c) != stream) continue;
-                const int buffer = kM == 2 ? stream : n & 1;
+                const int buffer = S::buffer(stream, n);
                 const uint32_t s_at = tlane + buffer * kTile;
-                role_wait(&x.sgo[buffer], S::phase(n), abort, p);
-                const uint4 seen = *reinterpret_cast<const uint4*>(x.mask[i % kMaskRing]);
-                role_wait(&x.sready[buffer], S::phase(n), abort, p);
+                phase_wait(&x.sready[buffer], S::phase(n), abort, p);
                 tc::fence_after_sync();
-                if ((seen.x & seen.y & (kTile > 64 ? seen.z & seen.w : kFull)) != kFull)
+                const uint2 seen = *reinterpret_cast<const uint2*>(x.mask[i % kMaskRing]);
+                if ((seen.x & seen.y) != kFull)
 #pragma unroll 1
                 for (int k = 0; k < kTile / 32; ++k) {   // scores of tokens that are not there
                     const uint32_t on = x.mask[i % kMaskRing][k];
@@ -478,20 +498,14 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                     }
                     tc::wait_st();
                 }
-                // 64 tokens at a time; the last ones stay for what follows
-                float z[64], top = -INFINITY;
+                float z[64], a = -INFINITY, b = -INFINITY;
+                tmem_ld64(s_at, z);
 #pragma unroll
-                for (int k = 0; k < kTile; k += 64) {
-                    tmem_ld64(s_at + k, z);
-                    float a = top, b = -INFINITY;
-#pragma unroll
-                    for (int j = 0; j < 64; j += 4) {
-                        a = fmaxf(fmaxf(a, z[j]), z[j + 1]);
-                        b = fmaxf(fmaxf(b, z[j + 2]), z[j + 3]);
-                    }
-                    top = fmaxf(a, b);
+                for (int j = 0; j < 64; j += 4) {
+                    a = fmaxf(fmaxf(a, z[j]), z[j + 1]);
+                    b = fmaxf(fmaxf(b, z[j + 2]), z[j + 3]);
                 }
-                top *= zs;
+                const float top = fmaxf(a, b) * zs;
                 float now = m;
                 if (kF16) {
                     if (top > m + kAbove || m == -INFINITY) now = fmaxf(m, top - kLiftLatent);
@@ -506,7 +520,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                     lr *= c;
                     m = now;
                     if (any) {
-                        role_wait(&x.odone[kM == 2 ? stream : buffer ^ 1], S::phase(n - 1), abort, p);   // the products so far are in
+                        phase_wait(&x.odone[S::buffer(stream, n - 1)], S::phase(n - 1), abort, p);   // the products so far are in
                         tc::fence_after_sync();
 #pragma unroll 1
                         for (int k = 0; k < D; k += 16) {
@@ -521,24 +535,19 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                 const float mz = m == -INFINITY ? 0.0f : m;
                 const float2 zs2 = make_float2(zs, zs), mz2 = make_float2(-mz, -mz);
                 float2 ls = make_float2(0.0f, 0.0f), lrs = ls;
-                // P of the last tokens over the second half of S, whose scores are in registers, then the others'
 #pragma unroll
-                for (int k = kTile - 64; k >= 0; k -= 64) {
-                    if (k < kTile - 64) tmem_ld64(s_at + k, z);
+                for (int k = 0; k < 64; k += 32) {
+                    uint32_t w16[16];
 #pragma unroll
-                    for (int part = 0; part < 64; part += 32) {
-                        uint32_t w16[16];
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            float2 y = __ffma2_rn(make_float2(z[part + 2 * j], z[part + 2 * j + 1]), zs2, mz2);
-                            y.x = exp2_fast(y.x);
-                            y.y = exp2_fast(y.y);
-                            ls = __fadd2_rn(ls, y);
-                            w16[j] = pack2<kF16>(y.x, y.y);
-                            lrs = __fadd2_rn(lrs, unpack2<kF16>(w16[j]));
-                        }
-                        tmem_st16u(s_at + kTile / 2 + (k + part) / 2, w16);
+                    for (int j = 0; j < 16; ++j) {
+                        float2 y = __ffma2_rn(make_float2(z[k + 2 * j], z[k + 2 * j + 1]), zs2, mz2);
+                        y.x = exp2_fast(y.x);
+                        y.y = exp2_fast(y.y);
+                        ls = __fadd2_rn(ls, y);
+                        w16[j] = pack2<kF16>(y.x, y.y);
+                        lrs = __fadd2_rn(lrs, unpack2<kF16>(w16[j]));
                     }
+                    tmem_st16u(s_at + k / 2, w16);   // over scores that are in registers
                 }
                 l += ls.x + ls.y;
                 lr += lrs.x + lrs.y;
@@ -553,10 +562,10 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
             const SharedPart was = w;
             more = w.next(groups, p.Hkv, kTile);
             if (more) {
-                role_wait(&x.qfree, parts++ & 1, abort, p);   // S of this part is done with its queries
+                phase_wait(&x.qfree, parts++ & 1, abort, p);   // S of this part is done with its queries
                 queries();
             }
-            if (any) role_wait(&x.odone[kM == 2 ? stream : (n - 1) & 1], S::phase(n - 1), abort, p);
+            if (any) phase_wait(&x.odone[S::buffer(stream, n - 1)], S::phase(n - 1), abort, p);
             tc::fence_after_sync();
             const bool whole = was.whole();
             const int at = two ? stream * 128 + row : row, at_row = i0 + at, member = at_row / G;   // of the block, of the group
