@@ -11,9 +11,9 @@
 //     O [128 rows x d]     += P V       P in tensor memory over S itself, V in shared memory, entries contiguous (N-major)
 //   warps 0-3, 4-7  copy queries, softmax: a row each, of the block's first and second 128 rows; of a block with no second half, of its even and
 //                   odd tiles, which make a part each (at 256 entries there is room for one O only: warps 0-3, and two buffers of S)
-//   warps 8 and 9   issue S and O: each waits for nothing but what its next product needs, and a stream's O runs while the other one's
-//                   softmax does
-//   warps 10-13     copy keys and values, 16 bytes at a time (e4m3: they turn codes into bf16 on the way, exactly: a code has
+//   warps 8-11      issue S and O of either stream: each waits for nothing but what its next product needs (in fewer warps, the
+//                   instructions between products, at some ten clocks each, were what everyone waited for)
+//   warps 12-15     copy keys and values, 16 bytes at a time (e4m3: they turn codes into bf16 on the way, exactly: a code has
 //                   4 bits and its power of two is one of the type's)
 // The units of all blocks (a tile; kSharedRowUnits more for the block itself) are dealt out evenly, as the rows' are in
 // qs_kv_tiles.cuh: a block that several CTAs share leaves a part from each.
@@ -40,8 +40,8 @@ struct SharedShape {
     static constexpr int kQBlock = 128 * 128, kQTile = kBlocks * kQBlock;
     static constexpr int kStages = D == 64 ? 16 : D == 128 ? 10 : 5;
     static constexpr int kRing = kM * kQTile, kMisc = kRing + kStages * kTensor;
-    static constexpr int kSoftmax = 4 * kM, kIssuer = kSoftmax, kCopiers = 4;
-    static constexpr int kThreads = (kSoftmax + 2 + kCopiers) * 32;
+    static constexpr int kSoftmax = 4 * kM, kIssuer = kSoftmax, kIssuers = 2 * kM, kCopier = kIssuer + kIssuers, kCopiers = 4;   // warps
+    static constexpr int kThreads = (kCopier + kCopiers) * 32;
     // S, P and O of a stream's job n are waited for at barriers of its buffer, whose next phase needs all who wait for this one:
     // a parity tells neighbouring phases apart only.
     static __device__ __forceinline__ int buffer(int stream, int n) { return stream * kBuffers + (n & 1); }
@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
     if (tid == 0) {
         for (int s = 0; s < S::kStages; ++s) {
             tc::mbar_init(&x.full[s], S::kCopiers * (kE4M3 || box_rows ? 1 : 33));
-            tc::mbar_init(&x.free[s], 1);
+            tc::mbar_init(&x.free[s], kM);
         }
         for (int m = 0; m < 4; ++m) {
             tc::mbar_init(&x.sready[m], 2);   // the product, and its tile's mask
@@ -209,13 +209,13 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
             tc::mbar_init(&x.odone[m], 1);
         }
         tc::mbar_init(&x.qfull, S::kSoftmax * 33);
-        tc::mbar_init(&x.qfree, 1);
-        tc::mbar_init(&x.drain, 2);
+        tc::mbar_init(&x.qfree, kM);
+        tc::mbar_init(&x.drain, S::kIssuers);
         tc::mbar_fence_init();
         x.abort = 0;
         for (int c = 0; c < S::kCopiers; ++c) x.started[c] = 0;
     }
-    if (!kE4M3 && box_rows && warp == S::kIssuer + 2) {
+    if (!kE4M3 && box_rows && warp == S::kCopier) {
         prefetch_map(&k_map);
         prefetch_map(&v_map);
     }
@@ -245,9 +245,9 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
     auto two_halves = [&](int rows) { return kM == 2 && rows > 128; };
     auto stream_of = [&](int t) { return kM == 2 ? t & 1 : 0; };   // of a part's tile where there is one half
 
-    if (live && warp > S::kIssuer + 1) {
+    if (live && warp >= S::kCopier) {
         // ---- copies ----
-        const int pw = warp - S::kIssuer - 2, page_mask = (1 << p.page_shift) - 1;
+        const int pw = warp - S::kCopier, page_mask = (1 << p.page_shift) - 1;
         auto look_up = [&](int tile) {
             const int t = tile * kTile + pw * S::kWarpTokens + lane;
             return lane < S::kWarpTokens && t < w.g.tokens ? __ldcg(p.table + static_cast<size_t>(w.g.owner) * p.max_pages + (t >> p.page_shift)) : -1;
@@ -358,73 +358,64 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
         if (lane == 0) x.started[pw] = used;
         cp_commit();
         cp_wait<0>();
-    } else if (live && warp == S::kIssuer) {
-        // ---- S ----
-        // A scale below zero is taken as S = -Q K^T (bit 13: A negated)
-        const uint32_t id = idesc_f16(kF16, 128, kTile, false) | (p.scale < 0.0f ? 1u << 13 : 0u);
-        const uint32_t lead = elect_lane(), dq = desc_lo(smem_u32(smem), 16), ring = desc_lo(smem_u32(smem + S::kRing), 16);
-        int s = 0, phase = 0, parts = 0, n0 = 0, n1 = 0;   // n: jobs of a stream that have been issued
+    } else if (live && warp >= S::kIssuer) {
+        // ---- products ----
+        const int stream = (warp - S::kIssuer) % kM;
+        const bool scores = warp < S::kIssuer + kM;
+        // S = Q K^T; a scale below zero is taken as -Q K^T (bit 13: A negated).  O += P V, B N-major.
+        const uint32_t idS = idesc_f16(kF16, 128, kTile, false) | (p.scale < 0.0f ? 1u << 13 : 0u);
+        constexpr uint32_t idO = idesc_f16(kF16, 128, D, false) | 1u << 16;
+        const uint32_t lead = elect_lane(), base = smem_u32(smem);
+        const uint32_t ring = desc_lo(base + S::kRing, scores ? 16 : S::kBlock), s_at = tmem + stream * S::kBuffers * kTile;
+        int s = scores ? 0 : 1, phase = 0, parts = 0, n = 0;   // n: jobs that have been issued
         bool ok = true, more = true;
         while (more && ok) {
             const bool two = two_halves(min(S::kRows, w.g.rows - w.row0(S::kRows)));
-            ok = phase_wait(&x.qfull, parts++ & 1, abort, p);
-            tc::fence_async_smem();   // the copies' writes, for the tensor core's reads
+            const uint32_t dq = desc_lo(base + (two ? stream * S::kQTile : 0), 16);
+            if (scores) {
+                ok = phase_wait(&x.qfull, parts++ & 1, abort, p);
+                tc::fence_async_smem();   // the copies' writes, for the tensor core's reads
+            }
+            bool first = true;
+#pragma unroll 1
             for (int c = 0; c < w.count && ok; ++c) {
                 ok = phase_wait(&x.full[s], phase, abort, p);
-                if (fences) tc::fence_async_smem();
-#pragma unroll 1
-                for (int h = two ? 0 : stream_of(c), end = two ? 2 : h + 1; h < end && ok; ++h) {
-                    const int n = h ? n1 : n0, buffer = S::buffer(h, n);
-                    if (n >= S::kBuffers) ok = phase_wait(&x.odone[buffer], S::phase(n - S::kBuffers), abort, p);   // p before has been read
-                    if (!ok) break;
-                    if (lane == 0) mbar_arrive(&x.sready[buffer]);   // the tile's mask is there
-                    tc::fence_after_sync();
-                    const uint32_t d = tmem + buffer * kTile;
-                    uint32_t a0 = dq + (two ? h : 0) * (S::kQTile / 16), b0 = ring + s * (S::kTensor / 16);
-#pragma unroll 1
-                    for (int b = 0; b < S::kBlocks; ++b, a0 += S::kQBlock / 16, b0 += S::kBlock / 16)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) mma_f16_ss<kDescHi>(d, a0 + 2 * k, b0 + 2 * k, id, b > 0 || k > 0, lead);
-                    commit_by(&x.sready[buffer], lead);
-                    (h ? n1 : n0) = n + 1;
-                }
                 if (!ok) break;
-                commit_by(&x.free[s], lead);
-                if (c == w.count - 1) commit_by(&x.qfree, lead);
+                if (fences) tc::fence_async_smem();
+                if (!two && stream_of(c) != stream) {   // the other stream's tile
+                    if (lane == 0) mbar_arrive(&x.free[s]);
+                } else {
+                    const int buffer = S::buffer(stream, n);
+                    const uint32_t buffer_at = s_at + (n & 1) * kTile, b0 = ring + s * (S::kTensor / 16);
+                    if (scores) {
+                        if (n >= S::kBuffers) ok = phase_wait(&x.odone[buffer], S::phase(n - S::kBuffers), abort, p);   // p before has been read
+                        if (!ok) break;
+                        if (lane == 0) mbar_arrive(&x.sready[buffer]);   // the tile's mask is there
+                        tc::fence_after_sync();
+#pragma unroll
+                        for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                mma_f16_ss<kDescHi>(buffer_at, dq + (b * S::kQBlock + k * 32) / 16, b0 + (b * S::kBlock + k * 32) / 16, idS,
+                                                    b > 0 || k > 0, lead);
+                        commit_by(&x.sready[buffer], lead);
+                    } else {
+                        ok = phase_wait(&x.pready[buffer], S::phase(n), abort, p);
+                        if (!ok) break;
+                        tc::fence_after_sync();
+#pragma unroll
+                        for (int k = 0; k < kTile / 16; ++k)
+                            mma_f16_ts<kDescHi>(tmem + S::kOCol + stream * D, buffer_at + k * 8, b0 + k * 128, idO, !first || k > 0, lead);
+                        commit_by(&x.odone[buffer], lead);
+                        first = false;
+                    }
+                    commit_by(&x.free[s], lead);
+                    ++n;
+                }
                 s += 2;
                 if (s >= S::kStages) s -= S::kStages, phase ^= 1;
             }
-            more = w.next(groups, p.Hkv, kTile);
-        }
-    } else if (live && warp == S::kIssuer + 1) {
-        // ---- O ----
-        constexpr uint32_t id = idesc_f16(kF16, 128, D, false) | 1u << 16;   // B N-major
-        const uint32_t lead = elect_lane(), ring = desc_lo(smem_u32(smem + S::kRing), S::kBlock);
-        int s = 1, phase = 0, n0 = 0, n1 = 0;
-        bool ok = true, more = true;
-        while (more && ok) {
-            const bool two = two_halves(min(S::kRows, w.g.rows - w.row0(S::kRows)));
-            for (int c = 0; c < w.count && ok; ++c) {
-                ok = phase_wait(&x.full[s], phase, abort, p);
-                if (fences) tc::fence_async_smem();
-#pragma unroll 1
-                for (int h = two ? 0 : stream_of(c), end = two ? 2 : h + 1; h < end && ok; ++h) {
-                    const int n = h ? n1 : n0, buffer = S::buffer(h, n);
-                    ok = phase_wait(&x.pready[buffer], S::phase(n), abort, p);
-                    if (!ok) break;
-                    tc::fence_after_sync();
-                    const uint32_t d = tmem + S::kOCol + h * D, a0 = tmem + buffer * kTile, b0 = ring + s * (S::kTensor / 16);
-                    const bool first = c < (two ? 1 : kM);   // of the stream's in this part
-#pragma unroll
-                    for (int k = 0; k < kTile / 16; ++k) mma_f16_ts<kDescHi>(d, a0 + k * 8, b0 + k * 128, id, !first || k > 0, lead);
-                    commit_by(&x.odone[buffer], lead);
-                    (h ? n1 : n0) = n + 1;
-                }
-                if (!ok) break;
-                commit_by(&x.free[s], lead);
-                s += 2;
-                if (s >= S::kStages) s -= S::kStages, phase ^= 1;
-            }
+            if (scores && ok) commit_by(&x.qfree, lead);
             more = w.next(groups, p.Hkv, kTile);
         }
     } else if (live && warp < S::kSoftmax) {
@@ -606,10 +597,10 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
 
     tc::fence_before_sync();
     __syncthreads();
-    if (!kE4M3 && box_rows && *abort && warp > S::kIssuer + 1) {
+    if (!kE4M3 && box_rows && *abort && warp >= S::kCopier) {
         // Boxes may be under way: none may land in a CTA that has gone.  A warp that gave up earlier than others arrives for
         // the tensors that those have begun.
-        const int pw = warp - S::kIssuer - 2;
+        const int pw = warp - S::kCopier;
         int most = 0;
         for (int c = 0; c < S::kCopiers; ++c) most = max(most, x.started[c]);
         if (lane == 0) {
@@ -618,7 +609,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
         }
         __syncwarp();
     }
-    if (*abort && (warp == S::kIssuer || warp == S::kIssuer + 1)) commit_by(&x.drain, elect_lane());   // of the products that it issued
+    if (*abort && warp >= S::kIssuer && warp < S::kCopier) commit_by(&x.drain, elect_lane());   // of the products that it issued
     if (warp == S::kIssuer) {
         // products may be under way: wait for them before tensor memory goes back
         if (*abort && lane == 0 && !tc::mbar_wait(&x.drain, 0, kDefaultWaitPolls)) raise_status(p.status, QS_DEV_TEARDOWN);
