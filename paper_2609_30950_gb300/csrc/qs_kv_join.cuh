@@ -3,8 +3,8 @@
 // o = sum_parts 2^{m - M} sums / sum_parts 2^{m - M} l over the parts of both, each one unsplit row in a store or a run of
 // slots in the order of the tokens.  A CTA takes eight rows (requests and query heads of one key head, as they lie in a block
 // of rows), a warp 32 columns of them: the parts of shared tokens lie column by column, as the tensor memory's lanes
-// write them, so that eight rows are a line.  Where there are few rows and so many parts of each, four warps share the parts
-// out and join in shared memory.  A row is read once and o written once: a chain of latencies (lengths and records, where
+// write them, so that eight rows are a line.  Where there are few rows and so many parts of each, two to eight warps share the
+// parts out and join in shared memory.  A row is read once and o written once: a chain of latencies (lengths and records, where
 // the parts are, the parts, four at a time).
 #pragma once
 
@@ -32,11 +32,14 @@ struct PartList {
     }
 };
 
-constexpr int kJoinRows = 8, kJoinShares = 4, kJoinBatch = 4;   // rows of a CTA, warps that share a row's parts, parts in flight
+constexpr int kJoinRows = 8, kJoinBatch = 4;   // rows of a CTA, parts in flight
+// Warps that share a row's parts: 512 threads at most, which leave them their registers.
+template <int D>
+__host__ __device__ constexpr int join_shares() { return D == 64 ? 8 : D == 128 ? 4 : 2; }
 
 template <int D, bool kF16, bool kMany>
-__global__ void __launch_bounds__(D* (kMany ? kJoinShares : 1)) kv_join_shared_kernel(const KvAttendParams p, const JoinGeo g) {
-    constexpr int kColumns = D / 32, kShares = kMany ? kJoinShares : 1, kRows = kv_shared_rows(D);
+__global__ void __launch_bounds__(D * (kMany ? join_shares<D>() : 1)) kv_join_shared_kernel(const KvAttendParams p, const JoinGeo g) {
+    constexpr int kColumns = D / 32, kShares = kMany ? join_shares<D>() : 1, kRows = kv_shared_rows(D);
     __shared__ float4 s_ml[kShares][kJoinRows], s_acc[kMany ? kShares : 1][kMany ? kJoinRows : 1][D / 4];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = warp / kColumns;
     chain_wait();
@@ -146,7 +149,7 @@ cudaError_t launch_join_shared(const KvAttendParams& p, const JoinGeo& g, cudaSt
     const int items = (p.R * g.G + kJoinRows - 1) / kJoinRows * p.Hkv;
     // rows of half the SMs and fewer: a block's have a part from many SMs
     if (items < 2 * device_sm_count())
-        return launch_chained(kv_join_shared_kernel<D, kF16, true>, items, D * kJoinShares, 0, stream, true, p, g);
+        return launch_chained(kv_join_shared_kernel<D, kF16, true>, items, D * join_shares<D>(), 0, stream, true, p, g);
     return launch_chained(kv_join_shared_kernel<D, kF16, false>, items, D, 0, stream, true, p, g);
 }
 

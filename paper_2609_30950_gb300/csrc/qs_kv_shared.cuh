@@ -38,7 +38,8 @@ struct SharedShape {
     static constexpr int kTensor = kTile * D * 2;                     // bytes of a tile's keys
     static constexpr int kBlock = kTile * 128;                        // and of a block of them
     static constexpr int kQBlock = 128 * 128, kQTile = kBlocks * kQBlock;
-    static constexpr int kStages = D == 64 ? 16 : D == 128 ? 10 : 5;
+    // of the ring, keys' and values' tensors in turn; a multiple of the copying warps, so that a slot is always one warp's
+    static constexpr int kStages = D == 64 ? 16 : D == 128 ? 8 : 4;
     static constexpr int kRing = kM * kQTile, kMisc = kRing + kStages * kTensor;
     static constexpr int kSoftmax = 4 * kM, kIssuer = kSoftmax, kIssuers = 2 * kM, kCopier = kIssuer + kIssuers, kCopiers = 4;   // warps
     static constexpr int kThreads = (kCopier + kCopiers) * 32;
@@ -48,14 +49,12 @@ struct SharedShape {
     static __device__ __forceinline__ int phase(int n) { return (n >> 1) & 1; }
     static constexpr int kOCol = kM * kBuffers * kTile;               // columns of tensor memory in front of O
     static_assert(kStages <= kMaxRing && kOCol + kM * D <= 512, "barriers, tensor memory");
-    static constexpr int kWarpTokens = kTile / kCopiers;
-    static_assert(kWarpTokens == 16, "16 bits of a mask");
+    static_assert(kTile == 64 && kCopiers == 4 && kStages % kCopiers == 0, "a lane's two tokens, a copying warp's tensors");
 };
 
 struct SharedMisc {
     uint64_t full[kMaxRing], free[kMaxRing], sready[4], pready[4], odone[4], qfull, qfree, drain;
     alignas(8) uint32_t mask[kMaskRing][2];   // tokens of a tile that are there
-    int started[4];              // tensors that each copying warp has arrived for
     uint32_t tmem;
     int abort;
 };
@@ -200,7 +199,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
     }
     if (tid == 0) {
         for (int s = 0; s < S::kStages; ++s) {
-            tc::mbar_init(&x.full[s], S::kCopiers * (kE4M3 || box_rows ? 1 : 33));
+            tc::mbar_init(&x.full[s], kE4M3 || box_rows ? 1 : 33);
             tc::mbar_init(&x.free[s], kM);
         }
         for (int m = 0; m < 4; ++m) {
@@ -213,7 +212,6 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
         tc::mbar_init(&x.drain, S::kIssuers);
         tc::mbar_fence_init();
         x.abort = 0;
-        for (int c = 0; c < S::kCopiers; ++c) x.started[c] = 0;
     }
     if (!kE4M3 && box_rows && warp == S::kCopier) {
         prefetch_map(&k_map);
@@ -236,6 +234,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
     volatile int* const abort = &x.abort;
     const int G = p.Hq / p.Hkv;
     SharedPart w;
+    int copied = 0;   // tensors that this warp has begun to copy
     // a limit of no polls gives up at the first wait
     if (fits && head.groups > 0 && p.wait_polls == 0 && tid == 0) raise_status(p.status, QS_DEV_TIMEOUT);
     const bool live = fits && head.groups > 0 && p.wait_polls > 0 && w.start(head, groups, worker, p.workers, kTile);
@@ -247,85 +246,114 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
 
     if (live && warp >= S::kCopier) {
         // ---- copies ----
+        // A warp copies the keys or the values of every other tile; lanes look up two tokens each.
         const int pw = warp - S::kCopier, page_mask = (1 << p.page_shift) - 1;
-        auto look_up = [&](int tile) {
-            const int t = tile * kTile + pw * S::kWarpTokens + lane;
-            return lane < S::kWarpTokens && t < w.g.tokens ? __ldcg(p.table + static_cast<size_t>(w.g.owner) * p.max_pages + (t >> p.page_shift)) : -1;
-        };
+        const bool values = pw & 1;
+        const char* const pool = static_cast<const char*>(values ? p.v : p.k);
+        const uint8_t* const exps = values ? p.v_exp : p.k_exp;
         const uint32_t lead = elect_lane();
-        int s = 0, phase = 0, used = 0;
-        bool ok = true, more = true;   // ok: no wait has been given up
+        int s = pw, phase = 0, i = 0;   // i: tiles of the worker
+        bool ok = true, more = true;    // ok: no wait has been given up
         while (more && ok) {
-            int id = look_up(w.tile);
             const int kv_head = w.kv();
-            for (int c = 0; c < w.count && ok; ++c) {
-                const int t = (w.tile + c) * kTile + pw * S::kWarpTokens + lane;
-                const bool wanted = lane < S::kWarpTokens && t < w.g.tokens, there = wanted && id >= 0 && id < p.n_pages;
-                if (wanted && !there) raise_status(p.status, QS_DEV_PAGES);
-                const uint32_t on = __ballot_sync(kFull, there);
-                uint32_t* const mask = x.mask[(used >> 1) % kMaskRing];
-                if (lane == 0) reinterpret_cast<volatile uint16_t*>(mask)[pw] = static_cast<uint16_t>(on);
-                const bool whole = on == (1u << S::kWarpTokens) - 1;
-                const long long row = there ? ((static_cast<long long>(id) * p.Hkv + kv_head) << p.page_shift) + (t & page_mask) : 0;
-                if (c + 1 < w.count) id = look_up(w.tile + c + 1);
+            const int32_t* const pages = p.table + static_cast<size_t>(w.g.owner) * p.max_pages;
+            int id[2];
+            auto look_up = [&](int tile) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int t = tile * kTile + k * 32 + lane;
+                    id[k] = t < w.g.tokens ? __ldcg(pages + (t >> p.page_shift)) : -1;
+                }
+            };
+            int c = (i & 1) == pw >> 1 ? 0 : 1;   // the first tile that is this warp's
+            if (c < w.count) look_up(w.tile + c);
+            for (; c < w.count && ok; c += 2) {
+                uint32_t on[2];
+                long long row[2];   // of the pool
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int t = (w.tile + c) * kTile + k * 32 + lane;
+                    const bool wanted = t < w.g.tokens, there = wanted && id[k] >= 0 && id[k] < p.n_pages;
+                    if (wanted && !there) raise_status(p.status, QS_DEV_PAGES);
+                    on[k] = __ballot_sync(kFull, there);
+                    row[k] = there ? ((static_cast<long long>(id[k]) * p.Hkv + kv_head) << p.page_shift) + (t & page_mask) : 0;
+                }
+                if (c + 2 < w.count) look_up(w.tile + c + 2);
+                if (!values && lane == 0) {
+                    volatile uint32_t* const mask = x.mask[(i + c) % kMaskRing];
+                    mask[0] = on[0];
+                    mask[1] = on[1];
+                }
+                const uint32_t stage = smem_u32(smem + S::kRing + s * S::kTensor);
+                const bool whole = (on[0] & on[1]) == kFull;
+                if constexpr (!kE4M3) {
+                    if (copied * S::kCopiers >= S::kStages) ok = phase_wait(&x.free[s], phase ^ 1, abort, p);
+                    if (!ok) break;
+                    if (box_rows && whole) {
+                        if (lane == 0) mbar_arrive_expect(&x.full[s], S::kTensor);
+                        __syncwarp();
+                        const uint32_t bar = smem_u32(&x.full[s]);
+                        const CUtensorMap* const map = values ? &v_map : &k_map;
 #pragma unroll 1
-                for (int kv = 0; kv < 2 && ok; ++kv) {
-                    const char* const pool = static_cast<const char*>(kv ? p.v : p.k);
-                    const uint32_t stage = smem_u32(smem + S::kRing + s * S::kTensor) + pw * S::kWarpTokens * 128;   // the warp's tokens
-                    if constexpr (!kE4M3) {
-                        if (used >= S::kStages) ok = phase_wait(&x.free[s], phase ^ 1, abort, p);
-                        if (!ok) break;
-                        if (box_rows && whole) {
-                            if (lane == 0) mbar_arrive_expect(&x.full[s], S::kWarpTokens * D * 2);
-                            __syncwarp();
-                            const uint32_t bar = smem_u32(&x.full[s]);
-                            for (int u = 0; u < S::kWarpTokens; u += box_rows) {
-                                const int at = static_cast<int>(__shfl_sync(kFull, row, u));
+                        for (int u = 0; u < kTile; u += box_rows) {
+                            const int at = __shfl_sync(kFull, static_cast<int>(u < 32 ? row[0] : row[1]), u & 31);
+#pragma unroll 1
+                            for (int b = 0; b < S::kBlocks; ++b) tma_box(stage + b * S::kBlock + u * 128, map, b * 64, at, bar, lead);
+                        }
+                    } else {
+                        // 16 bytes a lane; zeros in place of what is not there
+                        const int sg = lane & 7, row0 = lane >> 3;
 #pragma unroll
-                                for (int b = 0; b < S::kBlocks; ++b)
-                                    tma_box(stage + b * S::kBlock + u * 128, kv ? &v_map : &k_map, b * 64, at, bar, lead);
-                            }
-                        } else {
-                            // 16 bytes a lane; zeros in place of what is not there
-                            const int sg = lane & 7, row0 = lane >> 3;
-#pragma unroll
-                            for (int k = 0; k < S::kWarpTokens / 4; ++k) {
+                        for (int half = 0; half < 2; ++half)
+#pragma unroll 4
+                            for (int k = 0; k < 8; ++k) {
                                 const int u = k * 4 + row0;
-                                const char* const src = pool + __shfl_sync(kFull, row, u) * (2 * D) + sg * 16;
-                                const bool seen = (on >> u) & 1;
-                                const uint32_t to = stage + u * 128 + ((sg ^ (u & 7)) << 4);
+                                const char* const src = pool + __shfl_sync(kFull, row[half], u) * (2 * D) + sg * 16;
+                                const bool seen = (on[half] >> u) & 1;
+                                const uint32_t to = stage + (half * 32 + u) * 128 + ((sg ^ (u & 7)) << 4);
 #pragma unroll
                                 for (int b = 0; b < S::kBlocks; ++b) cp_async16(to + b * S::kBlock, src + b * 128, seen);
                             }
-                            if (box_rows) {   // one arrival a warp: the ends of what is shared only
-                                cp_commit();
-                                cp_wait<0>();
-                                tc::fence_async_smem();
-                            } else {
-                                cp_async_arrive(&x.full[s]);
-                            }
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(&x.full[s]);
+                        if (box_rows) {   // the ends of what is shared only
+                            cp_commit();
+                            cp_wait<0>();
+                            tc::fence_async_smem();
+                        } else {
+                            cp_async_arrive(&x.full[s]);
                         }
-                    } else {
-                        // 16 codes a lane and load, all of a tensor's in flight; D / 16 lanes take a token
-                        constexpr int kLanes = D / 16, kLoads = S::kWarpTokens * kLanes / 32;
-                        const uint8_t* const exps = kv ? p.v_exp : p.k_exp;
-                        const int sg = lane % kLanes, row0 = lane / kLanes;
-                        uint4 codes[kLoads];
-                        const int power = there ? __ldcg(exps + row) : 127;
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&x.full[s]);
+                    }
+                } else {
+                    // 16 codes a lane and load, a few tokens' in flight while those before are converted; D / 16 lanes take a token
+                    constexpr int kLanes = D / 16, kTokens = 32 / kLanes, kLoads = 4, kSteps = kTile / (kTokens * kLoads);
+                    const int sg = lane % kLanes, row0 = lane / kLanes;
+                    int power[2];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) power[k] = (on[k] >> lane) & 1 ? __ldcg(exps + row[k]) : 127;
+                    uint4 codes[kLoads], ahead[kLoads];
+                    auto load = [&](int step, uint4 (&to)[kLoads]) {
 #pragma unroll
                         for (int k = 0; k < kLoads; ++k) {
-                            const int u = k * (32 / kLanes) + row0;
-                            const char* const src = pool + __shfl_sync(kFull, row, u) * D + sg * 16;
-                            codes[k] = (on >> u) & 1 ? __ldcg(reinterpret_cast<const uint4*>(src)) : make_uint4(0, 0, 0, 0);
+                            const int u = (step * kLoads + k) * kTokens + row0;
+                            const long long a = __shfl_sync(kFull, row[0], u & 31), b = __shfl_sync(kFull, row[1], u & 31);
+                            const bool seen = ((u < 32 ? on[0] : on[1]) >> (u & 31)) & 1;
+                            const char* const src = pool + (u < 32 ? a : b) * D + sg * 16;
+                            to[k] = seen ? __ldcg(reinterpret_cast<const uint4*>(src)) : make_uint4(0, 0, 0, 0);
                         }
-                        if (used >= S::kStages) ok = phase_wait(&x.free[s], phase ^ 1, abort, p);
-                        if (!ok) break;
+                    };
+                    load(0, ahead);
+                    if (copied * S::kCopiers >= S::kStages) ok = phase_wait(&x.free[s], phase ^ 1, abort, p);
+                    if (!ok) break;
+#pragma unroll 1
+                    for (int step = 0; step < kSteps; ++step) {
+#pragma unroll
+                        for (int k = 0; k < kLoads; ++k) codes[k] = ahead[k];
+                        if (step + 1 < kSteps) load(step + 1, ahead);
 #pragma unroll
                         for (int k = 0; k < kLoads; ++k) {
-                            const int u = k * (32 / kLanes) + row0;
-                            const unsigned e = __shfl_sync(kFull, power, u);
+                            const int u = (step * kLoads + k) * kTokens + row0;
+                            const unsigned e0 = __shfl_sync(kFull, power[0], u & 31), e1 = __shfl_sync(kFull, power[1], u & 31), e = u < 32 ? e0 : e1;
                             // 2^(e - 127); 0 is the type's lowest power (2^-127, not a normal number), 255 NaN
                             const float two = e == 255 ? __uint_as_float(0x7fffffffu) : e ? __uint_as_float(e << 23) : 0x1p-127f;
                             const uint32_t w4[4] = {codes[k].x, codes[k].y, codes[k].z, codes[k].w};
@@ -335,9 +363,10 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                                 uint32_t lo, hi;
                                 asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h;}"
                                     : "=r"(lo), "=r"(hi) : "r"(w4[j]));
-                                const float2 a = unpack2<true>(lo), b = unpack2<true>(hi);
-                                y[2 * j] = pack2<false>(a.x * two, a.y * two);
-                                y[2 * j + 1] = pack2<false>(b.x * two, b.y * two);
+                                const float2 a = __fmul2_rn(unpack2<true>(lo), make_float2(two, two));
+                                const float2 b = __fmul2_rn(unpack2<true>(hi), make_float2(two, two));
+                                y[2 * j] = pack2<false>(a.x, a.y);
+                                y[2 * j + 1] = pack2<false>(b.x, b.y);
                             }
                             // entries 16 sg ...: pieces 2 (sg % 4) and the next of block sg / 4
                             const int piece = (sg & 3) * 2;
@@ -345,17 +374,18 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                             st_shared16(to + ((piece ^ (u & 7)) << 4), y[0], y[1], y[2], y[3]);
                             st_shared16(to + (((piece + 1) ^ (u & 7)) << 4), y[4], y[5], y[6], y[7]);
                         }
-                        tc::fence_async_smem();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&x.full[s]);
                     }
-                    ++used;
-                    if (++s == S::kStages) s = 0, phase ^= 1;
+                    tc::fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&x.full[s]);
                 }
+                ++copied;
+                s += S::kCopiers;
+                if (s >= S::kStages) s -= S::kStages, phase ^= 1;
             }
+            i += w.count;
             more = w.next(groups, p.Hkv, kTile);
         }
-        if (lane == 0) x.started[pw] = used;
         cp_commit();
         cp_wait<0>();
     } else if (live && warp >= S::kIssuer) {
@@ -597,18 +627,13 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
 
     tc::fence_before_sync();
     __syncthreads();
-    if (!kE4M3 && box_rows && *abort && warp >= S::kCopier) {
-        // Boxes may be under way: none may land in a CTA that has gone.  A warp that gave up earlier than others arrives for
-        // the tensors that those have begun.
-        const int pw = warp - S::kCopier;
-        int most = 0;
-        for (int c = 0; c < S::kCopiers; ++c) most = max(most, x.started[c]);
-        if (lane == 0) {
-            for (int k = x.started[pw]; k < most; ++k) mbar_arrive(&x.full[k % S::kStages]);
-            for (int k = max(0, most - S::kStages); k < most; ++k) tc::mbar_wait(&x.full[k % S::kStages], (k / S::kStages) & 1, kDefaultWaitPolls);
-        }
-        __syncwarp();
+    if (!kE4M3 && box_rows && *abort && warp >= S::kCopier && lane == 0) {
+        // boxes may be under way: none may land in a CTA that has gone
+        constexpr int kOwn = S::kStages / S::kCopiers;
+        for (int k = max(0, copied - kOwn); k < copied; ++k)
+            tc::mbar_wait(&x.full[warp - S::kCopier + k % kOwn * S::kCopiers], (k / kOwn) & 1, kDefaultWaitPolls);
     }
+    __syncwarp();
     if (*abort && warp >= S::kIssuer && warp < S::kCopier) commit_by(&x.drain, elect_lane());   // of the products that it issued
     if (warp == S::kIssuer) {
         // products may be under way: wait for them before tensor memory goes back
@@ -628,13 +653,13 @@ cudaError_t launch_shared(const qstate_kv_cfg& c, KvAttendParams p, cudaStream_t
     if (e != cudaSuccess) return e;
     const int sms = device_sm_count();
     p.workers = sms < kKvSms ? sms : kKvSms;
-    // Boxes of a page's tokens, as many as a warp copies at most: whole groups of eight rows of the swizzle, and rows of the pool
+    // Boxes of a page's tokens, a tile's at most: whole groups of eight rows of the swizzle, and rows of the pool
     // that 31 bits number.
     CUtensorMap k_map = {}, v_map = {};
     int box_rows = 0;
     const long long rows = static_cast<long long>(c.n_pages) * c.Hkv * c.page;
     if (!kE4M3 && c.page >= 8 && rows <= 0x7fffffffLL) {
-        box_rows = c.page < S::kWarpTokens ? c.page : S::kWarpTokens;
+        box_rows = c.page < S::kTile ? c.page : S::kTile;
         if (!pool_map(&k_map, p.k, D, rows, box_rows) || !pool_map(&v_map, p.v, D, rows, box_rows)) box_rows = 0;
     }
     return launch_chained(kv_shared_kernel<D, kF16, kE4M3>, p.workers, S::kThreads, kBytes, stream, true, p, box_rows, k_map, v_map);
