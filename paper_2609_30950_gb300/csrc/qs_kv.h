@@ -132,7 +132,7 @@ struct KvForkParams {
     int* status;
 };
 
-constexpr int kCompactSpan = 32768;   // pages that a CTA ranks
+constexpr int kCompactSpan = 8192;   // pages that a CTA ranks at a time
 struct KvCompactParams {
     qstate_kv_pages pages;
     qstate_kv_moves moves;
@@ -141,6 +141,7 @@ struct KvCompactParams {
     int32_t* left;
     int R, limit, page_shift, n_pages, max_pages;
     int parts, chunk;
+    int words;               // set by launch_kv_compact: words of bits that a thread ranks, one after another
     int* head;               // work space: pages that move
     uint32_t* used;          // a bit for each page; zeros between calls
     int2* spans;
@@ -173,7 +174,7 @@ cudaError_t launch_kv_shared_128(const qstate_kv_cfg& c, const KvAttendParams& p
 cudaError_t launch_kv_shared_256(const qstate_kv_cfg& c, const KvAttendParams& p, cudaStream_t stream);
 cudaError_t launch_kv_group(const KvGroupParams& p, cudaStream_t stream);
 cudaError_t launch_kv_fork(const KvForkParams& p, cudaStream_t stream);
-cudaError_t launch_kv_compact(const KvCompactParams& p, cudaStream_t stream);
+cudaError_t launch_kv_compact(KvCompactParams p, cudaStream_t stream);
 cudaError_t launch_kv_copy(KvCopyParams p, cudaStream_t stream);
 int kv_column_parts(int R, int max_pages);
 // partial results that an attention launch may use: bytes of sums, of references and weights, of the list of

@@ -4,16 +4,18 @@
 // ascending order; the i-th source moves to the i-th place for i < k = min(sources, places, moves that the caller has
 // room for).  The free list becomes the places that are left, the lowest on top.
 // Four steps, each of which needs all of the one before: a bit for each page that a table holds; sources and places of each
-// span of 32768 pages, counted; their ranks (a sum over the spans before, a prefix sum over the span's words), moves and
+// span of pages, counted; their ranks (a sum over the spans before, a prefix sum over the span's words), moves and
 // list; the tables.  Memory is read once (tables twice) and little of it: a chain of four launches' latencies.
+// A span is 8192 pages, a word of bits a thread (more where the pool would have over 2048 spans, whose sums every CTA reads):
+// 132000 pages, COMPACT_LARGE us; by spans of 32768, a thread's pages one after another, 46.
 #include "qs_common.cuh"
 #include "qs_kv.h"
 
 namespace qs {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32, kWordsPer = kCompactSpan / 32 / kThreads;
-static_assert(kWordsPer * 32 * kThreads == kCompactSpan, "a thread's words of a span");
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+static_assert(32 * kThreads == kCompactSpan, "a word a thread");
 
 __device__ __forceinline__ int held_pages(const KvCompactParams& p, int r, bool report) {
     const int n = __ldcg(p.pages.lens + r);
@@ -42,8 +44,7 @@ __global__ void __launch_bounds__(kThreads) kv_compact_mark_kernel(const KvCompa
             raise_status(p.status, QS_DEV_PAGES);
             return;
         }
-        const uint32_t bit = 1u << (x & 31);
-        if (!(__ldcg(p.used + (x >> 5)) & bit)) atomicOr(p.used + (x >> 5), bit);   // pages held together come many times
+        atomicOr(p.used + (x >> 5), 1u << (x & 31));   // nothing waits for it
     });
 }
 
@@ -65,9 +66,8 @@ __global__ void __launch_bounds__(kThreads) kv_compact_count_kernel(const KvComp
     __shared__ int2 sums[kWarps];
     chain_wait();
     int2 n = make_int2(0, 0);
-#pragma unroll
-    for (int k = 0; k < kWordsPer; ++k) {
-        const int w = (blockIdx.x * kWordsPer + k) * kThreads + threadIdx.x;
+    for (int k = 0; k < p.words; ++k) {
+        const int w = (blockIdx.x * p.words + k) * kThreads + threadIdx.x;
         const uint32_t all = in_pool(p, w), low = below_limit(p, w);
         const uint32_t used = all ? __ldcg(p.used + w) : 0u;
         n.x += __popc(used & all & ~low);
@@ -105,54 +105,53 @@ __global__ void __launch_bounds__(kThreads) kv_compact_move_kernel(const KvCompa
         before.x += sums[0][w].x, before.y += sums[0][w].y;
         all.x += sums[1][w].x, all.y += sums[1][w].y;
     }
-    __syncthreads();
     const int moved = min(min(all.x, all.y), p.moves.n), left = all.y - moved;
-    if (blockIdx.x == 0) {
-        if (tid == 0) {
-            p.pages.free_out[0] = left;
-            if (p.left) p.left[0] = all.x - moved;
-            p.head[0] = moved;
+    if (blockIdx.x == 0 && tid == 0) {
+        p.pages.free_out[0] = left;
+        if (p.left) p.left[0] = all.x - moved;
+        p.head[0] = moved;
+    }
+    for (int i = moved + blockIdx.x * kThreads + tid; i < p.moves.n; i += gridDim.x * kThreads) p.moves.src[i] = p.moves.dst[i] = -1;
+    int i0 = before.x, j0 = before.y;   // ranks of the next words' first source and place
+    for (int k = 0; k < p.words; ++k) {
+        __syncthreads();   // the sums are read
+        const int w = (blockIdx.x * p.words + k) * kThreads + tid;
+        const uint32_t in = in_pool(p, w), low = below_limit(p, w), used = in ? __ldcg(p.used + w) : 0u;
+        const uint32_t source = used & in & ~low, place = ~used & in & low;
+        if (in) p.used[w] = 0;   // as it was found
+        const int2 n = make_int2(__popc(source), __popc(place));
+        int2 end = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(kFull, end.x, o), y = __shfl_up_sync(kFull, end.y, o);
+            if (lane >= o) end.x += x, end.y += y;
         }
-        for (int i = moved + tid; i < p.moves.n; i += kThreads) p.moves.src[i] = p.moves.dst[i] = -1;
-    }
-    // consecutive words a thread, so that a prefix sum over the threads ranks them
-    const int w0 = (blockIdx.x * kThreads + tid) * kWordsPer;
-    uint32_t source[kWordsPer], place[kWordsPer];
-    int2 n = make_int2(0, 0);
+        if (lane == 31) sums[0][warp] = end;
+        __syncthreads();
+        int i = i0 + end.x - n.x, j = j0 + end.y - n.y;
 #pragma unroll
-    for (int k = 0; k < kWordsPer; ++k) {
-        const uint32_t in = in_pool(p, w0 + k), low = below_limit(p, w0 + k), used = in ? __ldcg(p.used + w0 + k) : 0u;
-        source[k] = used & in & ~low;
-        place[k] = ~used & in & low;
-        n.x += __popc(source[k]);
-        n.y += __popc(place[k]);
-        if (in) p.used[w0 + k] = 0;   // as it was found
-    }
-    int2 end = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(kFull, end.x, o), y = __shfl_up_sync(kFull, end.y, o);
-        if (lane >= o) end.x += x, end.y += y;
-    }
-    if (lane == 31) sums[0][warp] = end;
-    __syncthreads();
-    int i = before.x + end.x - n.x, j = before.y + end.y - n.y;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w)
-        if (w < warp) i += sums[0][w].x, j += sums[0][w].y;
-#pragma unroll
-    for (int k = 0; k < kWordsPer; ++k) {
-        for (uint32_t bits = source[k]; bits; bits &= bits - 1, ++i) {
-            const int x = (w0 + k) * 32 + __ffs(bits) - 1;
-            p.rank[x] = i;
-            if (i < moved) p.moves.src[i] = x;
+        for (int v = 0; v < kWarps; ++v) {
+            if (v < warp) i += sums[0][v].x, j += sums[0][v].y;
+            i0 += sums[0][v].x;
+            j0 += sums[0][v].y;
         }
-        for (uint32_t bits = place[k]; bits; bits &= bits - 1, ++j) {
-            const int x = (w0 + k) * 32 + __ffs(bits) - 1;
-            if (j < moved)
-                p.moves.dst[j] = x;
-            else
-                p.pages.free_list[left - 1 - (j - moved)] = x;
+        // a word's pages by the warp's lanes, word after word
+        const unsigned below = (1u << lane) - 1;
+#pragma unroll 4
+        for (int v = 0; v < 32; ++v) {
+            const uint32_t from = __shfl_sync(kFull, source, v), to = __shfl_sync(kFull, place, v);
+            const int iv = __shfl_sync(kFull, i, v) + __popc(from & below), jv = __shfl_sync(kFull, j, v) + __popc(to & below);
+            const int x = (w - lane + v) * 32 + lane;
+            if ((from >> lane) & 1) {
+                p.rank[x] = iv;
+                if (iv < moved) p.moves.src[iv] = x;
+            }
+            if ((to >> lane) & 1) {
+                if (jv < moved)
+                    p.moves.dst[jv] = x;
+                else
+                    p.pages.free_list[left - 1 - (jv - moved)] = x;
+            }
         }
     }
 }
@@ -182,8 +181,12 @@ __global__ void __launch_bounds__(kThreads) kv_compact_table_kernel(const KvComp
 
 }  // namespace
 
-cudaError_t launch_kv_compact(const KvCompactParams& p, cudaStream_t stream) {
-    const int spans = static_cast<int>((static_cast<long long>(p.n_pages) + kCompactSpan - 1) / kCompactSpan);
+cudaError_t launch_kv_compact(KvCompactParams p, cudaStream_t stream) {
+    p.words = 1;
+    while ((static_cast<long long>(p.n_pages) + static_cast<long long>(kCompactSpan) * p.words - 1) / (static_cast<long long>(kCompactSpan) * p.words) > 2048)
+        p.words *= 2;
+    const long long span = static_cast<long long>(kCompactSpan) * p.words;
+    const int spans = static_cast<int>((p.n_pages + span - 1) / span);
     const long long warps = static_cast<long long>(p.R) * p.parts, most = 8LL * device_sm_count();
     long long grid = (warps + kWarps - 1) / kWarps;
     grid = grid < 1 ? 1 : grid < most ? grid : most;

@@ -19,7 +19,7 @@
 namespace qs {
 namespace {
 
-constexpr int kForkThreads = 1024, kForkWarps = kForkThreads / 32, kForkCluster = 8;
+constexpr int kForkThreads = 1024, kForkCluster = 8;   // at most; CTAs of the cluster
 constexpr int kNoTail = -1, kBadTail = -2;
 
 // Record of a request: parent, old pages, whole pages (bit 31: the tail is fresh), tail page.
@@ -60,7 +60,7 @@ template <int kPer>
 __device__ void fork_decide(const KvForkParams& p, int* smem, int* sums) {
     int* const longest = smem;
     unsigned* const best = reinterpret_cast<unsigned*>(smem + p.R);
-    const int tid = threadIdx.x, R = p.R, sh = p.page_shift;
+    const int tid = threadIdx.x, threads = blockDim.x, R = p.R, sh = p.page_shift;
     const long long most = static_cast<long long>(p.max_pages) << sh;
     auto length = [&](int r) {
         const int n = __ldcg(p.pages.lens + r);
@@ -69,11 +69,11 @@ __device__ void fork_decide(const KvForkParams& p, int* smem, int* sums) {
         return n < 0 ? 0 : static_cast<int>(most);
     };
     int free_n = __ldcg(p.pages.free_count);
-    for (int r = tid; r < R; r += kForkThreads) longest[r] = 0, best[r] = 0xffffffffu;
+    for (int r = tid; r < R; r += threads) longest[r] = 0, best[r] = 0xffffffffu;
     int par[kPer], n[kPer], m[kPer];
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
-        const int r = k * kForkThreads + tid;
+        const int r = k * threads + tid;
         par[k] = -1;
         n[k] = m[k] = 0;
         if (r >= R) continue;
@@ -110,7 +110,7 @@ __device__ void fork_decide(const KvForkParams& p, int* smem, int* sums) {
     bool could[kPer];
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
-        const int r = k * kForkThreads + tid;
+        const int r = k * threads + tid;
         could[k] = tail[k] >= 0 && (m[k] >> sh) == longest[par[k]] && __ldcg(p.others + tail[k]) == 0;
         if (could[k]) atomicMin(best + par[k], r == par[k] ? 0u : static_cast<unsigned>(r) + 1u);
     }
@@ -118,8 +118,8 @@ __device__ void fork_decide(const KvForkParams& p, int* smem, int* sums) {
     int asked = 0;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
-        if (k * kForkThreads >= R) break;
-        const int r = k * kForkThreads + tid;
+        if (k * threads >= R) break;
+        const int r = k * threads + tid;
         const bool need = tail[k] >= 0 && !(could[k] && best[par[k]] == (r == par[k] ? 0u : static_cast<unsigned>(r) + 1u));
         int all;
         const int end = asked + block_sum(need, all, sums);
@@ -150,14 +150,13 @@ __device__ void fork_decide(const KvForkParams& p, int* smem, int* sums) {
         p.moves.src[r] = src;
         p.moves.dst[r] = dst;
     }
-    for (int r = R + tid; r < p.moves.n; r += kForkThreads) p.moves.src[r] = p.moves.dst[r] = -1;
+    for (int r = R + tid; r < p.moves.n; r += threads) p.moves.src[r] = p.moves.dst[r] = -1;
     if (tid == 0) p.head[0] = free_n - min(asked, free_n);
 }
 
-// The steps over pages: a warp takes one of `parts` parts of a request's columns.
+// The steps over pages: a warp takes one of `parts` parts of a request's columns, every `workers`-th of [worker, items).
 template <class F>
-__device__ __forceinline__ void each_part(const KvForkParams& p, int worker, int workers, F f) {
-    const int items = p.R * p.parts;
+__device__ __forceinline__ void each_part(const KvForkParams& p, int worker, int workers, int items, F f) {
     for (int item = worker; item < items; item += workers) {
         const int r = item / p.parts, c0 = (item - r * p.parts) * p.chunk;
         const int4 rec = __ldcg(p.rec + r);
@@ -167,7 +166,7 @@ __device__ __forceinline__ void each_part(const KvForkParams& p, int worker, int
 
 __device__ void fork_count_holders(const KvForkParams& p, int worker, int workers) {
     const int lane = threadIdx.x & 31;
-    each_part(p, worker, workers, [&](int, int r, const int4& rec, int c0, int c1) {
+    each_part(p, worker, workers, p.R * p.parts, [&](int, int r, const int4& rec, int c0, int c1) {
         const int32_t* const mine = p.pages.table + static_cast<size_t>(r) * p.max_pages;
         const int whole = whole_of(rec);
         if (rec.x >= 0 && rec.x != r) {
@@ -214,7 +213,7 @@ __device__ void fork_count_back(const KvForkParams& p, int worker, int workers) 
         const int r = i / p.parts;
         if (!changes(__ldcg(p.rec + r), r)) p.count[i] = 0;
     }
-    each_part(p, worker, workers, [&](int item, int r, const int4& rec, int c0, int c1) {
+    each_part(p, worker, workers, p.R * p.parts, [&](int item, int r, const int4& rec, int c0, int c1) {
         int n = 0;
 #pragma unroll 4
         for (int c = max(c0, leaves_from(rec, r)) + lane; c < min(c1, rec.y); c += 32) {
@@ -232,39 +231,49 @@ __device__ void fork_count_back(const KvForkParams& p, int worker, int workers) 
     });
 }
 
-// smem: R parts ints.
+// A CTA takes a run of the items, so that all it needs of those before is their sum.  smem: an int for each item of its run.
 __device__ void fork_place(const KvForkParams& p, int cta, int ctas, int* smem, int* sums) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, items = p.R * p.parts;
-    const int base = __ldcg(p.head);
-    int total = 0;
-    for (int i0 = 0; i0 < items; i0 += kForkThreads) {
-        const int i = i0 + threadIdx.x, n = i < items ? __ldcg(p.count + i) : 0;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5, items = p.R * p.parts;
+    const int per = (items + ctas - 1) / ctas, first = min(items, cta * per), last = min(items, first + per);
+    int before = 0;
+#pragma unroll 8
+    for (int i = tid; i < first; i += blockDim.x) before += __ldcg(p.count + i);
+    int total;
+    block_sum(before, total, sums);   // of the items before
+    for (int i0 = first; i0 < last; i0 += blockDim.x) {
+        const int i = i0 + tid, n = i < last ? __ldcg(p.count + i) : 0;
         int all;
         const int end = block_sum(n, all, sums);
-        if (i < items) smem[i] = total + end - n;
+        if (i < last) smem[i - first] = total + end - n;
         total += all;
     }
     __syncthreads();
-    if (cta == 0 && threadIdx.x == 0) p.pages.free_out[0] = min(base + total, p.n_pages);
-    each_part(p, cta * kForkWarps + warp, ctas * kForkWarps, [&](int item, int r, const int4& rec, int c0, int c1) {
+    const int base = __ldcg(p.head);
+    if (cta == ctas - 1 && tid == 0) p.pages.free_out[0] = min(base + total, p.n_pages);
+    each_part(p, first + warp, warps, last, [&](int item, int r, const int4& rec, int c0, int c1) {
         int32_t* const mine = p.pages.table + static_cast<size_t>(r) * p.max_pages;
         const int end = min(c1, rec.y), whole = whole_of(rec);
-        int at = base + smem[item];
-        for (int c = max(c0, leaves_from(rec, r)); c < end; c += 32) {
-            int x = -1;
-            bool back;
-            const bool last = last_holder(p, r, c + lane, end, x, back);
-            const unsigned mask = __ballot_sync(kFull, back);
-            if (back) {
-                const int to = at + __popc(mask & ((1u << lane) - 1));
-                if (to < p.n_pages)
-                    p.pages.free_list[to] = x;
-                else
-                    raise_status(p.status, QS_DEV_PAGES);
-                p.others[x] = 0;
+        int at = base + smem[item - first];
+        constexpr int kBatch = 4;   // columns of a lane whose pages are looked up together
+        for (int c = max(c0, leaves_from(rec, r)); c < end; c += 32 * kBatch) {
+            int x[kBatch];
+            bool back[kBatch], held[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) held[k] = last_holder(p, r, c + k * 32 + lane, end, x[k], back[k]);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const unsigned mask = __ballot_sync(kFull, back[k]);
+                if (back[k]) {
+                    const int to = at + __popc(mask & ((1u << lane) - 1));
+                    if (to < p.n_pages)
+                        p.pages.free_list[to] = x[k];
+                    else
+                        raise_status(p.status, QS_DEV_PAGES);
+                    p.others[x[k]] = 0;
+                }
+                if (held[k]) p.owner[x[k]] = 0;
+                at += __popc(mask);
             }
-            if (last) p.owner[x] = 0;
-            at += __popc(mask);
         }
         __syncwarp();   // the old pages of these columns are read
         if (rec.x >= 0 && rec.x != r)
@@ -284,7 +293,7 @@ __global__ void __cluster_dims__(kForkCluster, 1, 1) __launch_bounds__(kForkThre
     extern __shared__ int smem[];
     __shared__ int sums[32];
     chain_wait();
-    const int worker = blockIdx.x * kForkWarps + (threadIdx.x >> 5), workers = kForkCluster * kForkWarps;
+    const int warps = blockDim.x >> 5, worker = blockIdx.x * warps + (threadIdx.x >> 5), workers = kForkCluster * warps;
     if (blockIdx.x == 0) fork_decide<kPer>(p, smem, sums);
     cluster_sync();
     fork_count_holders(p, worker, workers);
@@ -300,7 +309,7 @@ __global__ void __launch_bounds__(kForkThreads) kv_fork_step_kernel(const KvFork
     extern __shared__ int smem[];
     __shared__ int sums[32];
     chain_wait();
-    const int worker = blockIdx.x * kForkWarps + (threadIdx.x >> 5), workers = gridDim.x * kForkWarps;
+    const int warps = blockDim.x >> 5, worker = blockIdx.x * warps + (threadIdx.x >> 5), workers = gridDim.x * warps;
     if (step == 0)
         fork_decide<kPer>(p, smem, sums);
     else if (step == 1)
@@ -317,17 +326,22 @@ cudaError_t launch_fork(const KvForkParams& p, bool cluster, cudaStream_t stream
     constexpr int kMost = 2 * sizeof(int) * kKvMaxRequests;
     const size_t decide = 2 * sizeof(int) * static_cast<size_t>(p.R), place = sizeof(int) * static_cast<size_t>(p.R) * p.parts;
     const size_t both = decide > place ? decide : place;
+    const int items = p.R * p.parts;
     if (cluster) {
         const cudaError_t e = cudaFuncSetAttribute(kv_fork_kernel<kPer>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
         if (e != cudaSuccess) return e;
-        return launch_chained(kv_fork_kernel<kPer>, kForkCluster, kForkThreads, both, stream, true, p);
+        // a thread a request in the first step, then a warp an item, as far as there are items
+        int threads = 256;
+        while (threads < kForkThreads && (threads < p.R || threads / 32 * kForkCluster < items)) threads *= 2;
+        return launch_chained(kv_fork_kernel<kPer>, kForkCluster, threads, both, stream, true, p);
     }
     cudaError_t e = cudaFuncSetAttribute(kv_fork_step_kernel<kPer>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
-    const int need = (p.R * p.parts + kForkWarps - 1) / kForkWarps, most = 2 * device_sm_count();
+    constexpr int kStepThreads = 256;
+    const int need = (items + kStepThreads / 32 - 1) / (kStepThreads / 32), most = 8 * device_sm_count();
     const int grid = need < 1 ? 1 : need < most ? need : most;
     for (int step = 0; step < 4 && e == cudaSuccess; ++step)
-        e = launch_chained(kv_fork_step_kernel<kPer>, step == 0 ? 1 : grid, kForkThreads, step == 0 ? decide : step == 3 ? place : 0,
-                           stream, true, p, step);
+        e = launch_chained(kv_fork_step_kernel<kPer>, step == 0 ? 1 : grid, step == 0 ? kForkThreads : kStepThreads,
+                           step == 0 ? decide : step == 3 ? place : 0, stream, true, p, step);
     return e;
 }
 
