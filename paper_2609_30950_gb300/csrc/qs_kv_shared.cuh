@@ -65,33 +65,49 @@ struct SharedPart {
     int e, hb, tile, count, tiles;   // group; key head and block of rows in one; first tile and how many; the block's
     int left;                        // units from the first tile to the share's end
 
-    __device__ __forceinline__ void load(const KvGroup* groups, int index, int kTile) {
-        e = index;
-        const int4* const src = reinterpret_cast<const int4*>(groups + index);
-        const int4 a = __ldcg(src), b = __ldcg(src + 1);
+    __device__ __forceinline__ void take(const int4& a, const int4& b, int kTile) {
         g.first = a.x, g.rows = a.y, g.owner = a.z, g.tokens = a.w;
         g.blocks = b.x, g.block0 = b.y;
         g.unit0 = static_cast<long long>(static_cast<unsigned>(b.z)) | static_cast<long long>(b.w) << 32;
         tiles = (g.tokens + kTile - 1) / kTile;
     }
-    __device__ __forceinline__ bool start(const KvGroupHead& head, const KvGroup* groups, int worker, int workers, int kTile) {
+    __device__ __forceinline__ void load(const KvGroup* groups, int index, int kTile) {
+        e = index;
+        const int4* const src = reinterpret_cast<const int4*>(groups + index);
+        const int4 a = __ldcg(src), b = __ldcg(src + 1);
+        take(a, b, kTile);
+    }
+    // a and b: this lane's group, of the first 32, as they lie in memory (anything behind the last group); a whole warp.
+    __device__ __forceinline__ bool start(const KvGroupHead& head, const KvGroup* groups, const int4& a, const int4& b, int worker,
+                                          int workers, int kTile) {
         const long long u0 = share_start(head.units, worker, workers), u1 = share_start(head.units, worker + 1, workers);
         left = static_cast<int>(u1 - u0);
         if (left <= 0) return false;
-        int lo = 0, n = head.groups;   // last group that begins at u0 or before
-        while (n > 1) {
-            const int half = n >> 1;
-            if (__ldcg(&groups[lo + half].unit0) <= u0) {
-                lo += half;
-                n -= half;
-            } else {
-                n = half;
+        const long long mine = static_cast<long long>(static_cast<unsigned>(b.z)) | static_cast<long long>(b.w) << 32;
+        const int lane = threadIdx.x & 31;
+        // the last group that begins at u0 or before
+        const unsigned before = __ballot_sync(kFull, lane < head.groups && mine <= u0);
+        if (before != kFull || head.groups == 32) {
+            const int l = 31 - __clz(before);
+            e = l;
+            auto from = [&](int v) { return __shfl_sync(kFull, v, l); };
+            take(make_int4(from(a.x), from(a.y), from(a.z), from(a.w)), make_int4(from(b.x), from(b.y), from(b.z), from(b.w)), kTile);
+        } else {
+            int lo = 31, n = head.groups - 31;
+            while (n > 1) {
+                const int half = n >> 1;
+                if (__ldcg(&groups[lo + half].unit0) <= u0) {
+                    lo += half;
+                    n -= half;
+                } else {
+                    n = half;
+                }
             }
+            load(groups, lo, kTile);
         }
-        load(groups, lo, kTile);
         const int per = tiles + kSharedRowUnits;
         const long long at = u0 - g.unit0;
-        hb = static_cast<int>(at / per);
+        hb = static_cast<int>(divided(at, per));
         tile = static_cast<int>(at - static_cast<long long>(hb) * per) - kSharedRowUnits;
         if (tile < 0) {
             left += tile;
@@ -179,7 +195,7 @@ __device__ __forceinline__ bool phase_wait(uint64_t* bar, uint32_t parity, volat
 }
 
 template <int D, bool kF16, bool kE4M3>
-__global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(const KvAttendParams p, const int box_rows,
+__global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(const KvAttendParams p, const int box_rows, const int most_groups,
                                                                                 const __grid_constant__ CUtensorMap k_map,
                                                                                 const __grid_constant__ CUtensorMap v_map) {
     using S = SharedShape<D>;
@@ -217,13 +233,20 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
         prefetch_map(&k_map);
         prefetch_map(&v_map);
     }
+    // the head, and a lane's group of the first 32 (there is room for most_groups)
     KvGroupHead head;
-    head.groups = __ldcg(&head_at->groups);
-    head.R = __ldcg(&head_at->R);
-    head.Hq = __ldcg(&head_at->Hq);
-    head.Hkv = __ldcg(&head_at->Hkv);
-    head.tile = __ldcg(&head_at->tile);
-    head.units = __ldcg(&head_at->units);
+    int4 g0 = make_int4(0, 0, 0, 0), g1 = g0;
+    {
+        const int4* const src = reinterpret_cast<const int4*>(head_at);
+        const int4 h0 = __ldcg(src), h1 = __ldcg(src + 1);
+        if (lane < most_groups) {
+            g0 = __ldcg(reinterpret_cast<const int4*>(groups + lane));
+            g1 = __ldcg(reinterpret_cast<const int4*>(groups + lane) + 1);
+        }
+        head.groups = h0.x, head.R = h0.y, head.Hq = h0.z, head.Hkv = h0.w;
+        head.tile = h1.x;
+        head.units = static_cast<long long>(static_cast<unsigned>(h1.z)) | static_cast<long long>(h1.w) << 32;
+    }
     // groups that were made for other requests or another kind of layer are none
     const bool fits = head.groups == 0 || (head.R == p.R && head.Hq == p.Hq && head.Hkv == p.Hkv && head.tile == kTile);
     if (!fits && tid == 0) raise_status(p.status, QS_DEV_PAGES);
@@ -237,7 +260,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
     int copied = 0;   // tensors that this warp has begun to copy
     // a limit of no polls gives up at the first wait
     if (fits && head.groups > 0 && p.wait_polls == 0 && tid == 0) raise_status(p.status, QS_DEV_TIMEOUT);
-    const bool live = fits && head.groups > 0 && p.wait_polls > 0 && w.start(head, groups, worker, p.workers, kTile);
+    const bool live = fits && head.groups > 0 && p.wait_polls > 0 && w.start(head, groups, g0, g1, worker, p.workers, kTile);
     // Streams have their own S, P, O and softmax warps.  They are a block's halves (`two`), or, where it has one half, the part's
     // even and odd tiles.
     const bool fences = !kE4M3 && !box_rows;   // copies by cp.async, whose writes the product's issuer makes visible to the tensor core
@@ -326,7 +349,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                     }
                 } else {
                     // 16 codes a lane and load, a few tokens' in flight while those before are converted; D / 16 lanes take a token
-                    constexpr int kLanes = D / 16, kTokens = 32 / kLanes, kLoads = 4, kSteps = kTile / (kTokens * kLoads);
+                    constexpr int kLanes = D / 16, kTokens = 32 / kLanes, kLoads = D == 64 ? 4 : 8, kSteps = kTile / (kTokens * kLoads);
                     const int sg = lane % kLanes, row0 = lane / kLanes;
                     int power[2];
 #pragma unroll
@@ -662,7 +685,8 @@ cudaError_t launch_shared(const qstate_kv_cfg& c, KvAttendParams p, cudaStream_t
         box_rows = c.page < S::kTile ? c.page : S::kTile;
         if (!pool_map(&k_map, p.k, D, rows, box_rows) || !pool_map(&v_map, p.v, D, rows, box_rows)) box_rows = 0;
     }
-    return launch_chained(kv_shared_kernel<D, kF16, kE4M3>, p.workers, S::kThreads, kBytes, stream, true, p, box_rows, k_map, v_map);
+    return launch_chained(kv_shared_kernel<D, kF16, kE4M3>, p.workers, S::kThreads, kBytes, stream, true, p, box_rows, kv_most_groups(p.R),
+                          k_map, v_map);
 }
 
 template <int D>
