@@ -288,11 +288,10 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                     id[k] = t < w.g.tokens ? __ldcg(pages + (t >> p.page_shift)) : -1;
                 }
             };
-            int c = (i & 1) == pw >> 1 ? 0 : 1;   // the first tile that is this warp's
-            if (c < w.count) look_up(w.tile + c);
-            for (; c < w.count && ok; c += 2) {
-                uint32_t on[2];
-                long long row[2];   // of the pool
+            uint32_t on[2];     // tokens that are there
+            long long row[2];   // of the pool
+            int power[2];       // e4m3
+            auto prepare = [&](int c) {   // the tile's rows; the pages of the warp's next one are looked up meanwhile
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int t = (w.tile + c) * kTile + k * 32 + lane;
@@ -300,8 +299,34 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                     if (wanted && !there) raise_status(p.status, QS_DEV_PAGES);
                     on[k] = __ballot_sync(kFull, there);
                     row[k] = there ? ((static_cast<long long>(id[k]) * p.Hkv + kv_head) << p.page_shift) + (t & page_mask) : 0;
+                    if (kE4M3) power[k] = there ? __ldcg(exps + row[k]) : 127;
                 }
                 if (c + 2 < w.count) look_up(w.tile + c + 2);
+            };
+            // e4m3: 16 codes a lane and load, some tokens' in flight while those before are converted; D / 16 lanes take a token
+            constexpr int kLanes = D / 16, kTokens = 32 / kLanes, kLoads = D == 64 ? 4 : 8, kSteps = kTile / (kTokens * kLoads);
+            const int code_sg = lane % kLanes, code_row = lane / kLanes;
+            uint4 codes[kE4M3 ? kLoads : 1], ahead[kE4M3 ? kLoads : 1];
+            auto load = [&](int step) {
+#pragma unroll
+                for (int k = 0; k < (kE4M3 ? kLoads : 0); ++k) {
+                    const int u = (step * kLoads + k) * kTokens + code_row;
+                    const long long a = __shfl_sync(kFull, row[0], u & 31), b = __shfl_sync(kFull, row[1], u & 31);
+                    const bool seen = ((u < 32 ? on[0] : on[1]) >> (u & 31)) & 1;
+                    const char* const src = pool + (u < 32 ? a : b) * D + code_sg * 16;
+                    ahead[kE4M3 ? k : 0] = seen ? __ldcg(reinterpret_cast<const uint4*>(src)) : make_uint4(0, 0, 0, 0);
+                }
+            };
+            int c = (i & 1) == pw >> 1 ? 0 : 1;   // the first tile that is this warp's
+            if (c < w.count) {
+                look_up(w.tile + c);
+                if (kE4M3) {
+                    prepare(c);
+                    load(0);
+                }
+            }
+            for (; c < w.count && ok; c += 2) {
+                if (!kE4M3) prepare(c);
                 if (!values && lane == 0) {
                     volatile uint32_t* const mask = x.mask[(i + c) % kMaskRing];
                     mask[0] = on[0];
@@ -348,35 +373,23 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                         if (lane == 0) mbar_arrive(&x.full[s]);
                     }
                 } else {
-                    // 16 codes a lane and load, a few tokens' in flight while those before are converted; D / 16 lanes take a token
-                    constexpr int kLanes = D / 16, kTokens = 32 / kLanes, kLoads = D == 64 ? 4 : 8, kSteps = kTile / (kTokens * kLoads);
-                    const int sg = lane % kLanes, row0 = lane / kLanes;
-                    int power[2];
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) power[k] = (on[k] >> lane) & 1 ? __ldcg(exps + row[k]) : 127;
-                    uint4 codes[kLoads], ahead[kLoads];
-                    auto load = [&](int step, uint4 (&to)[kLoads]) {
-#pragma unroll
-                        for (int k = 0; k < kLoads; ++k) {
-                            const int u = (step * kLoads + k) * kTokens + row0;
-                            const long long a = __shfl_sync(kFull, row[0], u & 31), b = __shfl_sync(kFull, row[1], u & 31);
-                            const bool seen = ((u < 32 ? on[0] : on[1]) >> (u & 31)) & 1;
-                            const char* const src = pool + (u < 32 ? a : b) * D + sg * 16;
-                            to[k] = seen ? __ldcg(reinterpret_cast<const uint4*>(src)) : make_uint4(0, 0, 0, 0);
-                        }
-                    };
-                    load(0, ahead);
+                    const int powers[2] = {power[0], power[1]};
                     if (copied * S::kCopiers >= S::kStages) ok = phase_wait(&x.free[s], phase ^ 1, abort, p);
                     if (!ok) break;
 #pragma unroll 1
                     for (int step = 0; step < kSteps; ++step) {
 #pragma unroll
                         for (int k = 0; k < kLoads; ++k) codes[k] = ahead[k];
-                        if (step + 1 < kSteps) load(step + 1, ahead);
+                        if (step + 1 < kSteps) {
+                            load(step + 1);
+                        } else if (c + 2 < w.count) {   // the warp's next tile
+                            prepare(c + 2);
+                            load(0);
+                        }
 #pragma unroll
                         for (int k = 0; k < kLoads; ++k) {
-                            const int u = (step * kLoads + k) * kTokens + row0;
-                            const unsigned e0 = __shfl_sync(kFull, power[0], u & 31), e1 = __shfl_sync(kFull, power[1], u & 31), e = u < 32 ? e0 : e1;
+                            const int u = (step * kLoads + k) * kTokens + code_row;
+                            const unsigned e0 = __shfl_sync(kFull, powers[0], u & 31), e1 = __shfl_sync(kFull, powers[1], u & 31), e = u < 32 ? e0 : e1;
                             // 2^(e - 127); 0 is the type's lowest power (2^-127, not a normal number), 255 NaN
                             const float two = e == 255 ? __uint_as_float(0x7fffffffu) : e ? __uint_as_float(e << 23) : 0x1p-127f;
                             const uint32_t w4[4] = {codes[k].x, codes[k].y, codes[k].z, codes[k].w};
@@ -392,8 +405,8 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                                 y[2 * j + 1] = pack2<false>(b.x, b.y);
                             }
                             // entries 16 sg ...: pieces 2 (sg % 4) and the next of block sg / 4
-                            const int piece = (sg & 3) * 2;
-                            const uint32_t to = stage + (sg >> 2) * S::kBlock + u * 128;
+                            const int piece = (code_sg & 3) * 2;
+                            const uint32_t to = stage + (code_sg >> 2) * S::kBlock + u * 128;
                             st_shared16(to + ((piece ^ (u & 7)) << 4), y[0], y[1], y[2], y[3]);
                             st_shared16(to + (((piece + 1) ^ (u & 7)) << 4), y[4], y[5], y[6], y[7]);
                         }
