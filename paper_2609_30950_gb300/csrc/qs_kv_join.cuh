@@ -13,25 +13,6 @@
 namespace qs {
 namespace kv {
 
-// The parts of a row, addresses in float4: part i of the columns 4 c ... 4 c + 3 is at sums + at(i) + c * column.
-struct PartList {
-    const float4* sums;
-    const float4* ml;
-    size_t slot, offset, ml_slot, ml_offset;   // sizes of a slot, place of the row in one
-    size_t pair, ml_pair;                      // from a part's first stream to its second
-    int column, worker, n, streams;
-
-    __device__ __forceinline__ size_t slot_of(int i) const { return worker < 0 ? 0 : part_slot(worker + i, i == 0); }
-    __device__ __forceinline__ const float4* sums_at(int i) const {
-        const int s = streams == 2 ? i & 1 : 0;
-        return sums + slot_of(streams == 2 ? i >> 1 : i) * slot + offset + s * pair;
-    }
-    __device__ __forceinline__ const float4* ml_at(int i) const {
-        const int s = streams == 2 ? i & 1 : 0;
-        return ml + slot_of(streams == 2 ? i >> 1 : i) * ml_slot + ml_offset + s * ml_pair;
-    }
-};
-
 constexpr int kJoinRows = 8, kJoinBatch = 4;   // rows of a CTA, parts in flight
 // Warps that share a row's parts: 512 threads at most, which leave them their registers.
 template <int D>
@@ -55,54 +36,76 @@ __global__ void __launch_bounds__(D * (kMany ? join_shares<D>() : 1)) kv_join_sh
     int2 own_dir = make_int2(0, 0), pre_dir = own_dir;
     if (has_own) own_dir = __ldcg(p.dir + static_cast<size_t>(r) * groups + kv * g.groups_per_kv + in_kv / g.per_group);
     if (has_pre) pre_dir = __ldcg(p.pre_dir + rec.y + kv * rec.z + (rec.w + in_kv) / kRows);
-    PartList own{}, pre{};
-    if (has_own) {
-        const size_t at = in_kv % g.per_group;
-        own = own_dir.x < 0
-                  ? PartList{reinterpret_cast<const float4*>(p.store), p.store_ml, 0, row * (D / 4), 0, row, 0, 0, 1, -1, 1, 1}
-                  : PartList{reinterpret_cast<const float4*>(p.part), reinterpret_cast<const float4*>(p.part_ml),
-                             static_cast<size_t>(g.rows) * (D / 4), at * (D / 4), static_cast<size_t>(g.rows), at, 0, 0, 1, own_dir.x, own_dir.y, 1};
-    }
-    if (has_pre) {
-        const size_t at = (rec.w + in_kv) % kRows;
-        const int streams = pre_dir.y < 0 ? 2 : 1, many = abs(pre_dir.y) * streams;
-        pre = pre_dir.x < 0
-                  ? PartList{reinterpret_cast<const float4*>(p.pre_store), p.pre_store_ml, 0, row * (D / 4), 0, row, rows * (D / 4), rows, 1,
-                             -1, many, streams}
-                  : PartList{reinterpret_cast<const float4*>(p.pre_part), p.pre_ml, static_cast<size_t>(kRows) * (D / 4), at,
-                             static_cast<size_t>(kRows), at, 128, 128, kRows, pre_dir.x, many, streams};
-    }
-    const int all = own.n + pre.n, most = __reduce_max_sync(kFull, all);
+    // The parts' places, in float4 of references (of sums: D / 4 times as much, but that shared tokens' parts lie column by
+    // column in a slot): 32 bits, and few instructions, whose latencies are what a join takes.  Part 0 of a split row is in the first
+    // worker's slot 1, part k behind it in slot 0 of the k-th worker on.
+    auto slot_of = [](int worker, int k) { return static_cast<unsigned>(part_slot(worker + k, k == 0)); };
+    const unsigned own_at = in_kv % g.per_group, pre_at = (rec.w + in_kv) % kRows, row32 = static_cast<unsigned>(row);
+    const float4* const own_ml = own_dir.x < 0 ? p.store_ml : reinterpret_cast<const float4*>(p.part_ml);
+    const float4* const own_sums = reinterpret_cast<const float4*>(own_dir.x < 0 ? p.store : p.part) + c;
+    const bool pre_whole = pre_dir.x < 0;
+    const float4* const pre_ml = pre_whole ? p.pre_store_ml : p.pre_ml;
+    const float4* const pre_sums = reinterpret_cast<const float4*>(pre_whole ? p.pre_store : p.pre_part) + c * (pre_whole ? 1 : kRows);
+    const int pair = pre_dir.y < 0 ? 1 : 0, pre_n = abs(pre_dir.y) << pair;   // two streams of one half
+    const unsigned column = 4 * (pre_whole ? 1 : kRows);                     // to the lane's other columns
+    auto load_own = [&](int k, float4& y, float4 (&x)[2]) {
+        const unsigned ml = own_dir.x < 0 ? row32 : slot_of(own_dir.x, k) * g.rows + own_at;
+        y = __ldcg(own_ml + ml);
+        const float4* const src = own_sums + static_cast<size_t>(ml) * (D / 4);
+        x[0] = __ldcg(src);
+        x[1] = __ldcg(src + 4);
+    };
+    auto load_pre = [&](int i, float4& y, float4 (&x)[2]) {
+        const int k = i >> pair, s = i & pair;
+        const unsigned slot = pre_whole ? 0u : slot_of(pre_dir.x, k) * kRows;
+        const unsigned at = pre_whole ? row32 + (s ? static_cast<unsigned>(rows) : 0u) : pre_at + s * 128u;
+        y = __ldcg(pre_ml + slot + at);
+        const float4* const src = pre_sums + (pre_whole ? static_cast<size_t>(at) * (D / 4) : static_cast<size_t>(slot) * (D / 4) + at);
+        x[0] = __ldcg(src);
+        x[1] = __ldcg(src + column);
+    };
     float Mo = -INFINITY, M = -INFINITY, L = 0.0f, Lo = 0.0f;
     float4 acc[2] = {};
+    auto take = [&](const float4& y, const float4 (&x)[2]) {
+        if (y.x == -INFINITY && y.w == 0.0f) return;   // no token, or none that weighs anything: no sums (NaN are none of these)
+        const float to = fmaxf(Mo, y.x), tm = fmaxf(M, y.y);
+        const float co = part_weight(Mo, to), cy = part_weight(y.x, to), cm = part_weight(M, tm), cl = part_weight(y.y, tm);
+        L = L * cm + y.z * cl;
+        Lo = Lo * cm + y.w * cl;
+        Mo = to;
+        M = tm;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            acc[k] = make_float4(acc[k].x * co + cy * x[k].x, acc[k].y * co + cy * x[k].y, acc[k].z * co + cy * x[k].z, acc[k].w * co + cy * x[k].w);
+    };
+    const float4 none = make_float4(-INFINITY, -INFINITY, 0.0f, 0.0f);
+    const int most = __reduce_max_sync(kFull, pre_n), most_own = __reduce_max_sync(kFull, own_dir.y);
+    // own parts by the shares from the last on, so that the one that has the fewest of the others begins
+    float4 y0 = none, x0[2];
+    const int own_first = kShares - 1 - share;
+    if (own_first < own_dir.y) load_own(own_first, y0, x0);
+#pragma unroll 1
     for (int i0 = share * kJoinBatch; i0 < most; i0 += kShares * kJoinBatch) {
         float4 y[kJoinBatch], x[kJoinBatch][2];
 #pragma unroll
         for (int b = 0; b < kJoinBatch; ++b) {
-            const int i = i0 + b;
-            const bool shared = i < pre.n;
-            y[b] = make_float4(-INFINITY, -INFINITY, 0.0f, 0.0f);
-            if (i >= all) continue;
-            y[b] = __ldcg(shared ? pre.ml_at(i) : own.ml_at(i - pre.n));
-            const float4* const src = shared ? pre.sums_at(i) : own.sums_at(i - pre.n);
-            const int column = shared ? pre.column : own.column;
-            x[b][0] = __ldcg(src + c * column);
-            x[b][1] = __ldcg(src + (c + 4) * column);
+            y[b] = none;
+            if (i0 + b < pre_n) load_pre(i0 + b, y[b], x[b]);
         }
+#pragma unroll
+        for (int b = 0; b < kJoinBatch; ++b) take(y[b], x[b]);
+    }
+    take(y0, x0);
+#pragma unroll 1
+    for (int i0 = own_first + kShares; i0 < most_own; i0 += kShares * kJoinBatch) {
+        float4 y[kJoinBatch], x[kJoinBatch][2];
 #pragma unroll
         for (int b = 0; b < kJoinBatch; ++b) {
-            if (y[b].x == -INFINITY && y[b].w == 0.0f) continue;   // no token, or none that weighs anything: no sums (NaN are none of these)
-            const float to = fmaxf(Mo, y[b].x), tm = fmaxf(M, y[b].y);
-            const float co = part_weight(Mo, to), cy = part_weight(y[b].x, to), cm = part_weight(M, tm), cl = part_weight(y[b].y, tm);
-            L = L * cm + y[b].z * cl;
-            Lo = Lo * cm + y[b].w * cl;
-            Mo = to;
-            M = tm;
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-                acc[k] = make_float4(acc[k].x * co + cy * x[b][k].x, acc[k].y * co + cy * x[b][k].y, acc[k].z * co + cy * x[b][k].z,
-                                     acc[k].w * co + cy * x[b][k].w);
+            y[b] = none;
+            if (i0 + b * kShares < own_dir.y) load_own(i0 + b * kShares, y[b], x[b]);
         }
+#pragma unroll
+        for (int b = 0; b < kJoinBatch; ++b) take(y[b], x[b]);
     }
     if constexpr (kMany) {
         s_acc[share][rr][c] = acc[0];
