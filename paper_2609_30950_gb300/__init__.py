@@ -731,7 +731,7 @@ class KvGroups(_Kept):
 
     def __post_init__(self):
         import torch
-        _keep(self, _at=_typed(self.data, "data", torch.uint8), _fits=None)
+        _keep(self, _at=_typed(self.data, "data", torch.uint8), _fits=None, _made=None)
 
     def _check(self, cfg):
         """The memory is enough for the description; looked at once for each description."""
@@ -844,6 +844,8 @@ def qstate_kv_group(cfg: KvConfig, lens, start, common, groups: KvGroups, stream
     """Which requests share their first tokens (see include/qstate.h): lens (R), start (N + 1), common (N), int32."""
     if groups._fits is not cfg:
         groups._check(cfg)
+    if groups._made is not cfg:
+        _keep(groups, _made=cfg)
     N = common.numel()
     rc = (_lib or load()).qstate_kv_group(cfg._at, _ints(lens, "lens", groups.R), groups.R, _ints(start, "start", N + 1),
                                           _ints(common, "common", N), N, groups._at,
@@ -882,6 +884,9 @@ def qstate_kv_attend_shared(cfg: KvConfig, cache: KvCache, q, table, lens, group
         groups._check(cfg)
     if groups.R != R:
         raise ValueError(f"groups were made for {groups.R} requests, got {R}")
+    made = groups._made
+    if made is not None and made is not cfg and (made.Hq, made.Hkv, made.dk, made.window) != (cfg.Hq, cfg.Hkv, cfg.dk, cfg.window):
+        raise ValueError("groups were made for a layer of other heads or another window")
     rc = (_lib or load()).qstate_kv_attend_shared(cfg._at, cache._at, q.data_ptr(), qr, qh, table.data_ptr(), lens.data_ptr(), R,
                                                   groups._at, o.data_ptr(), sums,
                                                   _work_of("qstate_kv_shared_work_bytes", cfg, work, R),

@@ -30,7 +30,8 @@ __global__ void __launch_bounds__(D * (kMany ? join_shares<D>() : 1)) kv_join_sh
     const bool mine = v < p.R * g.G;
     const int r = mine ? v / g.G : 0, in_kv = mine ? v - r * g.G : 0;
     const size_t rows = static_cast<size_t>(p.R) * p.Hq, row = static_cast<size_t>(r) * p.Hq + kv * g.G + in_kv;
-    const int4 rec = __ldcg(p.shared + r);
+    int4 rec = __ldcg(p.shared + r);
+    if (!groups_fit(p, kRows)) rec = make_int4(0, 0, 0, 0);
     const int n = clamped_len(p, r, false), begin = min(max(p.window > 0 && n > p.window ? n - p.window : 0, rec.x), n);
     const bool has_own = mine && begin < n, has_pre = mine && rec.x > 0;
     int2 own_dir = make_int2(0, 0), pre_dir = own_dir;

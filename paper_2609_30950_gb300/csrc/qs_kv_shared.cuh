@@ -245,10 +245,11 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
         }
         head.groups = h0.x, head.R = h0.y, head.Hq = h0.z, head.Hkv = h0.w;
         head.tile = h1.x;
+        head.rows = h1.y;
         head.units = static_cast<long long>(static_cast<unsigned>(h1.z)) | static_cast<long long>(h1.w) << 32;
     }
     // groups that were made for other requests or another kind of layer are none
-    const bool fits = head.groups == 0 || (head.R == p.R && head.Hq == p.Hq && head.Hkv == p.Hkv && head.tile == kTile);
+    const bool fits = head.groups == 0 || (head.R == p.R && head.Hq == p.Hq && head.Hkv == p.Hkv && head.tile == kTile && head.rows == S::kRows);
     if (!fits && tid == 0) raise_status(p.status, QS_DEV_PAGES);
     tc::fence_before_sync();
     __syncthreads();

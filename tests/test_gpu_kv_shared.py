@@ -291,3 +291,49 @@ def test_two_streams_with_work_spaces_of_their_own(qs):
     torch.cuda.synchronize()
     for b in batches:
         b.check(qs)
+
+
+def test_across_32_bit_offsets(qs):
+    """Pages whose entries lie behind 2^31 entries (4 GB and more) of the pool."""
+    page, Hkv, d = 1024, 4, 256
+    n_pages = 2 ** 31 // (page * Hkv * d) + 40
+    small = share.Batch(qs, [2500, 2200, 2100], [(0, 3, 2050)], 8, Hkv, d, page=page, spare=1)
+    cfg = qs.KvConfig(Hq=8, Hkv=Hkv, dk=d, dv=d, page=page, n_pages=n_pages, max_pages=3, scale=d ** -0.5)
+    cache = qs.new_kv_cache(cfg)
+    shift = n_pages - small.cfg.n_pages
+    cache.k[shift:], cache.v[shift:] = small.k, small.v
+    table = torch.where(small.d_table >= 0, small.d_table + shift, -1)[:, :3].contiguous()
+    small.group(qs)
+    groups = qs.KvGroups(small.d_groups.data, 3)
+    qs.qstate_kv_attend_shared(cfg, cache, small.q, table, small.d_lens, groups, small.o, small.lse, small.work)
+    small.check(qs)
+    # and a copy there
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    qs.qstate_kv_copy(cfg, cache, qs.KvMoves(i32(n_pages - 1, 3), i32(2, n_pages - 2)))
+    qs.qstate_check()
+    assert torch.equal(cache.k[2], cache.k[n_pages - 1]) and not bool(cache.v[n_pages - 2].any())
+
+
+def test_groups_of_another_layer_are_refused(qs):
+    b = share.Batch(qs, [300, 310, 305], [(0, 3, 280)], 4, 2, 64, seed=20)
+    other = share.Batch(qs, [300, 310, 305], [(0, 3, 280)], 4, 2, 256, seed=20)
+    other.group(qs)
+    b.group(qs)
+    with pytest.raises(ValueError):
+        qs.qstate_kv_attend_shared(b.cfg, b.cache, b.q, b.d_table, b.d_lens, other.d_groups, b.o, b.lse, b.work)
+    # through the C interface: reported on the device, and what is wrong stays inside the buffers
+    groups = qs.KvGroups(torch.zeros_like(other.d_groups.data), 3)
+    groups.data.copy_(other.d_groups.data)
+    qs.qstate_kv_attend_shared(b.cfg, b.cache, b.q, b.d_table, b.d_lens, groups, b.o, b.lse, b.work)
+    with pytest.raises(qs.QstateError):
+        qs.qstate_check()
+    b.run(qs)
+    b.check(qs)
+
+
+def test_the_work_space_serves_the_other_attention_too(qs):
+    b = share.Batch(qs, LENS, GROUPS, 8, 2, 128, seed=21)
+    check(qs, b)
+    b.o.fill_(3)
+    qs.qstate_kv_attend(b.cfg, b.cache, b.q, b.d_table, b.d_lens, b.o, b.lse, b.work)
+    b.check(qs)
