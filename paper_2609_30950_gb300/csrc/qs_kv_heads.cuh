@@ -89,7 +89,12 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
     constexpr int kSteps = D / 16, kOut = D / 8;
     constexpr float kLog2e = 1.4426950408889634f;
     extern __shared__ __align__(128) char smem[];
-    chain_wait();   // and the kernel that joins split rows may take its place
+    // kShared: nothing here needs the kernel before, which works on the shared tokens and has itself waited for all that came
+    // before it: CTAs begin where its CTAs end, and the wait, for the kernel behind this one, comes last.
+    if (kShared)
+        chain_release();
+    else
+        chain_wait();   // and the kernel that joins split rows may take its place
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane >> 2, t4 = lane & 3;
     const int groups = p.Hkv * groups_per_kv, G = p.Hq / p.Hkv;
 
@@ -607,6 +612,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
         }
     if (!kShared && !p.whole_rows && tid == 0) p.split[blockIdx.x] = split;
     cp_wait<0>();
+    if (kShared) chain_enter();
 }
 
 template <int D, bool kF16, bool kE4M3, bool kHalf, int kStages, int kCtas, bool kShared>

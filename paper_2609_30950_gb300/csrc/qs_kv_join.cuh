@@ -23,7 +23,6 @@ __global__ void __launch_bounds__(D * (kMany ? join_shares<D>() : 1)) kv_join_sh
     constexpr int kColumns = D / 32, kShares = kMany ? join_shares<D>() : 1, kRows = kv_shared_rows(D);
     __shared__ float4 s_ml[kShares][kJoinRows], s_acc[kMany ? kShares : 1][kMany ? kJoinRows : 1][D / 4];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = warp / kColumns;
-    chain_wait();
     const int chunks = (p.R * g.G + kJoinRows - 1) / kJoinRows, groups = p.Hkv * g.groups_per_kv;
     const int kv = blockIdx.x / chunks, rr = lane & 7, v = (blockIdx.x - kv * chunks) * kJoinRows + rr;
     const int c = (warp % kColumns) * 8 + (lane >> 3);   // the lane's columns: 4 c ... 4 c + 3 and 16 more on
@@ -32,9 +31,11 @@ __global__ void __launch_bounds__(D * (kMany ? join_shares<D>() : 1)) kv_join_sh
     const size_t rows = static_cast<size_t>(p.R) * p.Hq, row = static_cast<size_t>(r) * p.Hq + kv * g.G + in_kv;
     int4 rec = __ldcg(p.shared + r);
     if (!groups_fit(p, kRows)) rec = make_int4(0, 0, 0, 0);
+    // records and lengths are older than the kernels that this one waits for
     const int n = clamped_len(p, r, false), begin = min(max(p.window > 0 && n > p.window ? n - p.window : 0, rec.x), n);
     const bool has_own = mine && begin < n, has_pre = mine && rec.x > 0;
     int2 own_dir = make_int2(0, 0), pre_dir = own_dir;
+    chain_wait();
     if (has_own) own_dir = __ldcg(p.dir + static_cast<size_t>(r) * groups + kv * g.groups_per_kv + in_kv / g.per_group);
     if (has_pre) pre_dir = __ldcg(p.pre_dir + rec.y + kv * rec.z + (rec.w + in_kv) / kRows);
     // The parts' places, in float4 of references (of sums: D / 4 times as much, but that shared tokens' parts lie column by
