@@ -8,6 +8,8 @@
 // the parts are, the parts, four at a time).
 #pragma once
 
+#include <type_traits>
+
 #include "qs_kv_tiles.cuh"
 
 namespace qs {
@@ -68,24 +70,42 @@ __global__ void __launch_bounds__(D * (kMany ? join_shares<D>() : 1)) kv_join_sh
     };
     float Mo = -INFINITY, M = -INFINITY, L = 0.0f, Lo = 0.0f;
     float4 acc[2] = {};
-    auto take = [&](const float4& y, const float4 (&x)[2]) {
-        if (y.x == -INFINITY && y.w == 0.0f) return;   // no token, or none that weighs anything: no sums (NaN are none of these)
-        const float to = fmaxf(Mo, y.x), tm = fmaxf(M, y.y);
-        const float co = part_weight(Mo, to), cy = part_weight(y.x, to), cm = part_weight(M, tm), cl = part_weight(y.y, tm);
-        L = L * cm + y.z * cl;
-        Lo = Lo * cm + y.w * cl;
+    // n parts at once: one reference for all, so that their weights do not wait for one another
+    auto take = [&](auto count, const float4* y, const float4 (*x)[2]) {
+        constexpr int n = decltype(count)::value;
+        float to = Mo, tm = M;
+#pragma unroll
+        for (int b = 0; b < n; ++b) to = fmaxf(to, y[b].x), tm = fmaxf(tm, y[b].y);
+        const float co = part_weight(Mo, to), cm = part_weight(M, tm);
+        L *= cm;
+        Lo *= cm;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) acc[k] = make_float4(acc[k].x * co, acc[k].y * co, acc[k].z * co, acc[k].w * co);
         Mo = to;
         M = tm;
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-            acc[k] = make_float4(acc[k].x * co + cy * x[k].x, acc[k].y * co + cy * x[k].y, acc[k].z * co + cy * x[k].z, acc[k].w * co + cy * x[k].w);
+        for (int b = 0; b < n; ++b) {
+            const float cy = part_weight(y[b].x, to), cl = part_weight(y[b].y, tm);
+            if (y[b].x == -INFINITY && y[b].w == 0.0f) continue;   // no token, or none that weighs anything: no sums (NaN are none of these)
+            L += y[b].z * cl;
+            Lo += y[b].w * cl;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                acc[k].x += cy * x[b][k].x;
+                acc[k].y += cy * x[b][k].y;
+                acc[k].z += cy * x[b][k].z;
+                acc[k].w += cy * x[b][k].w;
+            }
+        }
     };
+    using One = std::integral_constant<int, 1>;
+    using Batch = std::integral_constant<int, kJoinBatch>;
     const float4 none = make_float4(-INFINITY, -INFINITY, 0.0f, 0.0f);
     const int most = __reduce_max_sync(kFull, pre_n), most_own = __reduce_max_sync(kFull, own_dir.y);
     // own parts by the shares from the last on, so that the one that has the fewest of the others begins
-    float4 y0 = none, x0[2];
+    float4 y0[1] = {none}, x0[1][2];
     const int own_first = kShares - 1 - share;
-    if (own_first < own_dir.y) load_own(own_first, y0, x0);
+    if (own_first < own_dir.y) load_own(own_first, y0[0], x0[0]);
 #pragma unroll 1
     for (int i0 = share * kJoinBatch; i0 < most; i0 += kShares * kJoinBatch) {
         float4 y[kJoinBatch], x[kJoinBatch][2];
@@ -94,10 +114,9 @@ __global__ void __launch_bounds__(D * (kMany ? join_shares<D>() : 1)) kv_join_sh
             y[b] = none;
             if (i0 + b < pre_n) load_pre(i0 + b, y[b], x[b]);
         }
-#pragma unroll
-        for (int b = 0; b < kJoinBatch; ++b) take(y[b], x[b]);
+        take(Batch{}, y, x);
     }
-    take(y0, x0);
+    take(One{}, y0, x0);
 #pragma unroll 1
     for (int i0 = own_first + kShares; i0 < most_own; i0 += kShares * kJoinBatch) {
         float4 y[kJoinBatch], x[kJoinBatch][2];
@@ -106,8 +125,7 @@ __global__ void __launch_bounds__(D * (kMany ? join_shares<D>() : 1)) kv_join_sh
             y[b] = none;
             if (i0 + b * kShares < own_dir.y) load_own(i0 + b * kShares, y[b], x[b]);
         }
-#pragma unroll
-        for (int b = 0; b < kJoinBatch; ++b) take(y[b], x[b]);
+        take(Batch{}, y, x);
     }
     if constexpr (kMany) {
         s_acc[share][rr][c] = acc[0];
