@@ -443,7 +443,8 @@ size_t qstate_kv_shared_work_bytes(const qstate_kv_cfg* cfg, int32_t R);
 
 /* Which of R requests share their first tokens: group g of N (0 <= N <= R) is the requests [start[g], start[g + 1]) (start: N + 1,
  * not falling, within [0, R]), whose first common[g] tokens are the same.  Requests outside all groups, those with fewer tokens and
- * those whose window begins behind token 0 read theirs by themselves, and so does a group that only one could share in.  Made from lens (R) as
+ * those whose window begins behind token 0 read theirs by themselves, and so does a group that only one could share in, or everyone where
+ * sharing would take longer (see qstate_set_shared_gain).  Made from lens (R) as
  * they are at the attention, for layers of one Hq, Hkv, dk and window.  A start outside its bounds or a number of tokens
  * outside the table sets the device status, and nothing (or that group) is shared. */
 int qstate_kv_group(const qstate_kv_cfg* cfg, const int32_t* lens, int32_t R, const int32_t* start, const int32_t* common, int32_t N,
@@ -472,6 +473,12 @@ int qstate_check(void* stream);
  * beyond any product's latency).  The wait before freeing tensor memory always uses the
  * default.  Always QSTATE_OK.  Not part of the paper's method: a diagnostic of this library. */
 int qstate_set_wait_limit(int32_t polls);
+
+/* What sharing has to gain, in ns, for the calls of qstate_kv_group that follow (process-wide; read when a call is enqueued):
+ * an estimate from the groups' sizes of what their requests' own reading of the common tokens would take, less what a
+ * block of shared rows does.  ns > 0 sets it, 0 shares wherever two requests can, whatever it costs; ns < 0 restores the
+ * default (12000, the launches and joins that sharing adds).  The answers do not depend on it but for roundings.  Always QSTATE_OK. */
+int qstate_set_shared_gain(int32_t ns);
 
 /* Batch partitions of qstate_scan for the calls that follow (process-wide; read when a call is
  * enqueued).  The batch elements of a scan are independent problems (Eq. 1 and the allocation

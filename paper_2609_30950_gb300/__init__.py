@@ -93,7 +93,8 @@ EXPORTS = ["qstate_validate", "qstate_region_bytes", "qstate_units", "qstate_sca
            "qstate_scan_partition_count", "qstate_last_error", "qstate_kv_validate", "qstate_kv_cache_bytes",
            "qstate_kv_work_bytes", "qstate_kv_plan", "qstate_kv_append", "qstate_kv_attend",
            "qstate_kv_pages_work_bytes", "qstate_kv_fork", "qstate_kv_compact", "qstate_kv_copy",
-           "qstate_kv_group_bytes", "qstate_kv_shared_work_bytes", "qstate_kv_group", "qstate_kv_attend_shared"]
+           "qstate_kv_group_bytes", "qstate_kv_shared_work_bytes", "qstate_kv_group", "qstate_kv_attend_shared",
+           "qstate_set_shared_gain"]
 
 _lib = None
 
@@ -158,6 +159,7 @@ def load(path: str | None = None, build_if_missing: bool = False):
     L.qstate_kv_fork.argtypes = [P, P, P, P, P, I32, P, P, P, P]
     L.qstate_kv_compact.argtypes = [P, P, P, I32, I32, P, P, P, P, P]
     L.qstate_kv_copy.argtypes = [P, P, P, P]
+    L.qstate_set_shared_gain.argtypes = [I32]
     L.qstate_kv_group.argtypes = [P, P, I32, P, P, I32, P, P]
     L.qstate_kv_attend_shared.argtypes = [P, P, P, I64, I64, P, P, I32, P, P, P, P, P]
     for name in EXPORTS:
@@ -838,6 +840,11 @@ def qstate_kv_copy(cfg: KvConfig, cache: KvCache, moves: KvMoves, stream=None) -
     rc = (_lib or load()).qstate_kv_copy(cfg._at, cache._at, moves._at, _current_stream() if stream is None else stream.cuda_stream)
     if rc:
         _check(rc)
+
+
+def qstate_set_shared_gain(ns: int) -> None:
+    """What sharing has to gain for later calls of qstate_kv_group (ns; 0: share wherever two can, negative: the default)."""
+    _check(_lib_or_raise().qstate_set_shared_gain(int(ns)))
 
 
 def qstate_kv_group(cfg: KvConfig, lens, start, common, groups: KvGroups, stream=None) -> None:

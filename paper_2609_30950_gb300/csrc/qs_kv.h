@@ -69,7 +69,7 @@ struct KvAttendParams {
     const int* groups;       // the groups (KvGroup)
     float* store;            // unsplit rows of a request's own tokens: sums, and references and weights
     float4* store_ml;
-    int2* dir;               // of each row of work: the worker that begins it (-1: unsplit, in the store), its parts
+    int2* dir;               // of each row of work: the worker that begins it (-1: unsplit, in the store; -2: done), its parts
     float* pre_part;         // the same of the groups' blocks of rows
     float4* pre_ml;
     float* pre_store;
@@ -80,7 +80,11 @@ struct KvAttendParams {
 // Tokens of a tile, and rows (requests' heads) of a block, in the attention over tokens that requests share.
 constexpr int kSharedTile = 64;
 constexpr int kv_shared_rows(int d) { return d == 256 ? 128 : 256; }
-constexpr int kSharedRowUnits = 4;   // tiles that a block of rows costs by itself: its queries, its end
+constexpr int kSharedRowUnits = 4;
+// What the launches and joins of shared tokens cost beside their tiles.  With 16-bit keys and values of 128 entries, sharing took and
+// reading by oneself took: 4 requests of 8 key heads behind 3001 tokens 19.8 and 14.7 us, 16 x 12 behind 100 34.5 and 23.6, 38 x 3 of 3
+// key heads behind 200 to 600 21.5 and 18.0; 35 x 7 of 7 key heads behind 50 to 370 34.7 and 39.7, 4 x 32 behind up to 2000 48.7 and 72.2.
+constexpr long long kSharedLeastNs = 12000;   // tiles that a block of rows costs by itself: its queries, its end
 
 // What qstate_kv_group leaves behind: a head, the requests' records, the groups that share anything.
 struct KvGroupHead {
@@ -108,6 +112,11 @@ struct KvGroupParams {
     const int32_t* common;
     int N, R, G, Hkv, tile, rows, window;
     long long most;          // tokens of a table's row
+    // What a tile of shared tokens of one key head takes, in ns of the whole GPU: for each request that reads it by itself, and
+    // for each half of a block of rows (e4m3: for each block).
+    float alone_ns, block_ns;
+    int half_rows;           // of what block_ns is for
+    long long least_ns;      // that sharing has to gain, over all groups and key heads; 0: whatever it costs
     KvGroupHead head;        // host: what the head is to say, but for sums
     KvGroupHead* out;
     int4* shared;
@@ -189,5 +198,6 @@ int fail(int code, const char* fmt, ...);
 int cuda_fail(cudaError_t e, const char* what);
 int acquire_status(int** out);
 int wait_polls();
+long long shared_least_ns();
 
 }  // namespace qs

@@ -3,7 +3,7 @@
 // Group g is the requests [start_g, start_g+1) and has c_g tokens in common.  A request takes part if it has them all and sees
 // them all (n >= c, and no window or n <= window), the group shares if two take part; its rows are its requests' query
 // heads of a key head, in blocks.  Every row of a block sees all c tokens, so that no row has a mask of its own there; a request that
-// does not take part reads its tokens by itself.  One CTA: two searches and a prefix sum in shared memory, some
+// does not take part reads its tokens by itself, and so do all of them where sharing would gain nothing (qs_kv.h).  One CTA: two searches and a prefix sum in shared memory, some
 // latencies (256 requests: see the table of the design notes).
 #include "qs_common.cuh"
 #include "qs_kv.h"
@@ -14,12 +14,12 @@ namespace {
 constexpr int kMostThreads = 1024;
 
 struct Sums {
-    long long units;
+    long long units, gain;   // gain: ns
     int groups, blocks;
 };
-__device__ __forceinline__ Sums plus(const Sums& a, const Sums& b) { return {a.units + b.units, a.groups + b.groups, a.blocks + b.blocks}; }
+__device__ __forceinline__ Sums plus(const Sums& a, const Sums& b) { return {a.units + b.units, a.gain + b.gain, a.groups + b.groups, a.blocks + b.blocks}; }
 __device__ __forceinline__ Sums shuffled(const Sums& a, int o) {
-    return {__shfl_up_sync(kFull, a.units, o), __shfl_up_sync(kFull, a.groups, o), __shfl_up_sync(kFull, a.blocks, o)};
+    return {__shfl_up_sync(kFull, a.units, o), __shfl_up_sync(kFull, a.gain, o), __shfl_up_sync(kFull, a.groups, o), __shfl_up_sync(kFull, a.blocks, o)};
 }
 // Inclusive prefix sum over a warp's lanes.
 __device__ __forceinline__ Sums scanned(Sums a) {
@@ -95,24 +95,31 @@ __global__ void __launch_bounds__(kMostThreads) kv_group_kernel(const KvGroupPar
     // a thread's groups, one after another
     const int per = (N + threads - 1) / threads, g0 = min(N, tid * per), g1 = min(N, g0 + per);
     auto sums_of = [&](int g) {
-        if (count[g] < 2) return Sums{0, 0, 0};
-        const int blocks = static_cast<int>((static_cast<long long>(start[g + 1] - start[g]) * p.G + p.rows - 1) / p.rows);
-        return Sums{static_cast<long long>(blocks) * p.Hkv * ((common[g] + p.tile - 1) / p.tile + kSharedRowUnits), 1, blocks * p.Hkv};
+        if (count[g] < 2) return Sums{0, 0, 0, 0};
+        const long long rows = static_cast<long long>(start[g + 1] - start[g]) * p.G;
+        const int blocks = static_cast<int>((rows + p.rows - 1) / p.rows), tiles = (common[g] + p.tile - 1) / p.tile;
+        const float halves = static_cast<float>((rows + p.half_rows - 1) / p.half_rows);
+        const float gain = (static_cast<float>(count[g]) * tiles * p.alone_ns - halves * (tiles + kSharedRowUnits) * p.block_ns) * p.Hkv;
+        if (p.least_ns > 0 && gain <= 0.0f) return Sums{0, 0, 0, 0};
+        return Sums{static_cast<long long>(blocks) * p.Hkv * (tiles + kSharedRowUnits), static_cast<long long>(gain), 1, blocks * p.Hkv};
     };
-    Sums mine{0, 0, 0};
+    Sums mine{0, 0, 0, 0};
     for (int g = g0; g < g1; ++g) mine = plus(mine, sums_of(g));
     const Sums end = scanned(mine);
     if (lane == 31) s_warp[warp] = end;
     __syncthreads();
-    const Sums warps = scanned(lane < threads / 32 ? s_warp[lane] : Sums{0, 0, 0});
+    const Sums warps = scanned(lane < threads / 32 ? s_warp[lane] : Sums{0, 0, 0, 0});
     auto from = [](const Sums& a, int l) {
-        return Sums{__shfl_sync(kFull, a.units, l), __shfl_sync(kFull, a.groups, l), __shfl_sync(kFull, a.blocks, l)};
+        return Sums{__shfl_sync(kFull, a.units, l), __shfl_sync(kFull, a.gain, l), __shfl_sync(kFull, a.groups, l), __shfl_sync(kFull, a.blocks, l)};
     };
-    const Sums all = from(warps, 31), lower = from(warps, (warp + 31) & 31), before = shuffled(end, 1);
-    Sums at = warp ? lower : Sums{0, 0, 0};
+    Sums all = from(warps, 31);
+    const bool worth = p.least_ns <= 0 || all.gain >= p.least_ns;
+    if (!worth) all = Sums{0, 0, 0, 0};
+    const Sums lower = from(warps, (warp + 31) & 31), before = shuffled(end, 1);
+    Sums at = warp ? lower : Sums{0, 0, 0, 0};
     if (lane) at = plus(at, before);
     for (int g = g0; g < g1; ++g) {
-        const Sums s = sums_of(g);
+        const Sums s = worth ? sums_of(g) : Sums{0, 0, 0, 0};
         const int blocks = s.blocks / p.Hkv;
         if (blocks) p.groups[at.groups] = {start[g], (start[g + 1] - start[g]) * p.G, owner[g], common[g], blocks, at.blocks, at.units};
         count[g] = blocks;

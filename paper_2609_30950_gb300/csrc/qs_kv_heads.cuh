@@ -540,8 +540,9 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
             __syncthreads();
             const float* const all = reinterpret_cast<const float*>(smem + stage * S::kSlot);
             const size_t out_row = static_cast<size_t>(cw.r) * p.Hq + h0;
+            const bool joined = kShared && p.shared[cw.r].x > 0;   // with shared tokens' parts
             auto finish = [&](int row, int col, float4 acc, float4 sums) {
-                if (kShared) {
+                if (joined) {
                     reinterpret_cast<float4*>(p.store)[((out_row + row) * D + col) / 4] = acc;
                     if (col == 0) p.store_ml[out_row + row] = sums;
                     return;
@@ -589,7 +590,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
             }
             if (kShared && tid == 0 && began == 0)
                 p.dir[static_cast<size_t>(cw.r) * groups + cw.group] =
-                    whole ? make_int2(-1, 1)
+                    whole ? make_int2(joined ? -1 : -2, joined ? 1 : 0)   // -2: done
                           : make_int2(blockIdx.x, row_parts(p, share, blockIdx.x, cw.left, cw.tile, cw.span.tiles));
             if (!kShared && tid == 0 && !whole && began == 0) {
                 split = row_parts(p, share, blockIdx.x, cw.left, cw.tile, cw.span.tiles);

@@ -44,6 +44,8 @@ __global__ void __launch_bounds__(D * (kMany ? join_shares<D>() : 1)) kv_join_sh
     // column in a slot): 32 bits, and few instructions, whose latencies are what a join takes.  Part 0 of a split row is in the first
     // worker's slot 1, part k behind it in slot 0 of the k-th worker on.
     auto slot_of = [](int worker, int k) { return static_cast<unsigned>(part_slot(worker + k, k == 0)); };
+    const bool done = own_dir.x == -2;   // by the kernel before
+    if (__all_sync(kFull, done || !mine) && !kMany) return;
     const unsigned own_at = in_kv % g.per_group, pre_at = (rec.w + in_kv) % kRows, row32 = static_cast<unsigned>(row);
     const float4* const own_ml = own_dir.x < 0 ? p.store_ml : reinterpret_cast<const float4*>(p.part_ml);
     const float4* const own_sums = reinterpret_cast<const float4*>(own_dir.x < 0 ? p.store : p.part) + c;
@@ -157,7 +159,7 @@ __global__ void __launch_bounds__(D * (kMany ? join_shares<D>() : 1)) kv_join_sh
             }
         }
     }
-    if (!mine) return;
+    if (!mine || done) return;
     // values and weights have references of their own where values carry powers of two
     const float inv = (Lo == 0.0f ? 0.0f : 1.0f / Lo) * (Mo == M ? 1.0f : exp2_fast(Mo - M));
 #pragma unroll

@@ -12,6 +12,14 @@ from test_gpu_hybrid_example import attention
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def share_everything(qs):
+    """Groups share whatever it costs: the cases here are small."""
+    qs.qstate_set_shared_gain(0)
+    yield
+    qs.qstate_set_shared_gain(-1)
+
+
 class Layer:
     def __init__(self, qs, pool, e4m3, d, seed):
         self.qs, self.e4m3 = qs, e4m3

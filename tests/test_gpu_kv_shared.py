@@ -8,6 +8,14 @@ import kv_share_reference as share
 
 pytestmark = pytest.mark.gpu
 
+
+@pytest.fixture(autouse=True)
+def share_everything(qs):
+    """Groups share whatever it costs: the cases here are small."""
+    qs.qstate_set_shared_gain(0)
+    yield
+    qs.qstate_set_shared_gain(-1)
+
 # groups of three and nine (one empty, one that lacks a common token), one request by itself before, between and behind
 LENS = [70, 200, 205, 333, 1, 129, 128, 0, 400, 131, 129, 300, 900, 130, 55]
 GROUPS = [(1, 4, 200), (5, 14, 129)]
@@ -337,3 +345,22 @@ def test_the_work_space_serves_the_other_attention_too(qs):
     b.o.fill_(3)
     qs.qstate_kv_attend(b.cfg, b.cache, b.q, b.d_table, b.d_lens, b.o, b.lse, b.work)
     b.check(qs)
+
+
+def test_groups_share_where_it_gains(qs):
+    """By default a few requests read for themselves; the answers are the same within both bounds, and a request that shares nothing
+    has the other attention's to the bit."""
+    few = share.Batch(qs, [300, 310, 305], [(0, 3, 280)], 4, 2, 64, seed=22)
+    many = share.Batch(qs, [3000] * 200, [(0, 200, 2990)], 8, 8, 128, page=64, seed=23)
+    for b, shares in ((few, False), (many, True)):
+        for ns in (0, -1):
+            qs.qstate_set_shared_gain(ns)
+            b.group(qs)
+            assert bool(b.d_groups.data[:4].view(torch.int32).item()) == (shares or ns == 0)
+            b.o.fill_(7)
+            b.attend(qs)
+            b.check(qs)
+        if not shares:
+            got, lse = b.o.clone(), b.lse.clone()
+            qs.qstate_kv_attend(b.cfg, b.cache, b.q, b.d_table, b.d_lens, b.o, b.lse, b.work)
+            assert torch.equal(b.o, got) and torch.equal(b.lse, lse)
