@@ -33,6 +33,11 @@ __device__ __forceinline__ void chain_wait() {
     chain_release();
 }
 
+// The CTAs of a cluster meet; what each wrote before is seen by all after it.
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+}
+
 // Record a QS_DEV_* condition in the status word (one per device, see qs_api.cu).
 __device__ __forceinline__ void raise_status(int* status, int bits) {
     if (status) atomicOr(status, bits);

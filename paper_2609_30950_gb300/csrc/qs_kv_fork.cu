@@ -12,7 +12,11 @@
 // Four steps, each of which needs all of the one before: who gets what (one CTA: R <= 8192, prefix sums and two reductions
 // in shared memory); counts of holders and the new rows, to the work space (atomic sums of whole numbers: any order gives the same, and
 // a maximum that says who held a page last); pages that come back, counted; their places, and the rows in place.
-// A chain of latencies: one cluster whose CTAs meet at its barrier where tables are short, a launch a step else.
+// A page that a request held and takes over again, the prefix of a beam that goes on with its sibling, is not counted: 64 requests of
+// 80 pages 12.9 -> 11.0 us, 975 of up to 656 29.2 -> 24.5.
+// A chain of latencies.  One cluster whose CTAs meet at its barrier where tables are short, a launch a step else.  Host included, the
+// cluster against the launches, requests x columns: 64 x 82 11.0 and 14.8 us, 16 x 1019 13.6 and 16.6, 256 x 82 14.0 and 14.9,
+// 256 x 144 15.5 and 15.2, 1000 x 26 25.4 and 14.9, 256 x 519 31.2 and 15.6.
 #include "qs_common.cuh"
 #include "qs_kv.h"
 
@@ -20,6 +24,7 @@ namespace qs {
 namespace {
 
 constexpr int kForkThreads = 1024, kForkCluster = 8;   // at most; CTAs of the cluster
+constexpr int kForkClusterRequests = 256, kForkClusterEntries = 1 << 15;   // at most; a thread a request
 constexpr int kNoTail = -1, kBadTail = -2;
 
 // Record of a request: parent, old pages, whole pages (bit 31: the tail is fresh), tail page.
@@ -154,6 +159,9 @@ __device__ void fork_decide(const KvForkParams& p, int* smem, int* sums) {
     if (tid == 0) p.head[0] = free_n - min(asked, free_n);
 }
 
+// Columns that the request takes from another's row, [0, this).
+__device__ __forceinline__ int taken_to(const int4& rec, int r) { return rec.x >= 0 && rec.x != r ? whole_of(rec) : 0; }
+
 // The steps over pages: a warp takes one of `parts` parts of a request's columns, every `workers`-th of [worker, items).
 template <class F>
 __device__ __forceinline__ void each_part(const KvForkParams& p, int worker, int workers, int items, F f) {
@@ -168,40 +176,48 @@ __device__ void fork_count_holders(const KvForkParams& p, int worker, int worker
     const int lane = threadIdx.x & 31;
     each_part(p, worker, workers, p.R * p.parts, [&](int, int r, const int4& rec, int c0, int c1) {
         const int32_t* const mine = p.pages.table + static_cast<size_t>(r) * p.max_pages;
-        const int whole = whole_of(rec);
-        if (rec.x >= 0 && rec.x != r) {
-            const int32_t* const from = p.pages.table + static_cast<size_t>(rec.x) * p.max_pages;
-#pragma unroll 4
-            for (int c = c0 + lane; c < min(c1, whole); c += 32) {
-                const int x = __ldcg(from + c);
-                p.stage[static_cast<size_t>(r) * p.max_pages + c] = x;
-                if (x >= 0 && x < p.n_pages)
-                    atomicAdd(p.others + x, 1);
-                else
-                    raise_status(p.status, QS_DEV_PAGES);
-            }
-        }
+        const int taken = taken_to(rec, r), whole = whole_of(rec), end = min(c1, max(taken, rec.y));
+        const int32_t* const from = p.pages.table + static_cast<size_t>(taken ? rec.x : r) * p.max_pages;
         // the tail that is kept under a new name, and a fresh one (see fork_count_back)
         if (lane == 0 && whole >= c0 && whole < c1 && rec.w >= 0 && (rec.x != r || fresh_of(rec))) atomicAdd(p.others + rec.w, 1);
-#pragma unroll 4
-        for (int c = max(c0, leaves_from(rec, r)) + lane; c < min(c1, rec.y); c += 32) {
-            const int x = __ldcg(mine + c);
-            if (x >= 0 && x < p.n_pages) {
-                atomicAdd(p.others + x, -1);
-                atomicMax(p.owner + x, r + 1);
-            } else {
-                raise_status(p.status, QS_DEV_PAGES);
+        constexpr int kBatch = 4;   // columns of a lane that are read together
+        for (int c = max(c0, leaves_from(rec, r)) + lane; c < end; c += 32 * kBatch) {
+            int now[kBatch], old[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int at = c + k * 32;
+                now[k] = at < min(c1, taken) ? __ldcg(from + at) : 0;
+                old[k] = at < min(c1, rec.y) ? __ldcg(mine + at) : 0;
+            }
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int at = c + k * 32;
+                const bool takes = at < min(c1, taken), leaves = at < min(c1, rec.y);
+                if (takes) p.stage[static_cast<size_t>(r) * p.max_pages + at] = now[k];
+                if ((takes && static_cast<unsigned>(now[k]) >= static_cast<unsigned>(p.n_pages)) ||
+                    (leaves && static_cast<unsigned>(old[k]) >= static_cast<unsigned>(p.n_pages))) {
+                    raise_status(p.status, QS_DEV_PAGES);
+                }
+                if (takes && leaves && now[k] == old[k]) continue;   // held before and after
+                if (takes && static_cast<unsigned>(now[k]) < static_cast<unsigned>(p.n_pages)) atomicAdd(p.others + now[k], 1);
+                if (leaves && static_cast<unsigned>(old[k]) < static_cast<unsigned>(p.n_pages)) {
+                    atomicAdd(p.others + old[k], -1);
+                    atomicMax(p.owner + old[k], r + 1);
+                }
             }
         }
     });
 }
 
-// Whether request r is the last that held the page in this column, and whether it comes back.
-__device__ __forceinline__ bool last_holder(const KvForkParams& p, int r, int c, int c1, int& x, bool& back) {
+// Whether request r is the last that left the page in this column, and whether it comes back.  taken: columns below it have their
+// new page in the work space; where that is the old one, the request has not left it.
+__device__ __forceinline__ bool last_holder(const KvForkParams& p, int r, int taken, int c, int c1, int& x, bool& back) {
     back = false;
     if (c >= c1) return false;
-    x = __ldcg(p.pages.table + static_cast<size_t>(r) * p.max_pages + c);
-    if (x < 0 || x >= p.n_pages) return false;
+    const size_t at = static_cast<size_t>(r) * p.max_pages + c;
+    x = __ldcg(p.pages.table + at);
+    const int now = c < taken ? __ldcg(p.stage + at) : -1;
+    if (x < 0 || x >= p.n_pages || x == now) return false;
     const int who = __ldcg(p.owner + x), others = __ldcg(p.others + x);
     back = who == r + 1 && others == -1;
     return who == r + 1;
@@ -219,7 +235,7 @@ __device__ void fork_count_back(const KvForkParams& p, int worker, int workers) 
         for (int c = max(c0, leaves_from(rec, r)) + lane; c < min(c1, rec.y); c += 32) {
             int x;
             bool back;
-            last_holder(p, r, c, min(c1, rec.y), x, back);
+            last_holder(p, r, taken_to(rec, r), c, min(c1, rec.y), x, back);
             n += back;
         }
         n = __reduce_add_sync(kFull, n);
@@ -252,14 +268,14 @@ __device__ void fork_place(const KvForkParams& p, int cta, int ctas, int* smem, 
     if (cta == ctas - 1 && tid == 0) p.pages.free_out[0] = min(base + total, p.n_pages);
     each_part(p, first + warp, warps, last, [&](int item, int r, const int4& rec, int c0, int c1) {
         int32_t* const mine = p.pages.table + static_cast<size_t>(r) * p.max_pages;
-        const int end = min(c1, rec.y), whole = whole_of(rec);
+        const int end = min(c1, rec.y), whole = whole_of(rec), taken = taken_to(rec, r);
         int at = base + smem[item - first];
         constexpr int kBatch = 4;   // columns of a lane whose pages are looked up together
         for (int c = max(c0, leaves_from(rec, r)); c < end; c += 32 * kBatch) {
             int x[kBatch];
             bool back[kBatch], held[kBatch];
 #pragma unroll
-            for (int k = 0; k < kBatch; ++k) held[k] = last_holder(p, r, c + k * 32 + lane, end, x[k], back[k]);
+            for (int k = 0; k < kBatch; ++k) held[k] = last_holder(p, r, taken, c + k * 32 + lane, end, x[k], back[k]);
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
                 const unsigned mask = __ballot_sync(kFull, back[k]);
@@ -276,25 +292,26 @@ __device__ void fork_place(const KvForkParams& p, int cta, int ctas, int* smem, 
             }
         }
         __syncwarp();   // the old pages of these columns are read
-        if (rec.x >= 0 && rec.x != r)
-#pragma unroll 4
-            for (int c = c0 + lane; c < min(c1, whole); c += 32) mine[c] = __ldcg(p.stage + static_cast<size_t>(r) * p.max_pages + c);
+        for (int c = c0 + lane; c < min(c1, taken); c += 32 * kBatch) {
+            int now[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k)
+                if (c + k * 32 < min(c1, taken)) now[k] = __ldcg(p.stage + static_cast<size_t>(r) * p.max_pages + c + k * 32);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k)
+                if (c + k * 32 < min(c1, taken)) mine[c + k * 32] = now[k];
+        }
         if (lane == 0 && whole >= c0 && whole < c1 && rec.w != kNoTail) mine[whole] = rec.w >= 0 ? rec.w : -1;
     });
 }
 
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-}
-
 // All four steps; CTAs of one cluster.
-template <int kPer>
 __global__ void __cluster_dims__(kForkCluster, 1, 1) __launch_bounds__(kForkThreads) kv_fork_kernel(const KvForkParams p) {
     extern __shared__ int smem[];
     __shared__ int sums[32];
     chain_wait();
     const int warps = blockDim.x >> 5, worker = blockIdx.x * warps + (threadIdx.x >> 5), workers = kForkCluster * warps;
-    if (blockIdx.x == 0) fork_decide<kPer>(p, smem, sums);
+    if (blockIdx.x == 0) fork_decide<1>(p, smem, sums);
     cluster_sync();
     fork_count_holders(p, worker, workers);
     cluster_sync();
@@ -320,25 +337,25 @@ __global__ void __launch_bounds__(kForkThreads) kv_fork_step_kernel(const KvFork
         fork_place(p, blockIdx.x, gridDim.x, smem, sums);
 }
 
-template <int kPer>
-cudaError_t launch_fork(const KvForkParams& p, bool cluster, cudaStream_t stream) {
-    // The limit is the kernel's, not the call's: every call sets the same one.
-    constexpr int kMost = 2 * sizeof(int) * kKvMaxRequests;
-    const size_t decide = 2 * sizeof(int) * static_cast<size_t>(p.R), place = sizeof(int) * static_cast<size_t>(p.R) * p.parts;
-    const size_t both = decide > place ? decide : place;
+cudaError_t launch_cluster(const KvForkParams& p, cudaStream_t stream) {
+    // a thread a request in the first step, then a warp an item, as far as there are items
     const int items = p.R * p.parts;
-    if (cluster) {
-        const cudaError_t e = cudaFuncSetAttribute(kv_fork_kernel<kPer>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
-        if (e != cudaSuccess) return e;
-        // a thread a request in the first step, then a warp an item, as far as there are items
-        int threads = 256;
-        while (threads < kForkThreads && (threads < p.R || threads / 32 * kForkCluster < items)) threads *= 2;
-        return launch_chained(kv_fork_kernel<kPer>, kForkCluster, threads, both, stream, true, p);
-    }
-    cudaError_t e = cudaFuncSetAttribute(kv_fork_step_kernel<kPer>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+    int threads = 256;
+    while (threads < kForkThreads && threads / 32 * kForkCluster < items) threads *= 2;
+    const int ints = 2 * p.R > items ? 2 * p.R : items;   // of the first and of the last step
+    return launch_chained(kv_fork_kernel, kForkCluster, threads, sizeof(int) * static_cast<size_t>(ints), stream, true, p);
+}
+
+template <int kPer>
+cudaError_t launch_steps(const KvForkParams& p, cudaStream_t stream) {
+    // The limit is the kernel's, not the call's: every call sets the same one.
+    cudaError_t e = cudaFuncSetAttribute(kv_fork_step_kernel<kPer>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         2 * sizeof(int) * kKvMaxRequests);
     constexpr int kStepThreads = 256;
+    const int items = p.R * p.parts;
     const int need = (items + kStepThreads / 32 - 1) / (kStepThreads / 32), most = 8 * device_sm_count();
     const int grid = need < 1 ? 1 : need < most ? need : most;
+    const size_t decide = 2 * sizeof(int) * static_cast<size_t>(p.R), place = sizeof(int) * static_cast<size_t>((items + grid - 1) / grid);
     for (int step = 0; step < 4 && e == cudaSuccess; ++step)
         e = launch_chained(kv_fork_step_kernel<kPer>, step == 0 ? 1 : grid, step == 0 ? kForkThreads : kStepThreads,
                            step == 0 ? decide : step == 3 ? place : 0, stream, true, p, step);
@@ -355,8 +372,9 @@ int kv_column_parts(int R, int max_pages) {
 }
 
 cudaError_t launch_kv_fork(const KvForkParams& p, cudaStream_t stream) {
-    const bool cluster = static_cast<long long>(p.R) * p.max_pages <= 1 << 19;
-    return p.R <= kForkThreads ? launch_fork<1>(p, cluster, stream) : launch_fork<kKvMaxRequests / kForkThreads>(p, cluster, stream);
+    // an item or so for each warp of the cluster, and few columns to an item
+    if (p.R <= kForkClusterRequests && static_cast<long long>(p.R) * p.max_pages <= kForkClusterEntries) return launch_cluster(p, stream);
+    return p.R <= kForkThreads ? launch_steps<1>(p, stream) : launch_steps<kKvMaxRequests / kForkThreads>(p, stream);
 }
 
 }  // namespace qs
