@@ -66,6 +66,40 @@ def test_long_tables_in_parts(qs):
     qs.qstate_check()
 
 
+@pytest.mark.parametrize("R,n_pages,max_pages", [
+    (12, 30000, 1000), (12, 70000, 1000),   # one cluster with several spans of the pool, more spans than it has CTAs
+    (33, 9000, 500), (31, 9000, 500),       # compact by steps and fork by the cluster, both by the cluster
+    (256, 20000, 128), (257, 20000, 100)])  # fork by the cluster, fork by steps
+def test_both_forms_of_the_launch(qs, R, n_pages, max_pages):
+    pool = share.Pool(qs, R, 2, n_pages, max_pages, R)
+    rng = random.Random(n_pages)
+    pool.grow([rng.randrange(min(2 * max_pages, 2 * n_pages // (2 * R))) for _ in range(R)])
+    for _ in range(3):
+        pool.fork(*random_step(pool, rng))
+        pool.sound()
+    pool.compact(n_pages // 3, n_pages)
+    pool.compact(n_pages, 0)
+    pool.sound()
+    qs.qstate_check()
+
+
+def test_families_whose_members_take_over_from_each_other(qs):
+    """Prefixes that are held before and after: their holders stay, whoever changes places and whoever leaves."""
+    R = 24
+    pool = share.Pool(qs, R, 4, 900, 60, 9)
+    pool.grow([150 if r % 8 == 0 else 0 for r in range(R)])
+    pool.fork([r // 8 * 8 for r in range(R)])          # three families of eight
+    rng = random.Random(10)
+    for step in range(6):
+        pool.grow([rng.randrange(9) for _ in range(R)])
+        parent = [r // 8 * 8 + rng.randrange(8) for r in range(R)]
+        if step % 2:
+            parent[8:16] = [-1] * 8 if step == 3 else [0] * 8   # a family ends, or goes over to another
+        pool.fork(parent, [rng.choice([-1, 120, 151]) for _ in range(R)])
+        pool.sound()
+    qs.qstate_check()
+
+
 def test_beams_that_change_places(qs):
     pool = share.Pool(qs, 8, 16, 200, 20, 3)
     pool.grow([100] * 8)
