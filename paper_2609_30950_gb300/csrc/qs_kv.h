@@ -135,7 +135,7 @@ struct KvForkParams {
     int parts, chunk;        // of a request's columns: warps that share them, columns of each
     int* head;               // work space: entries of the list below the pages that come back
     int4* rec;
-    int* count;              // pages of a part that come back
+    int* count;              // pages of a part that come back; from kKvMaxRequests on, those of a CTA's parts
     int* owner;              // of each page: the last request that held it, plus 1; zeros between calls
     int* stage;              // the new rows
     int* status;

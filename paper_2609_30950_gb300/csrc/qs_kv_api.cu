@@ -86,7 +86,7 @@ PagesWork pages_work(const qstate_kv_cfg& c, int R) {
     w.spans = w.used + whole((n / 32 + 1) * sizeof(uint32_t));
     w.rank = w.spans + whole((n / kCompactSpan + 1) * sizeof(int2));
     w.count = w.rank + whole(n * sizeof(int));
-    w.rec = w.count + whole(kKvMaxRequests * sizeof(int));
+    w.rec = w.count + whole(2 * kKvMaxRequests * sizeof(int));   // of parts, of CTAs
     w.stage = w.rec + whole(r * sizeof(int4));
     w.all = w.stage + whole(r * static_cast<size_t>(c.max_pages) * sizeof(int));
     return w;

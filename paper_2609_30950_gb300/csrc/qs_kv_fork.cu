@@ -11,12 +11,14 @@
 //     pages with h' = 0 come back, in the order of the last request that held them and of its pages.
 // Four steps, each of which needs all of the one before: who gets what (one CTA: R <= 8192, prefix sums and two reductions
 // in shared memory); counts of holders and the new rows, to the work space (atomic sums of whole numbers: any order gives the same, and
-// a maximum that says who held a page last); pages that come back, counted; their places, and the rows in place.
-// A page that a request held and takes over again, the prefix of a beam that goes on with its sibling, is not counted: 64 requests of
-// 80 pages 12.9 -> 11.0 us, 975 of up to 656 29.2 -> 24.5.
-// A chain of latencies.  One cluster whose CTAs meet at its barrier where tables are short, a launch a step else.  Host included, the
-// cluster against the launches, requests x columns: 64 x 82 11.0 and 14.8 us, 16 x 1019 13.6 and 16.6, 256 x 82 14.0 and 14.9,
-// 256 x 144 15.5 and 15.2, 1000 x 26 25.4 and 14.9, 256 x 519 31.2 and 15.6.
+// a maximum that says who held a page last); pages that come back, counted; their places, and the rows in place.  Every held
+// page is looked at, not only those of requests that change: the formula then holds whatever the counts were before.
+// Memory is read a few times and little of it; a chain of latencies bounds it (64 requests of 82 pages 9.7 us, 975 of up to 656 28.6).
+// A page that a request held and takes over again, the prefix of a beam that goes on with its sibling, needs no counting, and
+// columns are looked up four at a time, not behind one another: 12.9 -> 9.7 us for the 64.
+// One cluster whose CTAs meet at its barrier where tables are short, a launch a step else.  The cluster against the launches,
+// host included (in a graph), requests x columns: 64 x 82 10.0 and 13.2 us (9.6 and 11.0), 128 x 82 13.2 and 14.3 (12.8 and
+// 12.4), 256 x 82 18.4 and 14.0, 16 x 1019 14.8 and 13.7, 256 x 519 47 and 15.4.
 #include "qs_common.cuh"
 #include "qs_kv.h"
 
@@ -24,7 +26,8 @@ namespace qs {
 namespace {
 
 constexpr int kForkThreads = 1024, kForkCluster = 8;   // at most; CTAs of the cluster
-constexpr int kForkClusterRequests = 256, kForkClusterEntries = 1 << 15;   // at most; a thread a request
+constexpr int kForkClusterRequests = 256, kForkClusterEntries = 1 << 13;   // at most; a thread a request
+constexpr int kBatch = 4;   // columns of a lane that are read together
 constexpr int kNoTail = -1, kBadTail = -2;
 
 // Record of a request: parent, old pages, whole pages (bit 31: the tail is fresh), tail page.
@@ -34,10 +37,6 @@ __device__ __forceinline__ bool fresh_of(const int4& rec) { return rec.z < 0; }
 __device__ __forceinline__ int leaves_from(const int4& rec, int r) {
     return rec.x == r ? whole_of(rec) + (rec.w >= 0 && !fresh_of(rec) ? 1 : 0) : 0;
 }
-__device__ __forceinline__ bool changes(const int4& rec, int r) {
-    return rec.x != r || fresh_of(rec) || rec.w == kBadTail || rec.y != whole_of(rec) + (rec.w >= 0 ? 1 : 0);
-}
-
 // Inclusive prefix sum of x over the CTA's threads; all of them in `all`.
 __device__ __forceinline__ int block_sum(int x, int& all, int* sums) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
@@ -168,7 +167,7 @@ __device__ __forceinline__ void each_part(const KvForkParams& p, int worker, int
     for (int item = worker; item < items; item += workers) {
         const int r = item / p.parts, c0 = (item - r * p.parts) * p.chunk;
         const int4 rec = __ldcg(p.rec + r);
-        if (changes(rec, r)) f(item, r, rec, c0, c0 + p.chunk);
+        f(item, r, rec, c0, c0 + p.chunk);
     }
 }
 
@@ -180,8 +179,8 @@ __device__ void fork_count_holders(const KvForkParams& p, int worker, int worker
         const int32_t* const from = p.pages.table + static_cast<size_t>(taken ? rec.x : r) * p.max_pages;
         // the tail that is kept under a new name, and a fresh one (see fork_count_back)
         if (lane == 0 && whole >= c0 && whole < c1 && rec.w >= 0 && (rec.x != r || fresh_of(rec))) atomicAdd(p.others + rec.w, 1);
-        constexpr int kBatch = 4;   // columns of a lane that are read together
-        for (int c = max(c0, leaves_from(rec, r)) + lane; c < end; c += 32 * kBatch) {
+        const int kept = leaves_from(rec, r);
+        for (int c = c0 + lane; c < end; c += 32 * kBatch) {
             int now[kBatch], old[kBatch];
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
@@ -192,16 +191,16 @@ __device__ void fork_count_holders(const KvForkParams& p, int worker, int worker
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
                 const int at = c + k * 32;
-                const bool takes = at < min(c1, taken), leaves = at < min(c1, rec.y);
+                const bool takes = at < min(c1, taken), had = at < min(c1, rec.y);
                 if (takes) p.stage[static_cast<size_t>(r) * p.max_pages + at] = now[k];
                 if ((takes && static_cast<unsigned>(now[k]) >= static_cast<unsigned>(p.n_pages)) ||
-                    (leaves && static_cast<unsigned>(old[k]) >= static_cast<unsigned>(p.n_pages))) {
+                    (had && static_cast<unsigned>(old[k]) >= static_cast<unsigned>(p.n_pages))) {
                     raise_status(p.status, QS_DEV_PAGES);
                 }
-                if (takes && leaves && now[k] == old[k]) continue;   // held before and after
-                if (takes && static_cast<unsigned>(now[k]) < static_cast<unsigned>(p.n_pages)) atomicAdd(p.others + now[k], 1);
-                if (leaves && static_cast<unsigned>(old[k]) < static_cast<unsigned>(p.n_pages)) {
-                    atomicAdd(p.others + old[k], -1);
+                const bool stays = had && (at < kept || (takes && now[k] == old[k]));   // held before and after: nothing to count
+                if (!stays && takes && static_cast<unsigned>(now[k]) < static_cast<unsigned>(p.n_pages)) atomicAdd(p.others + now[k], 1);
+                if (had && static_cast<unsigned>(old[k]) < static_cast<unsigned>(p.n_pages)) {
+                    if (!stays) atomicAdd(p.others + old[k], -1);
                     atomicMax(p.owner + old[k], r + 1);
                 }
             }
@@ -209,85 +208,113 @@ __device__ void fork_count_holders(const KvForkParams& p, int worker, int worker
     });
 }
 
-// Whether request r is the last that left the page in this column, and whether it comes back.  taken: columns below it have their
-// new page in the work space; where that is the old one, the request has not left it.
-__device__ __forceinline__ bool last_holder(const KvForkParams& p, int r, int taken, int c, int c1, int& x, bool& back) {
-    back = false;
-    if (c >= c1) return false;
-    const size_t at = static_cast<size_t>(r) * p.max_pages + c;
-    x = __ldcg(p.pages.table + at);
-    const int now = c < taken ? __ldcg(p.stage + at) : -1;
-    if (x < 0 || x >= p.n_pages || x == now) return false;
-    const int who = __ldcg(p.owner + x), others = __ldcg(p.others + x);
-    back = who == r + 1 && others == -1;
-    return who == r + 1;
+// Columns c, c + 32, ... in front of `end`: their pages, whether request r is the last that held them, and holders beside the first
+// (-1: nobody, so it comes back; less only where the counts did not agree with the tables).  Looked up together.
+__device__ __forceinline__ void last_held(const KvForkParams& p, int r, int c, int end, int (&x)[kBatch], bool (&held)[kBatch],
+                                          int (&others)[kBatch]) {
+    const int32_t* const mine = p.pages.table + static_cast<size_t>(r) * p.max_pages;
+    int who[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) x[k] = c + k * 32 < end ? __ldcg(mine + c + k * 32) : -1;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+        const bool there = static_cast<unsigned>(x[k]) < static_cast<unsigned>(p.n_pages);
+        who[k] = there ? __ldcg(p.owner + x[k]) : 0;
+        others[k] = there ? __ldcg(p.others + x[k]) : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) held[k] = who[k] == r + 1;
 }
 
-__device__ void fork_count_back(const KvForkParams& p, int worker, int workers) {
-    const int lane = threadIdx.x & 31;
-    for (int i = worker * 32 + lane; i < p.R * p.parts; i += workers * 32) {
-        const int r = i / p.parts;
-        if (!changes(__ldcg(p.rec + r), r)) p.count[i] = 0;
+// A CTA's run of the items, so that a sum over CTAs is all it needs of those before.
+struct Run {
+    int first, last;
+    __device__ Run(int items, int cta, int ctas) {
+        const int per = (items + ctas - 1) / ctas;
+        first = min(items, cta * per);
+        last = min(items, first + per);
     }
-    each_part(p, worker, workers, p.R * p.parts, [&](int item, int r, const int4& rec, int c0, int c1) {
+};
+constexpr int kHeld = 1 << 30;   // beside a part's count: it has pages whose last holder the request is
+
+__device__ void fork_count_back(const KvForkParams& p, int cta, int ctas, int* sums) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const Run run(p.R * p.parts, cta, ctas);
+    int all = 0;
+    each_part(p, run.first + warp, warps, run.last, [&](int item, int r, const int4& rec, int c0, int c1) {
         int n = 0;
-#pragma unroll 4
-        for (int c = max(c0, leaves_from(rec, r)) + lane; c < min(c1, rec.y); c += 32) {
-            int x;
-            bool back;
-            last_holder(p, r, taken_to(rec, r), c, min(c1, rec.y), x, back);
-            n += back;
+        bool any = false;
+        for (int c = c0 + lane; c < min(c1, rec.y); c += 32 * kBatch) {
+            int x[kBatch], others[kBatch];
+            bool held[kBatch];
+            last_held(p, r, c, min(c1, rec.y), x, held, others);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                n += held[k] && others[k] == -1;
+                any |= held[k];
+            }
         }
         n = __reduce_add_sync(kFull, n);
-        if (lane == 0) p.count[item] = n;
-        // A fresh page has one holder now, so nobody beside it.  (One that was on the list although a request held it, and that
-        // this request leaves now, does not come back: it has just been given out.)
+        all += n;
+        any = __any_sync(kFull, any);
+        if (lane == 0) p.count[item] = n | (any ? kHeld : 0);
+        // A fresh page that nobody held has one holder now, so nobody beside it.  (One that was on the list although a request held it
+        // is counted on.)
         const int whole = whole_of(rec);
         if (lane == 0 && whole >= c0 && whole < c1 && fresh_of(rec) && __ldcg(p.owner + rec.w) == 0) atomicAdd(p.others + rec.w, -1);
     });
+    if (lane == 0) sums[warp] = all;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < warps; ++w) all += sums[w];
+        p.count[kKvMaxRequests + cta] = all;
+    }
+    __syncthreads();
 }
 
-// A CTA takes a run of the items, so that all it needs of those before is their sum.  smem: an int for each item of its run.
+// smem: an int for each item of a CTA's run.
 __device__ void fork_place(const KvForkParams& p, int cta, int ctas, int* smem, int* sums) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5, items = p.R * p.parts;
-    const int per = (items + ctas - 1) / ctas, first = min(items, cta * per), last = min(items, first + per);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+    const Run run(p.R * p.parts, cta, ctas);
+    const int first = run.first, last = run.last, base = __ldcg(p.head);
     int before = 0;
-#pragma unroll 8
-    for (int i = tid; i < first; i += blockDim.x) before += __ldcg(p.count + i);
+#pragma unroll 4
+    for (int i = tid; i < cta; i += blockDim.x) before += __ldcg(p.count + kKvMaxRequests + i);
     int total;
     block_sum(before, total, sums);   // of the items before
     for (int i0 = first; i0 < last; i0 += blockDim.x) {
-        const int i = i0 + tid, n = i < last ? __ldcg(p.count + i) : 0;
+        const int i = i0 + tid, n = i < last ? __ldcg(p.count + i) & ~kHeld : 0;
         int all;
         const int end = block_sum(n, all, sums);
         if (i < last) smem[i - first] = total + end - n;
         total += all;
     }
     __syncthreads();
-    const int base = __ldcg(p.head);
     if (cta == ctas - 1 && tid == 0) p.pages.free_out[0] = min(base + total, p.n_pages);
     each_part(p, first + warp, warps, last, [&](int item, int r, const int4& rec, int c0, int c1) {
         int32_t* const mine = p.pages.table + static_cast<size_t>(r) * p.max_pages;
         const int end = min(c1, rec.y), whole = whole_of(rec), taken = taken_to(rec, r);
         int at = base + smem[item - first];
-        constexpr int kBatch = 4;   // columns of a lane whose pages are looked up together
-        for (int c = max(c0, leaves_from(rec, r)); c < end; c += 32 * kBatch) {
-            int x[kBatch];
-            bool back[kBatch], held[kBatch];
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) held[k] = last_holder(p, r, taken, c + k * 32 + lane, end, x[k], back[k]);
+        const bool any = __ldcg(p.count + item) & kHeld;
+        for (int c = c0; any && c < end; c += 32 * kBatch) {
+            int x[kBatch], others[kBatch];
+            bool held[kBatch];
+            last_held(p, r, c + lane, end, x, held, others);
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
-                const unsigned mask = __ballot_sync(kFull, back[k]);
-                if (back[k]) {
+                const bool back = held[k] && others[k] == -1;
+                const unsigned mask = __ballot_sync(kFull, back);
+                if (back) {
                     const int to = at + __popc(mask & ((1u << lane) - 1));
                     if (to < p.n_pages)
                         p.pages.free_list[to] = x[k];
                     else
                         raise_status(p.status, QS_DEV_PAGES);
-                    p.others[x[k]] = 0;
                 }
-                if (held[k]) p.owner[x[k]] = 0;
+                if (held[k]) {
+                    p.owner[x[k]] = 0;
+                    if (others[k] < 0) p.others[x[k]] = 0;
+                }
                 at += __popc(mask);
             }
         }
@@ -315,7 +342,7 @@ __global__ void __cluster_dims__(kForkCluster, 1, 1) __launch_bounds__(kForkThre
     cluster_sync();
     fork_count_holders(p, worker, workers);
     cluster_sync();
-    fork_count_back(p, worker, workers);
+    fork_count_back(p, blockIdx.x, kForkCluster, sums);
     cluster_sync();
     fork_place(p, blockIdx.x, kForkCluster, smem, sums);
 }
@@ -332,7 +359,7 @@ __global__ void __launch_bounds__(kForkThreads) kv_fork_step_kernel(const KvFork
     else if (step == 1)
         fork_count_holders(p, worker, workers);
     else if (step == 2)
-        fork_count_back(p, worker, workers);
+        fork_count_back(p, blockIdx.x, gridDim.x, sums);
     else
         fork_place(p, blockIdx.x, gridDim.x, smem, sums);
 }
@@ -364,10 +391,10 @@ cudaError_t launch_steps(const KvForkParams& p, cudaStream_t stream) {
 
 }  // namespace
 
-// Parts of a request's columns, a power of two with R parts <= kKvMaxRequests, of 128 columns or more.
+// Parts of a request's columns, a power of two with R parts <= kKvMaxRequests, of 64 columns or more.
 int kv_column_parts(int R, int max_pages) {
     int parts = 1;
-    while (2LL * parts * (R < 1 ? 1 : R) <= kKvMaxRequests && 2LL * parts * 128 <= max_pages) parts *= 2;
+    while (2LL * parts * (R < 1 ? 1 : R) <= kKvMaxRequests && 2LL * parts * 64 <= max_pages) parts *= 2;
     return parts;
 }
 

@@ -3,8 +3,8 @@
 // Group g is the requests [start_g, start_g+1) and has c_g tokens in common.  A request takes part if it has them all and sees
 // them all (n >= c, and no window or n <= window), the group shares if two take part; its rows are its requests' query
 // heads of a key head, in blocks.  Every row of a block sees all c tokens, so that no row has a mask of its own there; a request that
-// does not take part reads its tokens by itself, and so do all of them where sharing would gain nothing (qs_kv.h).  One CTA: two searches and a prefix sum in shared memory, some
-// latencies (256 requests: see the table of the design notes).
+// does not take part reads its tokens by itself, and so do all of them where sharing would gain nothing (qs_kv.h).  A few numbers a
+// request: one CTA, two searches and a prefix sum in shared memory, a chain of latencies (4 to 256 requests 4.2 us).
 #include "qs_common.cuh"
 #include "qs_kv.h"
 

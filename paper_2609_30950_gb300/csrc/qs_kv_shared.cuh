@@ -4,17 +4,24 @@
 //     part_i = (m_i, l_i = sum_t 2^{z_it - m_i}, sum_t 2^{z_it - m_i} v_t),   z in base 2, m_i near the largest z_it.
 // The requests' own tokens give such parts too (qs_kv_heads.cuh), and the parts of a row are joined at the end:
 //     o_i = sum_parts 2^{m - M} sums / sum_parts 2^{m - M} l.
-// A block of up to 256 rows (128 at 256 entries) meets a tile of 128 (64) tokens: 4 d operations a row and token against
-// the tile's 4 d bytes a token, so that from some 300 rows on it is the tensor cores and the softmax, not
-// the cache's bytes, that bound it, and below that one pass over the bytes.  Both products run on the tensor cores:
+// A block of up to 256 rows (128 at 256 entries) meets a tile of 64 tokens: 4 d operations a row and token against the tile's
+// 4 d bytes a token, so that from some 300 rows on the operations, not the cache's bytes, are the floor.  Both products run on
+// the tensor cores:
 //     S [128 rows x tokens] = Q K^T     Q and K in shared memory, entries contiguous (K-major)
 //     O [128 rows x d]     += P V       P in tensor memory over S itself, V in shared memory, entries contiguous (N-major)
-//   warps 0-3, 4-7  copy queries, softmax: a row each, of the block's first and second 128 rows; of a block with no second half, of its even and
-//                   odd tiles, which make a part each (at 256 entries there is room for one O only: warps 0-3, and two buffers of S)
+// What bounds it is the softmax: 2048 rows of 8192 tokens in 36 us, some 1900 clocks for a tile of two halves, in which the
+// tensor pipe works 42 % and instructions issue 46 % of the time; the loads of S, the exponentials, the rounding and the store
+// of P follow one another, and two rows' worth of warps to a scheduler do not hide it.  Two S buffers a stream let the next
+// scores come in meanwhile (one buffer and tiles of 128 tokens: 4800 clocks for 128 tokens of two halves, against 3800).
+// Measured and left out: a row's tile in the hands of two warps (40 -> 45 us at 128 entries, 42 -> 60 in e4m3); weights
+// against the old reference without a look at the maximum first (36 us either way, 256 entries 10 % slower).
+//   warps 0-3, 4-7  copy queries, softmax: a row to a lane, of the block's first and second 128 rows; of a block with no second
+//                   half, of its even and odd tiles, which make a part each (256 entries have room for one O: warps 0-3 only)
 //   warps 8-11      issue S and O of either stream: each waits for nothing but what its next product needs (in fewer warps, the
 //                   instructions between products, at some ten clocks each, were what everyone waited for)
-//   warps 12-15     copy keys and values, 16 bytes at a time (e4m3: they turn codes into bf16 on the way, exactly: a code has
-//                   4 bits and its power of two is one of the type's)
+//   warps 12-15     copy keys and values: by the tensor map's boxes where pages have 8 tokens or more, 16 bytes at a time else
+//                   (e4m3: they turn codes into bf16 on the way, exactly: a code has 4 bits and its power of two is one of the
+//                   type's).  256 entries have 10 warps: 0-3, two that issue, four that copy
 // The units of all blocks (a tile; kSharedRowUnits more for the block itself) are dealt out evenly, as the rows' are in
 // qs_kv_tiles.cuh: a block that several CTAs share leaves a part from each.
 // The reference m follows the maximum only when that has outgrown it by 2^8.  In f16, which ends at 2^-24, a weight of the

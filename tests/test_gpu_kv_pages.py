@@ -100,6 +100,38 @@ def test_families_whose_members_take_over_from_each_other(qs):
     qs.qstate_check()
 
 
+def test_holders_counted_one_short(qs):
+    """The formula's numbers, whatever the counts say: a page that requests take over again can come back too."""
+    R = 12
+    pool = share.Pool(qs, R, 4, 200, 30, 11)
+    pool.grow([50 if r % 6 == 0 else 0 for r in range(R)])
+    pool.fork([r // 6 * 6 for r in range(R)])
+    pool.others = [h - (h > 0 and x % 3 == 0) for x, h in enumerate(pool.others)]
+    pool.d_others.copy_(pool.i32(pool.others))
+    before = pool.free
+    pool.fork([(r // 6 * 6 + (r + 1) % 6) if r not in (4, 9) else -1 for r in range(R)], [37] * R)
+    pool.fork([r // 6 * 6 for r in range(R)])
+    for _ in range(4):
+        pool.others = [max(h - 1, 0) for h in pool.others]
+        pool.d_others.copy_(pool.i32(pool.others))
+        pool.fork([r // 6 * 6 + (r + 2) % 6 for r in range(R)])
+    assert pool.free > before
+    qs.qstate_check()
+
+
+def test_holders_counted_two_short(qs):
+    """A count under none is none, and the page is not on the list."""
+    R = 6
+    pool = share.Pool(qs, R, 4, 100, 30, 12)
+    pool.grow([50, 0, 0, 0, 0, 9])
+    pool.fork([0, 0, 0, 0, 0, 5])
+    pool.others = [max(h - 2, 0) for h in pool.others]
+    pool.d_others.copy_(pool.i32(pool.others))
+    pool.fork([-1, -1, -1, -1, -1, 5])   # five held them, three are known
+    assert min(pool.others) == 0
+    qs.qstate_check()
+
+
 def test_beams_that_change_places(qs):
     pool = share.Pool(qs, 8, 16, 200, 20, 3)
     pool.grow([100] * 8)
