@@ -416,7 +416,8 @@ size_t qstate_kv_pages_work_bytes(const qstate_kv_cfg* cfg, int32_t R);
  * the first); otherwise it gets a page from the free list's top and moves->src[r], dst[r] say what to copy, before the next append (-1, -1
  * without, and in entries behind R; n >= R).  If the list, as it is before the call, has no page left for it, it is refused: ok[r]
  * (R bytes) is 0 and it ends; requests are served in their order.  Pages that nobody holds any more go back on the list, in the order of
- * the last request that held them and of its pages.  The table is changed in place, columns behind a request's pages
+ * the last request that held them and of its pages; others is 0 for all that no more than one of the R requests holds, so these are
+ * all that share the pool.  The table is changed in place, columns behind a request's pages
  * stay; lens_out and free_out may be lens and free_count.  Page ids outside the pool, lengths outside the table and
  * parents of R and more (which count as the request itself) set the device status. */
 int qstate_kv_fork(const qstate_kv_cfg* cfg, const qstate_kv_pages* pages, int32_t* others, const int32_t* parent,

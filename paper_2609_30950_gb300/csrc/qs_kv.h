@@ -80,11 +80,11 @@ struct KvAttendParams {
 // Tokens of a tile, and rows (requests' heads) of a block, in the attention over tokens that requests share.
 constexpr int kSharedTile = 64;
 constexpr int kv_shared_rows(int d) { return d == 256 ? 128 : 256; }
-constexpr int kSharedRowUnits = 4;
+constexpr int kSharedRowUnits = 4;   // tiles that a block of rows costs by itself: its queries, its end
 // What the launches and joins of shared tokens cost beside their tiles.  With 16-bit keys and values of 128 entries, sharing took and
 // reading by oneself took: 4 requests of 8 key heads behind 3001 tokens 19.8 and 14.7 us, 16 x 12 behind 100 34.5 and 23.6, 38 x 3 of 3
 // key heads behind 200 to 600 21.5 and 18.0; 35 x 7 of 7 key heads behind 50 to 370 34.7 and 39.7, 4 x 32 behind up to 2000 48.7 and 72.2.
-constexpr long long kSharedLeastNs = 12000;   // tiles that a block of rows costs by itself: its queries, its end
+constexpr long long kSharedLeastNs = 12000;
 
 // What qstate_kv_group leaves behind: a head, the requests' records, the groups that share anything.
 struct KvGroupHead {

@@ -12,10 +12,11 @@
 // Four steps, each of which needs all of the one before: who gets what (one CTA: R <= 8192, prefix sums and two reductions
 // in shared memory); counts of holders and the new rows, to the work space (atomic sums of whole numbers: any order gives the same, and
 // a maximum that says who held a page last); pages that come back, counted; their places, and the rows in place.  Every held
-// page is looked at, not only those of requests that change: the formula then holds whatever the counts were before.
-// Memory is read a few times and little of it; a chain of latencies bounds it (64 requests of 82 pages 9.7 us, 975 of up to 656 28.6).
+// page is looked at, not only those of requests that change, and every page's count: the formula then holds whatever the counts
+// were before.
+// Memory is read a few times and little of it; a chain of latencies bounds it (64 requests of 82 pages 10.0 us, 975 of up to 656 29.0).
 // A page that a request held and takes over again, the prefix of a beam that goes on with its sibling, needs no counting, and
-// columns are looked up four at a time, not behind one another: 12.9 -> 9.7 us for the 64.
+// columns are looked up four at a time, not behind one another: 12.9 -> 10.0 us for the 64.
 // One cluster whose CTAs meet at its barrier where tables are short, a launch a step else.  The cluster against the launches,
 // host included (in a graph), requests x columns: 64 x 82 10.0 and 13.2 us (9.6 and 11.0), 128 x 82 13.2 and 14.3 (12.8 and
 // 12.4), 256 x 82 18.4 and 14.0, 16 x 1019 14.8 and 13.7, 256 x 519 47 and 15.4.
@@ -26,7 +27,7 @@ namespace qs {
 namespace {
 
 constexpr int kForkThreads = 1024, kForkCluster = 8;   // at most; CTAs of the cluster
-constexpr int kForkClusterRequests = 256, kForkClusterEntries = 1 << 13;   // at most; a thread a request
+constexpr int kForkClusterRequests = 256, kForkClusterEntries = 1 << 13, kForkClusterPages = 1 << 14;   // at most; a thread a request
 constexpr int kBatch = 4;   // columns of a lane that are read together
 constexpr int kNoTail = -1, kBadTail = -2;
 
@@ -241,6 +242,22 @@ __device__ void fork_count_back(const KvForkParams& p, int cta, int ctas, int* s
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const Run run(p.R * p.parts, cta, ctas);
     int all = 0;
+    // A page that no request held has nobody beside its first holder, a fresh one's, if it has one.  (One that was on the list although a
+    // request held it is counted on.)
+    constexpr int kPages = 8;   // of a thread that are read together
+    const long long step = static_cast<long long>(ctas) * blockDim.x;
+    for (long long x0 = cta * blockDim.x + threadIdx.x; x0 < p.n_pages; x0 += step * kPages) {
+        int who[kPages], others[kPages];
+#pragma unroll
+        for (int k = 0; k < kPages; ++k) {
+            const bool there = x0 + k * step < p.n_pages;
+            who[k] = there ? __ldcg(p.owner + x0 + k * step) : 1;
+            others[k] = there ? __ldcg(p.others + x0 + k * step) : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < kPages; ++k)
+            if (who[k] == 0 && others[k] != 0) p.others[x0 + k * step] = 0;
+    }
     each_part(p, run.first + warp, warps, run.last, [&](int item, int r, const int4& rec, int c0, int c1) {
         int n = 0;
         bool any = false;
@@ -258,10 +275,6 @@ __device__ void fork_count_back(const KvForkParams& p, int cta, int ctas, int* s
         all += n;
         any = __any_sync(kFull, any);
         if (lane == 0) p.count[item] = n | (any ? kHeld : 0);
-        // A fresh page that nobody held has one holder now, so nobody beside it.  (One that was on the list although a request held it
-        // is counted on.)
-        const int whole = whole_of(rec);
-        if (lane == 0 && whole >= c0 && whole < c1 && fresh_of(rec) && __ldcg(p.owner + rec.w) == 0) atomicAdd(p.others + rec.w, -1);
     });
     if (lane == 0) sums[warp] = all;
     __syncthreads();
@@ -380,7 +393,9 @@ cudaError_t launch_steps(const KvForkParams& p, cudaStream_t stream) {
                                          2 * sizeof(int) * kKvMaxRequests);
     constexpr int kStepThreads = 256;
     const int items = p.R * p.parts;
-    const int need = (items + kStepThreads / 32 - 1) / (kStepThreads / 32), most = 8 * device_sm_count();
+    // a warp an item, and no more than some pages a thread
+    const int for_items = (items + kStepThreads / 32 - 1) / (kStepThreads / 32), for_pages = p.n_pages / (kStepThreads * 8);
+    const int need = for_items > for_pages ? for_items : for_pages, most = 8 * device_sm_count();
     const int grid = need < 1 ? 1 : need < most ? need : most;
     const size_t decide = 2 * sizeof(int) * static_cast<size_t>(p.R), place = sizeof(int) * static_cast<size_t>((items + grid - 1) / grid);
     for (int step = 0; step < 4 && e == cudaSuccess; ++step)
@@ -399,8 +414,9 @@ int kv_column_parts(int R, int max_pages) {
 }
 
 cudaError_t launch_kv_fork(const KvForkParams& p, cudaStream_t stream) {
-    // an item or so for each warp of the cluster, and few columns to an item
-    if (p.R <= kForkClusterRequests && static_cast<long long>(p.R) * p.max_pages <= kForkClusterEntries) return launch_cluster(p, stream);
+    // an item or so for each warp of the cluster, few columns to an item, eight pages a thread
+    if (p.R <= kForkClusterRequests && static_cast<long long>(p.R) * p.max_pages <= kForkClusterEntries && p.n_pages <= kForkClusterPages)
+        return launch_cluster(p, stream);
     return p.R <= kForkThreads ? launch_steps<1>(p, stream) : launch_steps<kKvMaxRequests / kForkThreads>(p, stream);
 }
 

@@ -9,7 +9,7 @@
 // the tensor cores:
 //     S [128 rows x tokens] = Q K^T     Q and K in shared memory, entries contiguous (K-major)
 //     O [128 rows x d]     += P V       P in tensor memory over S itself, V in shared memory, entries contiguous (N-major)
-// What bounds it is the softmax: 2048 rows of 8192 tokens in 36 us, some 1900 clocks for a tile of two halves, in which the
+// What bounds it is the softmax: 8 key heads of 1024 rows by 8192 tokens in 36 us, some 1900 clocks for a tile of two halves, in which the
 // tensor pipe works 42 % and instructions issue 46 % of the time; the loads of S, the exponentials, the rounding and the store
 // of P follow one another, and two rows' worth of warps to a scheduler do not hide it.  Two S buffers a stream let the next
 // scores come in meanwhile (one buffer and tiles of 128 tokens: 4800 clocks for 128 tokens of two halves, against 3800).

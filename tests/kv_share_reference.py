@@ -43,20 +43,20 @@ def fork(lens, table, free_list, free, others, parent, keep, page):
                     ok[r], m[r], mine = 0, 0, []
         new.append(mine)
     change = [0] * n_pages
+    last = {x: r for r in range(R) for x in old[r]}   # who held it last
     for r in range(R):
         for x in old[r]:
             change[x] -= 1
         for x in new[r]:
-            change[x] += x not in fresh
+            change[x] += x not in fresh or x in last
     count = top
-    last = {x: r for r in range(R) for x in old[r]}   # who held it last
     for r in range(R):
         for x in old[r]:
             if others[x] + change[x] == -1 and last[x] == r:
                 free_list[count] = x
                 count += 1
     for x in range(n_pages):
-        others[x] = max(others[x] + change[x], 0)
+        others[x] = max(others[x] + change[x], 0) if x in last else 0
     for r in range(R):
         table[r][: len(new[r])] = new[r]
     return dict(lens=m, free=count, src=src, dst=dst, ok=ok)

@@ -132,6 +132,22 @@ def test_holders_counted_two_short(qs):
     qs.qstate_check()
 
 
+@pytest.mark.parametrize("n_pages", [100, 40000])   # one cluster, and by steps
+def test_lengths_of_before_with_tables_of_after(qs, n_pages):
+    """A call made again on the lengths it has replaced: counts, list and tables by the formula, though they do not agree."""
+    R = 12
+    pool = share.Pool(qs, R, 4, n_pages, 30, 13)
+    pool.grow([20 + 3 * r for r in range(R)] if n_pages > 100 else [5 + r for r in range(R)])
+    lens = list(pool.lens)
+    pool.others[pool.free_list[0]] = 3   # of a page that nobody holds
+    pool.d_others.copy_(pool.i32(pool.others))
+    for k in range(3):
+        pool.fork([r // 4 * 4 + (r * (k + 2) + 1) % 4 if r % 5 else -1 for r in range(R)])
+        pool.lens = list(lens)
+        pool.pages.lens.copy_(pool.i32(lens))
+    qs.qstate_check()
+
+
 def test_beams_that_change_places(qs):
     pool = share.Pool(qs, 8, 16, 200, 20, 3)
     pool.grow([100] * 8)
