@@ -892,8 +892,9 @@ def qstate_kv_attend_shared(cfg: KvConfig, cache: KvCache, q, table, lens, group
     if groups.R != R:
         raise ValueError(f"groups were made for {groups.R} requests, got {R}")
     made = groups._made
-    if made is not None and made is not cfg and (made.Hq, made.Hkv, made.dk, made.window) != (cfg.Hq, cfg.Hkv, cfg.dk, cfg.window):
-        raise ValueError("groups were made for a layer of other heads or another window")
+    if made is not None and made is not cfg and (made.Hq, made.Hkv, made.dk, made.window, made.store) != (
+            cfg.Hq, cfg.Hkv, cfg.dk, cfg.window, cfg.store):
+        raise ValueError("groups were made for a layer of other heads, another window or another store")
     rc = (_lib or load()).qstate_kv_attend_shared(cfg._at, cache._at, q.data_ptr(), qr, qh, table.data_ptr(), lens.data_ptr(), R,
                                                   groups._at, o.data_ptr(), sums,
                                                   _work_of("qstate_kv_shared_work_bytes", cfg, work, R),

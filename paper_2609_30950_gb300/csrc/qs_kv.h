@@ -80,6 +80,9 @@ struct KvAttendParams {
 // Tokens of a tile, and rows (requests' heads) of a block, in the attention over tokens that requests share.
 constexpr int kSharedTile = 64;
 constexpr int kv_shared_rows(int d) { return d == 256 ? 128 : 256; }
+// What groups are marked with: they are dealt out otherwise where keys and values are codes.
+constexpr int kv_shared_mark(int d, bool e4m3) { return kv_shared_rows(d) + (e4m3 ? 1 : 0); }
+constexpr int kSharedWeight = 3, kSharedHalfWeight = 2;   // units of a tile; of a block with one half (see SharedPart)
 constexpr int kSharedRowUnits = 4;   // tiles that a block of rows costs by itself: its queries, its end
 // What the launches and joins of shared tokens cost beside their tiles.  With 16-bit keys and values of 128 entries, sharing took and
 // reading by oneself took: 4 requests of 8 key heads behind 3001 tokens 19.8 and 14.7 us, 16 x 12 behind 100 34.5 and 23.6, 38 x 3 of 3
@@ -89,7 +92,7 @@ constexpr long long kSharedLeastNs = 12000;
 // What qstate_kv_group leaves behind: a head, the requests' records, the groups that share anything.
 struct KvGroupHead {
     int groups;              // that share
-    int R, Hq, Hkv, tile, rows;
+    int R, Hq, Hkv, tile, rows;   // rows: kv_shared_mark
     long long units;         // of all blocks
 };
 struct KvGroup {
@@ -116,6 +119,7 @@ struct KvGroupParams {
     // for each half of a block of rows (e4m3: for each block).
     float alone_ns, block_ns;
     int half_rows;           // of what block_ns is for
+    int light_rows;          // a block of up to so many has kSharedHalfWeight
     long long least_ns;      // that sharing has to gain, over all groups and key heads; 0: whatever it costs
     KvGroupHead head;        // host: what the head is to say, but for sums
     KvGroupHead* out;

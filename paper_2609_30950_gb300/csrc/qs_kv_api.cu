@@ -414,12 +414,13 @@ int qstate_kv_group(const qstate_kv_cfg* cfg, const int32_t* lens, int32_t R, co
     p.alone_ns = (e4m3 ? 0.026f : 0.023f) * cfg->dk;
     p.block_ns = e4m3 ? 0.1f * cfg->dk : cfg->dk == 64 ? 3.0f : cfg->dk == 128 ? 3.3f : 8.6f;
     p.half_rows = e4m3 ? p.rows : 128;
+    p.light_rows = !e4m3 && p.rows == 256 ? 128 : 0;
     p.least_ns = shared_least_ns();
     p.head.R = R;
     p.head.Hq = cfg->Hq;
     p.head.Hkv = cfg->Hkv;
     p.head.tile = p.tile;
-    p.head.rows = p.rows;
+    p.head.rows = kv_shared_mark(cfg->dk, e4m3);
     char* const base = static_cast<char*>(groups);
     p.out = reinterpret_cast<KvGroupHead*>(base);
     p.groups = reinterpret_cast<KvGroup*>(base + kKvGroupHeadBytes);

@@ -101,7 +101,9 @@ __global__ void __launch_bounds__(kMostThreads) kv_group_kernel(const KvGroupPar
         const float halves = static_cast<float>((rows + p.half_rows - 1) / p.half_rows);
         const float gain = (static_cast<float>(count[g]) * tiles * p.alone_ns - halves * (tiles + kSharedRowUnits) * p.block_ns) * p.Hkv;
         if (p.least_ns > 0 && gain <= 0.0f) return Sums{0, 0, 0, 0};
-        return Sums{static_cast<long long>(blocks) * p.Hkv * (tiles + kSharedRowUnits), static_cast<long long>(gain), 1, blocks * p.Hkv};
+        const bool light = rows - static_cast<long long>(blocks - 1) * p.rows <= p.light_rows;
+        const long long units = static_cast<long long>(tiles + kSharedRowUnits) * ((blocks - 1) * kSharedWeight + (light ? kSharedHalfWeight : kSharedWeight));
+        return Sums{units * p.Hkv, static_cast<long long>(gain), 1, blocks * p.Hkv};
     };
     Sums mine{0, 0, 0, 0};
     for (int g = g0; g < g1; ++g) mine = plus(mine, sums_of(g));

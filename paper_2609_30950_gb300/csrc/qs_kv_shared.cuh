@@ -22,7 +22,7 @@
 //   warps 12-15     copy keys and values: by the tensor map's boxes where pages have 8 tokens or more, 16 bytes at a time else
 //                   (e4m3: they turn codes into bf16 on the way, exactly: a code has 4 bits and its power of two is one of the
 //                   type's).  256 entries have 10 warps: 0-3, two that issue, four that copy
-// The units of all blocks (a tile; kSharedRowUnits more for the block itself) are dealt out evenly, as the rows' are in
+// The units of all blocks (some for a tile; those of kSharedRowUnits tiles more for the block itself) are dealt out evenly, as the rows' are in
 // qs_kv_tiles.cuh: a block that several CTAs share leaves a part from each.
 // The reference m follows the maximum only when that has outgrown it by 2^8.  In f16, which ends at 2^-24, a weight of the
 // reference is 2^7, and the reference also goes down, to a tile whose largest weight is under 2^-16 of it (see
@@ -66,11 +66,39 @@ struct SharedMisc {
     int abort;
 };
 
-// A worker's units, part after part: a part is the worker's tiles of one block of rows.
+// A worker's units, part after part: a part is the worker's tiles of one block of rows, those whose first unit is in its share.
+// kHalves: a tile of a block with one half weighs two units, others three (1270 and 1900 clocks): 304 rows of four key heads by 100000
+// tokens 99.1 -> 90.6 us; 1024 rows of eight by 8192, all blocks alike, 80.6 -> 81.7.  In e4m3, where the copying warps set the pace,
+// all are the same.
+template <int kRows, bool kHalves>
 struct SharedPart {
     KvGroup g;
     int e, hb, tile, count, tiles;   // group; key head and block of rows in one; first tile and how many; the block's
     int left;                        // units from the first tile to the share's end
+
+    __device__ __forceinline__ int weight_of(int block) const {
+        return kHalves && g.rows - block * kRows <= 128 ? kSharedHalfWeight : kSharedWeight;
+    }
+    __device__ __forceinline__ int weight() const { return weight_of(hb % g.blocks); }
+    // Shares are no smaller than a tile weighs, so that every one between a block's first and last has a tile of it.
+    static __device__ __forceinline__ int sharing(long long units, int workers) {
+        return units < static_cast<long long>(workers) * kSharedWeight ? static_cast<int>(units) / kSharedWeight : workers;
+    }
+    // Of a key head's blocks; only the last may have one half.
+    __device__ __forceinline__ long long head_units() const {
+        return static_cast<long long>(tiles + kSharedRowUnits) * ((g.blocks - 1) * kSharedWeight + weight_of(g.blocks - 1));
+    }
+    // The first unit of this block's last tile.
+    __device__ __forceinline__ long long last_tile() const {
+        const int kv = hb / g.blocks, b = hb - kv * g.blocks;
+        return g.unit0 + kv * head_units() + static_cast<long long>(tiles + kSharedRowUnits) * (b * kSharedWeight) +
+               static_cast<long long>(tiles + kSharedRowUnits - 1) * weight_of(b);
+    }
+    // The block's tiles from this one on, as far as the share goes.
+    __device__ __forceinline__ void from(int first, int weight) {
+        tile = first;
+        count = min(tiles - first, static_cast<int>(static_cast<unsigned>(left + weight - 1) / static_cast<unsigned>(weight)));
+    }
 
     __device__ __forceinline__ void take(const int4& a, const int4& b, int kTile) {
         g.first = a.x, g.rows = a.y, g.owner = a.z, g.tokens = a.w;
@@ -86,8 +114,10 @@ struct SharedPart {
     }
     // a and b: this lane's group, of the first 32, as they lie in memory (anything behind the last group); a whole warp.
     __device__ __forceinline__ bool start(const KvGroupHead& head, const KvGroup* groups, const int4& a, const int4& b, int worker,
-                                          int workers, int kTile) {
-        const long long u0 = share_start(head.units, worker, workers), u1 = share_start(head.units, worker + 1, workers);
+                                          int workers, int Hkv, int kTile) {
+        const int n = sharing(head.units, workers);
+        if (worker >= n) return false;
+        const long long u0 = share_start(head.units, worker, n), u1 = share_start(head.units, worker + 1, n);
         left = static_cast<int>(u1 - u0);
         if (left <= 0) return false;
         const long long mine = static_cast<long long>(static_cast<unsigned>(b.z)) | static_cast<long long>(b.w) << 32;
@@ -100,42 +130,49 @@ struct SharedPart {
             auto from = [&](int v) { return __shfl_sync(kFull, v, l); };
             take(make_int4(from(a.x), from(a.y), from(a.z), from(a.w)), make_int4(from(b.x), from(b.y), from(b.z), from(b.w)), kTile);
         } else {
-            int lo = 31, n = head.groups - 31;
-            while (n > 1) {
-                const int half = n >> 1;
+            int lo = 31, many = head.groups - 31;
+            while (many > 1) {
+                const int half = many >> 1;
                 if (__ldcg(&groups[lo + half].unit0) <= u0) {
                     lo += half;
-                    n -= half;
+                    many -= half;
                 } else {
-                    n = half;
+                    many = half;
                 }
             }
             load(groups, lo, kTile);
         }
-        const int per = tiles + kSharedRowUnits;
-        const long long at = u0 - g.unit0;
-        hb = static_cast<int>(divided(at, per));
-        tile = static_cast<int>(at - static_cast<long long>(hb) * per) - kSharedRowUnits;
-        if (tile < 0) {
-            left += tile;
-            tile = 0;
-        }
-        count = min(tiles - tile, left);
+        const int per = (tiles + kSharedRowUnits) * kSharedWeight;   // of a block
+        const long long at = u0 - g.unit0, all = head_units();
+        const long long kv = all >> 31 ? at / all : divided(at, static_cast<int>(all)), in_kv = at - kv * all;
+        const int block = min(static_cast<int>(divided(in_kv, per)), g.blocks - 1);
+        hb = static_cast<int>(kv) * g.blocks + block;
+        const int weight = weight_of(block);
+        const int in_block = static_cast<int>(in_kv - static_cast<long long>(block) * per);
+        const int first = max((in_block + weight - 1) / weight - kSharedRowUnits, 0);
+        left -= (first + kSharedRowUnits) * weight - in_block;   // to the first tile that begins in the share
+        if (first == tiles) return behind(groups, Hkv, kTile);
+        from(first, weight);
         return left > 0;
     }
-    __device__ __forceinline__ bool next(const KvGroup* groups, int Hkv, int kTile) {
-        left -= count + kSharedRowUnits;
+    // What is left begins behind this block.
+    __device__ __forceinline__ bool behind(const KvGroup* groups, int Hkv, int kTile) {
         if (left <= 0) return false;
-        tile = 0;
         if (++hb == g.blocks * Hkv) {
             hb = 0;
             load(groups, e + 1, kTile);
         }
-        count = min(tiles, left);
-        return true;
+        const int to = weight();
+        left -= kSharedRowUnits * to;
+        from(0, to);
+        return left > 0;
+    }
+    __device__ __forceinline__ bool next(const KvGroup* groups, int Hkv, int kTile) {
+        left -= count * weight();
+        return behind(groups, Hkv, kTile);
     }
     __device__ __forceinline__ int kv() const { return hb / g.blocks; }
-    __device__ __forceinline__ int row0(int kRows) const { return hb % g.blocks * kRows; }
+    __device__ __forceinline__ int row0() const { return hb % g.blocks * kRows; }
     __device__ __forceinline__ bool whole() const { return count == tiles; }
 };
 
@@ -256,7 +293,8 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
         head.units = static_cast<long long>(static_cast<unsigned>(h1.z)) | static_cast<long long>(h1.w) << 32;
     }
     // groups that were made for other requests or another kind of layer are none
-    const bool fits = head.groups == 0 || (head.R == p.R && head.Hq == p.Hq && head.Hkv == p.Hkv && head.tile == kTile && head.rows == S::kRows);
+    const bool fits = head.groups == 0 || (head.R == p.R && head.Hq == p.Hq && head.Hkv == p.Hkv && head.tile == kTile &&
+                                              head.rows == kv_shared_mark(D, kE4M3));
     if (!fits && tid == 0) raise_status(p.status, QS_DEV_PAGES);
     tc::fence_before_sync();
     __syncthreads();
@@ -264,11 +302,12 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
     const uint32_t tmem = __shfl_sync(kFull, x.tmem, 0);
     volatile int* const abort = &x.abort;
     const int G = p.Hq / p.Hkv;
-    SharedPart w;
+    using Part = SharedPart<S::kRows, S::kM == 2 && !kE4M3>;
+    Part w;
     int copied = 0;   // tensors that this warp has begun to copy
     // a limit of no polls gives up at the first wait
     if (fits && head.groups > 0 && p.wait_polls == 0 && tid == 0) raise_status(p.status, QS_DEV_TIMEOUT);
-    const bool live = fits && head.groups > 0 && p.wait_polls > 0 && w.start(head, groups, g0, g1, worker, p.workers, kTile);
+    const bool live = fits && head.groups > 0 && p.wait_polls > 0 && w.start(head, groups, g0, g1, worker, p.workers, p.Hkv, kTile);
     // Streams have their own S, P, O and softmax warps.  They are a block's halves (`two`), or, where it has one half, the part's
     // even and odd tiles.
     const bool fences = !kE4M3 && !box_rows;   // copies by cp.async, whose writes the product's issuer makes visible to the tensor core
@@ -444,7 +483,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
         int s = scores ? 0 : 1, phase = 0, parts = 0, n = 0;   // n: jobs that have been issued
         bool ok = true, more = true;
         while (more && ok) {
-            const bool two = two_halves(min(S::kRows, w.g.rows - w.row0(S::kRows)));
+            const bool two = two_halves(min(S::kRows, w.g.rows - w.row0()));
             const uint32_t dq = desc_lo(base + (two ? stream * S::kQTile : 0), 16);
             if (scores) {
                 ok = phase_wait(&x.qfull, parts++ & 1, abort, p);
@@ -503,7 +542,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
         float m = -INFINITY, high = -INFINITY, l = 0.0f, lr = 0.0f;   // reference, the highest so far, sums of p and of rounded p
         // Queries of w's block, this warp's 32 rows: a lane looks up a row, eight lanes copy it.
         auto queries = [&]() {
-            const int i0 = w.row0(S::kRows), rows = min(S::kRows, w.g.rows - i0), first = stream * 128 + (warp & 3) * 32, sg = lane & 7;
+            const int i0 = w.row0(), rows = min(S::kRows, w.g.rows - i0), first = stream * 128 + (warp & 3) * 32, sg = lane & 7;
             const bool in = first + lane < rows;
             const int at_row = i0 + first + lane, member = in ? at_row / G : 0;
             const uint16_t* const mine = static_cast<const uint16_t*>(p.q) + (w.g.first + member) * p.q_row +
@@ -536,7 +575,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
         queries();
         int n = 0, i = 0, parts = 0;   // the stream's jobs, all tiles
         for (bool more = true; more;) {
-            const int i0 = w.row0(S::kRows), rows = min(S::kRows, w.g.rows - i0);
+            const int i0 = w.row0(), rows = min(S::kRows, w.g.rows - i0);
             const bool two = two_halves(rows);
             bool any = false;   // the stream has had a tile of this part
             m = high = -INFINITY;
@@ -624,7 +663,10 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                 ++n;
             }
             // ---- the part's end ----
-            const SharedPart was = w;
+            const Part was = w;
+            const bool whole = was.whole();
+            int many = 1;   // workers that have a part of the block
+            if (tid == 0 && was.tile == 0 && !whole) many = share_owner(head.units, was.last_tile(), Part::sharing(head.units, p.workers)) - worker + 1;
             more = w.next(groups, p.Hkv, kTile);
             if (more) {
                 phase_wait(&x.qfree, parts++ & 1, abort, p);   // S of this part is done with its queries
@@ -632,7 +674,6 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
             }
             if (any) phase_wait(&x.odone[S::buffer(stream, n - 1)], S::phase(n - 1), abort, p);
             tc::fence_after_sync();
-            const bool whole = was.whole();
             const int at = two ? stream * 128 + row : row, at_row = i0 + at, member = at_row / G;   // of the block, of the group
             const size_t slot = part_slot(worker, was.tile == 0);
             const size_t out_row = (two ? 0 : static_cast<size_t>(stream) * p.R * p.Hq) +
@@ -659,8 +700,6 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                 }
             }
             if (tid == 0 && was.tile == 0) {
-                const long long last = was.g.unit0 + static_cast<long long>(was.hb + 1) * (was.tiles + kSharedRowUnits) - 1;
-                const int many = whole ? 1 : share_owner(head.units, last, p.workers) - worker + 1;
                 p.pre_dir[was.g.block0 + was.hb] = make_int2(whole ? -1 : worker, kM == 2 && !two ? -many : many);
             }
             tc::fence_before_sync();

@@ -32,11 +32,11 @@ __device__ __forceinline__ int clamped_len(const KvAttendParams& p, int r, bool 
     return n < 0 ? 0 : static_cast<int>(most);
 }
 
-// Whether the groups were made for these requests and this kind of layer, in blocks of `rows`; others count as none.
-__device__ __forceinline__ bool groups_fit(const KvAttendParams& p, int rows) {
+// Whether the groups were made for these requests and this kind of layer (kv_shared_mark); others count as none.
+__device__ __forceinline__ bool groups_fit(const KvAttendParams& p, int mark) {
     const int4* const head = reinterpret_cast<const int4*>(p.groups);
     const int4 a = __ldcg(head), b = __ldcg(head + 1);   // KvGroupHead
-    return a.x > 0 && a.y == p.R && a.z == p.Hq && a.w == p.Hkv && b.x == kSharedTile && b.y == rows;
+    return a.x > 0 && a.y == p.R && a.z == p.Hq && a.w == p.Hkv && b.x == kSharedTile && b.y == mark;
 }
 
 // kShared: without the tokens that request r shares with others, which another kernel reads.
