@@ -339,6 +339,31 @@ def test_groups_of_another_layer_are_refused(qs):
     b.check(qs)
 
 
+def test_groups_of_another_store_are_refused(qs):
+    b = share.Batch(qs, [300, 310, 305], [(0, 3, 280)], 4, 2, 128, seed=22)
+    codes = share.Batch(qs, [300, 310, 305], [(0, 3, 280)], 4, 2, 128, e4m3=True, seed=22)
+    codes.group(qs)
+    with pytest.raises(ValueError):
+        qs.qstate_kv_attend_shared(b.cfg, b.cache, b.q, b.d_table, b.d_lens, codes.d_groups, b.o, b.lse, b.work)
+    groups = qs.KvGroups(torch.zeros_like(codes.d_groups.data), 3)   # through the C interface: reported on the device
+    groups.data.copy_(codes.d_groups.data)
+    qs.qstate_kv_attend_shared(b.cfg, b.cache, b.q, b.d_table, b.d_lens, groups, b.o, b.lse, b.work)
+    with pytest.raises(qs.QstateError):
+        qs.qstate_check()
+    check(qs, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+def test_few_units_for_many_workers(qs, dtype):
+    """Blocks of one and of two halves with so few tiles that not every worker has one."""
+    lens, groups = [], []
+    for members, common in ((2, 1), (33, 64), (9, 65), (40, 130), (3, 200)):
+        groups.append((len(lens), len(lens) + members, common))
+        lens += [common + i % 3 for i in range(members)]
+    check(qs, share.Batch(qs, lens, groups, 8, 1, 128, e4m3=dtype == "e4m3", seed=23))
+    check(qs, share.Batch(qs, lens, groups[:1], 8, 1, 64, e4m3=dtype == "e4m3", seed=24))
+
+
 def test_the_work_space_serves_the_other_attention_too(qs):
     b = share.Batch(qs, LENS, GROUPS, 8, 2, 128, seed=21)
     check(qs, b)
