@@ -99,8 +99,12 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
     const int groups = p.Hkv * groups_per_kv, G = p.Hq / p.Hkv;
 
     Share& share = *reinterpret_cast<Share*>(smem + S::kShare);
+    const bool fits = kShared && groups_fit(p, kv_shared_mark(D, kE4M3));
+    if (kShared && tid == 0) share.fits = fits;
     if (!p.whole_rows)
-        make_share<S::kThreads, S::kTile, S::kChunk, kShared>(p, groups, blockIdx.x, reinterpret_cast<long long*>(smem + S::kScratch), &share);
+        make_share<S::kThreads, S::kTile, S::kChunk, kShared>(p, groups, blockIdx.x, reinterpret_cast<long long*>(smem + S::kScratch), &share, fits);
+    else if (kShared)
+        __syncthreads();
     int split = 0;   // parts of the row that this CTA begins and others end
     Walk<S::kTile, S::kChunk, kShared> cw;
     bool live = cw.start(p, share, groups, blockIdx.x);
@@ -203,7 +207,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
         if (fetching) {
             fetch(stage);
             row_begins = fw.ends(p);
-            fetching = fw.next(p, groups);
+            fetching = fw.next(p, share, groups);
             if (fetching) look_up();
         }
         cp_commit();
@@ -540,7 +544,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
             __syncthreads();
             const float* const all = reinterpret_cast<const float*>(smem + stage * S::kSlot);
             const size_t out_row = static_cast<size_t>(cw.r) * p.Hq + h0;
-            const bool joined = kShared && p.shared[cw.r].x > 0;   // with shared tokens' parts
+            const bool joined = kShared && share.fits && p.shared[cw.r].x > 0;   // with shared tokens' parts
             auto finish = [&](int row, int col, float4 acc, float4 sums) {
                 if (joined) {
                     reinterpret_cast<float4*>(p.store)[((out_row + row) * D + col) / 4] = acc;
@@ -602,7 +606,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
         __syncwarp();
         fetch_next(stage);
         stage = stage + 1 == kStages ? 0 : stage + 1;
-        live = cw.next(p, groups);
+        live = cw.next(p, share, groups);
     }
     for (int r = blockIdx.x; r < p.R; r += p.workers)   // requests without tokens
         if (clamped_len(p, r, true) == 0 && !kShared) {

@@ -20,6 +20,11 @@ constexpr int kJoinRows = 8, kJoinBatch = 4;   // rows of a CTA, parts in flight
 template <int D>
 __host__ __device__ constexpr int join_shares() { return D == 64 ? 8 : D == 128 ? 4 : 2; }
 
+// Whether a row's parts (KvAttendParams::dir), where it has any, lie with the workers that there are.
+__device__ __forceinline__ bool has_place(const int2& dir, bool any, int workers) {
+    return !any || (dir.x < 0 ? dir.x >= -2 && dir.y == (dir.x == -1 ? 1 : 0) : dir.y > 0 && dir.x + static_cast<unsigned>(dir.y) <= static_cast<unsigned>(workers));
+}
+
 template <int D, bool kF16, bool kMany>
 __global__ void __launch_bounds__(D * (kMany ? join_shares<D>() : 1)) kv_join_shared_kernel(const KvAttendParams p, const JoinGeo g) {
     constexpr int kColumns = D / 32, kShares = kMany ? join_shares<D>() : 1, kRows = kv_shared_rows(D);
@@ -40,6 +45,12 @@ __global__ void __launch_bounds__(D * (kMany ? join_shares<D>() : 1)) kv_join_sh
     chain_wait();
     if (has_own) own_dir = __ldcg(p.dir + static_cast<size_t>(r) * groups + kv * g.groups_per_kv + in_kv / g.per_group);
     if (has_pre) pre_dir = __ldcg(p.pre_dir + rec.y + kv * rec.z + (rec.w + in_kv) / kRows);
+    // Places that no worker has: calls that use the work space at once, from two streams.  They are not followed.
+    const bool bad = !has_place(own_dir, has_own, p.workers) || !has_place(make_int2(pre_dir.x, abs(pre_dir.y)), has_pre, kKvSms) || pre_dir.x < -1;
+    if (bad) {
+        raise_status(p.status, QS_DEV_PAGES);
+        own_dir = pre_dir = make_int2(0, 0);
+    }
     // The parts' places, in float4 of references (of sums: D / 4 times as much, but that shared tokens' parts lie column by
     // column in a slot): 32 bits, and few instructions, whose latencies are what a join takes.  Part 0 of a split row is in the first
     // worker's slot 1, part k behind it in slot 0 of the k-th worker on.

@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
             const bool first = begins;
             begins = w.ends(p);
             W after = w;
-            const bool more = after.next(p, 1);
+            const bool more = after.next(p, share, 1);
             uint64_t mask = 0;   // tokens that are seen: lanes take two each
             if (g.boxes) {
                 const int begin = w.span.begin - w.span.base - w.tile * kLatTile, end = w.span.end - w.span.base - w.tile * kLatTile;
@@ -656,7 +656,7 @@ __global__ void __launch_bounds__(kLatThreads, latent_ctas(DV, kN)) kv_latent_ke
             prev_phase = phase;
             if (++s == g.stages) s = 0, phase ^= 1;
             begins = ends;
-            live = w.next(p, 1);
+            live = w.next(p, share, 1);
         }
     }
     if (!p.whole_rows && group == 0 && tid == 0) p.split[worker] = split;

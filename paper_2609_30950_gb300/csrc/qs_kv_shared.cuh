@@ -280,6 +280,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
     // the head, and a lane's group of the first 32 (there is room for most_groups)
     KvGroupHead head;
     int4 g0 = make_int4(0, 0, 0, 0), g1 = g0;
+    bool fits;
     {
         const int4* const src = reinterpret_cast<const int4*>(head_at);
         const int4 h0 = __ldcg(src), h1 = __ldcg(src + 1);
@@ -287,15 +288,11 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
             g0 = __ldcg(reinterpret_cast<const int4*>(groups + lane));
             g1 = __ldcg(reinterpret_cast<const int4*>(groups + lane) + 1);
         }
-        head.groups = h0.x, head.R = h0.y, head.Hq = h0.z, head.Hkv = h0.w;
-        head.tile = h1.x;
-        head.rows = h1.y;
+        head.groups = h0.x;
         head.units = static_cast<long long>(static_cast<unsigned>(h1.z)) | static_cast<long long>(h1.w) << 32;
+        fits = groups_fit(p, kv_shared_mark(D, kE4M3), h0, h1);
     }
-    // groups that were made for other requests or another kind of layer are none
-    const bool fits = head.groups == 0 || (head.R == p.R && head.Hq == p.Hq && head.Hkv == p.Hkv && head.tile == kTile &&
-                                              head.rows == kv_shared_mark(D, kE4M3));
-    if (!fits && tid == 0) raise_status(p.status, QS_DEV_PAGES);
+    if (head.groups != 0 && !fits && tid == 0) raise_status(p.status, QS_DEV_PAGES);
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
@@ -306,8 +303,8 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
     Part w;
     int copied = 0;   // tensors that this warp has begun to copy
     // a limit of no polls gives up at the first wait
-    if (fits && head.groups > 0 && p.wait_polls == 0 && tid == 0) raise_status(p.status, QS_DEV_TIMEOUT);
-    const bool live = fits && head.groups > 0 && p.wait_polls > 0 && w.start(head, groups, g0, g1, worker, p.workers, p.Hkv, kTile);
+    if (fits && p.wait_polls == 0 && tid == 0) raise_status(p.status, QS_DEV_TIMEOUT);
+    const bool live = fits && p.wait_polls > 0 && w.start(head, groups, g0, g1, worker, p.workers, p.Hkv, kTile);
     // Streams have their own S, P, O and softmax warps.  They are a block's halves (`two`), or, where it has one half, the part's
     // even and odd tiles.
     const bool fences = !kE4M3 && !box_rows;   // copies by cp.async, whose writes the product's issuer makes visible to the tensor core

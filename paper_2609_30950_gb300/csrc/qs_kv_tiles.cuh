@@ -32,20 +32,24 @@ __device__ __forceinline__ int clamped_len(const KvAttendParams& p, int r, bool 
     return n < 0 ? 0 : static_cast<int>(most);
 }
 
-// Whether the groups were made for these requests and this kind of layer (kv_shared_mark); others count as none.
-__device__ __forceinline__ bool groups_fit(const KvAttendParams& p, int mark) {
-    const int4* const head = reinterpret_cast<const int4*>(p.groups);
-    const int4 a = __ldcg(head), b = __ldcg(head + 1);   // KvGroupHead
+// Whether the groups, whose head (KvGroupHead) begins with a and b, were made for these requests and this kind of layer
+// (kv_shared_mark).  Others count as none, in the kernel of shared tokens, in that of a request's own and in the join alike: what
+// one of them left out, or did not write, no other would make up for.
+__device__ __forceinline__ bool groups_fit(const KvAttendParams& p, int mark, const int4& a, const int4& b) {
     return a.x > 0 && a.y == p.R && a.z == p.Hq && a.w == p.Hkv && b.x == kSharedTile && b.y == mark;
 }
+__device__ __forceinline__ bool groups_fit(const KvAttendParams& p, int mark) {
+    const int4* const head = reinterpret_cast<const int4*>(p.groups);
+    return groups_fit(p, mark, __ldcg(head), __ldcg(head + 1));
+}
 
-// kShared: without the tokens that request r shares with others, which another kernel reads.
+// kShared: without the tokens that request r shares with others, which another kernel reads, if the groups fit.
 template <int kTile, int kGrain, bool kShared>
-__device__ __forceinline__ Span span_of(const KvAttendParams& p, int r, int n) {
+__device__ __forceinline__ Span span_of(const KvAttendParams& p, int r, int n, bool fits) {
     Span s;
     s.end = n;
     s.begin = p.window > 0 && n > p.window ? n - p.window : 0;
-    if (kShared) s.begin = min(max(s.begin, p.shared[r].x), n);
+    if (kShared && fits) s.begin = min(max(s.begin, p.shared[r].x), n);
     s.base = s.begin & ~(kGrain - 1);
     s.tiles = kShared && s.begin == n ? 0 : (n - s.base + kTile - 1) / kTile;
     return s;
@@ -60,6 +64,7 @@ struct Share {
     long long total;        // units of all rows
     long long u0, u1;
     int r, group, pos;      // where u0 is; tile t of a row is at pos kRowUnits + t
+    int fits;               // kShared: groups_fit
 };
 
 __device__ __forceinline__ long long divided(long long a, int b) {   // a >= 0, b > 0; 32 bits are mostly enough, and a tenth of the time
@@ -78,16 +83,17 @@ __device__ __forceinline__ int share_owner(long long total, long long u, int wor
 
 __device__ __forceinline__ int row_units(int tiles) { return tiles > 0 ? tiles + kRowUnits : 0; }
 
-// All threads of the CTA; `groups` rows a request.  scratch: kThreads / 32 + 2 long longs of shared memory; *out too.
+// All threads of the CTA; `groups` rows a request.  scratch: kThreads / 32 + 2 long longs of shared memory; *out too (`fits` is
+// the caller's to store).
 template <int kThreads, int kTile, int kGrain, bool kShared = false>
-__device__ __forceinline__ void make_share(const KvAttendParams& p, int groups, int worker, long long* scratch, Share* out) {
+__device__ __forceinline__ void make_share(const KvAttendParams& p, int groups, int worker, long long* scratch, Share* out, bool fits = false) {
     constexpr int kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (p.R + kThreads - 1) / kThreads, r0 = min(p.R, tid * per), r1 = min(p.R, r0 + per);
     long long mine = 0;
     int tiles = 0;
     for (int r = r0; r < r1; ++r) {
-        tiles = row_units(span_of<kTile, kGrain, kShared>(p, r, clamped_len(p, r, false)).tiles);
+        tiles = row_units(span_of<kTile, kGrain, kShared>(p, r, clamped_len(p, r, false), fits).tiles);
         mine += tiles;
     }
     long long before = mine;
@@ -118,7 +124,7 @@ __device__ __forceinline__ void make_share(const KvAttendParams& p, int groups, 
         int r = r0;
         if (per > 1)
             for (; r < r1; ++r) {
-                tiles = row_units(span_of<kTile, kGrain, kShared>(p, r, clamped_len(p, r, false)).tiles);
+                tiles = row_units(span_of<kTile, kGrain, kShared>(p, r, clamped_len(p, r, false), fits).tiles);
                 if (at < static_cast<long long>(tiles) * groups) break;
                 at -= static_cast<long long>(tiles) * groups;
             }
@@ -143,34 +149,34 @@ struct Walk {
         tile = 0;
         if (p.whole_rows) {
             left = worker - p.workers;
-            return next_row(p, groups);
+            return next_row(p, s, groups);
         }
         left = static_cast<int>(s.u1 - s.u0);
         if (left <= 0) return false;
         r = s.r;
         group = s.group;
         tile = s.pos - kRowUnits;
-        span = span_of<kTile, kGrain, kShared>(p, r, clamped_len(p, r, false));
+        span = span_of<kTile, kGrain, kShared>(p, r, clamped_len(p, r, false), kShared && s.fits);
         if (tile < 0) {
             left += tile;
             tile = 0;
         }
         return left > 0;
     }
-    __device__ __forceinline__ bool next_row(const KvAttendParams& p, int groups) {
+    __device__ __forceinline__ bool next_row(const KvAttendParams& p, const Share& s, int groups) {
         tile = 0;
         do {
             left += p.workers;
             if (left >= p.R * groups) return false;
             r = left / groups;
             group = left - r * groups;
-            span = span_of<kTile, kGrain, kShared>(p, r, clamped_len(p, r, false));
+            span = span_of<kTile, kGrain, kShared>(p, r, clamped_len(p, r, false), kShared && s.fits);
         } while (span.tiles == 0);
         return true;
     }
     // to the next unit, if there is one
-    __device__ __forceinline__ bool next(const KvAttendParams& p, int groups) {
-        if (p.whole_rows) return ++tile < span.tiles || next_row(p, groups);
+    __device__ __forceinline__ bool next(const KvAttendParams& p, const Share& s, int groups) {
+        if (p.whole_rows) return ++tile < span.tiles || next_row(p, s, groups);
         if (--left <= 0) return false;
         if (++tile < span.tiles) return true;
         tile = 0;
@@ -180,7 +186,7 @@ struct Walk {
         group = 0;
         do {
             ++r;
-            span = span_of<kTile, kGrain, kShared>(p, r, clamped_len(p, r, false));
+            span = span_of<kTile, kGrain, kShared>(p, r, clamped_len(p, r, false), kShared && s.fits);
         } while (span.tiles == 0);
         return true;
     }
