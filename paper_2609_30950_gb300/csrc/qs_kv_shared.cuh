@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
     // the head, and a lane's group of the first 32 (there is room for most_groups)
     KvGroupHead head;
     int4 g0 = make_int4(0, 0, 0, 0), g1 = g0;
-    bool fits;
+    bool fits;   // and the wait limit is not 0
     {
         const int4* const src = reinterpret_cast<const int4*>(head_at);
         const int4 h0 = __ldcg(src), h1 = __ldcg(src + 1);
@@ -291,8 +291,10 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
         head.groups = h0.x;
         head.units = static_cast<long long>(static_cast<unsigned>(h1.z)) | static_cast<long long>(h1.w) << 32;
         fits = groups_fit(p, kv_shared_mark(D, kE4M3), h0, h1);
+        // a limit of no polls gives up at the first wait
+        if (head.groups != 0 && !fits && tid == 0)
+            raise_status(p.status, groups_made_for(p, kv_shared_mark(D, kE4M3), h0, h1) ? QS_DEV_TIMEOUT : QS_DEV_PAGES);
     }
-    if (head.groups != 0 && !fits && tid == 0) raise_status(p.status, QS_DEV_PAGES);
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
@@ -302,9 +304,7 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
     using Part = SharedPart<S::kRows, S::kM == 2 && !kE4M3>;
     Part w;
     int copied = 0;   // tensors that this warp has begun to copy
-    // a limit of no polls gives up at the first wait
-    if (fits && p.wait_polls == 0 && tid == 0) raise_status(p.status, QS_DEV_TIMEOUT);
-    const bool live = fits && p.wait_polls > 0 && w.start(head, groups, g0, g1, worker, p.workers, p.Hkv, kTile);
+    const bool live = fits && w.start(head, groups, g0, g1, worker, p.workers, p.Hkv, kTile);
     // Streams have their own S, P, O and softmax warps.  They are a block's halves (`two`), or, where it has one half, the part's
     // even and odd tiles.
     const bool fences = !kE4M3 && !box_rows;   // copies by cp.async, whose writes the product's issuer makes visible to the tensor core

@@ -89,3 +89,31 @@ def test_a_work_space_of_more_requests_and_other_heads(qs):
         b.check(qs)
     large.run(qs)
     large.check(qs)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_a_wait_that_gives_up_at_once_reads_no_part_that_nobody_wrote(qs, kind):
+    """A limit of 0: reported, and the tokens are read as if nothing were shared."""
+    large = share.Batch(qs, [300 + 5 * i for i in range(20)], [(0, 20, 290)], 32, 8, 128, seed=6)
+    b = share.Batch(qs, LENS, GROUPS, 32, 8, 128, e4m3=kind == "e4m3", seed=7)
+    b.group(qs)
+
+    def gives_up():
+        qs.qstate_set_wait_limit(0)
+        try:
+            attend(qs, b, b.d_groups)
+            with pytest.raises(qs.QstateError) as e:
+                qs.qstate_check()
+            assert e.value.code == qs.QSTATE_ETIMEOUT
+        finally:
+            qs.qstate_set_wait_limit(-1)
+        b.check(qs)
+
+    for seed in range(3):
+        litter(b, seed)
+        gives_up()
+    large.run(qs)
+    b.work = large.work
+    gives_up()
+    b.run(qs)
+    b.check(qs)
