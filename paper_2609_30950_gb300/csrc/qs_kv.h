@@ -80,8 +80,6 @@ struct KvAttendParams {
 // Tokens of a tile, and rows (requests' heads) of a block, in the attention over tokens that requests share.
 constexpr int kSharedTile = 64;
 constexpr int kv_shared_rows(int d) { return d == 256 ? 128 : 256; }
-// What groups are marked with: they are dealt out otherwise where keys and values are codes.
-constexpr int kv_shared_mark(int d, bool e4m3) { return kv_shared_rows(d) + (e4m3 ? 1 : 0); }
 constexpr int kSharedWeight = 3, kSharedHalfWeight = 2;   // units of a tile; of a block with one half (see SharedPart)
 constexpr int kSharedRowUnits = 4;   // tiles that a block of rows costs by itself: its queries, its end
 // What the launches and joins of shared tokens cost beside their tiles.  With 16-bit keys and values of 128 entries, sharing took and
@@ -89,10 +87,13 @@ constexpr int kSharedRowUnits = 4;   // tiles that a block of rows costs by itse
 // key heads behind 200 to 600 21.5 and 18.0; 35 x 7 of 7 key heads behind 50 to 370 34.7 and 39.7, 4 x 32 behind up to 2000 48.7 and 72.2.
 constexpr long long kSharedLeastNs = 12000;
 
-// What qstate_kv_group leaves behind: a head, the requests' records, the groups that share anything.
+// What qstate_kv_group leaves behind: a head, the requests' records, the groups that share anything.  The head says what they
+// were made for (groups_made_for in qs_kv_tiles.cuh).
 struct KvGroupHead {
     int groups;              // that share
-    int R, Hq, Hkv, tile, rows;   // rows: kv_shared_mark
+    int R, Hq, Hkv;
+    int d, e4m3, window;
+    int unused;
     long long units;         // of all blocks
 };
 struct KvGroup {
@@ -102,7 +103,7 @@ struct KvGroup {
     long long unit0;         // units of the groups before it
 };
 constexpr int kKvGroupHeadBytes = 256;
-static_assert(sizeof(KvGroupHead) <= kKvGroupHeadBytes && sizeof(KvGroup) == 32, "layout");
+static_assert(sizeof(KvGroupHead) == 40 && sizeof(KvGroupHead) <= kKvGroupHeadBytes && sizeof(KvGroup) == 32, "layout");
 inline int kv_most_groups(int R) { return R / 2 + 1; }
 // Blocks of rows of at most R / 2 groups over R requests.
 inline long long kv_most_blocks(const qstate_kv_cfg& c, int R) {

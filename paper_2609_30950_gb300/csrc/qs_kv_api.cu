@@ -419,8 +419,9 @@ int qstate_kv_group(const qstate_kv_cfg* cfg, const int32_t* lens, int32_t R, co
     p.head.R = R;
     p.head.Hq = cfg->Hq;
     p.head.Hkv = cfg->Hkv;
-    p.head.tile = p.tile;
-    p.head.rows = kv_shared_mark(cfg->dk, e4m3);
+    p.head.d = cfg->dk;
+    p.head.e4m3 = e4m3;
+    p.head.window = cfg->window;
     char* const base = static_cast<char*>(groups);
     p.out = reinterpret_cast<KvGroupHead*>(base);
     p.groups = reinterpret_cast<KvGroup*>(base + kKvGroupHeadBytes);

@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
     const int groups = p.Hkv * groups_per_kv, G = p.Hq / p.Hkv;
 
     Share& share = *reinterpret_cast<Share*>(smem + S::kShare);
-    const bool fits = kShared && groups_fit(p, kv_shared_mark(D, kE4M3));
+    const bool fits = kShared && groups_fit(p);
     if (kShared && tid == 0) share.fits = fits;
     if (!p.whole_rows)
         make_share<S::kThreads, S::kTile, S::kChunk, kShared>(p, groups, blockIdx.x, reinterpret_cast<long long*>(smem + S::kScratch), &share, fits);

@@ -37,7 +37,7 @@ __global__ void __launch_bounds__(D * (kMany ? join_shares<D>() : 1)) kv_join_sh
     const int r = mine ? v / g.G : 0, in_kv = mine ? v - r * g.G : 0;
     const size_t rows = static_cast<size_t>(p.R) * p.Hq, row = static_cast<size_t>(r) * p.Hq + kv * g.G + in_kv;
     int4 rec = __ldcg(p.shared + r);
-    if (!groups_fit(p, kv_shared_mark(D, p.k_exp != nullptr))) rec = make_int4(0, 0, 0, 0);
+    if (!groups_fit(p)) rec = make_int4(0, 0, 0, 0);
     // records and lengths are older than the kernels that this one waits for
     const int n = clamped_len(p, r, false), begin = min(max(p.window > 0 && n > p.window ? n - p.window : 0, rec.x), n);
     const bool has_own = mine && begin < n, has_pre = mine && rec.x > 0;

@@ -284,16 +284,17 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
     {
         const int4* const src = reinterpret_cast<const int4*>(head_at);
         const int4 h0 = __ldcg(src), h1 = __ldcg(src + 1);
+        const long long units = __ldcg(&head_at->units);
         if (lane < most_groups) {
             g0 = __ldcg(reinterpret_cast<const int4*>(groups + lane));
             g1 = __ldcg(reinterpret_cast<const int4*>(groups + lane) + 1);
         }
         head.groups = h0.x;
-        head.units = static_cast<long long>(static_cast<unsigned>(h1.z)) | static_cast<long long>(h1.w) << 32;
-        fits = groups_fit(p, kv_shared_mark(D, kE4M3), h0, h1);
+        head.units = units;
+        fits = groups_fit(p, h0, h1);
         // a limit of no polls gives up at the first wait
         if (head.groups != 0 && !fits && tid == 0)
-            raise_status(p.status, groups_made_for(p, kv_shared_mark(D, kE4M3), h0, h1) ? QS_DEV_TIMEOUT : QS_DEV_PAGES);
+            raise_status(p.status, groups_made_for(p, h0, h1) ? QS_DEV_TIMEOUT : QS_DEV_PAGES);
     }
     tc::fence_before_sync();
     __syncthreads();

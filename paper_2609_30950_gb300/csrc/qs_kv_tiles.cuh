@@ -32,20 +32,19 @@ __device__ __forceinline__ int clamped_len(const KvAttendParams& p, int r, bool 
     return n < 0 ? 0 : static_cast<int>(most);
 }
 
-// Whether the groups, whose head (KvGroupHead) begins with a and b, were made for these requests and this kind of layer
-// (kv_shared_mark).
-__device__ __forceinline__ bool groups_made_for(const KvAttendParams& p, int mark, const int4& a, const int4& b) {
-    return a.y == p.R && a.z == p.Hq && a.w == p.Hkv && b.x == kSharedTile && b.y == mark;
+// Whether the groups, whose head (KvGroupHead) begins with a and b, were made for these requests and this kind of layer.
+__device__ __forceinline__ bool groups_made_for(const KvAttendParams& p, const int4& a, const int4& b) {
+    return a.y == p.R && a.z == p.Hq && a.w == p.Hkv && b.x == p.dk && b.y == (p.k_exp != nullptr) && b.z == p.window;
 }
 // And whether there are any, and the kernel of shared tokens waits for its products at all.  Else they count as none, in that
 // kernel, in that of a request's own tokens and in the join alike: what one of them left out, or did not write, no other
 // would make up for.
-__device__ __forceinline__ bool groups_fit(const KvAttendParams& p, int mark, const int4& a, const int4& b) {
-    return a.x > 0 && p.wait_polls > 0 && groups_made_for(p, mark, a, b);
+__device__ __forceinline__ bool groups_fit(const KvAttendParams& p, const int4& a, const int4& b) {
+    return a.x > 0 && p.wait_polls > 0 && groups_made_for(p, a, b);
 }
-__device__ __forceinline__ bool groups_fit(const KvAttendParams& p, int mark) {
+__device__ __forceinline__ bool groups_fit(const KvAttendParams& p) {
     const int4* const head = reinterpret_cast<const int4*>(p.groups);
-    return groups_fit(p, mark, __ldcg(head), __ldcg(head + 1));
+    return groups_fit(p, __ldcg(head), __ldcg(head + 1));
 }
 
 // kShared: without the tokens that request r shares with others, which another kernel reads, if the groups fit.

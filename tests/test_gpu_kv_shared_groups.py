@@ -117,3 +117,28 @@ def test_a_wait_that_gives_up_at_once_reads_no_part_that_nobody_wrote(qs, kind):
     gives_up()
     b.run(qs)
     b.check(qs)
+
+
+@pytest.mark.parametrize("made,used", [(0, 200), (200, 0), (100, 250), (10000, 0)])
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_groups_of_another_window_count_as_none(qs, made, used, kind):
+    """Layers with a window and without one stand beside each other: groups of one are not the other's, though nothing else differs."""
+    lens = [200, 230, 305, 0, 280, 90]
+    make = lambda w: share.Batch(qs, lens, [(0, 5, 180)], 8, 2, 64, window=w, e4m3=kind == "e4m3", seed=8)  # noqa: E731
+    b, other = make(used), make(made)
+    other.group(qs)
+    with pytest.raises(ValueError):   # the binding knows what they were made for
+        attend(qs, b, other.d_groups)
+    if int(other.d_groups.data[:4].view(torch.int32).item()) == 0:   # nothing is shared, whoever looks at it
+        attend(qs, b, raw(qs, other.d_groups, len(lens)))
+    else:
+        reported(qs, b, raw(qs, other.d_groups, len(lens)))
+    b.run(qs)
+    b.check(qs)
+
+
+@pytest.mark.parametrize("made,used", [(64, 128), (128, 64), (256, 128)])
+def test_groups_of_another_width_count_as_none(qs, made, used):
+    b, other = (share.Batch(qs, LENS, GROUPS, 8, 2, d, seed=9) for d in (used, made))
+    other.group(qs)
+    reported(qs, b, raw(qs, other.d_groups, len(LENS)))
