@@ -446,8 +446,8 @@ size_t qstate_kv_shared_work_bytes(const qstate_kv_cfg* cfg, int32_t R);
  * not falling, within [0, R]), whose first common[g] tokens are the same.  Requests outside all groups, those with fewer tokens and
  * those whose window begins behind token 0 read theirs by themselves, and so does a group that only one could share in, or everyone where
  * sharing would take longer (see qstate_set_shared_gain).  Made from lens (R) as
- * they are at the attention, for layers of one Hq, Hkv, dk, window and store; for others, and for
- * another R, the attention sets the device status and nothing is shared.  A start
+ * they are at the attention, for layers of one Hq, Hkv, dk, window and store, whatever their pages (for others, for another R and
+ * where a group has more in common than the layer's table holds, the attention sets the device status and nothing is shared).  A start
  * outside its bounds or a number of tokens outside the table sets the device status here, and nothing (or that group) is shared. */
 int qstate_kv_group(const qstate_kv_cfg* cfg, const int32_t* lens, int32_t R, const int32_t* start, const int32_t* common, int32_t N,
                     void* groups, void* stream);

@@ -93,7 +93,7 @@ struct KvGroupHead {
     int groups;              // that share
     int R, Hq, Hkv;
     int d, e4m3, window;
-    int unused;
+    int tokens;              // the most that one of them has in common
     long long units;         // of all blocks
 };
 struct KvGroup {

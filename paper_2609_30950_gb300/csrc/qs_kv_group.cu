@@ -36,6 +36,7 @@ template <int kPer>
 __global__ void __launch_bounds__(kMostThreads) kv_group_kernel(const KvGroupParams p) {
     extern __shared__ int smem[];
     __shared__ Sums s_warp[32];
+    __shared__ int s_tokens;
     chain_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, N = p.N;
     int* const start = smem;             // N + 1
@@ -56,6 +57,7 @@ __global__ void __launch_bounds__(kMostThreads) kv_group_kernel(const KvGroupPar
         owner[g] = p.R;
     }
     for (int g = tid; g <= N; g += threads) start[g] = __ldcg(p.start + g);
+    if (tid == 0) s_tokens = 0;
     __syncthreads();
     bool bad = tid == 0 && (start[0] < 0 || start[N] > p.R);
     for (int g = tid; g < N; g += threads) bad = bad || start[g] > start[g + 1];
@@ -123,18 +125,22 @@ __global__ void __launch_bounds__(kMostThreads) kv_group_kernel(const KvGroupPar
     for (int g = g0; g < g1; ++g) {
         const Sums s = worth ? sums_of(g) : Sums{0, 0, 0, 0};
         const int blocks = s.blocks / p.Hkv;
-        if (blocks) p.groups[at.groups] = {start[g], (start[g + 1] - start[g]) * p.G, owner[g], common[g], blocks, at.blocks, at.units};
+        if (blocks) {
+            p.groups[at.groups] = {start[g], (start[g + 1] - start[g]) * p.G, owner[g], common[g], blocks, at.blocks, at.units};
+            atomicMax(&s_tokens, common[g]);
+        }
         count[g] = blocks;
         owner[g] = at.blocks;
         at = plus(at, s);
     }
+    __syncthreads();
     if (tid == 0) {
         KvGroupHead head = p.head;
         head.groups = all.groups;
+        head.tokens = s_tokens;
         head.units = all.units;
         *p.out = head;
     }
-    __syncthreads();
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
         const int r = k * threads + tid, g = group[k];

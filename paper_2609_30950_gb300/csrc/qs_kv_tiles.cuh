@@ -32,9 +32,11 @@ __device__ __forceinline__ int clamped_len(const KvAttendParams& p, int r, bool 
     return n < 0 ? 0 : static_cast<int>(most);
 }
 
-// Whether the groups, whose head (KvGroupHead) begins with a and b, were made for these requests and this kind of layer.
+// Whether the groups, whose head (KvGroupHead) begins with a and b, were made for these requests and this kind of layer, and
+// what they have in common lies in its tables, which may be of other pages than those that the groups were made with.
 __device__ __forceinline__ bool groups_made_for(const KvAttendParams& p, const int4& a, const int4& b) {
-    return a.y == p.R && a.z == p.Hq && a.w == p.Hkv && b.x == p.dk && b.y == (p.k_exp != nullptr) && b.z == p.window;
+    return a.y == p.R && a.z == p.Hq && a.w == p.Hkv && b.x == p.dk && b.y == (p.k_exp != nullptr) && b.z == p.window &&
+           b.w <= static_cast<long long>(p.max_pages) << p.page_shift;
 }
 // And whether there are any, and the kernel of shared tokens waits for its products at all.  Else they count as none, in that
 // kernel, in that of a request's own tokens and in the join alike: what one of them left out, or did not write, no other

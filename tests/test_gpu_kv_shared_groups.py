@@ -142,3 +142,27 @@ def test_groups_of_another_width_count_as_none(qs, made, used):
     b, other = (share.Batch(qs, LENS, GROUPS, 8, 2, d, seed=9) for d in (used, made))
     other.group(qs)
     reported(qs, b, raw(qs, other.d_groups, len(LENS)))
+
+
+def test_groups_serve_layers_of_other_pages(qs):
+    """What is shared is counted in tokens: tables of other pages may be read with the same groups."""
+    made = share.Batch(qs, LENS, GROUPS, 8, 2, 128, page=16, seed=10)
+    made.group(qs)
+    for page in (1, 64, 256):
+        b = share.Batch(qs, LENS, GROUPS, 8, 2, 128, page=page, seed=page)
+        for groups in (made.d_groups, raw(qs, made.d_groups, len(LENS))):
+            attend(qs, b, groups)
+            b.check(qs)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_common_tokens_behind_the_table_count_as_none(qs, kind):
+    """Groups with more in common than a row of this layer's table holds: nothing is looked up behind it."""
+    made = share.Batch(qs, LENS, GROUPS, 8, 2, 64, page=16, e4m3=kind == "e4m3", seed=11)
+    b = share.Batch(qs, [40, 40, 44, 0, 40, 7], [(0, 5, 40)], 8, 2, 64, page=16, e4m3=kind == "e4m3", seed=12)
+    assert b.cfg.max_pages * 16 < 280
+    made.group(qs)
+    for groups in (made.d_groups, raw(qs, made.d_groups, len(LENS))):
+        reported(qs, b, groups)
+    b.run(qs)
+    b.check(qs)
