@@ -453,7 +453,9 @@ int qstate_kv_group(const qstate_kv_cfg* cfg, const int32_t* lens, int32_t R, co
                     void* groups, void* stream);
 
 /* qstate_kv_attend (HEADS), a group's common tokens read once, through the table of the first request that shares in
- * them.  The results are those of qstate_kv_attend up to FP32 rounding and one rounding of the weights to 16 bits. */
+ * them.  The results are those of qstate_kv_attend up to FP32 rounding and one rounding of the weights to 16 bits.  E4M3: shared
+ * keys and values are taken in bf16, which has all but the ends of the range that codes and powers span (2^128 counts as 2^-8 less,
+ * steps under 2^-126 are 2^-133), and sums of weights, of up to 2^8, times values are FP32, as in the 16-bit store. */
 int qstate_kv_attend_shared(const qstate_kv_cfg* cfg, const qstate_kv_cache* cache, const void* q, int64_t q_row,
                             int64_t q_head, const int32_t* table, const int32_t* lens, int32_t R, const void* groups, void* o,
                             float* lse, void* work, void* stream);

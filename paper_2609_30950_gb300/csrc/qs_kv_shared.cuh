@@ -20,8 +20,10 @@
 //   warps 8-11      issue S and O of either stream: each waits for nothing but what its next product needs (in fewer warps, the
 //                   instructions between products, at some ten clocks each, were what everyone waited for)
 //   warps 12-15     copy keys and values: by the tensor map's boxes where pages have 8 tokens or more, 16 bytes at a time else
-//                   (e4m3: they turn codes into bf16 on the way, exactly: a code has 4 bits and its power of two is one of the
-//                   type's).  256 entries have 10 warps: 0-3, two that issue, four that copy
+//                   (e4m3: they turn codes into bf16 on the way, exactly where bf16 has the product of a code, of 4 bits, and
+//                   its power: what is under 2^-126 has steps of 2^-133, half of one lost at most, and 2^128, to which the largest
+//                   bf16 is rounded in e4m3, becomes that bf16 again, 2^-8 less).  256 entries have 10 warps: 0-3, two that
+//                   issue, four that copy
 // The units of all blocks (some for a tile; those of kSharedRowUnits tiles more for the block itself) are dealt out evenly, as the rows' are in
 // qs_kv_tiles.cuh: a block that several CTAs share leaves a part from each.
 // The reference m follows the maximum only when that has outgrown it by 2^8.  In f16, which ends at 2^-24, a weight of the
@@ -212,6 +214,12 @@ __device__ __forceinline__ void tmem_st16u(uint32_t at, const uint32_t (&r)[16])
         "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
         "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
+}
+// Two bf16; what is above the largest becomes that, NaN stays.
+__device__ __forceinline__ uint32_t pack2_finite(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
 }
 __device__ __forceinline__ void st_shared16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -446,8 +454,8 @@ __global__ void __launch_bounds__(SharedShape<D>::kThreads, 1) kv_shared_kernel(
                                     : "=r"(lo), "=r"(hi) : "r"(w4[j]));
                                 const float2 a = __fmul2_rn(unpack2<true>(lo), make_float2(two, two));
                                 const float2 b = __fmul2_rn(unpack2<true>(hi), make_float2(two, two));
-                                y[2 * j] = pack2<false>(a.x, a.y);
-                                y[2 * j + 1] = pack2<false>(b.x, b.y);
+                                y[2 * j] = pack2_finite(a.x, a.y);
+                                y[2 * j + 1] = pack2_finite(b.x, b.y);
                             }
                             // entries 16 sg ...: pieces 2 (sg % 4) and the next of block sg / 4
                             const int piece = (code_sg & 3) * 2;
