@@ -119,3 +119,39 @@ def test_the_smallest_values_of_e4m3(qs, power):
         lost[r, :, 0] = 2 * n * 2.0 ** (-126 - power) / torch.exp(z - z.amax(0)).sum(0)
     assert bool(((b.o.double().cpu() * 2.0 ** -power - o).abs() <= do + lost + 2.0 ** (-133 - power)).all())
     assert bool(((b.lse.double().cpu() - lse).abs() <= dl).all())
+
+
+@pytest.mark.parametrize("first", [0, 5, 69, 3839])
+def test_small_weights_behind_and_before_large_ones_in_f16(qs, first):
+    """Every 60th tile has a token whose score is 20.58 above all others' and whose value is zero: the answer is what the others make
+    of it, 0.03 or so.  Beside the large one, whose weight is 2^7, theirs are 2.48 steps of 2^-24, the last that f16 has.  In a tile with a
+    large one they are off by up to half a step, a fifth of them; in all others the reference is theirs, and they are off by 2^-11 at
+    most.  (Were it the large one's, they would be 2 steps, a fifth less, in a fourth of all tiles or more: a worker goes through about 60
+    tiles, in two streams; against 2^7 less they would be nothing.)"""
+    n, Hkv, d, gap = 60 * 64 * 9 + 1920, 16, 64, 20.578125
+    b = share.Batch(qs, [n, n + 9], [(0, 2, n)], Hkv, Hkv, d, page=64, dtype="f16", scale=1.0, seed=4)
+    b.qval.zero_()
+    b.qval[..., 0] = 1.0
+    b.q.copy_(b.qval)
+    large = list(range(first, n, 60 * 64))
+    for k, v in ((b.k, b.v), (b.kval, b.vval)):
+        k[..., 0] = 0.0
+        v.abs_().mul_(2.0 ** 13)
+        for r in range(2):
+            for t in large:
+                k[b.table[r][t // 64], :, t % 64, 0] = gap
+                v[b.table[r][t // 64], :, t % 64] = 0.0
+    b.run(qs)
+    qs.qstate_check()
+    o, lse, _, dl = b.expect()
+    tiles = {t // 64 for t in large}
+    small = torch.exp(torch.tensor(-gap, dtype=torch.float64)) / len(large)   # a weight, but for 1e-4 of it
+    for r in range(2):
+        pages = torch.tensor(b.table[r][: -(-n // 64)])
+        V = torch.nan_to_num(b.vval[pages])                                  # (tiles, Hkv, 64, d); places behind the last token are NaN
+        beside = small * V[sorted(tiles)].sum((0, 2)).cpu()
+        # half a step; a weight's rounding, the sum's and o's, 2^-11 each; scores of 30 in base 2 and sums of 570 parts in FP32
+        bound = beside * (0.5 / 2.48) + o[r] * (3 * 2.0 ** -11 + 2.0 ** -17) + 2.0 ** -25
+        assert bool((o[r] > 0.01).all()) and bool((bound < 0.02 * o[r]).all())
+        assert bool(((b.o[r].double().cpu() - o[r]).abs() <= bound).all()), float(((b.o[r].double().cpu() - o[r]) / o[r]).abs().max())
+    assert bool(((b.lse.double().cpu() - lse).abs() <= dl).all())
