@@ -191,6 +191,11 @@ cudaError_t launch_kv_fork(const KvForkParams& p, cudaStream_t stream);
 cudaError_t launch_kv_compact(KvCompactParams p, cudaStream_t stream);
 cudaError_t launch_kv_copy(KvCopyParams p, cudaStream_t stream);
 int kv_column_parts(int R, int max_pages);
+// Columns of a part, and one behind the last of a part that begins with column c0 >= 0.  The widest tables have 2^31 - 1024: neither
+// sum here is an int there.
+constexpr int kv_part_columns(int max_pages, int parts) { return static_cast<int>((static_cast<long long>(max_pages) + parts - 1) / parts); }
+__host__ __device__ constexpr int kv_part_end(int c0, int chunk) { return chunk > 0x7fffffff - c0 ? 0x7fffffff : c0 + chunk; }
+static_assert(kv_part_columns(0x7ffffc00, kKvMaxRequests) == 1 << 18 && kv_part_end((kKvMaxRequests - 1) << 18, 1 << 18) == 0x7fffffff, "");
 // partial results that an attention launch may use: bytes of sums, of references and weights, of the list of
 // split rows
 struct KvPartBytes {

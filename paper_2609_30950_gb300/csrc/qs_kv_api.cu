@@ -315,7 +315,7 @@ int qstate_kv_fork(const qstate_kv_cfg* cfg, const qstate_kv_pages* pages, int32
     p.n_pages = cfg->n_pages;
     p.max_pages = cfg->max_pages;
     p.parts = kv_column_parts(R, cfg->max_pages);
-    p.chunk = (cfg->max_pages + p.parts - 1) / p.parts;
+    p.chunk = kv_part_columns(cfg->max_pages, p.parts);
     const PagesWork w = pages_work(*cfg, R);
     char* const base = static_cast<char*>(work);
     p.head = static_cast<int*>(work) + 1;
@@ -351,7 +351,7 @@ int qstate_kv_compact(const qstate_kv_cfg* cfg, const qstate_kv_pages* pages, in
     p.n_pages = cfg->n_pages;
     p.max_pages = cfg->max_pages;
     p.parts = kv_column_parts(R, cfg->max_pages);
-    p.chunk = (cfg->max_pages + p.parts - 1) / p.parts;
+    p.chunk = kv_part_columns(cfg->max_pages, p.parts);
     const PagesWork w = pages_work(*cfg, R);
     char* const base = static_cast<char*>(work);
     p.head = static_cast<int*>(work) + 2;

@@ -35,7 +35,8 @@ template <class F>
 __device__ __forceinline__ void each_entry(const KvCompactParams& p, bool report, F f) {
     const int lane = threadIdx.x & 31, workers = gridDim.x * kWarps, items = p.R * p.parts;
     for (int item = blockIdx.x * kWarps + (threadIdx.x >> 5); item < items; item += workers) {
-        const int r = item / p.parts, c0 = (item - r * p.parts) * p.chunk, c1 = min(c0 + p.chunk, held_pages(p, r, report && c0 == 0));
+        const int r = item / p.parts, c0 = (item - r * p.parts) * p.chunk;
+        const int c1 = min(kv_part_end(c0, p.chunk), held_pages(p, r, report && c0 == 0));
         const size_t row = static_cast<size_t>(r) * p.max_pages;
         for (int c = c0 + lane; c < c1; c += 32 * kBatch) {
             int x[kBatch];

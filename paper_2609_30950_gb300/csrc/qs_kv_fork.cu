@@ -168,7 +168,7 @@ __device__ __forceinline__ void each_part(const KvForkParams& p, int worker, int
     for (int item = worker; item < items; item += workers) {
         const int r = item / p.parts, c0 = (item - r * p.parts) * p.chunk;
         const int4 rec = __ldcg(p.rec + r);
-        f(item, r, rec, c0, c0 + p.chunk);
+        f(item, r, rec, c0, kv_part_end(c0, p.chunk));
     }
 }
 
