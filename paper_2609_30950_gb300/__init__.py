@@ -851,14 +851,14 @@ def qstate_kv_group(cfg: KvConfig, lens, start, common, groups: KvGroups, stream
     """Which requests share their first tokens (see include/qstate.h): lens (R), start (N + 1), common (N), int32."""
     if groups._fits is not cfg:
         groups._check(cfg)
-    if groups._made is not cfg:
-        _keep(groups, _made=cfg)
     N = common.numel()
     rc = (_lib or load()).qstate_kv_group(cfg._at, _ints(lens, "lens", groups.R), groups.R, _ints(start, "start", N + 1),
                                           _ints(common, "common", N), N, groups._at,
                                           _current_stream() if stream is None else stream.cuda_stream)
     if rc:
         _check(rc)
+    if groups._made is not cfg:
+        _keep(groups, _made=cfg)
 
 
 def _attend_args(cfg, cache, q, table, lens, o, lse):

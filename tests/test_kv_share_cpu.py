@@ -173,3 +173,15 @@ def test_tensor_memory_of_shared_tokens_is_taken_between_wait_and_release():
     at = [body.index(s) for s in ("chain_enter();", "tmem_alloc(", "tmem_relinquish();", "chain_release();", "__syncthreads();")]
     assert at == sorted(at)
     assert body.count("chain_") == 2 and "chain_wait" not in src
+
+
+def test_a_refused_call_makes_no_groups(q, monkeypatch):
+    """What groups were made for is what the last call that was accepted said."""
+    monkeypatch.setattr(q, "_ptr", lambda t: t.data_ptr())   # host tensors stand for device ones
+    i32 = lambda *n: torch.zeros(*n, dtype=torch.int32)  # noqa: E731
+    c, other = config(q), config(q, window=7)
+    groups = q.new_kv_groups(c, 5, device="cpu")
+    q._keep(groups, _made=c)   # as an accepted call leaves it
+    with pytest.raises(ValueError):   # no device tensors
+        q.qstate_kv_group(other, i32(5), i32(3), i32(2), groups)
+    assert groups._made is c
