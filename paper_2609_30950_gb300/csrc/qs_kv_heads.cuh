@@ -99,12 +99,12 @@ __global__ void __launch_bounds__(128, kCtas) kv_heads_kernel(const KvAttendPara
     const int groups = p.Hkv * groups_per_kv, G = p.Hq / p.Hkv;
 
     Share& share = *reinterpret_cast<Share*>(smem + S::kShare);
-    const bool fits = kShared && groups_fit(p);
-    if (kShared && tid == 0) share.fits = fits;
-    if (!p.whole_rows)
-        make_share<S::kThreads, S::kTile, S::kChunk, kShared>(p, groups, blockIdx.x, reinterpret_cast<long long*>(smem + S::kScratch), &share, fits);
-    else if (kShared)
+    if (!p.whole_rows) {
+        make_share<S::kThreads, S::kTile, S::kChunk, kShared>(p, groups, blockIdx.x, reinterpret_cast<long long*>(smem + S::kScratch), &share);
+    } else if (kShared) {
+        if (tid == 0) share.fits = groups_fit(p);
         __syncthreads();
+    }
     int split = 0;   // parts of the row that this CTA begins and others end
     Walk<S::kTile, S::kChunk, kShared> cw;
     bool live = cw.start(p, share, groups, blockIdx.x);

@@ -49,16 +49,24 @@ __device__ __forceinline__ bool groups_fit(const KvAttendParams& p) {
     return groups_fit(p, __ldcg(head), __ldcg(head + 1));
 }
 
-// kShared: without the tokens that request r shares with others, which another kernel reads, if the groups fit.
+// kShared: without the `common` tokens that a request shares with others, which another kernel reads.
 template <int kTile, int kGrain, bool kShared>
-__device__ __forceinline__ Span span_of(const KvAttendParams& p, int r, int n, bool fits) {
+__device__ __forceinline__ Span span_behind(const KvAttendParams& p, int n, int common) {
     Span s;
     s.end = n;
     s.begin = p.window > 0 && n > p.window ? n - p.window : 0;
-    if (kShared && fits) s.begin = min(max(s.begin, p.shared[r].x), n);
+    if (kShared) s.begin = min(max(s.begin, common), n);
     s.base = s.begin & ~(kGrain - 1);
     s.tiles = kShared && s.begin == n ? 0 : (n - s.base + kTile - 1) / kTile;
     return s;
+}
+
+// Those of request r's record, if the groups fit.
+template <int kTile, int kGrain, bool kShared>
+__device__ __forceinline__ Span span_of(const KvAttendParams& p, int r, int n, bool fits) {
+    int common = 0;
+    if (kShared) common = p.shared[r].x;   // on its way whether it counts or not
+    return span_behind<kTile, kGrain, kShared>(p, n, fits ? common : 0);
 }
 
 constexpr int kWholeTiles = 4;
@@ -89,16 +97,24 @@ __device__ __forceinline__ int share_owner(long long total, long long u, int wor
 
 __device__ __forceinline__ int row_units(int tiles) { return tiles > 0 ? tiles + kRowUnits : 0; }
 
-// All threads of the CTA; `groups` rows a request.  scratch: kThreads / 32 + 2 long longs of shared memory; *out too (`fits` is
-// the caller's to store).
+// All threads of the CTA; `groups` rows a request.  scratch: kThreads / 32 + 2 long longs of shared memory; *out too.
 template <int kThreads, int kTile, int kGrain, bool kShared = false>
-__device__ __forceinline__ void make_share(const KvAttendParams& p, int groups, int worker, long long* scratch, Share* out, bool fits = false) {
+__device__ __forceinline__ void make_share(const KvAttendParams& p, int groups, int worker, long long* scratch, Share* out) {
     constexpr int kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (p.R + kThreads - 1) / kThreads, r0 = min(p.R, tid * per), r1 = min(p.R, r0 + per);
     long long mine = 0;
-    int tiles = 0;
-    for (int r = r0; r < r1; ++r) {
+    int tiles = 0, first_len = 0, first_common = 0;
+    if (kShared && r0 < r1) {   // on their way while the head of the groups is looked at (a call of 4 requests 22.7 -> 22.1 us)
+        first_common = p.shared[r0].x;
+        first_len = clamped_len(p, r0, false);
+    }
+    const bool fits = kShared && groups_fit(p);
+    if (kShared && r0 < r1) {
+        tiles = row_units(span_behind<kTile, kGrain, kShared>(p, first_len, fits ? first_common : 0).tiles);
+        mine = tiles;
+    }
+    for (int r = kShared ? r0 + 1 : r0; r < r1; ++r) {
         tiles = row_units(span_of<kTile, kGrain, kShared>(p, r, clamped_len(p, r, false), fits).tiles);
         mine += tiles;
     }
@@ -123,6 +139,7 @@ __device__ __forceinline__ void make_share(const KvAttendParams& p, int groups, 
         out->total = total;
         out->u0 = u0;
         out->u1 = u1;
+        out->fits = fits;
     }
     const long long first = before * groups;
     if (u0 >= first && u0 < first + mine * groups) {
