@@ -119,7 +119,9 @@ __device__ void compact_move(const KvCompactParams& p, int spans, int2 (*sums)[k
         if (p.left) p.left[0] = all.x - moved;
         p.head[0] = moved;
     }
-    for (int i = moved + blockIdx.x * kThreads + tid; i < p.moves.n; i += spans * kThreads) p.moves.src[i] = p.moves.dst[i] = -1;
+    // unsigned: the step behind the last entry may be above 2^31
+    for (unsigned i = moved + blockIdx.x * kThreads + tid; i < static_cast<unsigned>(p.moves.n); i += spans * kThreads)
+        p.moves.src[i] = p.moves.dst[i] = -1;
     int i0 = before.x, j0 = before.y;   // ranks of the next words' first source and place
     for (int k = 0; k < p.words; ++k) {
         __syncthreads();   // the sums are read

@@ -155,7 +155,8 @@ __device__ void fork_decide(const KvForkParams& p, int* smem, int* sums) {
         p.moves.src[r] = src;
         p.moves.dst[r] = dst;
     }
-    for (int r = R + tid; r < p.moves.n; r += threads) p.moves.src[r] = p.moves.dst[r] = -1;
+    // unsigned: the step behind the last entry may be above 2^31
+    for (unsigned r = R + tid; r < static_cast<unsigned>(p.moves.n); r += threads) p.moves.src[r] = p.moves.dst[r] = -1;
     if (tid == 0) p.head[0] = free_n - min(asked, free_n);
 }
 

@@ -56,3 +56,27 @@ def test_the_last_columns_of_the_widest_table(qs):
     assert (lens_out.item(), free_out.item()) == (0, 1023 + width)
     assert same_as_range(free_list[1023:1023 + width], 0)
     assert not bool(others.any())
+
+
+def test_the_longest_list_of_moves(qs):
+    """2^31 - 1 entries, of which none is needed: all are -1, and nothing in front of the list is touched."""
+    if torch.cuda.mem_get_info()[0] < 30e9:
+        pytest.skip("needs 20 GB")
+    n = 2 ** 31 - 1
+    cfg = qs.KvConfig(page=4, n_pages=6, max_pages=2)
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    front = 1 << 20   # words in front of each list, which a step above 2^31 would reach
+    room = [torch.full((front + n,), 5, dtype=torch.int32, device="cuda") for _ in range(2)]
+    moves = qs.KvMoves(*(x[front:] for x in room))
+    pages = qs.KvPages(i32(), i32(), i32(3, 1, 2, 0, 4, 5), i32(4))
+    others, work = torch.zeros(6, dtype=torch.int32, device="cuda"), qs.new_kv_pages_work(cfg, 0)
+    for call in (lambda: qs.qstate_kv_compact(cfg, pages, None, 5, moves, None, work),
+                 lambda: qs.qstate_kv_fork(cfg, pages, others, i32(), None, moves, torch.zeros(0, dtype=torch.uint8, device="cuda"), work)):
+        for x in room:
+            x.fill_(5)
+        call()
+        qs.qstate_check()
+        for x in room:
+            step = 1 << 28
+            assert bool((x[:front] == 5).all())
+            assert all(bool((x[i:i + step] == -1).all()) for i in range(front, front + n, step))
